@@ -38,7 +38,10 @@ typedef enum {
     PEC_ERR_CUDA = -5,        /* a CUDA runtime/driver call or the launch failed       */
     PEC_ERR_TIMEOUT = -6,     /* value a kernel stores in *status when a bounded wait  */
                               /* inside it gave up (read it after synchronising)       */
-    PEC_ERR_CAPACITY = -7     /* a caller array of pec_plan is too small               */
+    PEC_ERR_CAPACITY = -7,    /* a caller array of pec_plan is too small               */
+    PEC_ERR_BAD_INDEX = -8    /* value a kernel stores in *status when it met a page   */
+                              /* number, a position or an offset out of range in the   */
+                              /* tables it reads on the device                         */
 } pec_status;
 
 typedef enum { PEC_BF16 = 1, PEC_F32 = 2 } pec_dtype;
@@ -441,6 +444,142 @@ int pec_rope_table(double theta, int64_t n_pos, int32_t D, float *table, void *c
 int pec_linear_merged(const void *const *o_parts, const float *const *lse_parts, int32_t n, int64_t rows, int32_t Hq,
                       int32_t D, const void *w, int64_t w_stride, void *y, int64_t y_stride, int32_t N,
                       int32_t *status, void *cuda_stream);
+
+/*
+ * Norm and rotary encoding of query and key heads in one pass, the step between the QKV generation (Eq. 2) and the
+ * attention in models that normalise each head.  (The paper names neither; pec_linear_rope has the rotation alone, in the
+ * GEMM's epilogue, where a norm over a whole head before it is not possible.)  Per token and head of 128 channels
+ *     y = x / sqrt(mean(x^2) + eps) * w                                     if norm, else y = x
+ *     z[i] = y[i] cos a - y[i + 64] sin a,  z[i + 64] = y[i + 64] cos a + y[i] sin a,  a = p * theta^(-2 i / 128)
+ *                                                                            if rope_table, else z = y
+ * in fp32, rounded once to the type of the output (that of the input).
+ * q [T, Hq, D], k [T, Hkv, D], channel-contiguous with free token and head strides (column slices of a fused QKV tensor);
+ * q_out, k_out likewise; q_out may be q (k_out k) with the same strides, any other overlap is not allowed.  Hq or Hkv may
+ * be 0: that side's pointers are then not used.  q_weight, k_weight: [D] of the same type, or NULL for 1; used with norm.
+ * rope_table, n_pos: from pec_rope_table, or NULL.  Token t is at position positions[t] (device int32 [T]) or, with
+ * positions == NULL, at pos0 + t.  A token with a negative position is padding: its rows are neither read into a result nor
+ * written.  A position from n_pos on stores PEC_ERR_BAD_INDEX in *status and its rows are not written (with positions == NULL
+ * the host rejects it).  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA.
+ */
+typedef struct {
+    const void *q, *k;          /* device; 16-byte aligned                                      */
+    int64_t q_stride_t, q_stride_h, k_stride_t, k_stride_h;              /* elements; multiples of 16 bytes, >= D */
+    void *q_out, *k_out;
+    int64_t q_out_stride_t, q_out_stride_h, k_out_stride_t, k_out_stride_h;
+    int32_t dtype;              /* pec_dtype of all of them                                     */
+    int32_t Hq, Hkv, D;         /* D must be 128                                                */
+    int64_t T;
+    const void *q_weight, *k_weight;
+    int32_t norm;               /* 0 or 1                                                       */
+    float eps;                  /* > 0 with norm                                                */
+    const float *rope_table;
+    int64_t n_pos;
+    const int32_t *positions;
+    int64_t pos0;
+    int32_t *status;
+} pec_norm_rope_args;
+
+int pec_qk_norm_rope(const pec_norm_rope_args *args, void *cuda_stream);
+
+/*
+ * Paged K/V cache (pec_kv_append, pec_paged_attn).  k_pages, v_pages: [num_pages, page_size, Hkv, D], channel-contiguous,
+ * with free page, token and head strides in elements (token-major and head-major pages alike).  page_size: a multiple of 8.
+ * Request b's token at position p lies in page block_table[b][p / page_size], slot p % page_size; block_table is a device
+ * int32 array of B rows of max_pages entries, table_stride entries apart.  Pages may be shared between requests for reading.
+ *
+ * Batch: request b brings the new tokens [cu_q[b], cu_q[b + 1]) of the packed rows (device int32 [B + 1], ascending; none is
+ * allowed); kv_lens[b] (device int32 [B]) counts its cached tokens INCLUDING the new ones, so that new token i of n is at
+ * position kv_lens[b] - n + i.  T is the number of rows of the packed buffers; rows outside [cu_q[0], cu_q[B]) are padding
+ * and their outputs are left as they were.  All tables are read on the device when the kernels run: a captured graph
+ * replays with whatever they hold then.
+ *
+ * Entries of block_table that a request does not reach are not read.  What a page holds past the request's end may be
+ * anything, NaN included.  A page number outside [0, num_pages), a position outside the table's row and offsets that are not
+ * ascending store PEC_ERR_BAD_INDEX in *status; no access leaves the cache, and the outputs of the requests concerned are
+ * undefined.
+ */
+
+/*
+ * Appends a batch's new keys and values to the cache: the key heads of token t normalised (norm) and rotated (rope_table)
+ * as in pec_qk_norm_rope, at the token's own position, the values as they are.  k, v: [T, Hkv, D], channel-contiguous with
+ * free strides, of the cache's type.  rope_table NULL stores keys unrotated (for keys that pec_linear_rope has turned
+ * already).  A position from n_pos on is a bad index, as above; tokens with a bad index are not stored.  Two tokens of one
+ * call must not share a slot.  Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA.
+ */
+typedef struct {
+    const void *k, *v;          /* device; 16-byte aligned                                      */
+    int64_t k_stride_t, k_stride_h, v_stride_t, v_stride_h;              /* elements; multiples of 16 bytes, >= D */
+    int32_t dtype;              /* pec_dtype of k, v, the weight and the cache                  */
+    void *k_pages, *v_pages;    /* device; 16-byte aligned                                      */
+    int64_t k_pages_stride_p, k_pages_stride_t, k_pages_stride_h;
+    int64_t v_pages_stride_p, v_pages_stride_t, v_pages_stride_h;
+    int32_t page_size;
+    int64_t num_pages;
+    const int32_t *block_table;
+    int64_t table_stride;
+    int32_t max_pages;
+    const int32_t *cu_q, *kv_lens;
+    int32_t B;
+    int64_t T;
+    int32_t Hkv, D;             /* D must be 128                                                */
+    const void *k_weight;       /* [D] or NULL for 1; used with norm                            */
+    int32_t norm;
+    float eps;
+    const float *rope_table;
+    int64_t n_pos;
+    int32_t *status;
+} pec_kv_append_args;
+
+int pec_kv_append(const pec_kv_append_args *args, void *cuda_stream);
+
+/*
+ * Attention (Eq. 3-4) of a batch's new tokens over the paged cache, which holds their own keys and values already
+ * (pec_kv_append): row t of q [T, Hq, D] at position p sees keys [0, p] of its request (causal = 1) or all
+ * kv_lens[b] of them (causal = 0).  One token per request is a decode step, many a chunk of a prefill resumed on its stored
+ * prefix (Section 5.1); both kinds may be in one batch.  o [T, Hq, D] and lse [T, Hq] as in pec_prefill_attn: a row that
+ * sees no key gets 0 and -inf; fp32 o is a partial fit for pec_attn_merge.  dtype PEC_BF16 runs the tensor cores (bf16 products,
+ * probabilities rounded to bf16, fp32 accumulation), PEC_F32 an fp32 FMA kernel with fp32 output.
+ * A value of a request that is not finite may spoil the rows of the same request that do not see it yet (0 * inf), never those
+ * of another request.
+ * max_q_len: an upper bound of the new tokens of any one request, 0 = none known (T); a request that brings more is a bad
+ * index.  It chooses the kernels: Hq / Hkv * max_q_len <= 128 needs only the one for few rows.
+ * workspace: device, 16-byte aligned, at least pec_paged_workspace_size() bytes; scratch for partial results of requests
+ * whose keys are worked on by several CTAs, undefined after the call.  How a request's keys are cut depends on the whole
+ * batch, and with it the last bits of its result; the same call gives the same bits.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE, CUDA.
+ */
+typedef struct {
+    const void *q;              /* device; 16-byte aligned                                      */
+    int64_t q_stride_t, q_stride_h;                                      /* elements; multiples of 16 bytes, >= D */
+    int32_t dtype;              /* pec_dtype of q and the cache                                 */
+    const void *k_pages, *v_pages;
+    int64_t k_pages_stride_p, k_pages_stride_t, k_pages_stride_h;
+    int64_t v_pages_stride_p, v_pages_stride_t, v_pages_stride_h;
+    int32_t page_size;
+    int64_t num_pages;
+    const int32_t *block_table;
+    int64_t table_stride;
+    int32_t max_pages;
+    const int32_t *cu_q, *kv_lens;
+    int32_t B;
+    int64_t T;
+    int32_t max_q_len;
+    void *o;                    /* device; [T, Hq, D] contiguous, 16-byte aligned               */
+    int32_t o_dtype;
+    float *lse;                 /* device; [T, Hq]                                              */
+    int32_t Hq, Hkv, D;         /* D must be 128; Hkv | Hq; Hq / Hkv <= 128                     */
+    int32_t causal;
+    float softmax_scale;        /* 0 selects 1/sqrt(D)                                          */
+    void *workspace;
+    size_t workspace_bytes;
+    int32_t *status;
+} pec_paged_args;
+
+int pec_paged_attn(const pec_paged_args *args, void *cuda_stream);
+
+/* Bytes of workspace pec_paged_attn needs for these arguments (0 if they are invalid): a function of T, B, Hq, Hkv, dtype,
+ * max_q_len, the causal flag and the current device's SM count, not of what the tables hold. */
+size_t pec_paged_workspace_size(const pec_paged_args *args);
 
 /*
  * Process-wide settings (the paper has no counterpart; they exist for operations and tests).

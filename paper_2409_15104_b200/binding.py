@@ -11,6 +11,7 @@ import torch
 
 PEC_OK = 0
 PEC_ERR_TIMEOUT = -6
+PEC_ERR_BAD_INDEX = -8
 PEC_BF16, PEC_F32 = 1, 2
 PEC_TILE_SKIP, PEC_TILE_PARTIAL, PEC_TILE_FULL = 0, 1, 2
 PEC_LAYOUT_ZIGZAG, PEC_LAYOUT_CONTIGUOUS = 0, 1
@@ -68,6 +69,60 @@ class pec_decode_args(ctypes.Structure):
     ]
 
 
+class pec_norm_rope_args(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p),
+        ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
+        ("k_stride_t", ctypes.c_int64), ("k_stride_h", ctypes.c_int64),
+        ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+        ("q_out_stride_t", ctypes.c_int64), ("q_out_stride_h", ctypes.c_int64),
+        ("k_out_stride_t", ctypes.c_int64), ("k_out_stride_h", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("T", ctypes.c_int64),
+        ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+        ("norm", ctypes.c_int32), ("eps", ctypes.c_float),
+        ("rope_table", ctypes.c_void_p), ("n_pos", ctypes.c_int64),
+        ("positions", ctypes.c_void_p), ("pos0", ctypes.c_int64),
+        ("status", ctypes.c_void_p),
+    ]
+
+
+_PAGED_FIELDS = [
+    ("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
+    ("k_pages_stride_p", ctypes.c_int64), ("k_pages_stride_t", ctypes.c_int64), ("k_pages_stride_h", ctypes.c_int64),
+    ("v_pages_stride_p", ctypes.c_int64), ("v_pages_stride_t", ctypes.c_int64), ("v_pages_stride_h", ctypes.c_int64),
+    ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int64),
+    ("block_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("max_pages", ctypes.c_int32),
+    ("cu_q", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p), ("B", ctypes.c_int32), ("T", ctypes.c_int64),
+]
+
+
+class pec_kv_append_args(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("k_stride_t", ctypes.c_int64), ("k_stride_h", ctypes.c_int64),
+        ("v_stride_t", ctypes.c_int64), ("v_stride_h", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), *_PAGED_FIELDS,
+        ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("k_weight", ctypes.c_void_p), ("norm", ctypes.c_int32), ("eps", ctypes.c_float),
+        ("rope_table", ctypes.c_void_p), ("n_pos", ctypes.c_int64),
+        ("status", ctypes.c_void_p),
+    ]
+
+
+class pec_paged_args(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), *_PAGED_FIELDS,
+        ("max_q_len", ctypes.c_int32),
+        ("o", ctypes.c_void_p), ("o_dtype", ctypes.c_int32), ("lse", ctypes.c_void_p),
+        ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("causal", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("status", ctypes.c_void_p),
+    ]
+
+
 class pec_sp_inputs(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in ("s", "d", "n_h", "n_kv", "d_h", "T", "G", "elem_bytes", "node_bw", "gpu_flops")]
 
@@ -94,7 +149,8 @@ class pec_plan(ctypes.Structure):
 EXPORTS = ("pec_prefill_attn", "pec_workspace_size", "pec_attn_merge", "pec_attn_merge_n", "pec_plan_partitions",
            "pec_last_error", "pec_decode_attn", "pec_decode_workspace_size", "pec_decode_attn_static", "pec_select_sp", "pec_linear",
            "pec_plan_ring", "pec_balance_batches", "pec_plan_worklist", "pec_worklist_block_m", "pec_control",
-           "pec_linear_merged", "pec_linear_rope", "pec_rope_table", "pec_rope_table_floats")
+           "pec_linear_merged", "pec_linear_rope", "pec_rope_table", "pec_rope_table_floats",
+           "pec_qk_norm_rope", "pec_kv_append", "pec_paged_attn", "pec_paged_workspace_size")
 PEC_CTL_WAIT_LIMIT_CYCLES, PEC_CTL_TEST_SKIP_LAST_LOAD = 1, 2
 PEC_DECODE_STATIC_SCRATCH_BYTES = 4 * 1024 * 1024
 PEC_MERGE_MAX_PARTS = 16
@@ -147,6 +203,14 @@ def load():
     lib.pec_linear_merged.argtypes = [ctypes.POINTER(ctypes.c_void_p), ctypes.POINTER(ctypes.c_void_p), ctypes.c_int32,
                                       ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64,
                                       ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]
+    lib.pec_qk_norm_rope.restype = ctypes.c_int
+    lib.pec_qk_norm_rope.argtypes = [ctypes.POINTER(pec_norm_rope_args), ctypes.c_void_p]
+    lib.pec_kv_append.restype = ctypes.c_int
+    lib.pec_kv_append.argtypes = [ctypes.POINTER(pec_kv_append_args), ctypes.c_void_p]
+    lib.pec_paged_attn.restype = ctypes.c_int
+    lib.pec_paged_attn.argtypes = [ctypes.POINTER(pec_paged_args), ctypes.c_void_p]
+    lib.pec_paged_workspace_size.restype = ctypes.c_size_t
+    lib.pec_paged_workspace_size.argtypes = [ctypes.POINTER(pec_paged_args)]
     lib.pec_select_sp.restype = ctypes.c_int
     lib.pec_select_sp.argtypes = [ctypes.POINTER(pec_sp_inputs), ctypes.POINTER(pec_sp_choice)]
     lib.pec_plan_ring.restype = ctypes.c_int
@@ -208,7 +272,8 @@ def check_status(device=None):
     code = int(w.item())
     if code != 0:
         w.zero_()
-        raise PecError(code, "a kernel's bounded wait expired" if code == PEC_ERR_TIMEOUT else "kernel status")
+        raise PecError(code, {PEC_ERR_TIMEOUT: "a kernel's bounded wait expired",
+                              PEC_ERR_BAD_INDEX: "a kernel met a page number, position or offset out of range"}.get(code, "kernel status"))
 
 
 def pec_prefill_attn(q, k, v, *, seq_len=None, chunk_start=0, chunk_len=None, kv_len=None,
@@ -444,6 +509,198 @@ def pec_linear_merged(o_parts, lse_parts, w, y=None, stream=None):
     _check(lib.pec_linear_merged(op, lp, n, rows, Hq, D, w.data_ptr(), w.stride(0), y.data_ptr(), y.stride(0), N,
                                  status_word(w.device).data_ptr(), _stream_ptr(stream)))
     return y
+
+
+def _need(ok, text):
+    if not ok:
+        raise ValueError(text)
+
+
+def _on(t, what, dtype, dims, device):
+    """Checks that the library cannot make: a tensor of this type and rank on this device, innermost dimension contiguous."""
+    _need(isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype and t.dim() == dims,
+          f"{what}: need a {dims}-dimensional {dtype} tensor on {device}")
+    _need(t.shape[-1] <= 1 or t.stride(-1) == 1, f"{what}: the innermost dimension must be contiguous")
+
+
+def _strides(t, n):
+    """Strides of the first n dimensions; a dimension of one entry has no stride of its own, whatever torch says."""
+    st, sh = t.stride(), t.shape
+    return [st[i] if sh[i] > 1 else 128 for i in range(n)]
+
+
+def _ready_status(device):
+    """The status word; it must exist before a capture, where its zeroing would become part of the graph."""
+    _need(device.index in _status_words or not torch.cuda.is_current_stream_capturing(),
+          "call status_word() once on this device before capturing")
+    return status_word(device).data_ptr()
+
+
+class _Launch:
+    """Makes `device` current, and `stream` (when given) too, so that outputs and workspaces allocated for the call belong to it."""
+
+    def __init__(self, device, stream):
+        _need(device.type == "cuda", "tensors must be on a CUDA device")
+        self.contexts = []
+        if device.index != torch.cuda.current_device():
+            self.contexts.append(torch.cuda.device(device))
+        if stream is not None:
+            _need(stream.device == device, "the stream belongs to another device")
+            self.contexts.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        for c in self.contexts:
+            c.__enter__()
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        for c in reversed(self.contexts):
+            c.__exit__(*exc)
+
+
+def _rope(tables, device):
+    if tables is None:
+        return None, 0
+    table, n_pos = tables
+    _on(table, "tables", torch.float32, 1, device)
+    _need(table.numel() >= load().pec_rope_table_floats(n_pos), "tables: the table is shorter than n_pos asks for")
+    return table.data_ptr(), n_pos
+
+
+def _weight(w, what, norm, dtype, device):
+    if w is None:
+        return None
+    _need(norm, f"{what}: a weight needs norm=True")
+    _on(w, what, dtype, 1, device)
+    _need(w.numel() == 128, f"{what}: need 128 entries")
+    return w.data_ptr()
+
+
+def pec_qk_norm_rope(q, k=None, *, norm=True, q_weight=None, k_weight=None, eps=1e-6, tables=None, positions=None, pos0=0,
+                     q_out=None, k_out=None, inplace=False, stream=None):
+    """RMS norm of every head (norm=True) and rotary encoding (tables = pec_rope_table(...)) in one pass; returns (q_out, k_out).
+
+    q [T, Hq, 128], k [T, Hkv, 128] or None: CUDA tensors of one type (bf16 or fp32), last dimension contiguous (column slices
+    of a fused projection are fine).  Token t is at positions[t] (int32 CUDA tensor; negative: padding, its rows are not
+    written) or at pos0 + t.  inplace=True writes into q and k.
+    """
+    lib = load()
+    dev, dt = q.device, q.dtype
+    code = _dtype_code(dt)
+    with _Launch(dev, stream) as handle:
+        _on(q, "q", dt, 3, dev)
+        T, Hq, D = q.shape
+        q_out = (q if inplace else torch.empty((T, Hq, D), dtype=dt, device=dev)) if q_out is None else q_out
+        _on(q_out, "q_out", dt, 3, dev)
+        _need(q_out.shape == q.shape, "q_out: need q's shape")
+        side_k = (None, 0, 0, None, 0, 0, 0)
+        if k is not None:
+            _on(k, "k", dt, 3, dev)
+            _need(k.shape[0] == T and k.shape[2] == D, "k: need q's tokens and head dimension")
+            k_out = (k if inplace else torch.empty(k.shape, dtype=dt, device=dev)) if k_out is None else k_out
+            _on(k_out, "k_out", dt, 3, dev)
+            _need(k_out.shape == k.shape, "k_out: need k's shape")
+            side_k = (k.data_ptr(), *_strides(k, 2), k_out.data_ptr(), *_strides(k_out, 2), k.shape[1])
+        if positions is not None:
+            _on(positions, "positions", torch.int32, 1, dev)
+            _need(positions.numel() == T, "positions: need one per token")
+        table, n_pos = _rope(tables, dev)
+        if T == 0 or Hq + side_k[6] == 0:                     # tensors without elements have no address
+            return q_out, k_out
+        a = pec_norm_rope_args(q.data_ptr(), side_k[0], *_strides(q, 2), side_k[1], side_k[2], q_out.data_ptr(), side_k[3],
+                               *_strides(q_out, 2), side_k[4], side_k[5], code, Hq, side_k[6], D, T,
+                               _weight(q_weight, "q_weight", norm, dt, dev), _weight(k_weight, "k_weight", norm, dt, dev),
+                               1 if norm else 0, eps, table, n_pos, positions.data_ptr() if positions is not None else None, pos0,
+                               _ready_status(dev))
+        _check(lib.pec_qk_norm_rope(ctypes.byref(a), handle))
+    return q_out, k_out
+
+
+def _paged(k_pages, v_pages, block_table, cu_q, kv_lens, T, dtype, device):
+    """The checked cache and batch fields of the paged calls, in the order of _PAGED_FIELDS."""
+    _on(k_pages, "k_pages", dtype, 4, device)
+    _on(v_pages, "v_pages", dtype, 4, device)
+    _on(block_table, "block_table", torch.int32, 2, device)
+    _on(cu_q, "cu_q", torch.int32, 1, device)
+    _on(kv_lens, "kv_lens", torch.int32, 1, device)
+    B = kv_lens.shape[0]
+    num_pages, page_size = k_pages.shape[:2]
+    _need(v_pages.shape == k_pages.shape, "v_pages: need k_pages' shape")
+    _need(cu_q.shape[0] == B + 1 and block_table.shape[0] == B, "need cu_q [B + 1], kv_lens [B] and block_table [B, pages]")
+    return (k_pages.data_ptr(), v_pages.data_ptr(), *_strides(k_pages, 3), *_strides(v_pages, 3), page_size, num_pages,
+            block_table.data_ptr(), block_table.stride(0) if B > 1 else block_table.shape[1], block_table.shape[1],
+            cu_q.data_ptr(), kv_lens.data_ptr(), B, T)
+
+
+def pec_kv_append(k, v, k_pages, v_pages, block_table, cu_q, kv_lens, *, norm=False, k_weight=None, eps=1e-6, tables=None,
+                  stream=None):
+    """Appends a batch's new keys (normalised with norm=True, rotated with tables) and values to a paged cache.
+
+    k, v [T, Hkv, 128]; k_pages, v_pages [pages, page_size, Hkv, 128] (any strides but the last: transpose head-major pages
+    into this order); block_table int32 [B, pages per request], cu_q int32 [B + 1] offsets of the requests' new tokens in k, v,
+    kv_lens int32 [B] cached tokens including the new ones.  All CUDA tensors; the tables are read when the kernel runs.
+    """
+    lib = load()
+    dev, dt = k.device, k.dtype
+    code = _dtype_code(dt)
+    with _Launch(dev, stream) as handle:
+        _on(k, "k", dt, 3, dev)
+        _on(v, "v", dt, 3, dev)
+        T, Hkv, D = k.shape
+        _need(v.shape == k.shape, "v: need k's shape")
+        cache = _paged(k_pages, v_pages, block_table, cu_q, kv_lens, T, dt, dev)
+        _need(k_pages.shape[2] == Hkv and k_pages.shape[3] == D, "k_pages: need k's heads and head dimension")
+        table, n_pos = _rope(tables, dev)
+        if T == 0:                                            # tensors without elements have no address
+            return
+        a = pec_kv_append_args(k.data_ptr(), v.data_ptr(), *_strides(k, 2), *_strides(v, 2), code, *cache, Hkv, D,
+                               _weight(k_weight, "k_weight", norm, dt, dev), 1 if norm else 0, eps, table, n_pos,
+                               _ready_status(dev))
+        _check(lib.pec_kv_append(ctypes.byref(a), handle))
+
+
+def pec_paged_attn(q, k_pages, v_pages, block_table, cu_q, kv_lens, *, max_q_len=0, causal=True, softmax_scale=0.0,
+                   out_dtype=None, o=None, lse=None, workspace=None, stream=None):
+    """Attention of a batch's new tokens q [T, Hq, 128] over a paged cache that holds their keys and values already (see
+    pec_kv_append for the cache and the tables); returns (o [T, Hq, 128], lse [T, Hq]).
+
+    max_q_len: an upper bound of any request's new tokens (0: unknown); the kernels are chosen by it.  workspace: uint8 CUDA
+    tensor of at least the size the library asks for, allocated here when not given.
+    """
+    lib = load()
+    dev, dt = q.device, q.dtype
+    code = _dtype_code(dt)
+    with _Launch(dev, stream) as handle:
+        _on(q, "q", dt, 3, dev)
+        T, Hq, D = q.shape
+        cache = _paged(k_pages, v_pages, block_table, cu_q, kv_lens, T, dt, dev)
+        _need(k_pages.shape[3] == D, "k_pages: need q's head dimension")
+        if o is None:
+            o = torch.empty((T, Hq, D), dtype=dt if out_dtype is None else out_dtype, device=dev)
+        if lse is None:
+            lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
+        _need(o.device == dev and o.is_contiguous() and o.shape == q.shape and (out_dtype is None or o.dtype == out_dtype),
+              "o: need a contiguous tensor of q's shape")
+        _need(lse.device == dev and lse.is_contiguous() and lse.dtype == torch.float32 and lse.shape == (T, Hq),
+              "lse: need a contiguous fp32 tensor [T, Hq]")
+        if T == 0:                                            # tensors without elements have no address
+            return o, lse
+        a = pec_paged_args(q.data_ptr(), *_strides(q, 2), code, *cache, max_q_len, o.data_ptr(), _dtype_code(o.dtype),
+                           lse.data_ptr(), Hq, k_pages.shape[2], D, 1 if causal else 0, softmax_scale, None, 0, _ready_status(dev))
+        ref = ctypes.byref(a)
+        if workspace is None:
+            need = lib.pec_paged_workspace_size(ref)
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        if workspace is not None:
+            _need(workspace.device == dev and workspace.is_contiguous(), "workspace: need a contiguous tensor on q's device")
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _check(lib.pec_paged_attn(ref, handle))
+    return o, lse
+
+
+def pec_paged_workspace_size(a) -> int:
+    """Bytes of workspace for a filled pec_paged_args."""
+    return int(load().pec_paged_workspace_size(ctypes.byref(a)))
 
 
 def pec_select_sp(s, d, n_h, n_kv, d_h, T, G, elem_bytes=2.0, node_bw=1.0, gpu_flops=1.0):

@@ -1,0 +1,217 @@
+// How a batch's work is cut for the kernels behind pec_paged_attn, worked out on the device by every CTA from the tables
+// themselves (no host plan: a captured graph replays with whatever lengths the tables then hold).
+//
+// Query rows are packed: the g = Hq / Hkv heads of a KV head and the new tokens of a request are the rows of one matrix,
+// row = token * g + head of the group, so that a key tile read once serves all of them.
+//
+// Two classes of requests, by their packed rows n * g:
+//   few  (at most 128: decode steps)  worked on by a persistent grid.  The key tiles of all (request, KV head) pairs lie on
+//        one line that is cut into equal pieces, one per CTA; a pair that crosses a cut leaves one partial result per piece.
+//   many (chunks)                     blocks of rows, each block's keys cut into slices where a unit of work would be longer
+//        than an SM's fair share of the whole.
+// Partials are merged by their LSE by one kernel for both classes (combine), which finds them by the same arithmetic.
+#pragma once
+#include "pec_internal.h"
+#include "pec_paged.h"
+
+namespace pec {
+namespace paged {
+
+constexpr int kKeyTile = 128;                 // keys per tile
+constexpr int kFewRows = 128;                 // packed rows of the few class
+constexpr int kMinSliceTiles = 4;             // shortest slice of the many class: its partial costs as much traffic as 1-2 tiles
+constexpr int64_t kNoSplit = (int64_t)1 << 40;
+
+// Device-side description of one call, passed to the kernels by value.
+struct Params {
+    const void *q, *k_pages, *v_pages;
+    int64_t q_st, q_sh;
+    PagedCache c;
+    void *o;
+    float *lse;
+    int32_t o_is_bf16;
+    int32_t Hq, Hkv, g;
+    int32_t causal;
+    float scale_log2;
+    int32_t max_q;                            // a request with more new tokens is a bad index
+    int32_t *status;
+    int64_t wait_cycles;
+    // few class
+    int32_t few;                              // 0: every request is of the many class (fp32)
+    int32_t few_ctas;
+    int32_t few_rows;                         // rows of a partial slot
+    float *few_o, *few_lse;                   // [2 * few_ctas][few_rows][128], [..][few_rows]
+    // many class: blocks of a request = ceil(n * blk_mul / blk_div)
+    int32_t blk_mul, blk_div;
+    int32_t many_slots;                       // fair share = all tiles / many_slots
+    int32_t many_rows;                        // rows of a partial slot
+    int32_t many_cap;                         // slots that the workspace holds
+    float *many_o, *many_lse;
+};
+
+struct Request {
+    int32_t start, n, kv;                     // first packed token row, new tokens, cached tokens
+    __device__ __forceinline__ int32_t pos0() const { return kv - n; }
+    __device__ __forceinline__ int32_t tiles() const { return kv > 0 ? (kv + kKeyTile - 1) / kKeyTile : 1; }
+};
+
+// The request's entry in the tables, checked: anything out of range is reported and gives a request without new tokens.
+__device__ __forceinline__ Request load_request(const Params &p, int b)
+{
+    Request r;
+    const int64_t start = p.c.cu_q[b], end = p.c.cu_q[b + 1], kv = p.c.kv_lens[b], n = end - start;
+    if (start < 0 || n < 0 || end > p.c.T || kv < 0 || n > p.max_q || kv > (int64_t)p.c.max_pages * p.c.page_size) {
+        raise_status(p.status, PEC_ERR_BAD_INDEX);
+        r.start = 0; r.n = 0; r.kv = 0;
+        return r;
+    }
+    r.start = (int32_t)start; r.n = (int32_t)n; r.kv = (int32_t)kv;
+    return r;
+}
+__device__ __forceinline__ bool is_few(const Params &p, const Request &r) { return p.few && r.n > 0 && (int64_t)r.n * p.g <= kFewRows; }
+__device__ __forceinline__ bool is_many(const Params &p, const Request &r) { return r.n > 0 && !is_few(p, r); }
+__device__ __forceinline__ int32_t blocks_of(const Params &p, const Request &r) { return (int32_t)(((int64_t)r.n * p.blk_mul + p.blk_div - 1) / p.blk_div); }
+
+__device__ __forceinline__ int64_t warp_sum(int64_t v)
+{
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+__device__ __forceinline__ int64_t warp_prefix(int64_t v, int lane)    // inclusive
+{
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t up = __shfl_up_sync(0xffffffffu, v, d);
+        if (lane >= d) v += up;
+    }
+    return v;
+}
+
+// Key tiles of the whole batch, per KV head.  One converged warp.
+__device__ __forceinline__ void batch_tiles(const Params &p, int64_t &few, int64_t &many)
+{
+    const int lane = threadIdx.x & 31;
+    few = many = 0;
+    for (int b = lane; b < p.c.B; b += 32) {
+        const Request r = load_request(p, b);
+        if (is_few(p, r)) few += r.tiles();
+        else if (is_many(p, r)) many += (int64_t)blocks_of(p, r) * r.tiles();
+    }
+    few = warp_sum(few);
+    many = warp_sum(many);
+}
+// few: tiles per CTA.  many: tiles per slice; a request is cut into ceil(tiles / slice) slices of equal length.
+// Slots that split requests take: each has tiles > S, so ceil(tiles / S) < 2 tiles / S, and S >= many * Hkv / many_slots makes
+// the sum over all of them, times Hkv, less than 2 * many_slots.
+__device__ __forceinline__ int64_t few_piece(const Params &p, int64_t few)
+{
+    const int64_t all = few * p.Hkv;
+    return all > 0 ? (all + p.few_ctas - 1) / p.few_ctas : 1;
+}
+__device__ __forceinline__ int64_t many_slice(const Params &p, int64_t many)
+{
+    const int64_t s = (many * p.Hkv + p.many_slots - 1) / p.many_slots;
+    return s < kMinSliceTiles ? kMinSliceTiles : s;
+}
+__device__ __forceinline__ int32_t slices_of(const Request &r, int64_t slice) { return (int32_t)((r.tiles() + slice - 1) / slice); }
+
+// One item of the many class: rows of one request's block against one slice of its keys (for one KV head, the grid's y).
+struct Item {
+    Request r;
+    int32_t b, block, slices;
+    int32_t key_lo, key_hi;                   // key positions of the slice
+    int64_t slot;                             // partial slot of KV head 0 (slot * Hkv + kvh), where slices > 1
+};
+// Item `idx`; one converged warp, every lane returns the same.  False past the last item.
+__device__ __forceinline__ bool locate_many(const Params &p, int64_t idx, Item &it)
+{
+    const int lane = threadIdx.x & 31;
+    int64_t few, many;
+    batch_tiles(p, few, many);
+    if (many == 0) return false;
+    const int64_t slice = many_slice(p, many);
+    int64_t before = 0, slots = 0;            // items and partial slots of earlier groups of 32 requests
+    for (int b0 = 0; b0 < p.c.B; b0 += 32) {
+        Request r;
+        r.start = r.n = r.kv = 0;
+        if (b0 + lane < p.c.B) r = load_request(p, b0 + lane);
+        int64_t items = 0, mine = 0;
+        int32_t ns = 0;
+        if (is_many(p, r)) {
+            ns = slices_of(r, slice);
+            items = (int64_t)blocks_of(p, r) * ns;
+            mine = ns > 1 ? items : 0;
+        }
+        const int64_t incl = warp_prefix(items, lane), incl_s = warp_prefix(mine, lane);
+        const unsigned who = __ballot_sync(0xffffffffu, idx >= before + incl - items && idx < before + incl);
+        if (who) {
+            const int src = __ffs(who) - 1;
+            it.b = b0 + src;
+            it.r.start = __shfl_sync(0xffffffffu, r.start, src);
+            it.r.n = __shfl_sync(0xffffffffu, r.n, src);
+            it.r.kv = __shfl_sync(0xffffffffu, r.kv, src);
+            it.slices = __shfl_sync(0xffffffffu, ns, src);
+            const int64_t at = idx - __shfl_sync(0xffffffffu, before + incl - items, src);
+            const int64_t first_slot = __shfl_sync(0xffffffffu, slots + incl_s - mine, src);
+            // The last block sees the most keys: it goes first.
+            const int32_t nb = blocks_of(p, it.r), blk = (int32_t)(at / it.slices), sl = (int32_t)(at % it.slices);
+            it.block = nb - 1 - blk;
+            const int32_t per = (it.r.tiles() + it.slices - 1) / it.slices;
+            it.key_lo = min((int64_t)sl * per * kKeyTile, (int64_t)it.r.kv);
+            it.key_hi = min((int64_t)(sl + 1) * per * kKeyTile, (int64_t)it.r.kv);
+            it.slot = first_slot + (int64_t)it.block * it.slices + sl;
+            return true;
+        }
+        before += __shfl_sync(0xffffffffu, incl, 31);
+        slots += __shfl_sync(0xffffffffu, incl_s, 31);
+    }
+    return false;
+}
+
+// Where the partials of a token's request lie, for the combining kernel.  One converged warp.
+struct Parts {
+    int32_t count;                            // 1: the result is in place already
+    // few: slots of KV head kvh are 2 c (+ 1 in the first CTA if its piece began with another unit), c = c0 .. c0 + count - 1
+    // many: slots (first + s) * Hkv + kvh
+    int64_t first;
+};
+__device__ __forceinline__ Parts parts_many(const Params &p, int b, const Request &r, int32_t block)
+{
+    const int lane = threadIdx.x & 31;
+    int64_t few, many;
+    batch_tiles(p, few, many);
+    const int64_t slice = many_slice(p, many);
+    Parts out;
+    out.count = slices_of(r, slice);
+    out.first = 0;
+    if (out.count <= 1) return out;
+    int64_t slots = 0;
+    for (int i = lane; i < b; i += 32) {
+        const Request x = load_request(p, i);
+        if (is_many(p, x)) {
+            const int32_t ns = slices_of(x, slice);
+            if (ns > 1) slots += (int64_t)blocks_of(p, x) * ns;
+        }
+    }
+    out.first = warp_sum(slots) + (int64_t)block * out.count;
+    return out;
+}
+// Tiles on the few class's line before request b.
+__device__ __forceinline__ int64_t few_before(const Params &p, int b)
+{
+    int64_t t = 0;
+    for (int i = threadIdx.x & 31; i < b; i += 32) {
+        const Request x = load_request(p, i);
+        if (is_few(p, x)) t += x.tiles();
+    }
+    return warp_sum(t) * p.Hkv;
+}
+
+}  // namespace paged
+
+// Launchers (each returns a pec_status).
+int launch_paged_simple(const paged::Params &p, int32_t dtype, int64_t items, cudaStream_t stream);
+int launch_paged_combine(const paged::Params &p, cudaStream_t stream);
+
+}  // namespace pec

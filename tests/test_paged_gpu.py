@@ -1,0 +1,398 @@
+"""The paged serving calls on the GPU against 64-bit references: head norm with rotation, cache append, paged attention, and a
+serving step made of them."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paged_reference as ref
+from paper_2409_15104_b200 import binding, workloads
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+THETA = 500000.0
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def dev(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+# ------------------------------------------------------------------------------------------ norm and rotation
+def check_heads(got, x, weight, positions, dtype, norm, turn, skip=(), before=None):
+    want, size = ref.norm_rope(x, weight, 1e-6, positions, THETA, norm, turn)
+    off = np.abs(got.double().cpu().numpy() - want)
+    bound = ref.norm_rope_bound(want, size, dtype) + 1e-37
+    keep = [t for t in range(x.shape[0]) if t not in skip]
+    assert (off[keep] <= bound[keep]).all(), float((off / bound)[keep].max())
+    for t in skip:
+        assert torch.equal(got[t], before[t])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,hq,hkv", [(1, 1, 1), (1, 32, 8), (3, 5, 1), (64, 32, 8), (257, 8, 8), (1000, 64, 8), (5, 100, 3), (2048, 2, 1)])
+@pytest.mark.parametrize("norm,turn", [(True, True), (False, True), (True, False)])
+def test_norm_rope(pec, dtype, T, hq, hkv, norm, turn):
+    n_pos = 200000
+    tables = pec.pec_rope_table(THETA, n_pos, DEV) if turn else None
+    g = torch.Generator().manual_seed(T * 100 + hq)
+    qkv = torch.randn((T, hq + 2 * hkv, 128), generator=g).to(dtype).to(DEV)
+    q, k = qkv[:, :hq], qkv[:, hq:hq + hkv]
+    qw, kw = [(1 + 0.2 * torch.randn(128, generator=g)).to(dtype).to(DEV) for _ in range(2)] if norm else (None, None)
+    pos = torch.randint(0, n_pos, (T,), generator=g).int()
+    skip = [t for t in range(T) if t % 7 == 5]
+    pos[skip] = -1
+    qo = torch.full((T, hq, 128), 7.0, dtype=dtype, device=DEV)
+    ko = torch.full((T, hkv, 128), 7.0, dtype=dtype, device=DEV)
+    before = qkv.clone()
+    pec.pec_qk_norm_rope(q, k, norm=norm, q_weight=qw, k_weight=kw, tables=tables, positions=pos.to(DEV), q_out=qo, k_out=ko)
+    pec.check_status()
+    seven = torch.full((T, 128, 128), 7.0, dtype=dtype, device=DEV)
+    p = pos.clamp(min=0).numpy()
+    check_heads(qo, q, qw, p, dtype, norm, turn, skip, seven[:, :hq])
+    check_heads(ko, k, kw, p, dtype, norm, turn, skip, seven[:, :hkv])
+    assert torch.equal(qkv, before)
+    # in place, on slices of the fused tensor: the same bits, and the value columns as they were
+    pec.pec_qk_norm_rope(q, k, norm=norm, q_weight=qw, k_weight=kw, tables=tables, positions=pos.to(DEV), inplace=True)
+    keep = [t for t in range(T) if t not in skip]
+    assert torch.equal(q[keep], qo[keep]) and torch.equal(k[keep], ko[keep])
+    assert torch.equal(qkv[:, hq + hkv:], before[:, hq + hkv:]) and torch.equal(qkv[skip], before[skip])
+
+
+def test_norm_rope_of_queries_alone_at_a_chunks_positions(pec):
+    tables = pec.pec_rope_table(THETA, 5000, DEV)
+    q = torch.randn((100, 6, 128), device=DEV)
+    out, none = pec.pec_qk_norm_rope(q, norm=False, tables=tables, pos0=4900)
+    assert none is None
+    check_heads(out, q, None, np.arange(4900, 5000), F32, False, True)
+    with pytest.raises(binding.PecError):
+        pec.pec_qk_norm_rope(q, norm=False, tables=tables, pos0=4901)
+
+
+def test_norm_rope_extreme_values(pec):
+    """Zero heads stay zero; large and tiny magnitudes are normalised; a head that is not finite spoils no other."""
+    x = torch.randn((6, 2, 128), device=DEV).to(BF16)
+    x[0] = 0
+    x[1] *= 1e15
+    x[2] *= 1e-15
+    x[3, 0, 5] = float("nan")
+    x[4, 1, 77] = float("inf")
+    out, _ = pec.pec_qk_norm_rope(x, tables=pec.pec_rope_table(THETA, 64, DEV), pos0=3)
+    assert (out[0] == 0).all() and torch.isnan(out[3, 0]).all()
+    for t, h in [(1, 0), (2, 1), (3, 1), (4, 0), (5, 0)]:
+        check_heads(out[t:t + 1, h:h + 1], x[t:t + 1, h:h + 1], None, [3 + t], BF16, True, True)
+
+
+def test_norm_rope_reports_positions_past_the_table(pec):
+    tables = pec.pec_rope_table(THETA, 100, DEV)
+    q = torch.randn((4, 2, 128), device=DEV)
+    out = torch.full_like(q, 7.0)
+    pec.pec_qk_norm_rope(q, tables=tables, positions=dev([3, 100, 99, 2 ** 31 - 1]), q_out=out)
+    with pytest.raises(binding.PecError) as e:
+        pec.check_status()
+    assert e.value.code == binding.PEC_ERR_BAD_INDEX
+    assert (out[[1, 3]] == 7.0).all() and not (out[[0, 2]] == 7.0).any()
+    pec.check_status()
+
+
+# ------------------------------------------------------------------------------------------ append
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,kv,page,hkv,head_major", [
+    ([1], [1], 16, 1, False), ([1] * 40, list(range(1, 41)), 16, 8, False), ([5, 0, 1, 33, 0], [5, 9, 64, 100, 0], 24, 3, True),
+    ([200, 3], [200, 130], 128, 2, False), ([1] * 33 + [70], [17 * (i % 9) + 1 for i in range(33)] + [1000], 8, 4, True),
+])
+@pytest.mark.parametrize("norm,turn", [(False, True), (True, True), (False, False)])
+def test_append(pec, dtype, n, kv, page, hkv, head_major, norm, turn):
+    kp, vp, table = ref.make_cache(11, kv, page, hkv, dtype, DEV, head_major, poison=False)
+    k0, v0 = kp.clone(), vp.clone()
+    cu = ref.offsets(n)
+    T = cu[-1] + 3                                                # three rows of padding
+    g = torch.Generator().manual_seed(7)
+    kvs = torch.randn((T, 2 * hkv, 128), generator=g).to(dtype).to(DEV)
+    k, v = kvs[:, :hkv], kvs[:, hkv:]
+    w = (1 + 0.2 * torch.randn(128, generator=g)).to(dtype).to(DEV) if norm else None
+    tables = pec.pec_rope_table(THETA, 2000, DEV) if turn else None
+    pec.pec_kv_append(k, v, kp, vp, table, dev(cu), dev(kv), norm=norm, k_weight=w, tables=tables)
+    pec.check_status()
+    seen = torch.zeros(kp.shape[:2], dtype=torch.bool, device=DEV)
+    for b in range(len(n)):
+        for i in range(n[b]):
+            pos, t = kv[b] - n[b] + i, cu[b] + i
+            pg, slot = int(table[b, pos // page]), pos % page
+            seen[pg, slot] = True
+            assert torch.equal(vp[pg, slot], v[t])
+            if norm or turn:
+                check_heads(kp[pg, slot][None], k[t:t + 1], w, [pos], dtype, norm, turn)
+            else:
+                assert torch.equal(kp[pg, slot], k[t])
+    assert torch.equal(kp[~seen], k0[~seen]) and torch.equal(vp[~seen], v0[~seen])
+
+
+def test_append_reports_what_is_out_of_range_and_stores_the_rest(pec):
+    page, hkv = 16, 2
+    kp, vp, table = ref.make_cache(12, [40, 40, 40, 40], page, hkv, F32, DEV, poison=False)
+    k0 = kp.clone()
+    table[1, 2] = kp.shape[0]                                     # one page past the cache
+    table[2, 2] = -1
+    k, v = torch.randn((4, hkv, 128), device=DEV), torch.randn((4, hkv, 128), device=DEV)
+    kv = dev([40, 40, 40, 4000])                                  # the last one's position is past its row of the table
+    pec.pec_kv_append(k, v, kp, vp, table, dev([0, 1, 2, 3, 4]), kv)
+    with pytest.raises(binding.PecError) as e:
+        pec.check_status()
+    assert e.value.code == binding.PEC_ERR_BAD_INDEX
+    at = (int(table[0, 2]), 39 % page)
+    assert torch.equal(kp[at], k[0])
+    k0[at] = k[0]
+    assert torch.equal(kp, k0)
+    for cu, lens in (([0, 3, 1, 4, 4], [40] * 4), ([0, 1, 2, 3, 9], [40] * 4), ([0, 4, 4, 4, 4], [2, 1, 1, 1])):
+        pec.pec_kv_append(k, v, kp, vp, table.clamp(0, kp.shape[0] - 1), dev(cu), dev(lens))
+        with pytest.raises(binding.PecError):
+            pec.check_status()
+
+
+# ------------------------------------------------------------------------------------------ attention
+def attend(pec, seed, n, kv, hq, hkv, page, dtype, *, head_major=False, causal=True, out_dtype=None, pad=0, fused=False, known=True,
+           scale=0.0, what=""):
+    kp, vp, table = ref.make_cache(seed, kv, page, hkv, dtype, DEV, head_major)
+    cu = ref.offsets(n)
+    T = cu[-1] + pad
+    g = torch.Generator().manual_seed(seed + 1)
+    q = torch.randn((T, hq + (2 if fused else 0), 128), generator=g).to(dtype).to(DEV)[:, :hq]
+    out_dtype = dtype if out_dtype is None else out_dtype
+    o = torch.full((T, hq, 128), 7.0, dtype=out_dtype, device=DEV)
+    lse = torch.full((T, hq), 7.0, device=DEV)
+    call = lambda: pec.pec_paged_attn(q, kp, vp, table, dev(cu), dev(kv), max_q_len=max(n) if known else 0, causal=causal, softmax_scale=scale, o=o, lse=lse)
+    call()
+    pec.check_status()
+    want = ref.attend(q, kp, vp, table, cu, kv, causal, scale or None)
+    if pad:
+        assert (o[cu[-1]:] == 7.0).all() and (lse[cu[-1]:] == 7.0).all(), "padding rows were written"
+    ref.check_attend(o, lse, want, dtype, what)
+    first = (o.clone(), lse.clone())
+    call()
+    assert torch.equal(first[0], o) and torch.equal(first[1], lse), "the same call gave other bits"
+    return o, lse
+
+
+SHAPES = [
+    # n, kv, hq, hkv, page
+    ([1], [1], 1, 1, 16), ([1], [1], 8, 1, 8), ([1], [128], 4, 4, 16), ([1], [129], 8, 2, 16), ([1], [127], 16, 2, 128),
+    ([1], [0], 4, 2, 16),                                          # a token before its request's first position: sees nothing
+    ([3], [1], 4, 2, 16), ([5, 2], [0, 1], 8, 8, 16),              # leading rows that see nothing
+    ([1] * 7, [1, 2, 63, 64, 65, 300, 1000], 32, 8, 16), ([1] * 64, [37 * (i % 11) + 1 for i in range(64)], 8, 2, 48),
+    ([1] * 70, [(i * i) % 700 + 1 for i in range(70)], 4, 1, 64), ([1, 0, 1, 0, 0], [500, 30, 0, 0, 700], 8, 4, 24),
+    ([4, 1, 2, 3], [400, 129, 128, 131], 14, 2, 16), ([18], [200], 7, 1, 136), ([42], [170], 3, 1, 32), ([128], [128], 1, 1, 16),
+    ([1], [5000], 64, 8, 128), ([2], [9000], 5, 1, 256), ([1], [20000], 8, 1, 16), ([1, 1], [1, 12000], 16, 2, 64),
+    ([1], [700], 128, 1, 16), ([2], [300], 128, 1, 40), ([1], [300], 67, 1, 16),
+    ([129], [129], 1, 1, 16), ([130], [500], 4, 4, 16), ([200], [200], 8, 2, 16), ([33], [1000], 32, 8, 64), ([300], [1000], 8, 8, 24),
+    ([257, 1, 100, 0, 64], [257, 900, 1100, 50, 64], 8, 2, 48), ([100], [3000], 7, 1, 104), ([513], [2049], 4, 2, 128),
+    ([40, 1, 1, 90], [6000, 3000, 10, 95], 16, 2, 16), ([150], [100], 4, 2, 16), ([3, 300], [9000, 310], 8, 1, 8),
+]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("i", range(len(SHAPES)))
+def test_paged_attention(pec, dtype, i):
+    n, kv, hq, hkv, page = SHAPES[i]
+    attend(pec, 100 + i, n, kv, hq, hkv, page, dtype, head_major=i % 2 == 1, pad=i % 3, fused=i % 2 == 0, known=i % 4 != 3,
+           what=f"{n} of {kv}, {hq}/{hkv} heads, pages of {page}"[:120])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("i", [1, 3, 5, 6, 12, 17, 26, 28, 31])
+def test_paged_attention_without_the_causal_mask(pec, dtype, i):
+    n, kv, hq, hkv, page = SHAPES[i]
+    attend(pec, 300 + i, n, kv, hq, hkv, page, dtype, causal=False, what=f"not causal, {n} of {kv}"[:100])
+
+
+@pytest.mark.parametrize("i", [2, 8, 16, 18, 24, 28, 30, 31])
+def test_paged_attention_fp32_output_and_scale(pec, i):
+    n, kv, hq, hkv, page = SHAPES[i]
+    attend(pec, 400 + i, n, kv, hq, hkv, page, BF16, out_dtype=F32, scale=0.3, what=f"fp32 output, {n} of {kv}"[:100])
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_paged_attention_random_batches(pec, seed):
+    r = np.random.RandomState(seed)
+    g, hkv = int(r.choice([1, 2, 3, 4, 5, 7, 8, 16])), int(r.choice([1, 2, 4]))
+    B = int(r.randint(1, 20))
+    n = [int(x) for x in r.choice([0, 1, 1, 1, 2, 7, 40, 150], B)]
+    if sum(n) == 0:
+        n[0] = 1
+    kv = [int(m + r.choice([0, 1, 5, 127, 128, 400, 2000])) for m in n]
+    attend(pec, 500 + seed, n, kv, g * hkv, hkv, 8 * int(r.randint(1, 33)), BF16 if seed % 3 else F32, head_major=bool(r.randint(2)),
+           pad=int(r.randint(4)), known=bool(r.randint(2)), what=f"random {seed}")
+
+
+def test_moving_maxima_and_large_scores(pec):
+    """Scores that grow along the keys move the running maximum in every tile; scores near +-1e4 stay exact enough."""
+    for dtype in (F32, BF16):
+        for n in (1, 130):
+            kp, vp, table = ref.make_cache(9, [1500], 16, 1, dtype, DEV)
+            q = torch.randn((n, 4, 128), device=DEV).to(dtype)
+            ids = table[0, :94].long()
+            ramp = torch.linspace(0.1, 40.0, 94 * 16, device=DEV).view(94, 16, 1, 1)
+            kp[ids] = (kp[ids].float() * ramp).to(dtype)
+            o, lse = pec.pec_paged_attn(q, kp, vp, table, dev([0, n]), dev([1500]), max_q_len=n)
+            pec.check_status()
+            ref.check_attend(o, lse, ref.attend(q, kp, vp, table, [0, n], [1500]), dtype, f"ramp {dtype} {n}")
+
+
+def test_a_request_that_is_not_finite_spoils_no_other(pec):
+    for dtype in (F32, BF16):
+        n, kv, page = [1, 1, 140, 3], [300, 200, 400, 90], 16
+        kp, vp, table = ref.make_cache(21, kv, page, 2, dtype, DEV)
+        clean = ref.make_cache(21, kv, page, 2, dtype, DEV)
+        cu = ref.offsets(n)
+        q = torch.randn((cu[-1], 8, 128), device=DEV).to(dtype)
+        for b in (0, 2):
+            kp[table[b, 3].long(), 2] = float("inf")
+            vp[table[b, 5].long(), 7] = float("nan")
+        o, lse = pec.pec_paged_attn(q, kp, vp, table, dev(cu), dev(kv), max_q_len=140)
+        pec.check_status()
+        want = ref.attend(q, *clean, cu, kv)
+        for s, e in ((1, 2), (cu[3], cu[4])):
+            ref.check_attend(o[s:e], lse[s:e], [x[s:e] for x in want], dtype, "a neighbour of a request that is not finite")
+
+
+def test_bad_tables_are_reported(pec):
+    for dtype in (F32, BF16):
+        for n in (1, 200):
+            kp, vp, table = ref.make_cache(13, [300], 16, 1, dtype, DEV, poison=False, wild=False)
+            q = torch.randn((n, 2, 128), device=DEV).to(dtype)
+            cases = []
+            for bad in (-1, kp.shape[0], 2 ** 31 - 1):
+                t = table.clone()
+                t[0, 7] = bad
+                cases.append((t, [0, n], [300], n))
+            cases += [(table, [0, n + 1], [300], n), (table, [-1, n], [300], n), (table, [n, 0], [300], n), (table, [0, n], [-1], n),
+                      (table, [0, n], [10000], n), (table, [0, n], [2 ** 31 - 1], n)]
+            if n > 1:
+                cases.append((table, [0, n], [300], n - 1))       # more new tokens than max_q_len allows
+            for t, cu, kv, most in cases:
+                pec.pec_paged_attn(q, kp, vp, t, dev(cu), dev(kv), max_q_len=most)
+                with pytest.raises(binding.PecError) as e:
+                    pec.check_status()
+                assert e.value.code == binding.PEC_ERR_BAD_INDEX
+            o, lse = pec.pec_paged_attn(q, kp, vp, table, dev([0, n]), dev([300]), max_q_len=n)
+            pec.check_status()
+            ref.check_attend(o, lse, ref.attend(q, kp, vp, table, [0, n], [300]), dtype, "after bad tables")
+
+
+def test_pages_beyond_32_bits_of_elements(pec):
+    """Pages whose offsets pass 2^32 elements: append and attend at the far end of a 10 GB cache."""
+    page, hkv = 64, 8
+    num = (1 << 32) // (page * hkv * 128) + 50
+    kp = torch.empty((num, page, hkv, 128), dtype=BF16, device=DEV)
+    vp = torch.empty((num, page, hkv, 128), dtype=BF16, device=DEV)
+    for n, kv in ((1, 100), (170, 250)):
+        table = dev([[num - 1, num - 7, num - 3, num - 20, 0]])
+        kp[-40:].normal_()
+        vp[-40:].normal_()
+        k, v, q = (torch.randn((n, h, 128), device=DEV).to(BF16) for h in (hkv, hkv, 16))
+        pec.pec_kv_append(k, v, kp, vp, table, dev([0, n]), dev([kv]))
+        o, lse = pec.pec_paged_attn(q, kp, vp, table, dev([0, n]), dev([kv]), max_q_len=n)
+        pec.check_status()
+        small_k, small_v, small_t = kp[-40:], vp[-40:], table.clone()
+        small_t[0, :4] -= num - 40
+        at = kv - 1
+        assert torch.equal(small_k[small_t[0, at // page].long(), at % page], k[-1])
+        ref.check_attend(o, lse, ref.attend(q, small_k, small_v, small_t, [0, n], [kv]), BF16, f"far pages {n}")
+    del kp, vp
+    torch.cuda.empty_cache()
+
+
+def test_streams_graphs_and_a_shared_workspace(pec):
+    """A step captured on one stream and replayed after the tables and inputs have changed; two graphs that share a workspace
+    and run one after the other; an eager call on a stream of its own."""
+    page, hkv, hq = 16, 2, 8
+    binding.status_word(torch.device(DEV))
+    kp, vp, table = ref.make_cache(31, [900, 400, 333], page, hkv, BF16, DEV, poison=False, wild=False)
+    tables = pec.pec_rope_table(THETA, 4000, DEV)
+    steps = []
+    for n in ([1, 1, 1], [40, 1, 150]):
+        cu, kv = dev(ref.offsets(n)), dev([900, 400, 333])
+        T = sum(n)
+        q, k, v = (torch.randn((T, h, 128), device=DEV).to(BF16) for h in (hq, hkv, hkv))
+        o, lse = torch.empty((T, hq, 128), dtype=BF16, device=DEV), torch.empty((T, hq), device=DEV)
+        steps.append(dict(n=n, cu=cu, kv=kv, q=q, k=k, v=v, o=o, lse=lse))
+    ws = torch.empty(256 << 20, dtype=torch.uint8, device=DEV)
+
+    def issue(s):
+        qr, _ = pec.pec_qk_norm_rope(s["q"], norm=True, tables=tables, positions=s["pos"])
+        pec.pec_kv_append(s["k"], s["v"], kp, vp, table, s["cu"], s["kv"], norm=True, tables=tables)
+        pec.pec_paged_attn(qr, kp, vp, table, s["cu"], s["kv"], max_q_len=max(s["n"]), o=s["o"], lse=s["lse"], workspace=ws)
+
+    def positions(n, kv):
+        return [kv[b] - n[b] + i for b in range(len(n)) for i in range(n[b])]
+
+    graphs = []
+    for s in steps:
+        s["pos"] = dev(positions(s["n"], [900, 400, 333]))
+        issue(s)                                                  # warm up outside the capture
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            issue(s)
+        graphs.append(g)
+    for lens in ([900, 400, 333], [700, 123, 208]):
+        for s in steps:
+            s["kv"].copy_(dev(lens))
+            s["pos"].copy_(dev(positions(s["n"], lens)))
+            s["q"].normal_()
+        for s, g in zip(steps, graphs):
+            g.replay()
+            pec.check_status()
+            got = s["o"].clone(), s["lse"].clone()
+            qr, _ = pec.pec_qk_norm_rope(s["q"], tables=tables, positions=s["pos"])
+            ref.check_attend(*got, ref.attend(qr, kp, vp, table, s["cu"].tolist(), lens), BF16, f"replayed {lens}")
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            o, lse = pec.pec_paged_attn(qr, kp, vp, table, s["cu"], s["kv"], max_q_len=max(s["n"]), stream=side)
+            side.synchronize()
+            assert torch.equal(o, got[0]) and torch.equal(lse, got[1])
+
+
+def test_a_serving_step_against_the_prefill_path(pec):
+    """A prompt fed as chunks, then single tokens, through projection, norm and rotation, append and paged attention; the
+    result of the last rows against pec_prefill_attn over the whole request's contiguous q, k, v."""
+    hq, hkv, page, S, width = 8, 2, 16, 700, 512
+    torch.manual_seed(3)
+    x = (torch.randn((S, width), device=DEV) / 4).to(BF16)
+    w = (torch.randn(((hq + 2 * hkv) * 128, width), device=DEV) / 16).to(BF16)
+    qw, kw = [(1 + 0.1 * torch.randn(128, device=DEV)).to(BF16) for _ in range(2)]
+    tables = pec.pec_rope_table(THETA, 1024, DEV)
+    num = -(-S // page) + 1
+    kp, vp = [torch.full((num, page, hkv, 128), float("nan"), dtype=BF16, device=DEV) for _ in range(2)]
+    table = torch.randperm(num, device=DEV)[None, :num - 1].int()
+    whole = pec.pec_linear(x, w).view(S, hq + 2 * hkv, 128)
+    q_all, k_all = pec.pec_qk_norm_rope(whole[:, :hq], whole[:, hq:hq + hkv], q_weight=qw, k_weight=kw, tables=tables)
+    want_o, want_l = pec.pec_prefill_attn(q_all, k_all, whole[:, hq + hkv:], out_dtype=BF16)
+    at = 0
+    for n in (300, 1, 37, 256, 5, 1, 100):
+        qkv = pec.pec_linear(x[at:at + n], w).view(n, hq + 2 * hkv, 128)
+        at += n
+        q, _ = pec.pec_qk_norm_rope(qkv[:, :hq], q_weight=qw, tables=tables, pos0=at - n)
+        pec.pec_kv_append(qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], kp, vp, table, dev([0, n]), dev([at]), norm=True, k_weight=kw, tables=tables)
+        o, lse = pec.pec_paged_attn(q, kp, vp, table, dev([0, n]), dev([at]), max_q_len=n)
+        pec.check_status()
+        assert torch.equal(q, q_all[at - n:at])
+        # two roundings of o to bf16 and two of p: the values are averages of |v| of order 1
+        assert (o.float() - want_o[at - n:at].float()).abs().max() <= 4 * 2.0 ** -8 * whole.float().abs().max()
+        assert (lse - want_l[at - n:at]).abs().max() <= 1e-4
+        ref.check_attend(o, lse, ref.attend(q, kp, vp, table, [0, n], [at]), BF16, f"step of {n} at {at}")
+    assert at == S
+
+
+def test_calls_without_tokens(pec):
+    kp, vp, table = ref.make_cache(1, [20], 16, 2, BF16, DEV)
+    none = torch.empty((0, 4, 128), dtype=BF16, device=DEV)
+    o, lse = pec.pec_paged_attn(none, kp, vp, table, dev([0, 0]), dev([20]))
+    assert o.shape == (0, 4, 128) and lse.shape == (0, 4)
+    pec.pec_kv_append(none[:, :2], none[:, :2], kp, vp, table, dev([0, 0]), dev([20]))
+    pec.pec_qk_norm_rope(none)
+    q = torch.full((3, 4, 128), 1.0, dtype=BF16, device=DEV)       # padding alone
+    o = torch.full_like(q, 7.0)
+    pec.pec_paged_attn(q, kp, vp, table, dev([0, 0]), dev([20]), o=o)
+    pec.check_status()
+    assert (o == 7.0).all()
