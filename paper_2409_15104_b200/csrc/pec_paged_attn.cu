@@ -320,14 +320,14 @@ namespace paged {
 
 struct Call {
     Params p;
-    int64_t many_items;                       // grid bound of the many class
+    int64_t many_items;                       // grid bound of the many class; 0: no request can be of it
     size_t bytes;                             // workspace
 };
 
 inline bool aligned16(const void *x) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Checks the arguments and works out the launch; the workspace pointers are left for the caller.
+// Checks the arguments and works out the launch.
 static int resolve(const char *who, const pec_paged_args *a, Call &c)
 {
     if (!a) { set_error("%s: args is NULL", who); return PEC_ERR_INVALID_ARG; }
@@ -371,19 +371,39 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
         (void)cudaGetLastError();
         sms = 148;                            // no device here (size queries on a host without one): a B200's
     }
+    // bf16 requests with at most 128 packed rows go to the persistent kernel.
+    const bool tensor = a->dtype == PEC_BF16;
+    p.few = tensor ? 1 : 0;
+    p.few_ctas = sms;
+    size_t floats = 0;
+    if (p.few) {
+        p.few_rows = (int32_t)((int64_t)p.max_q * p.g < kFewRows ? p.max_q * p.g : kFewRows);
+        floats = 2 * (size_t)p.few_ctas * p.few_rows * (kHeadDim + 1);
+        floats = (floats + 3) & ~(size_t)3;
+    }
     // Blocks of the many class, the grid bound and the partial slots it may take (see many_slice).
-    p.few = 0;
     p.blk_mul = p.g; p.blk_div = kBM;
     p.many_rows = kBM;
     p.many_slots = 2 * sms;
-    const int64_t blocks = a->T * p.g / kBM + (a->B < a->T ? a->B : a->T);
-    c.many_items = blocks + ceil_div(p.many_slots, p.Hkv);
-    const int64_t most_slices = ceil_div(ceil_div((int64_t)a->max_pages * a->page_size, kKeyTile), kMinSliceTiles);
-    int64_t cap = 2 * (int64_t)p.many_slots;
-    if (most_slices <= 1) cap = 0;
-    else if (blocks * most_slices * p.Hkv < cap) cap = blocks * most_slices * p.Hkv;
-    p.many_cap = (int32_t)cap;
-    c.bytes = (size_t)cap * p.many_rows * (kHeadDim + 1) * sizeof(float);
+    c.many_items = 0;
+    if (!p.few || (int64_t)p.max_q * p.g > kFewRows) {
+        const int64_t shortest = p.few ? kFewRows / p.g + 1 : 1, most = a->T / shortest;       // new tokens of such a request; how many there can be
+        const int64_t blocks = a->T * p.blk_mul / p.blk_div + (a->B < most ? a->B : most);
+        c.many_items = blocks + ceil_div(p.many_slots, p.Hkv);
+        const int64_t most_slices = ceil_div(ceil_div((int64_t)a->max_pages * a->page_size, kKeyTile), kMinSliceTiles);
+        int64_t cap = 2 * (int64_t)p.many_slots;
+        if (most_slices <= 1) cap = 0;
+        else if (blocks * most_slices * p.Hkv < cap) cap = blocks * most_slices * p.Hkv;
+        p.many_cap = (int32_t)cap;
+    }
+    c.bytes = (floats + (size_t)p.many_cap * p.many_rows * (kHeadDim + 1)) * sizeof(float);
+    if (a->workspace) {
+        float *ws = static_cast<float *>(a->workspace);
+        p.few_o = ws;
+        p.few_lse = ws + 2 * (size_t)p.few_ctas * p.few_rows * kHeadDim;
+        p.many_o = ws + floats;
+        p.many_lse = p.many_o + (size_t)p.many_cap * p.many_rows * kHeadDim;
+    }
     return PEC_OK;
 }
 
@@ -410,11 +430,9 @@ extern "C" int pec_paged_attn(const pec_paged_args *args, void *cuda_stream)
         return PEC_ERR_WORKSPACE;
     }
     if (args->T == 0) return PEC_OK;
-    float *ws = static_cast<float *>(args->workspace);
-    c.p.many_o = ws;
-    c.p.many_lse = ws + (size_t)c.p.many_cap * c.p.many_rows * kHeadDim;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    rc = launch_paged_simple(c.p, args->dtype, c.many_items, stream);
+    if (c.many_items > 0) rc = launch_paged_simple(c.p, args->dtype, c.many_items, stream);
+    if (rc == PEC_OK && c.p.few) rc = launch_paged_few(c.p, stream);
     if (rc != PEC_OK || c.bytes == 0) return rc;
     return launch_paged_combine(c.p, stream);
 }

@@ -1,0 +1,494 @@
+// Paged attention of requests with few packed rows (n * g <= 128: decode steps) on the sm_100a tensor cores.
+//
+// Bound by the K/V stream from HBM: 2 * kv * Hkv * 256 bytes a request, each byte read once for all the rows of its KV head.
+// The kernel is persistent, one CTA per SM.  The key tiles of all (request, KV head) units lie on one line, request by request
+// and head by head, and each CTA walks an equal piece of it (few_piece), so that every SM streams the same number of bytes
+// whatever the requests' lengths; a unit inside one piece is finished there, one that crosses a cut leaves a partial result
+// per piece for the combining kernel.  A unit's part in a piece is a "segment".
+//
+// Warp roles (three warpgroups):
+//   warps 0-3, 4-7  softmax and epilogue of even and odd segments (a thread = a packed row = a TMEM lane); with two groups the
+//                   epilogue of one segment runs beside the first tiles of the next.  Warps whose 32 rows are all past the
+//                   segment's rows only keep the barriers in step (they never look at PV's).
+//   warp 8          MMA issuer       warp 9  TMA loader: segment descriptors, Q (two buffers), K and V tiles (a ring of five)
+//   warps 10-11     idle (they complete the third warpgroup, which hands its registers over)
+// The loader runs through segment borders, so the stream from memory does not stop at them.
+//
+// Per tile: S(n) = Q K^T into one of two TMEM buffers; the softmax warps read their rows, and write P (bf16) over the same
+// buffer; O += P V.  The issuer's order S(n + 1), PV(n) has the next scores ready when the softmax comes back for them; S(n + 2)
+// may overwrite P(n) because the issuing thread's products execute in order.  O has one accumulator per group.
+// TMEM columns: S [0, 256), two buffers; O [256, 512), one per group.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include "pec_paged_tma.cuh"
+
+namespace pec {
+using namespace sm100;
+namespace paged {
+namespace few {
+
+constexpr int kSlots = 5;                                  // K/V ring
+constexpr int kThreads = 384;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kSpareWarp = 10;
+constexpr int kLightRegs = 56, kSoftmaxRegs = 224;         // 256 * 224 + 128 * 56 = 384 * 168 (the launch allocation)
+constexpr uint32_t kTmemCols = 512, kColO = 256;
+constexpr float kRescaleThreshold = 8.0f;                  // log2 units
+
+struct Segment {
+    int32_t tiles;                                         // 0: no more segments
+    int32_t key0;                                          // position of the first tile's first key
+    int32_t kv, pos0, rows;
+    int32_t tile0;                                         // the CTA's count of tiles before this segment
+    int64_t out;                                           // whole unit: (first token row * Hq + first head); else partial slot * few_rows
+    int32_t whole;
+};
+
+struct Shared {
+    uint64_t q_full[2], q_empty[2];                        // per group: descriptor and Q of its next segment
+    uint64_t kv_full[kSlots], kv_empty[kSlots];
+    uint64_t s_full[2][2], p_ready[2][2];                  // [group][TMEM buffer]
+    uint64_t pv_done[2], o_free[2];                        // [group]
+    Segment seg[2];
+    int64_t first;                                         // this CTA's piece of the line
+    int32_t count;
+    uint32_t tmem_base;
+    volatile int abort_flag;
+};
+constexpr size_t kSmemBytes = (2 + kSlots) * kTileBytes + 1024 /*alignment slack*/ + sizeof(Shared);
+
+__device__ __forceinline__ bool wait_bar(uint64_t *bar, uint32_t parity, Shared *sh, const Params &p)
+{
+    return mbar_wait_bounded(smem_u32(bar), parity, &sh->abort_flag, p.status, p.wait_cycles, (int)PEC_ERR_TIMEOUT);
+}
+__device__ __forceinline__ bool wait_all(uint64_t *bar, uint32_t parity, Shared *sh, const Params &p)   // warp-uniform
+{
+    return __all_sync(0xffffffffu, wait_bar(bar, parity, sh, p));
+}
+
+// The loader's walk along the line.  The 32 requests around the current one sit in the lanes' registers.
+struct Walk {
+    int32_t b0, b;                                         // first request of the lanes' group; current request
+    Request mine, r;                                       // this lane's, the current one
+    int32_t kvh, tile;                                     // current KV head and tile of the request
+    int64_t u0;                                            // the unit's first tile on the line
+};
+__device__ __forceinline__ void walk_take(Walk &w, int src)
+{
+    w.b = w.b0 + src;
+    w.r.start = __shfl_sync(0xffffffffu, w.mine.start, src);
+    w.r.n = __shfl_sync(0xffffffffu, w.mine.n, src);
+    w.r.kv = __shfl_sync(0xffffffffu, w.mine.kv, src);
+}
+__device__ __forceinline__ void walk_group(const Params &p, Walk &w, int lane)
+{
+    w.mine.start = w.mine.n = w.mine.kv = 0;
+    if (w.b0 + lane < p.c.B) w.mine = load_request(p, w.b0 + lane);
+}
+// To place `at` on the line (below its end).
+__device__ __forceinline__ void walk_to(const Params &p, Walk &w, int64_t at, int lane)
+{
+    int64_t before = 0;
+    for (w.b0 = 0; w.b0 < p.c.B; w.b0 += 32) {
+        walk_group(p, w, lane);
+        const int64_t len = is_few(p, w.mine) ? (int64_t)w.mine.tiles() * p.Hkv : 0, incl = warp_prefix(len, lane);
+        const unsigned who = __ballot_sync(0xffffffffu, at >= before + incl - len && at < before + incl);
+        if (who) {
+            const int src = __ffs(who) - 1;
+            walk_take(w, src);
+            const int64_t off = at - __shfl_sync(0xffffffffu, before + incl - len, src);
+            w.kvh = (int32_t)(off / w.r.tiles());
+            w.tile = (int32_t)(off % w.r.tiles());
+            w.u0 = at - w.tile;
+            return;
+        }
+        before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+}
+// To the next unit (there is one).
+__device__ __forceinline__ void walk_next(const Params &p, Walk &w, int lane)
+{
+    w.u0 += w.r.tiles();
+    w.tile = 0;
+    if (++w.kvh < p.Hkv) return;
+    w.kvh = 0;
+    unsigned left = __ballot_sync(0xffffffffu, is_few(p, w.mine) && w.b0 + lane > w.b);
+    while (!left && w.b0 + 32 < p.c.B) {
+        w.b0 += 32;
+        walk_group(p, w, lane);
+        left = __ballot_sync(0xffffffffu, is_few(p, w.mine));
+    }
+    walk_take(w, left ? __ffs(left) - 1 : 0);
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                 const __grid_constant__ CUtensorMap tm_v, const Params p, const int box, const int q_tokens, const int skip_last)
+{
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t sQ = (raw + 1023u) & ~1023u, sRing = sQ + 2 * kTileBytes;
+    Shared *sh = reinterpret_cast<Shared *>(smem_raw + (sQ - raw) + (2 + kSlots) * kTileBytes);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    // The loader warp works out this CTA's piece of the line while others set up barriers and tensor memory.
+    Walk walk;
+    if (warp == kLoadWarp) {
+        int64_t all, rest;
+        batch_tiles(p, all, rest);
+        const int64_t piece = few_piece(p, all), first = blockIdx.x * piece;
+        const int64_t count = all * p.Hkv - first;
+        const int32_t n = (int32_t)(count < 0 ? 0 : (count < piece ? count : piece));
+        if (n > 0) walk_to(p, walk, first, lane);
+        if (lane == 0) { sh->first = first; sh->count = n; }
+    } else if (tid == 0) {
+        sh->abort_flag = 0;
+        for (int g = 0; g < 2; ++g) {
+            mbar_init(smem_u32(&sh->q_full[g]), 1);
+            mbar_init(smem_u32(&sh->q_empty[g]), 5);       // four softmax warps, the issuer's commit
+            for (int i = 0; i < 2; ++i) {
+                mbar_init(smem_u32(&sh->s_full[g][i]), 1);
+                mbar_init(smem_u32(&sh->p_ready[g][i]), 4);
+            }
+            mbar_init(smem_u32(&sh->pv_done[g]), 1);
+            mbar_init(smem_u32(&sh->o_free[g]), 4);
+        }
+        for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&sh->kv_full[s]), 1); mbar_init(smem_u32(&sh->kv_empty[s]), 1); }
+        mbar_init_fence();
+        prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
+    }
+    __syncthreads();
+    const int32_t count = sh->count;
+    if (count == 0) return;
+    if (warp == 4) {
+        tmem_alloc(smem_u32(&sh->tmem_base), kTmemCols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh->tmem_base;
+
+    if (warp == kLoadWarp) {
+        // ------------------------------------------------------------------ loader
+        reg_dealloc<kLightRegs>();
+        const BoxLane bl = box_lane(box, lane);
+        const int64_t first = sh->first, end = first + count;
+        int32_t page = box_page(p, walk.b, walk.tile * kKeyTile, walk.r.kv, bl);
+        int segs = 0, n = 0;
+        uint32_t issued = 0, q_issued = 0;                 // ring items and segments whose loads are under way
+        bool ok = true;
+        while (n < count && ok) {
+            // a segment: descriptor and Q
+            const int g = segs & 1;
+            const int64_t lo = walk.u0 > first ? walk.u0 : first;
+            const int64_t hi = walk.u0 + walk.r.tiles() < end ? walk.u0 + walk.r.tiles() : end;
+            const int32_t tiles = (int32_t)(hi - lo);
+            if (segs >= 2) ok = wait_all(&sh->q_empty[g], ((segs >> 1) - 1) & 1, sh, p);
+            if (!ok) break;
+            if (lane == 0) {
+                Segment s;
+                s.tiles = tiles;
+                s.key0 = walk.tile * kKeyTile;
+                s.kv = walk.r.kv; s.pos0 = walk.r.pos0(); s.rows = walk.r.n * p.g;
+                s.tile0 = n;
+                s.whole = tiles == walk.r.tiles();
+                s.out = s.whole ? (int64_t)walk.r.start * p.Hq + (int64_t)walk.kvh * p.g
+                                : (2 * (int64_t)blockIdx.x + (walk.u0 > first ? 1 : 0)) * p.few_rows;
+                sh->seg[g] = s;
+                const uint32_t bar = smem_u32(&sh->q_full[g]), dst = sQ + (uint32_t)g * kTileBytes;
+                mbar_arrive_expect_tx(bar, (uint32_t)(q_tokens * p.g) * 256u);
+                tma_load_4d(dst, &tm_q, bar, 0, 0, walk.kvh, walk.r.start);
+                tma_load_4d(dst + kHalfTileBytes, &tm_q, bar, 64, 0, walk.kvh, walk.r.start);
+            }
+            __syncwarp();
+            ++segs; ++q_issued;
+            // its tiles; the pages of the tile after the current one are looked up ahead
+            const int32_t b = walk.b, kv = walk.r.kv, kvh = walk.kvh;
+            int32_t k0 = walk.tile * kKeyTile;
+            if (n + tiles < count) walk_next(p, walk, lane);
+            for (int j = 0; j < tiles && ok; ++j, ++n, k0 += kKeyTile) {
+                int32_t page_next = 0;
+                if (j + 1 < tiles) page_next = box_page(p, b, k0 + kKeyTile, kv, bl);
+                else if (n + 1 < count) page_next = box_page(p, walk.b, walk.tile * kKeyTile, walk.r.kv, bl);
+                const uint32_t bytes = tile_bytes(k0, kv, box);
+                const int32_t row = (k0 + bl.first) % p.c.page_size;
+#pragma unroll
+                for (int which = 0; which < 2; ++which) {  // K, V
+                    const int item = 2 * n + which, slot = item % kSlots, fill = item / kSlots;
+                    if (skip_last && count > 1 && item == 2 * count - 1) { ok = false; break; }   // test hook: the wait for it runs out
+                    if (fill > 0) ok = wait_all(&sh->kv_empty[slot], (fill - 1) & 1, sh, p);
+                    if (!ok) break;
+                    const uint32_t bar = smem_u32(&sh->kv_full[slot]);
+                    if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
+                    __syncwarp();
+                    if (bl.used && k0 + bl.first < kv)
+                        tma_load_4d(sRing + (uint32_t)slot * kTileBytes + bl.offset, which ? (const void *)&tm_v : (const void *)&tm_k, bar,
+                                    bl.half * 64, kvh, row, page);
+                    ++issued;
+                }
+                page = page_next;
+            }
+        }
+        // No more segments for either group.
+        for (int e = 0; e < 2 && ok; ++e, ++segs) {
+            const int g = segs & 1;
+            if (segs >= 2) ok = wait_all(&sh->q_empty[g], ((segs >> 1) - 1) & 1, sh, p);
+            if (ok && lane == 0) { sh->seg[g].tiles = 0; mbar_arrive(smem_u32(&sh->q_full[g])); }
+        }
+        if (!ok && lane == 0) {
+            // Given up: the copies under way must land before the CTA may leave (each wait with the usual limit).
+            auto landed = [&](uint64_t *bar, uint32_t parity) {
+                const long long t0 = clock64();
+                while (!mbar_try_wait_suspend(smem_u32(bar), parity, 2000u) && clock64() - t0 < p.wait_cycles) {}
+            };
+            for (uint32_t i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i) landed(&sh->kv_full[i % kSlots], (i / kSlots) & 1);
+            for (uint32_t i = q_issued > 2 ? q_issued - 2 : 0; i < q_issued; ++i) landed(&sh->q_full[i & 1], (i >> 1) & 1);
+        }
+        __syncwarp();
+    } else if (warp == kMmaWarp) {
+        // ------------------------------------------------------------------ MMA issuer (the whole warp walks, one lane issues)
+        reg_dealloc<kLightRegs>();
+        const bool leader = elect_one();
+        constexpr uint32_t idesc_qk = idesc_bf16_f32(128, 128, 0, 0), idesc_pv = idesc_bf16_f32(128, kHeadDim, 0, 1);
+        constexpr uint32_t kBox16 = kHalfTileBytes >> 4;
+        const uint64_t k_ring = smem_desc_sw128(sRing, 16, 1024), v_ring = smem_desc_sw128(sRing, kHalfTileBytes, 1024);
+        uint32_t p_phase = 0;                              // bit 2 g + buffer: parity of the next p_ready
+        auto kv_wait = [&](int item) { return wait_all(&sh->kv_full[item % kSlots], (item / kSlots) & 1, sh, p); };
+        auto kv_release = [&](int item) { if (leader) tc_commit(smem_u32(&sh->kv_empty[item % kSlots])); };
+        // S(n) of a segment of group g; `last`: the segment's Q is not needed after it
+        auto issue_qk = [&](int n, int g, bool last) {
+            if (!kv_wait(2 * n)) return false;
+            if (leader) {
+                uint64_t a[8];
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                    a[ks] = smem_desc_sw128(sQ + (uint32_t)g * kTileBytes + (uint32_t)(ks >> 2) * kHalfTileBytes + (uint32_t)(ks & 3) * 32u, 16, 1024);
+                mma_ss_k128_commit<kBox16>(tmem + (uint32_t)(n & 1) * 128u, a, k_ring + (uint32_t)(((2 * n) % kSlots) * (kTileBytes >> 4)),
+                                           idesc_qk, smem_u32(&sh->s_full[g][n & 1]));
+                if (last) tc_commit(smem_u32(&sh->q_empty[g]));
+            }
+            kv_release(2 * n);
+            return true;
+        };
+        int segs = 0;
+        bool ok = wait_all(&sh->q_full[0], 0, sh, p);
+        Segment cur = sh->seg[0];
+        if (ok) ok = issue_qk(0, 0, cur.tiles == 1);
+        int n = 0;
+        while (ok) {
+            const int g = segs & 1, k = segs >> 1;         // k: the group's count of segments before this one
+            Segment next;
+            next.tiles = 0;
+            for (int j = 0; j < cur.tiles && ok; ++j, ++n) {
+                if (j + 1 < cur.tiles) {
+                    ok = issue_qk(n + 1, g, j + 2 == cur.tiles);
+                } else if (n + 1 < count) {
+                    ok = wait_all(&sh->q_full[g ^ 1], ((segs + 1) >> 1) & 1, sh, p);
+                    if (!ok) break;
+                    next = sh->seg[g ^ 1];
+                    ok = issue_qk(n + 1, g ^ 1, next.tiles == 1);
+                }
+                if (!ok) break;
+                ok = kv_wait(2 * n + 1);
+                if (!ok) break;
+                const uint32_t slot = (uint32_t)((2 * n + 1) % kSlots);
+                const int32_t valid = cur.kv - cur.key0 - j * kKeyTile;
+                if (valid < kKeyTile) clear_tail(sRing + slot * kTileBytes, valid, lane);
+                if (j == 0 && k > 0) ok = wait_all(&sh->o_free[g], (k - 1) & 1, sh, p);
+                const int bit = 2 * g + (n & 1);
+                if (ok) ok = wait_all(&sh->p_ready[g][n & 1], (p_phase >> bit) & 1, sh, p);
+                if (!ok) break;
+                p_phase ^= 1u << bit;
+                tc_fence_after();
+                if (leader) {
+                    const uint64_t v0 = v_ring + slot * (kTileBytes >> 4);
+                    const uint32_t tO = tmem + kColO + (uint32_t)g * 128u, tP = tmem + (uint32_t)(n & 1) * 128u;
+                    mma_ts_k64(tO, tP, v0, idesc_pv, j > 0 ? 1u : 0u);
+                    mma_ts_k64(tO, tP + 32, v0 + (64 * 128 >> 4), idesc_pv, 1u);
+                    tc_commit(smem_u32(&sh->pv_done[g]));
+                }
+                kv_release(2 * n + 1);
+            }
+            if (next.tiles == 0) break;
+            cur = next;
+            ++segs;
+        }
+        __syncwarp();
+    } else if (warp > kLoadWarp) {
+        reg_dealloc<kLightRegs>();
+        // An earlier CTA's wait has run out: the launch is lost, every wait of this CTA gives up at its next try.
+        if (warp == kSpareWarp && lane == 0 && *reinterpret_cast<volatile int32_t *>(p.status) == PEC_ERR_TIMEOUT) sh->abort_flag = 1;
+    } else {
+        // ------------------------------------------------------------------ softmax and epilogue
+        reg_alloc<kSoftmaxRegs>();
+        const int g = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const uint32_t tO = tmem + lane_base + kColO + (uint32_t)g * 128u;
+        const int32_t tok = row / p.g, head = row - tok * p.g;
+        uint32_t s_phase = 0;                              // bit: parity of the buffer's next s_full
+        uint32_t pv = 0;                                   // the group's PV products before this segment
+        for (int k = 0;; ++k) {
+            bool ok = wait_all(&sh->q_full[g], k & 1, sh, p);
+            if (!ok) break;
+            const Segment s = sh->seg[g];
+            __syncwarp();
+            if (s.tiles == 0) break;
+            if (lane == 0) mbar_arrive(smem_u32(&sh->q_empty[g]));
+            const bool works = quarter * 32 < s.rows;
+            const int32_t see_all = (p.causal && s.pos0 + 1 < s.kv) ? s.pos0 + 1 : s.kv;           // keys below it are visible to every row
+            const int32_t see = (p.causal && s.pos0 + tok + 1 < s.kv) ? s.pos0 + tok + 1 : s.kv;   // ... to this row
+            float m_ref = -INFINITY, l_run = 0.f;          // m_ref in log2 units of the scaled scores
+            int32_t k0 = s.key0;
+            for (int j = 0; j < s.tiles; ++j, k0 += kKeyTile) {
+                const int buf = (s.tile0 + j) & 1;
+                const uint32_t tS = tmem + lane_base + (uint32_t)buf * 128u;
+                ok = wait_all(&sh->s_full[g][buf], (s_phase >> buf) & 1, sh, p);
+                if (!ok) break;
+                s_phase ^= 1u << buf;
+                if (works) {
+                    tc_fence_after();
+                    uint32_t r[kKeyTile];
+                    tmem_ld128(tS, r);
+                    if (k0 + kKeyTile > see_all) {         // by choice, not by arithmetic: a masked score may be anything
+                        int n_vis = see - k0;
+                        n_vis = n_vis < 0 ? 0 : (n_vis > kKeyTile ? kKeyTile : n_vis);
+#pragma unroll
+                        for (int c = 0; c < kKeyTile; ++c) r[c] = (c < n_vis) ? r[c] : 0xff800000u;
+                    }
+                    float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < kKeyTile; c += 8) {
+                        mx0 = fmax3(mx0, __uint_as_float(r[c + 0]), __uint_as_float(r[c + 1]));
+                        mx1 = fmax3(mx1, __uint_as_float(r[c + 2]), __uint_as_float(r[c + 3]));
+                        mx2 = fmax3(mx2, __uint_as_float(r[c + 4]), __uint_as_float(r[c + 5]));
+                        mx3 = fmax3(mx3, __uint_as_float(r[c + 6]), __uint_as_float(r[c + 7]));
+                    }
+                    const float m_new = fmax3(mx0, mx1, fmaxf(mx2, mx3)) * p.scale_log2;
+                    // The reference maximum moves only when outgrown by 2^8; O then waits for its product in flight.
+                    float alpha = 1.f;
+                    const bool grow = m_new > m_ref + kRescaleThreshold;
+                    if (grow) {
+                        alpha = ex2(m_ref - m_new);        // 0 when the row had no key so far
+                        m_ref = m_new;
+                        l_run *= alpha;
+                    }
+                    // PV(j - 1) is waited for in every tile: before O is rescaled where that is needed, before P(j) is handed over
+                    // otherwise.  S(j) is complete, and with it PV(j - 2), issued before it, and PV(j) needs this warp's P(j),
+                    // so the barrier's parity tells exactly that phase; a wait left out would make the next one ambiguous.
+                    bool pv_waited = j == 0;
+                    if (j > 0 && __any_sync(0xffffffffu, grow)) {
+                        ok = wait_all(&sh->pv_done[g], (pv + j - 1) & 1, sh, p);
+                        if (!ok) break;
+                        pv_waited = true;
+                        tc_fence_after();
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t o[32];
+                            tmem_ld32(tO + c * 32, o);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                            tmem_st32(tO + c * 32, o);
+                        }
+                    }
+                    const float neg_m = (m_ref == -INFINITY) ? 0.f : -m_ref;
+                    const float2 sc2 = make_float2(p.scale_log2, p.scale_log2), nm2 = make_float2(neg_m, neg_m);
+                    float2 sum[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[i] = make_float2(0.f, 0.f);
+                    // p = 2^(s scale - m), rounded to bf16 as the product's operand (the tensor cores take no wider one beside a
+                    // bf16 V); the row's sum takes p before it is rounded.
+#pragma unroll
+                    for (int i = 0; i < kKeyTile / 2; ++i) {
+                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), sc2, nm2);
+                        const float2 e = make_float2(ex2(x.x), ex2(x.y));
+                        sum[i & 3] = __fadd2_rn(sum[i & 3], e);
+                        r[i] = pack_bf16(e.x, e.y);
+                    }
+                    const float2 s01 = __fadd2_rn(__fadd2_rn(sum[0], sum[1]), __fadd2_rn(sum[2], sum[3]));
+                    l_run += s01.x + s01.y;
+                    if (!pv_waited) {
+                        ok = wait_all(&sh->pv_done[g], (pv + j - 1) & 1, sh, p);
+                        if (!ok) break;
+                    }
+                    tmem_st32(tS, r);
+                    tmem_st32(tS + 32, r + 32);
+                    tmem_st_wait();
+                    tc_fence_before();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh->p_ready[g][buf]));
+            }
+            if (!ok) break;
+            pv += s.tiles;
+            if (works) {
+                ok = wait_all(&sh->pv_done[g], (pv - 1) & 1, sh, p);
+                if (!ok) break;
+                tc_fence_after();
+                const bool valid = row < s.rows, empty = l_run == 0.f;
+                const float inv = empty ? 0.f : 1.f / l_run;
+                const int64_t at = s.whole ? s.out + (int64_t)tok * p.Hq + head : s.out + row;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t r[32];
+                    tmem_ld32(tO + c * 32, r);
+                    if (!valid) continue;
+                    float f[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) f[i] = empty ? 0.f : __uint_as_float(r[i]) * inv;
+                    if (s.whole && p.o_is_bf16) {
+                        __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.o) + at * kHeadDim + c * 32;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8)
+                            *reinterpret_cast<uint4 *>(o + i) = make_uint4(pack_bf16(f[i], f[i + 1]), pack_bf16(f[i + 2], f[i + 3]),
+                                                                           pack_bf16(f[i + 4], f[i + 5]), pack_bf16(f[i + 6], f[i + 7]));
+                    } else {
+                        float *o = (s.whole ? static_cast<float *>(p.o) : p.few_o) + at * kHeadDim + c * 32;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4 *>(o + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+                    }
+                }
+                if (valid) (s.whole ? p.lse : p.few_lse)[at] = empty ? -INFINITY : m_ref * 0.6931471805599453f + logf(l_run);
+                tc_fence_before();
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->o_free[g]));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 4) tmem_dealloc(tmem, kTmemCols);
+}
+
+}  // namespace few
+}  // namespace paged
+
+int launch_paged_few(const paged::Params &p, cudaStream_t stream)
+{
+    using namespace paged;
+    const int box = host_map::box_rows(p.c.page_size);
+    const int tps = kFewRows / p.g, q_tokens = tps < p.max_q ? tps : p.max_q;
+    CUtensorMap tm_q, tm_k, tm_v;
+    if (!host_map::queries(&tm_q, p, q_tokens) || !host_map::pages(&tm_k, p, p.k_pages, p.c.k_sp, p.c.k_st, p.c.k_sh, box) ||
+        !host_map::pages(&tm_v, p, p.v_pages, p.c.v_sp, p.c.v_st, p.c.v_sh, box)) {
+        set_error("pec_paged_attn: cuTensorMapEncodeTiled failed (driver too old, or strides/addresses not encodable)");
+        return PEC_ERR_CUDA;
+    }
+    static unsigned char ready[host::kMaxDevices] = {};
+    static std::mutex ready_mutex;
+    if (!host::once_per_device(ready, ready_mutex, [] {
+            cudaFuncAttributes attr;
+            return cudaFuncSetAttribute(few::paged_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few::kSmemBytes) == cudaSuccess &&
+                   cudaFuncGetAttributes(&attr, few::paged_few_kernel) == cudaSuccess &&
+                   attr.numRegs * few::kThreads >= 256 * few::kSoftmaxRegs + 128 * few::kLightRegs; })) {
+        (void)cudaGetLastError();
+        set_error("pec_paged_attn: kernel set-up failed (shared-memory limit, or the register allocation does not cover the warp-role split)");
+        return PEC_ERR_CUDA;
+    }
+    few::paged_few_kernel<<<p.few_ctas, few::kThreads, few::kSmemBytes, stream>>>(tm_q, tm_k, tm_v, p, box, q_tokens, test_skip_last_load());
+    const cudaError_t err = cudaGetLastError();
+    if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
+    return PEC_OK;
+}
+
+}  // namespace pec

@@ -212,6 +212,7 @@ __device__ __forceinline__ int64_t few_before(const Params &p, int b)
 
 // Launchers (each returns a pec_status).
 int launch_paged_simple(const paged::Params &p, int32_t dtype, int64_t items, cudaStream_t stream);
+int launch_paged_few(const paged::Params &p, cudaStream_t stream);
 int launch_paged_combine(const paged::Params &p, cudaStream_t stream);
 
 }  // namespace pec
