@@ -7,7 +7,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libpec.so")
 SOURCES = ["pec_api.cpp", "pec_plan.cpp", "pec_merge.cu", "pec_attn_f32.cu", "pec_attn_prefill_bf16.cu", "pec_attn_split_bf16.cu", "pec_decode.cu", "pec_linear.cu", "pec_linear_merged.cu",
-           "pec_heads.cu", "pec_paged_attn.cu", "pec_paged_few.cu"]
+           "pec_heads.cu", "pec_paged_attn.cu", "pec_paged_few.cu", "pec_paged_many.cu"]
 
 
 def _stale() -> bool:

@@ -20,15 +20,8 @@ constexpr int kBM = 64, kBN = 64, kThreads = 256;
 constexpr int kLd = kHeadDim + 4, kLdP = kBN + 4;
 constexpr size_t kSimpleSmem = sizeof(float) * (2 * kBM * kLd + kBN * kHeadDim + kBM * kLdP);
 
-template <class E> __device__ __forceinline__ float4 load4(const E *p);
-template <> __device__ __forceinline__ float4 load4<float>(const float *p) { return *reinterpret_cast<const float4 *>(p); }
-template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16 *p)
-{
-    const uint2 u = *reinterpret_cast<const uint2 *>(p);
-    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
-}
+__device__ __forceinline__ float4 load4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
 
-template <class E>
 __global__ void __launch_bounds__(kThreads)
 paged_simple_kernel(const Params p)
 {
@@ -56,7 +49,7 @@ paged_simple_kernel(const Params p)
         float4 val = make_float4(0.f, 0.f, 0.f, 0.f);
         if (r < rows) {
             const int32_t t = (row0 + r) / p.g, h = kvh * p.g + (row0 + r) % p.g;
-            val = load4(static_cast<const E *>(p.q) + (int64_t)(it.r.start + t) * p.q_st + (int64_t)h * p.q_sh + c);
+            val = load4(static_cast<const float *>(p.q) + (int64_t)(it.r.start + t) * p.q_st + (int64_t)h * p.q_sh + c);
         }
         *reinterpret_cast<float4 *>(sQ + r * kLd + c) = val;
     }
@@ -91,8 +84,8 @@ paged_simple_kernel(const Params p)
             const int64_t page = s_page[r];
             if (page >= 0) {
                 const int64_t slot = (k0 + r) % p.c.page_size;
-                kk = load4(static_cast<const E *>(p.k_pages) + page * p.c.k_sp + slot * p.c.k_st + (int64_t)kvh * p.c.k_sh + c);
-                vv = load4(static_cast<const E *>(p.v_pages) + page * p.c.v_sp + slot * p.c.v_st + (int64_t)kvh * p.c.v_sh + c);
+                kk = load4(static_cast<const float *>(p.k_pages) + page * p.c.k_sp + slot * p.c.k_st + (int64_t)kvh * p.c.k_sh + c);
+                vv = load4(static_cast<const float *>(p.v_pages) + page * p.c.v_sp + slot * p.c.v_st + (int64_t)kvh * p.c.v_sh + c);
             }
             *reinterpret_cast<float4 *>(sK + r * kLd + c) = kk;
             *reinterpret_cast<float4 *>(sV + r * kHeadDim + c) = vv;
@@ -183,15 +176,9 @@ paged_simple_kernel(const Params p)
             if (tx == 0) p.many_lse[slot * p.many_rows + r] = lse;
         } else {
             const int64_t item = (int64_t)(it.r.start + (row0 + r) / p.g) * p.Hq + kvh * p.g + (row0 + r) % p.g;
-            if (p.o_is_bf16) {
-                __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.o) + item * kHeadDim;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) { o[tx * 4 + c] = __float2bfloat16(out[c]); o[64 + tx * 4 + c] = __float2bfloat16(out[4 + c]); }
-            } else {
-                float *o = static_cast<float *>(p.o) + item * kHeadDim;
-                *reinterpret_cast<float4 *>(o + tx * 4) = make_float4(out[0], out[1], out[2], out[3]);
-                *reinterpret_cast<float4 *>(o + 64 + tx * 4) = make_float4(out[4], out[5], out[6], out[7]);
-            }
+            float *o = static_cast<float *>(p.o) + item * kHeadDim;
+            *reinterpret_cast<float4 *>(o + tx * 4) = make_float4(out[0], out[1], out[2], out[3]);
+            *reinterpret_cast<float4 *>(o + 64 + tx * 4) = make_float4(out[4], out[5], out[6], out[7]);
             if (tx == 0) p.lse[item] = lse;
         }
     }
@@ -278,21 +265,18 @@ paged_combine_kernel(const Params p)
 
 using namespace paged;
 
-int launch_paged_simple(const Params &p, int32_t dtype, int64_t items, cudaStream_t stream)
+int launch_paged_simple(const Params &p, int64_t items, cudaStream_t stream)
 {
     static unsigned char ready[host::kMaxDevices] = {};
     static std::mutex ready_mutex;
     if (!host::once_per_device(ready, ready_mutex, [] {
-            return cudaFuncSetAttribute(paged_simple_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSimpleSmem) == cudaSuccess &&
-                   cudaFuncSetAttribute(paged_simple_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSimpleSmem) == cudaSuccess; })) {
+            return cudaFuncSetAttribute(paged_simple_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSimpleSmem) == cudaSuccess; })) {
         (void)cudaGetLastError();
         set_error("pec_paged_attn: cannot raise the shared-memory limit");
         return PEC_ERR_CUDA;
     }
     if (items > 0x7fffffff) { set_error("pec_paged_attn: grid too large"); return PEC_ERR_UNSUPPORTED; }
-    const dim3 grid((unsigned)items, (unsigned)p.Hkv);
-    if (dtype == PEC_BF16) paged_simple_kernel<__nv_bfloat16><<<grid, kThreads, kSimpleSmem, stream>>>(p);
-    else                   paged_simple_kernel<float><<<grid, kThreads, kSimpleSmem, stream>>>(p);
+    paged_simple_kernel<<<dim3((unsigned)items, (unsigned)p.Hkv), kThreads, kSimpleSmem, stream>>>(p);
     const cudaError_t err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
@@ -382,8 +366,9 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
         floats = (floats + 3) & ~(size_t)3;
     }
     // Blocks of the many class, the grid bound and the partial slots it may take (see many_slice).
-    p.blk_mul = p.g; p.blk_div = kBM;
-    p.many_rows = kBM;
+    const int tps = kFewRows / p.g;           // tensor cores: two stages of whole tokens; FMA: 64 packed rows
+    p.blk_mul = tensor ? 1 : p.g; p.blk_div = tensor ? 2 * tps : kBM;
+    p.many_rows = tensor ? 2 * tps * p.g : kBM;
     p.many_slots = 2 * sms;
     c.many_items = 0;
     if (!p.few || (int64_t)p.max_q * p.g > kFewRows) {
@@ -431,7 +416,7 @@ extern "C" int pec_paged_attn(const pec_paged_args *args, void *cuda_stream)
     }
     if (args->T == 0) return PEC_OK;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (c.many_items > 0) rc = launch_paged_simple(c.p, args->dtype, c.many_items, stream);
+    if (c.many_items > 0) rc = args->dtype == PEC_BF16 ? launch_paged_many(c.p, c.many_items, stream) : launch_paged_simple(c.p, c.many_items, stream);
     if (rc == PEC_OK && c.p.few) rc = launch_paged_few(c.p, stream);
     if (rc != PEC_OK || c.bytes == 0) return rc;
     return launch_paged_combine(c.p, stream);

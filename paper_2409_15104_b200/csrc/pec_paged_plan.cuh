@@ -211,7 +211,8 @@ __device__ __forceinline__ int64_t few_before(const Params &p, int b)
 }  // namespace paged
 
 // Launchers (each returns a pec_status).
-int launch_paged_simple(const paged::Params &p, int32_t dtype, int64_t items, cudaStream_t stream);
+int launch_paged_simple(const paged::Params &p, int64_t items, cudaStream_t stream);       // fp32
+int launch_paged_many(const paged::Params &p, int64_t items, cudaStream_t stream);         // bf16
 int launch_paged_few(const paged::Params &p, cudaStream_t stream);
 int launch_paged_combine(const paged::Params &p, cudaStream_t stream);
 
