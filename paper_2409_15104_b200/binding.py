@@ -5,6 +5,7 @@ The library is loaded on first use; a missing or unloadable library raises - the
 fallback implementation.
 """
 import ctypes
+import functools
 import os
 
 import torch
@@ -517,45 +518,53 @@ def _need(ok, text):
 
 
 def _on(t, what, dtype, dims, device):
-    """Checks that the library cannot make: a tensor of this type and rank on this device, innermost dimension contiguous."""
-    _need(isinstance(t, torch.Tensor) and t.device == device and t.dtype == dtype and t.dim() == dims,
-          f"{what}: need a {dims}-dimensional {dtype} tensor on {device}")
-    _need(t.shape[-1] <= 1 or t.stride(-1) == 1, f"{what}: the innermost dimension must be contiguous")
+    """A check that the library cannot make: a tensor of this type and rank on this device, innermost dimension contiguous.
+    (The paged calls are a few microseconds of device work in a decode step, so their checks build no text unless they fail.)"""
+    if t.dtype is not dtype or t.dim() != dims or t.device != device:
+        raise ValueError(f"{what}: need a {dims}-dimensional {dtype} tensor on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{what}: the innermost dimension must be contiguous")
 
 
-def _strides(t, n):
-    """Strides of the first n dimensions; a dimension of one entry has no stride of its own, whatever torch says."""
-    st, sh = t.stride(), t.shape
-    return [st[i] if sh[i] > 1 else 128 for i in range(n)]
+def _row_strides(t):
+    """Token and head strides of [T, H, 128]; a dimension of one entry has no stride of its own, whatever torch says."""
+    st, sh, _ = t.stride()
+    n, h, _ = t.shape
+    return st if n > 1 else 128, sh if h > 1 else 128
+
+
+def _page_strides(t):
+    sp, st, sh, _ = t.stride()
+    pages, _, h, _ = t.shape                                  # pages hold at least eight tokens
+    return sp if pages > 1 else 128, st, sh if h > 1 else 128
 
 
 def _ready_status(device):
     """The status word; it must exist before a capture, where its zeroing would become part of the graph."""
-    _need(device.index in _status_words or not torch.cuda.is_current_stream_capturing(),
-          "call status_word() once on this device before capturing")
-    return status_word(device).data_ptr()
+    word = _status_words.get(device.index)
+    if word is None:
+        _need(not torch.cuda.is_current_stream_capturing(), "call status_word() once on this device before capturing")
+        word = status_word(device)
+    return word.data_ptr()
 
 
-class _Launch:
-    """Makes `device` current, and `stream` (when given) too, so that outputs and workspaces allocated for the call belong to it."""
+def _launching(call):
+    """The call with its first tensor's device current and, where `stream` is given, that stream, so that what it allocates
+    belongs to them; the call gets the stream's handle as `handle`."""
 
-    def __init__(self, device, stream):
-        _need(device.type == "cuda", "tensors must be on a CUDA device")
-        self.contexts = []
-        if device.index != torch.cuda.current_device():
-            self.contexts.append(torch.cuda.device(device))
-        if stream is not None:
-            _need(stream.device == device, "the stream belongs to another device")
-            self.contexts.append(torch.cuda.stream(stream))
+    @functools.wraps(call)
+    def run(x, *args, stream=None, **kw):
+        dev = x.device
+        if dev.type != "cuda":
+            _dtype_code(x.dtype)
+            raise ValueError("tensors must be on a CUDA device")
+        if stream is None and dev.index == torch.cuda.current_device():
+            return call(x, *args, handle=torch._C._cuda_getCurrentRawStream(dev.index), **kw)
+        _need(stream is None or stream.device == dev, "the stream belongs to another device")
+        with torch.cuda.device(dev), torch.cuda.stream(stream):
+            return call(x, *args, handle=torch._C._cuda_getCurrentRawStream(dev.index), **kw)
 
-    def __enter__(self):
-        for c in self.contexts:
-            c.__enter__()
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        for c in reversed(self.contexts):
-            c.__exit__(*exc)
+    return run
 
 
 def _rope(tables, device):
@@ -563,56 +572,69 @@ def _rope(tables, device):
         return None, 0
     table, n_pos = tables
     _on(table, "tables", torch.float32, 1, device)
-    _need(table.numel() >= load().pec_rope_table_floats(n_pos), "tables: the table is shorter than n_pos asks for")
+    if table.shape[0] < 8192 + (n_pos + 63) // 64 * 128:       # pec_rope_table_floats
+        raise ValueError("tables: the table is shorter than n_pos asks for")
     return table.data_ptr(), n_pos
 
 
 def _weight(w, what, norm, dtype, device):
     if w is None:
         return None
-    _need(norm, f"{what}: a weight needs norm=True")
+    _need(norm, "a weight needs norm=True")
     _on(w, what, dtype, 1, device)
-    _need(w.numel() == 128, f"{what}: need 128 entries")
+    _need(w.shape[0] == 128, "a norm's weight has 128 entries")
     return w.data_ptr()
 
 
+@_launching
 def pec_qk_norm_rope(q, k=None, *, norm=True, q_weight=None, k_weight=None, eps=1e-6, tables=None, positions=None, pos0=0,
-                     q_out=None, k_out=None, inplace=False, stream=None):
+                     q_out=None, k_out=None, inplace=False, handle=None):
     """RMS norm of every head (norm=True) and rotary encoding (tables = pec_rope_table(...)) in one pass; returns (q_out, k_out).
 
     q [T, Hq, 128], k [T, Hkv, 128] or None: CUDA tensors of one type (bf16 or fp32), last dimension contiguous (column slices
     of a fused projection are fine).  Token t is at positions[t] (int32 CUDA tensor; negative: padding, its rows are not
-    written) or at pos0 + t.  inplace=True writes into q and k.
+    written) or at pos0 + t.  inplace=True writes into q and k.  stream: a torch stream other than the current one.
     """
     lib = load()
     dev, dt = q.device, q.dtype
     code = _dtype_code(dt)
-    with _Launch(dev, stream) as handle:
-        _on(q, "q", dt, 3, dev)
-        T, Hq, D = q.shape
-        q_out = (q if inplace else torch.empty((T, Hq, D), dtype=dt, device=dev)) if q_out is None else q_out
+    _on(q, "q", dt, 3, dev)
+    T, Hq, D = q.shape
+    if q_out is None:
+        q_out = q if inplace else q.new_empty((T, Hq, D))
+    else:
         _on(q_out, "q_out", dt, 3, dev)
         _need(q_out.shape == q.shape, "q_out: need q's shape")
-        side_k = (None, 0, 0, None, 0, 0, 0)
-        if k is not None:
-            _on(k, "k", dt, 3, dev)
-            _need(k.shape[0] == T and k.shape[2] == D, "k: need q's tokens and head dimension")
-            k_out = (k if inplace else torch.empty(k.shape, dtype=dt, device=dev)) if k_out is None else k_out
+    kp = kop = None
+    kst = ksh = kost = kosh = Hkv = 0
+    if k is not None:
+        _on(k, "k", dt, 3, dev)
+        _, Hkv, Dk = k.shape
+        _need(k.shape[0] == T and Dk == D, "k: need q's tokens and head dimension")
+        if k_out is None:
+            k_out = k if inplace else k.new_empty((T, Hkv, D))
+        else:
             _on(k_out, "k_out", dt, 3, dev)
             _need(k_out.shape == k.shape, "k_out: need k's shape")
-            side_k = (k.data_ptr(), *_strides(k, 2), k_out.data_ptr(), *_strides(k_out, 2), k.shape[1])
-        if positions is not None:
-            _on(positions, "positions", torch.int32, 1, dev)
-            _need(positions.numel() == T, "positions: need one per token")
-        table, n_pos = _rope(tables, dev)
-        if T == 0 or Hq + side_k[6] == 0:                     # tensors without elements have no address
-            return q_out, k_out
-        a = pec_norm_rope_args(q.data_ptr(), side_k[0], *_strides(q, 2), side_k[1], side_k[2], q_out.data_ptr(), side_k[3],
-                               *_strides(q_out, 2), side_k[4], side_k[5], code, Hq, side_k[6], D, T,
-                               _weight(q_weight, "q_weight", norm, dt, dev), _weight(k_weight, "k_weight", norm, dt, dev),
-                               1 if norm else 0, eps, table, n_pos, positions.data_ptr() if positions is not None else None, pos0,
-                               _ready_status(dev))
-        _check(lib.pec_qk_norm_rope(ctypes.byref(a), handle))
+        kp, kop = k.data_ptr(), k_out.data_ptr()
+        kst, ksh = _row_strides(k)
+        kost, kosh = _row_strides(k_out)
+    pos = None
+    if positions is not None:
+        _on(positions, "positions", torch.int32, 1, dev)
+        _need(positions.shape[0] == T, "positions: need one per token")
+        pos = positions.data_ptr()
+    table, n_pos = _rope(tables, dev)
+    if T == 0 or Hq + Hkv == 0:                               # tensors without elements have no address
+        return q_out, k_out
+    qst, qsh = _row_strides(q)
+    qost, qosh = _row_strides(q_out)
+    a = pec_norm_rope_args(q.data_ptr(), kp, qst, qsh, kst, ksh, q_out.data_ptr(), kop, qost, qosh, kost, kosh, code, Hq, Hkv, D, T,
+                           _weight(q_weight, "q_weight", norm, dt, dev), _weight(k_weight, "k_weight", norm, dt, dev),
+                           1 if norm else 0, eps, table, n_pos, pos, pos0, _ready_status(dev))
+    rc = lib.pec_qk_norm_rope(a, handle)
+    if rc:
+        _check(rc)
     return q_out, k_out
 
 
@@ -623,78 +645,88 @@ def _paged(k_pages, v_pages, block_table, cu_q, kv_lens, T, dtype, device):
     _on(block_table, "block_table", torch.int32, 2, device)
     _on(cu_q, "cu_q", torch.int32, 1, device)
     _on(kv_lens, "kv_lens", torch.int32, 1, device)
-    B = kv_lens.shape[0]
+    B, = kv_lens.shape
     num_pages, page_size = k_pages.shape[:2]
+    rows, width = block_table.shape
     _need(v_pages.shape == k_pages.shape, "v_pages: need k_pages' shape")
-    _need(cu_q.shape[0] == B + 1 and block_table.shape[0] == B, "need cu_q [B + 1], kv_lens [B] and block_table [B, pages]")
-    return (k_pages.data_ptr(), v_pages.data_ptr(), *_strides(k_pages, 3), *_strides(v_pages, 3), page_size, num_pages,
-            block_table.data_ptr(), block_table.stride(0) if B > 1 else block_table.shape[1], block_table.shape[1],
-            cu_q.data_ptr(), kv_lens.data_ptr(), B, T)
+    _need(cu_q.shape[0] == B + 1 and rows == B, "need cu_q [B + 1], kv_lens [B] and block_table [B, pages]")
+    return (k_pages.data_ptr(), v_pages.data_ptr(), *_page_strides(k_pages), *_page_strides(v_pages), page_size, num_pages,
+            block_table.data_ptr(), block_table.stride(0) if B > 1 else width, width, cu_q.data_ptr(), kv_lens.data_ptr(), B, T)
 
 
+@_launching
 def pec_kv_append(k, v, k_pages, v_pages, block_table, cu_q, kv_lens, *, norm=False, k_weight=None, eps=1e-6, tables=None,
-                  stream=None):
+                  handle=None):
     """Appends a batch's new keys (normalised with norm=True, rotated with tables) and values to a paged cache.
 
     k, v [T, Hkv, 128]; k_pages, v_pages [pages, page_size, Hkv, 128] (any strides but the last: transpose head-major pages
     into this order); block_table int32 [B, pages per request], cu_q int32 [B + 1] offsets of the requests' new tokens in k, v,
     kv_lens int32 [B] cached tokens including the new ones.  All CUDA tensors; the tables are read when the kernel runs.
+    stream: a torch stream other than the current one.
     """
     lib = load()
     dev, dt = k.device, k.dtype
     code = _dtype_code(dt)
-    with _Launch(dev, stream) as handle:
-        _on(k, "k", dt, 3, dev)
-        _on(v, "v", dt, 3, dev)
-        T, Hkv, D = k.shape
-        _need(v.shape == k.shape, "v: need k's shape")
-        cache = _paged(k_pages, v_pages, block_table, cu_q, kv_lens, T, dt, dev)
-        _need(k_pages.shape[2] == Hkv and k_pages.shape[3] == D, "k_pages: need k's heads and head dimension")
-        table, n_pos = _rope(tables, dev)
-        if T == 0:                                            # tensors without elements have no address
-            return
-        a = pec_kv_append_args(k.data_ptr(), v.data_ptr(), *_strides(k, 2), *_strides(v, 2), code, *cache, Hkv, D,
-                               _weight(k_weight, "k_weight", norm, dt, dev), 1 if norm else 0, eps, table, n_pos,
-                               _ready_status(dev))
-        _check(lib.pec_kv_append(ctypes.byref(a), handle))
+    _on(k, "k", dt, 3, dev)
+    _on(v, "v", dt, 3, dev)
+    T, Hkv, D = k.shape
+    _need(v.shape == k.shape, "v: need k's shape")
+    cache = _paged(k_pages, v_pages, block_table, cu_q, kv_lens, T, dt, dev)
+    _need(k_pages.shape[2] == Hkv and k_pages.shape[3] == D, "k_pages: need k's heads and head dimension")
+    table, n_pos = _rope(tables, dev)
+    if T == 0:                                                # tensors without elements have no address
+        return
+    a = pec_kv_append_args(k.data_ptr(), v.data_ptr(), *_row_strides(k), *_row_strides(v), code, *cache, Hkv, D,
+                           _weight(k_weight, "k_weight", norm, dt, dev), 1 if norm else 0, eps, table, n_pos, _ready_status(dev))
+    rc = lib.pec_kv_append(a, handle)
+    if rc:
+        _check(rc)
 
 
+@_launching
 def pec_paged_attn(q, k_pages, v_pages, block_table, cu_q, kv_lens, *, max_q_len=0, causal=True, softmax_scale=0.0,
-                   out_dtype=None, o=None, lse=None, workspace=None, stream=None):
+                   out_dtype=None, o=None, lse=None, workspace=None, handle=None):
     """Attention of a batch's new tokens q [T, Hq, 128] over a paged cache that holds their keys and values already (see
     pec_kv_append for the cache and the tables); returns (o [T, Hq, 128], lse [T, Hq]).
 
     max_q_len: an upper bound of any request's new tokens (0: unknown); the kernels are chosen by it.  workspace: uint8 CUDA
-    tensor of at least the size the library asks for, allocated here when not given.
+    tensor of at least the size the library asks for, allocated here when not given.  stream: a torch stream other than the
+    current one.
     """
     lib = load()
     dev, dt = q.device, q.dtype
     code = _dtype_code(dt)
-    with _Launch(dev, stream) as handle:
-        _on(q, "q", dt, 3, dev)
-        T, Hq, D = q.shape
-        cache = _paged(k_pages, v_pages, block_table, cu_q, kv_lens, T, dt, dev)
-        _need(k_pages.shape[3] == D, "k_pages: need q's head dimension")
-        if o is None:
-            o = torch.empty((T, Hq, D), dtype=dt if out_dtype is None else out_dtype, device=dev)
-        if lse is None:
-            lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
-        _need(o.device == dev and o.is_contiguous() and o.shape == q.shape and (out_dtype is None or o.dtype == out_dtype),
+    _on(q, "q", dt, 3, dev)
+    T, Hq, D = q.shape
+    cache = _paged(k_pages, v_pages, block_table, cu_q, kv_lens, T, dt, dev)
+    _need(k_pages.shape[3] == D, "k_pages: need q's head dimension")
+    out_dtype = dt if out_dtype is None and o is None else out_dtype
+    if o is None:
+        o = torch.empty((T, Hq, D), dtype=out_dtype, device=dev)
+    else:
+        _need(o.device == dev and o.is_contiguous() and o.shape == q.shape and (out_dtype is None or o.dtype is out_dtype),
               "o: need a contiguous tensor of q's shape")
-        _need(lse.device == dev and lse.is_contiguous() and lse.dtype == torch.float32 and lse.shape == (T, Hq),
+    if lse is None:
+        lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
+    else:
+        _need(lse.device == dev and lse.is_contiguous() and lse.dtype is torch.float32 and lse.shape == (T, Hq),
               "lse: need a contiguous fp32 tensor [T, Hq]")
-        if T == 0:                                            # tensors without elements have no address
-            return o, lse
-        a = pec_paged_args(q.data_ptr(), *_strides(q, 2), code, *cache, max_q_len, o.data_ptr(), _dtype_code(o.dtype),
-                           lse.data_ptr(), Hq, k_pages.shape[2], D, 1 if causal else 0, softmax_scale, None, 0, _ready_status(dev))
-        ref = ctypes.byref(a)
-        if workspace is None:
-            need = lib.pec_paged_workspace_size(ref)
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-        if workspace is not None:
-            _need(workspace.device == dev and workspace.is_contiguous(), "workspace: need a contiguous tensor on q's device")
-            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        _check(lib.pec_paged_attn(ref, handle))
+    if T == 0:                                                # tensors without elements have no address
+        return o, lse
+    qst, qsh = _row_strides(q)
+    a = pec_paged_args(q.data_ptr(), qst, qsh, code, *cache, max_q_len, o.data_ptr(), _dtype_code(o.dtype), lse.data_ptr(), Hq,
+                       k_pages.shape[2], D, 1 if causal else 0, softmax_scale, None, 0, _ready_status(dev))
+    if workspace is None:
+        size = lib.pec_paged_workspace_size(a)
+        if size:
+            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), size
+    else:
+        _need(workspace.device == dev and workspace.is_contiguous(), "workspace: need a contiguous tensor on q's device")
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    rc = lib.pec_paged_attn(a, handle)
+    if rc:
+        _check(rc)
     return o, lse
 
 

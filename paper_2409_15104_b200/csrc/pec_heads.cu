@@ -6,12 +6,12 @@
 //     z[i] = y[i] cos a - y[i + 64] sin a,   z[i + 64] = y[i + 64] cos a + y[i] sin a,   a = p theta^(-2 i / 128)
 //
 // Bound by memory: every element is read once and written once, rounded once at the end (sums and products in fp32).  A
-// head's 128 elements are one 16-byte vector per lane: 16 lanes of a bf16 head, 32 of an fp32 head.  The sum of squares is
-// a shuffle tree over those lanes and a channel's partner 64 away sits half the lanes away, one shuffle per element.  The
-// angle depends on the token only, so a block works on whole tokens: it works out the 64 cosines and sines of each of its
-// tokens once (two-level table of pec_rope_table: 16 KB of fine entries that stay in L1 plus one coarse row) and every head
-// of the token reads them from shared memory.  Each lane issues the loads of kRows heads before anything else, so their
-// latency runs beside the search for the token's request and the table reads.
+// head is held by 16 lanes, each with channels 4 l .. 4 l + 3 and their partners 64 on, so that the rotation needs nothing from
+// another lane and the sum of squares four shuffles.  The angle depends on the token only: a warp takes some heads of one
+// token (two at a time, one per half warp, the loads of kRows pairs in flight), and its lanes work out the cosines and sines of
+// their four channels once, from the two-level table of pec_rope_table.  Nothing goes through shared memory.
+// (Measured on 8192 tokens of 64 + 8 bf16 heads, 302 MB: a block per token with the angles in shared memory and the partners by
+// shuffle took 132 us.)
 #include <cmath>
 #include <cstdio>
 #include <cuda_bf16.h>
@@ -23,95 +23,106 @@
 namespace pec {
 namespace heads {
 
-constexpr int kThreads = 256;
-constexpr int kRows = 4;                     // rows of a lane group in flight
-constexpr int kMaxTokens = 8;                // tokens of a block (one warp each looks a token up)
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kRows = 4;                     // heads of a half warp in flight
 
-template <class E> struct Vec;
-template <> struct Vec<__nv_bfloat16> {
-    static constexpr int kN = 8;
-    static __device__ __forceinline__ void unpack(const uint4 &u, float (&x)[8])
+// Four channels of a head as they lie in memory.
+template <class E> struct Quad;
+template <> struct Quad<__nv_bfloat16> {
+    typedef uint2 Raw;
+    static __device__ __forceinline__ void unpack(const Raw &u, float (&x)[4])
     {
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+        x[0] = __uint_as_float(u.x << 16); x[1] = __uint_as_float(u.x & 0xffff0000u);
+        x[2] = __uint_as_float(u.y << 16); x[3] = __uint_as_float(u.y & 0xffff0000u);
     }
-    static __device__ __forceinline__ uint4 pack(const float (&x)[8])
+    static __device__ __forceinline__ Raw pack(const float (&x)[4])
     {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t *>(&p);
-        }
-        return make_uint4(w[0], w[1], w[2], w[3]);
+        const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+        return make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
     }
 };
-template <> struct Vec<float> {
-    static constexpr int kN = 4;
-    static __device__ __forceinline__ void unpack(const uint4 &u, float (&x)[4])
-    {
-        x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y); x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
-    }
-    static __device__ __forceinline__ uint4 pack(const float (&x)[4])
-    {
-        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-    }
+template <> struct Quad<float> {
+    typedef float4 Raw;
+    static __device__ __forceinline__ void unpack(const Raw &u, float (&x)[4]) { x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; }
+    static __device__ __forceinline__ Raw pack(const float (&x)[4]) { return make_float4(x[0], x[1], x[2], x[3]); }
 };
+template <class E> struct Head { typename Quad<E>::Raw lo, hi; };    // a lane's eight channels
+template <class E>
+__device__ __forceinline__ Head<E> load_head(const E *head, int l)
+{
+    typedef typename Quad<E>::Raw Raw;
+    Head<E> u;
+    u.lo = *reinterpret_cast<const Raw *>(head + 4 * l);
+    u.hi = *reinterpret_cast<const Raw *>(head + 64 + 4 * l);
+    return u;
+}
+template <class E>
+__device__ __forceinline__ void store_head(E *head, int l, const Head<E> &u)
+{
+    typedef typename Quad<E>::Raw Raw;
+    *reinterpret_cast<Raw *>(head + 4 * l) = u.lo;
+    *reinterpret_cast<Raw *>(head + 64 + 4 * l) = u.hi;
+}
 
 struct Turn { const float *table; int64_t n_pos; };            // table of pec_rope_table, or NULL: no rotation
 constexpr int kFine = 64 * 64;
 
-// cos and sin of channel i at position p = 64 a + b by the addition theorem (see pec_rope_table).
-__device__ __forceinline__ void angle(const Turn &t, int32_t p, int i, float &c, float &s)
+// Cosines and sines of channels 4 l .. 4 l + 3 at position p = 64 a + b by the addition theorem (see pec_rope_table).
+__device__ __forceinline__ void angles(const Turn &t, int32_t p, int l, float (&c)[4], float (&s)[4])
 {
-    const int64_t na = (t.n_pos + 63) / 64, a = p >> 6;
+    const int64_t na = (t.n_pos + 63) / 64;
     const int b = p & 63;
-    const float *coarse = t.table + 2 * kFine + a * 64 + i;
-    const float cc = __ldg(coarse), cs = __ldg(coarse + na * 64);
-    const float fc = __ldg(t.table + i * 64 + b), fs = __ldg(t.table + kFine + i * 64 + b);
-    c = cc * fc - cs * fs;
-    s = cs * fc + cc * fs;
+    const float *coarse = t.table + 2 * kFine + (int64_t)(p >> 6) * 64 + 4 * l, *fine = t.table + 4 * l * 64 + b;
+    const float4 c4 = __ldg(reinterpret_cast<const float4 *>(coarse)), s4 = __ldg(reinterpret_cast<const float4 *>(coarse + na * 64));
+    const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, cs[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float fc = __ldg(fine + i * 64), fs = __ldg(fine + kFine + i * 64);
+        c[i] = cc[i] * fc - cs[i] * fs;
+        s[i] = cs[i] * fc + cc[i] * fs;
+    }
 }
 
-// Norm and rotation of one head held by a group of 128 / kN lanes, `l` the lane's place in it.  A lane of the lower half
-// of the head holds y[i], its partner y[i + 64].  cs, sn: the token's 64 cosines and sines in shared memory, or NULL.
+// Norm and rotation of one head held by a half warp.
 template <class E>
-__device__ __forceinline__ void head_math(float (&x)[Vec<E>::kN], int l, bool norm, const float (&w)[Vec<E>::kN], float eps,
-                                          const float *cs, const float *sn)
+__device__ __forceinline__ void head_math(Head<E> &u, bool norm, const float (&wl)[4], const float (&wh)[4], float eps,
+                                          bool turn, const float (&c)[4], const float (&s)[4])
 {
-    constexpr int kN = Vec<E>::kN, kLanes = kHeadDim / kN;
+    float lo[4], hi[4];
+    Quad<E>::unpack(u.lo, lo);
+    Quad<E>::unpack(u.hi, hi);
     if (norm) {
         float ss = 0.f;
 #pragma unroll
-        for (int i = 0; i < kN; ++i) ss = fmaf(x[i], x[i], ss);
+        for (int i = 0; i < 4; ++i) { ss = fmaf(lo[i], lo[i], ss); ss = fmaf(hi[i], hi[i], ss); }
 #pragma unroll
-        for (int d = kLanes / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-        const float r = 1.f / sqrtf(ss * (1.f / kHeadDim) + eps);
+        for (int d = 8; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+        const float r = rsqrtf(ss * (1.f / kHeadDim) + eps);
 #pragma unroll
-        for (int i = 0; i < kN; ++i) x[i] = x[i] * r * w[i];
+        for (int i = 0; i < 4; ++i) { lo[i] = lo[i] * r * wl[i]; hi[i] = hi[i] * r * wh[i]; }
     }
-    if (cs) {
-        const int i0 = (l * kN) & 63;
-        const bool upper = l >= kLanes / 2;
+    if (turn) {
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const float other = __shfl_xor_sync(0xffffffffu, x[i], kLanes / 2);
-            const float c = cs[i0 + i], s = sn[i0 + i];
-            x[i] = upper ? fmaf(x[i], c, other * s) : fmaf(x[i], c, -other * s);
+        for (int i = 0; i < 4; ++i) {
+            const float a = lo[i], b = hi[i];
+            lo[i] = fmaf(a, c[i], -b * s[i]);
+            hi[i] = fmaf(b, c[i], a * s[i]);
         }
     }
+    u.lo = Quad<E>::pack(lo);
+    u.hi = Quad<E>::pack(hi);
 }
 
 template <class E>
-__device__ __forceinline__ void load_weight(const void *w, int l, float (&out)[Vec<E>::kN])
+__device__ __forceinline__ void load_weight(const void *w, int l, float (&lo)[4], float (&hi)[4])
 {
     if (w) {
-        const uint4 u = *reinterpret_cast<const uint4 *>(static_cast<const E *>(w) + l * Vec<E>::kN);
-        Vec<E>::unpack(u, out);
+        const Head<E> u = load_head(static_cast<const E *>(w), l);
+        Quad<E>::unpack(u.lo, lo);
+        Quad<E>::unpack(u.hi, hi);
     } else {
 #pragma unroll
-        for (int i = 0; i < Vec<E>::kN; ++i) out[i] = 1.f;
+        for (int i = 0; i < 4; ++i) lo[i] = hi[i] = 1.f;
     }
 }
 
@@ -129,74 +140,52 @@ struct NormRope {
     int32_t *status;
 };
 
-// Block: tokens [tok * blockIdx.x, +tok), head rows dealt to lane groups; blockIdx.y takes its share of the heads.
+// Warp: heads [h0, h0 + per) of one token.
 template <class E>
 __global__ void __launch_bounds__(kThreads)
-norm_rope_kernel(const NormRope p, const int tok, const int heads_per_block)
+norm_rope_kernel(const NormRope p, const int parts, const int per)
 {
-    constexpr int kN = Vec<E>::kN, kLanes = kHeadDim / kN, kGroups = kThreads / kLanes;
-    __shared__ float s_cos[kMaxTokens][64], s_sin[kMaxTokens][64];
-    __shared__ int32_t s_ok[kMaxTokens];
-    const int tid = threadIdx.x, l = tid % kLanes, grp = tid / kLanes;
-    const int t0 = blockIdx.x * tok, nt = min(tok, p.T - t0);
-    const int h0 = blockIdx.y * heads_per_block, nh = min(heads_per_block, p.H - h0);
-    const int rows = nt * nh;
+    const int lane = threadIdx.x & 31, l = lane & 15, half = lane >> 4;
+    const int64_t unit = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const int32_t t = (int32_t)(unit / parts);
+    if (t >= p.T) return;
+    const int h0 = (int)(unit - (int64_t)t * parts) * per, h1 = min(h0 + per, p.H);
 
-    auto src = [&](int r) -> const uint4 * {
-        const int64_t t = t0 + r / nh;
-        const int h = h0 + r % nh;
-        const E *base = h < p.Hq ? static_cast<const E *>(p.q) + t * p.q_st + h * p.q_sh
-                                 : static_cast<const E *>(p.k) + t * p.k_st + (h - p.Hq) * p.k_sh;
-        return reinterpret_cast<const uint4 *>(base + l * kN);
-    };
-    auto fetch = [&](int r0, uint4 (&u)[kRows]) {
+    auto fetch = [&](int base, Head<E> (&u)[kRows]) {
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            u[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (r0 + i * kGroups < rows) u[i] = *src(r0 + i * kGroups);
+            const int h = base + half + 2 * i;
+            if (h < h1)
+                u[i] = load_head(h < p.Hq ? static_cast<const E *>(p.q) + t * p.q_st + h * p.q_sh
+                                          : static_cast<const E *>(p.k) + t * p.k_st + (h - p.Hq) * p.k_sh, l);
         }
     };
-    uint4 u[kRows];
-    fetch(grp, u);
-    float qw[kN], kw[kN];
-    load_weight<E>(p.norm ? p.qw : nullptr, l, qw);
-    load_weight<E>(p.norm ? p.kw : nullptr, l, kw);
-    // Positions and angles of the block's tokens.  A negative position marks a padding row; one past the table is reported.
-    for (int i = tid; i < nt * 64; i += kThreads) {
-        const int k = i >> 6, ch = i & 63;
-        const int64_t pos = p.positions ? (int64_t)p.positions[t0 + k] : p.pos0 + t0 + k;
-        bool ok = pos >= 0;
-        if (ok && p.turn.table) {
-            if (pos >= p.turn.n_pos) {
-                ok = false;
-                if (ch == 0) raise_status(p.status, PEC_ERR_BAD_INDEX);
-            } else {
-                angle(p.turn, (int32_t)pos, ch, s_cos[k][ch], s_sin[k][ch]);
-            }
-        }
-        if (ch == 0) s_ok[k] = ok;
+    Head<E> u[kRows] = {};
+    fetch(h0, u);
+    // A negative position marks a padding row; one past the table is reported.
+    const int64_t pos = p.positions ? (int64_t)p.positions[t] : p.pos0 + t;
+    if (pos < 0) return;
+    if (p.turn.table && pos >= p.turn.n_pos) {
+        if (lane == 0) raise_status(p.status, PEC_ERR_BAD_INDEX);
+        return;
     }
-    __syncthreads();
-    for (int r0 = grp; r0 - grp < rows; r0 += kRows * kGroups) {
-        if (r0 != grp) fetch(r0, u);
+    float c[4] = {}, s[4] = {}, ql[4], qh[4], kl[4], kh[4];
+    if (p.turn.table) angles(p.turn, (int32_t)pos, l, c, s);
+    load_weight<E>(p.norm && h0 < p.Hq ? p.qw : nullptr, l, ql, qh);
+    load_weight<E>(p.norm && h1 > p.Hq ? p.kw : nullptr, l, kl, kh);
+    for (int base = h0; base < h1; base += 2 * kRows) {
+        if (base != h0) fetch(base, u);
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int r = r0 + i * kGroups;
-            if (r - grp >= rows) break;                       // uniform over the block: shuffles stay converged
-            const int rr = min(r, rows - 1), k = rr / nh, h = h0 + rr % nh;
-            float x[kN];
-            Vec<E>::unpack(u[i], x);
+            const int h = base + half + 2 * i;
             const bool is_q = h < p.Hq;
-            float w[kN];
+            float wl[4], wh[4];
 #pragma unroll
-            for (int c = 0; c < kN; ++c) w[c] = is_q ? qw[c] : kw[c];
-            head_math<E>(x, l, p.norm != 0, w, p.eps, p.turn.table ? s_cos[k] : nullptr, s_sin[k]);
-            if (r < rows && s_ok[k]) {
-                const int64_t t = t0 + k;
-                E *dst = is_q ? static_cast<E *>(p.qo) + t * p.qo_st + h * p.qo_sh
-                              : static_cast<E *>(p.ko) + t * p.ko_st + (h - p.Hq) * p.ko_sh;
-                *reinterpret_cast<uint4 *>(dst + l * kN) = Vec<E>::pack(x);
-            }
+            for (int x = 0; x < 4; ++x) { wl[x] = is_q ? ql[x] : kl[x]; wh[x] = is_q ? qh[x] : kh[x]; }
+            head_math<E>(u[i], p.norm != 0, wl, wh, p.eps, p.turn.table != nullptr, c, s);
+            if (h < h1)
+                store_head(is_q ? static_cast<E *>(p.qo) + t * p.qo_st + h * p.qo_sh
+                                : static_cast<E *>(p.ko) + t * p.ko_st + (h - p.Hq) * p.ko_sh, l, u[i]);
         }
     }
 }
@@ -214,102 +203,72 @@ struct Append {
     int32_t *status;
 };
 
+// As above over a token's key heads and then its value heads.
 template <class E>
 __global__ void __launch_bounds__(kThreads)
-kv_append_kernel(const Append p, const int tok, const int heads_per_block)
+kv_append_kernel(const Append p, const int parts, const int per)
 {
-    constexpr int kN = Vec<E>::kN, kLanes = kHeadDim / kN, kGroups = kThreads / kLanes;
-    __shared__ float s_cos[kMaxTokens][64], s_sin[kMaxTokens][64];
-    __shared__ int32_t s_pos[kMaxTokens];                           // -1: nothing to store
-    __shared__ int64_t s_k[kMaxTokens], s_v[kMaxTokens];            // the token's slot in either cache, elements
-    const int tid = threadIdx.x, warp = tid >> 5, l = tid % kLanes, grp = tid / kLanes;
-    const int t0 = blockIdx.x * tok, nt = min(tok, p.c.T - t0);
-    const int H = 2 * p.Hkv, h0 = blockIdx.y * heads_per_block, nh = min(heads_per_block, H - h0);
-    const int rows = nt * nh;
+    const int lane = threadIdx.x & 31, l = lane & 15, half = lane >> 4;
+    const int64_t unit = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const int32_t t = (int32_t)(unit / parts);
+    if (t >= p.c.T) return;
+    const int H = 2 * p.Hkv, h0 = (int)(unit - (int64_t)t * parts) * per, h1 = min(h0 + per, H);
 
-    auto fetch = [&](int r0, uint4 (&u)[kRows]) {
+    auto fetch = [&](int base, Head<E> (&u)[kRows]) {
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int r = r0 + i * kGroups;
-            u[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < rows) {
-                const int64_t t = t0 + r / nh;
-                const int h = h0 + r % nh;
-                const E *base = h < p.Hkv ? static_cast<const E *>(p.k) + t * p.k_st + h * p.k_sh
-                                          : static_cast<const E *>(p.v) + t * p.v_st + (h - p.Hkv) * p.v_sh;
-                u[i] = *reinterpret_cast<const uint4 *>(base + l * kN);
-            }
+            const int h = base + half + 2 * i;
+            if (h < h1)
+                u[i] = load_head(h < p.Hkv ? static_cast<const E *>(p.k) + t * p.k_st + h * p.k_sh
+                                           : static_cast<const E *>(p.v) + t * p.v_st + (h - p.Hkv) * p.v_sh, l);
         }
     };
-    uint4 u[kRows];
-    fetch(grp, u);
-    float kw[kN];
-    load_weight<E>(p.norm ? p.kw : nullptr, l, kw);
-    if (warp < nt) {                                                // one warp per token: request, position, page, slot
-        const int32_t t = t0 + warp;
-        int32_t b, end, pos = -1;
-        if (find_request(p.c, t, p.status, b, end)) {
-            const int64_t at = (int64_t)p.c.kv_lens[b] - end + t;
-            const int64_t nth = at / p.c.page_size;
-            bool ok = at >= 0 && nth < p.c.max_pages && (!p.turn.table || at < p.turn.n_pos);
-            int64_t page = -1;
-            if (ok) {
-                page = p.c.table[b * p.c.table_stride + nth];
-                ok = page >= 0 && page < p.c.num_pages;
-            }
-            if (ok) {
-                pos = (int32_t)at;
-                const int64_t slot = at - nth * p.c.page_size;
-                s_k[warp] = page * p.c.k_sp + slot * p.c.k_st;
-                s_v[warp] = page * p.c.v_sp + slot * p.c.v_st;
-            } else if ((tid & 31) == 0) {
-                raise_status(p.status, PEC_ERR_BAD_INDEX);
-            }
-        }
-        s_pos[warp] = pos;
+    Head<E> u[kRows] = {};
+    fetch(h0, u);
+    float wl[4], wh[4], c[4] = {}, s[4] = {};
+    const bool math = h0 < p.Hkv && (p.norm || p.turn.table);      // values alone, or keys as they are: a copy
+    load_weight<E>(math && p.norm ? p.kw : nullptr, l, wl, wh);
+    int32_t b, end;
+    if (!find_request(p.c, t, p.status, b, end)) return;
+    const int64_t pos = (int64_t)p.c.kv_lens[b] - end + t, nth = pos / p.c.page_size;
+    bool ok = pos >= 0 && nth < p.c.max_pages && (!p.turn.table || pos < p.turn.n_pos);
+    int64_t page = -1;
+    if (ok) {
+        page = p.c.table[b * p.c.table_stride + nth];
+        ok = page >= 0 && page < p.c.num_pages;
     }
-    __syncthreads();
-    if (p.turn.table) {
-        for (int i = tid; i < nt * 64; i += kThreads) {
-            const int k = i >> 6, ch = i & 63;
-            if (s_pos[k] >= 0) angle(p.turn, s_pos[k], ch, s_cos[k][ch], s_sin[k][ch]);
-        }
-        __syncthreads();
+    if (!ok) {
+        if (lane == 0) raise_status(p.status, PEC_ERR_BAD_INDEX);
+        return;
     }
-    for (int r0 = grp; r0 - grp < rows; r0 += kRows * kGroups) {
-        if (r0 != grp) fetch(r0, u);
+    if (math && p.turn.table) angles(p.turn, (int32_t)pos, l, c, s);
+    const int64_t slot = pos - nth * p.c.page_size;
+    E *k_slot = static_cast<E *>(p.k_pages) + page * p.c.k_sp + slot * p.c.k_st;
+    E *v_slot = static_cast<E *>(p.v_pages) + page * p.c.v_sp + slot * p.c.v_st;
+    for (int base = h0; base < h1; base += 2 * kRows) {
+        if (base != h0) fetch(base, u);
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int r = r0 + i * kGroups;
-            if (r - grp >= rows) break;                             // uniform over the block
-            const int rr = min(r, rows - 1), k = rr / nh, h = h0 + rr % nh;
+            const int h = base + half + 2 * i;
             const bool is_k = h < p.Hkv;
-            if (__any_sync(0xffffffffu, is_k)) {                    // a bf16 warp holds two heads, perhaps a key and a value
-                float x[kN];
-                Vec<E>::unpack(u[i], x);
-                head_math<E>(x, l, p.norm != 0, kw, p.eps, p.turn.table ? s_cos[k] : nullptr, s_sin[k]);
-                if (is_k && (p.norm || p.turn.table)) u[i] = Vec<E>::pack(x);
+            if (math) {                                             // uniform over the warp; a pair may be a key and a value
+                Head<E> z = u[i];
+                head_math<E>(z, p.norm != 0, wl, wh, p.eps, p.turn.table != nullptr, c, s);
+                if (is_k) u[i] = z;
             }
-            if (r < rows && s_pos[k] >= 0) {
-                E *dst = is_k ? static_cast<E *>(p.k_pages) + s_k[k] + h * p.c.k_sh
-                              : static_cast<E *>(p.v_pages) + s_v[k] + (h - p.Hkv) * p.c.v_sh;
-                *reinterpret_cast<uint4 *>(dst + l * kN) = u[i];
-            }
+            if (h < h1) store_head(is_k ? k_slot + h * p.c.k_sh : v_slot + (h - p.Hkv) * p.c.v_sh, l, u[i]);
         }
     }
 }
 
-// Tokens and heads of a block.  Large calls: whole tokens, so that the angles are worked out once per token, and about 64
-// rows a block where a token has fewer heads than that.  Calls too small to fill the GPU that way (`rows` below two full
-// waves of lane groups) take one token a block and split its heads over grid.y.
-inline void block_shape(int64_t T, int H, int groups, int &tok, int &hpb)
+// Parts that a token's H heads are dealt to, one warp each: 16 heads a warp where there are tokens enough to fill the GPU (the
+// angles are then worked out once for 16 heads), fewer where there are not, down to one pair.
+inline void deal(int64_t T, int64_t H, int &parts, int &per)
 {
-    tok = 64 / H < 1 ? 1 : (64 / H > kMaxTokens ? kMaxTokens : 64 / H);
-    hpb = H;
-    if (T * H < (int64_t)2 * 148 * 8 * groups) {
-        tok = 1;
-        hpb = H > groups ? groups : H;
-    }
+    int64_t n = T * H / (148 * 32);
+    n = n < 2 ? 2 : (n > 16 ? 16 : (n + 1) / 2 * 2);
+    per = (int)(n < H ? n : H);
+    parts = (int)((H + per - 1) / per);
 }
 
 }  // namespace heads
@@ -414,12 +373,13 @@ extern "C" int pec_qk_norm_rope(const pec_norm_rope_args *a, void *cuda_stream)
     p.qw = a->q_weight; p.kw = a->k_weight; p.norm = a->norm; p.eps = a->eps;
     p.turn = {a->rope_table, a->n_pos};
     p.positions = a->positions; p.pos0 = a->pos0; p.status = a->status;
-    int tok, hpb;
-    heads::block_shape(p.T, p.H, heads::kThreads / (esz == 2 ? 16 : 32), tok, hpb);
-    const dim3 grid((unsigned)((p.T + tok - 1) / tok), (unsigned)((p.H + hpb - 1) / hpb));
+    int parts, per;
+    heads::deal(p.T, p.H, parts, per);
+    const int64_t blocks = ((int64_t)p.T * parts + heads::kWarps - 1) / heads::kWarps;
+    if (blocks > 0x7fffffff) { set_error("%s: grid too large", who); return PEC_ERR_UNSUPPORTED; }
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (esz == 2) heads::norm_rope_kernel<__nv_bfloat16><<<grid, heads::kThreads, 0, stream>>>(p, tok, hpb);
-    else          heads::norm_rope_kernel<float><<<grid, heads::kThreads, 0, stream>>>(p, tok, hpb);
+    if (esz == 2) heads::norm_rope_kernel<__nv_bfloat16><<<(unsigned)blocks, heads::kThreads, 0, stream>>>(p, parts, per);
+    else          heads::norm_rope_kernel<float><<<(unsigned)blocks, heads::kThreads, 0, stream>>>(p, parts, per);
     const cudaError_t err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("%s: launch failed: %s", who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
@@ -446,12 +406,13 @@ extern "C" int pec_kv_append(const pec_kv_append_args *a, void *cuda_stream)
     p.k = a->k; p.v = a->v; p.k_st = s[0]; p.k_sh = s[1]; p.v_st = s[2]; p.v_sh = s[3];
     p.k_pages = a->k_pages; p.v_pages = a->v_pages; p.Hkv = a->Hkv;
     p.kw = a->k_weight; p.norm = a->norm; p.eps = a->eps; p.turn = {a->rope_table, a->n_pos}; p.status = a->status;
-    int tok, hpb;
-    heads::block_shape(a->T, 2 * a->Hkv, heads::kThreads / (esz == 2 ? 16 : 32), tok, hpb);
-    const dim3 grid((unsigned)((a->T + tok - 1) / tok), (unsigned)((2 * (int64_t)a->Hkv + hpb - 1) / hpb));
+    int parts, per;
+    heads::deal(a->T, 2 * (int64_t)a->Hkv, parts, per);
+    const int64_t blocks = (a->T * parts + heads::kWarps - 1) / heads::kWarps;
+    if (blocks > 0x7fffffff) { set_error("%s: grid too large", who); return PEC_ERR_UNSUPPORTED; }
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (esz == 2) heads::kv_append_kernel<__nv_bfloat16><<<grid, heads::kThreads, 0, stream>>>(p, tok, hpb);
-    else          heads::kv_append_kernel<float><<<grid, heads::kThreads, 0, stream>>>(p, tok, hpb);
+    if (esz == 2) heads::kv_append_kernel<__nv_bfloat16><<<(unsigned)blocks, heads::kThreads, 0, stream>>>(p, parts, per);
+    else          heads::kv_append_kernel<float><<<(unsigned)blocks, heads::kThreads, 0, stream>>>(p, parts, per);
     const cudaError_t err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("%s: launch failed: %s", who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
