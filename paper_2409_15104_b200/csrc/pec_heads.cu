@@ -7,11 +7,15 @@
 //
 // Bound by memory: every element is read once and written once, rounded once at the end (sums and products in fp32).  A
 // head is held by 16 lanes, each with channels 4 l .. 4 l + 3 and their partners 64 on, so that the rotation needs nothing from
-// another lane and the sum of squares four shuffles.  The angle depends on the token only: a warp takes some heads of one
-// token (two at a time, one per half warp, the loads of kRows pairs in flight), and its lanes work out the cosines and sines of
-// their four channels once, from the two-level table of pec_rope_table.  Nothing goes through shared memory.
-// (Measured on 8192 tokens of 64 + 8 bf16 heads, 302 MB: a block per token with the angles in shared memory and the partners by
-// shuffle took 132 us.)
+// another lane and the sum of squares four shuffles.  With r = 1 / sqrt(..) both steps are one linear map of the pair,
+//     z[i] = r (x[i] (w[i] cos) - x[i + 64] (w[i + 64] sin)),   z[i + 64] = r (x[i + 64] (w[i + 64] cos) + x[i] (w[i] sin)),
+// whose coefficients depend on the token only and stay in registers while a warp walks the token's heads (two at a time, one per
+// half warp, kRows pairs of loads in flight).
+// A block takes eight tokens, a warp each.  Its threads work out the tokens' cosines and sines together, with neighbouring lanes
+// on neighbouring tokens: the fine part of pec_rope_table's table is stored channel-major, and a token looked up by itself
+// touches 128 lines of it for 4 bytes each, more than all the data of eight heads.
+// (8192 tokens of 64 + 8 bf16 heads, 302 MB: a block per token with angles per lane and partners by shuffle 132 us; a warp per 16
+// heads that looked its angles up itself 83 us, half of the LSU wavefronts spent on the table.)
 #include <cmath>
 #include <cstdio>
 #include <cuda_bf16.h>
@@ -66,71 +70,84 @@ __device__ __forceinline__ void store_head(E *head, int l, const Head<E> &u)
 
 struct Turn { const float *table; int64_t n_pos; };            // table of pec_rope_table, or NULL: no rotation
 constexpr int kFine = 64 * 64;
+constexpr int kLdAngle = 68;                                    // padded row: eight tokens x four channels without bank conflicts
+struct Angles { float cos[kWarps][kLdAngle], sin[kWarps][kLdAngle]; int32_t pos[kWarps]; };
 
-// Cosines and sines of channels 4 l .. 4 l + 3 at position p = 64 a + b by the addition theorem (see pec_rope_table).
-__device__ __forceinline__ void angles(const Turn &t, int32_t p, int l, float (&c)[4], float (&s)[4])
+// Cosines and sines of the block's tokens (position < 0: none) at p = 64 a + b by the addition theorem (see pec_rope_table).
+__device__ __forceinline__ void angles(const Turn &t, Angles &a)
 {
+    const int tok = threadIdx.x & 7;
+    const int32_t p = a.pos[tok];
+    if (p < 0) return;
     const int64_t na = (t.n_pos + 63) / 64;
-    const int b = p & 63;
-    const float *coarse = t.table + 2 * kFine + (int64_t)(p >> 6) * 64 + 4 * l, *fine = t.table + 4 * l * 64 + b;
-    const float4 c4 = __ldg(reinterpret_cast<const float4 *>(coarse)), s4 = __ldg(reinterpret_cast<const float4 *>(coarse + na * 64));
-    const float cc[4] = {c4.x, c4.y, c4.z, c4.w}, cs[4] = {s4.x, s4.y, s4.z, s4.w};
+    const float *coarse = t.table + 2 * kFine + (int64_t)(p >> 6) * 64, *fine = t.table + (p & 63);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float fc = __ldg(fine + i * 64), fs = __ldg(fine + kFine + i * 64);
-        c[i] = cc[i] * fc - cs[i] * fs;
-        s[i] = cs[i] * fc + cc[i] * fs;
+    for (int j = 0; j < 2; ++j) {
+        const int i = (threadIdx.x >> 3) + 32 * j;
+        const float cc = __ldg(coarse + i), cs = __ldg(coarse + na * 64 + i), fc = __ldg(fine + i * 64), fs = __ldg(fine + kFine + i * 64);
+        a.cos[tok][i] = cc * fc - cs * fs;
+        a.sin[tok][i] = cs * fc + cc * fs;
     }
+}
+
+// The linear map of a lane's four pairs: z_lo = lo * lc - hi * hs, z_hi = hi * hc + lo * ls.
+struct Map { float2 lc[2], hs[2], hc[2], ls[2]; };
+template <class E>
+__device__ __forceinline__ void make_map(Map &m, const void *w, const float *cos, const float *sin, int l)
+{
+    float wl[4] = {1.f, 1.f, 1.f, 1.f}, wh[4] = {1.f, 1.f, 1.f, 1.f};
+    if (w) {
+        const Head<E> u = load_head(static_cast<const E *>(w), l);
+        Quad<E>::unpack(u.lo, wl);
+        Quad<E>::unpack(u.hi, wh);
+    }
+    float4 c = make_float4(1.f, 1.f, 1.f, 1.f), s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (cos) {
+        c = *reinterpret_cast<const float4 *>(cos + 4 * l);
+        s = *reinterpret_cast<const float4 *>(sin + 4 * l);
+    }
+    m.lc[0] = make_float2(wl[0] * c.x, wl[1] * c.y); m.lc[1] = make_float2(wl[2] * c.z, wl[3] * c.w);
+    m.ls[0] = make_float2(wl[0] * s.x, wl[1] * s.y); m.ls[1] = make_float2(wl[2] * s.z, wl[3] * s.w);
+    m.hc[0] = make_float2(wh[0] * c.x, wh[1] * c.y); m.hc[1] = make_float2(wh[2] * c.z, wh[3] * c.w);
+    m.hs[0] = make_float2(-wh[0] * s.x, -wh[1] * s.y); m.hs[1] = make_float2(-wh[2] * s.z, -wh[3] * s.w);
 }
 
 // Norm and rotation of one head held by a half warp.
 template <class E>
-__device__ __forceinline__ void head_math(Head<E> &u, bool norm, const float (&wl)[4], const float (&wh)[4], float eps,
-                                          bool turn, const float (&c)[4], const float (&s)[4])
+__device__ __forceinline__ void head_math(Head<E> &u, bool norm, float eps, const Map &m)
 {
-    float lo[4], hi[4];
-    Quad<E>::unpack(u.lo, lo);
-    Quad<E>::unpack(u.hi, hi);
+    float a[4], b[4];
+    Quad<E>::unpack(u.lo, a);
+    Quad<E>::unpack(u.hi, b);
+    float2 lo[2] = {make_float2(a[0], a[1]), make_float2(a[2], a[3])}, hi[2] = {make_float2(b[0], b[1]), make_float2(b[2], b[3])};
     if (norm) {
-        float ss = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { ss = fmaf(lo[i], lo[i], ss); ss = fmaf(hi[i], hi[i], ss); }
+        float2 sq = __fmul2_rn(lo[0], lo[0]);
+        sq = __ffma2_rn(lo[1], lo[1], sq);
+        sq = __ffma2_rn(hi[0], hi[0], sq);
+        sq = __ffma2_rn(hi[1], hi[1], sq);
+        float ss = sq.x + sq.y;
 #pragma unroll
         for (int d = 8; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-        const float r = rsqrtf(ss * (1.f / kHeadDim) + eps);
+        const float r = rsqrtf(fmaf(ss, 1.f / kHeadDim, eps));
+        const float2 r2 = make_float2(r, r);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { lo[i] = lo[i] * r * wl[i]; hi[i] = hi[i] * r * wh[i]; }
+        for (int i = 0; i < 2; ++i) { lo[i] = __fmul2_rn(lo[i], r2); hi[i] = __fmul2_rn(hi[i], r2); }
     }
-    if (turn) {
+    float zl[4], zh[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float a = lo[i], b = hi[i];
-            lo[i] = fmaf(a, c[i], -b * s[i]);
-            hi[i] = fmaf(b, c[i], a * s[i]);
-        }
+    for (int i = 0; i < 2; ++i) {
+        const float2 x = __ffma2_rn(lo[i], m.lc[i], __fmul2_rn(hi[i], m.hs[i])), y = __ffma2_rn(hi[i], m.hc[i], __fmul2_rn(lo[i], m.ls[i]));
+        zl[2 * i] = x.x; zl[2 * i + 1] = x.y; zh[2 * i] = y.x; zh[2 * i + 1] = y.y;
     }
-    u.lo = Quad<E>::pack(lo);
-    u.hi = Quad<E>::pack(hi);
-}
-
-template <class E>
-__device__ __forceinline__ void load_weight(const void *w, int l, float (&lo)[4], float (&hi)[4])
-{
-    if (w) {
-        const Head<E> u = load_head(static_cast<const E *>(w), l);
-        Quad<E>::unpack(u.lo, lo);
-        Quad<E>::unpack(u.hi, hi);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) lo[i] = hi[i] = 1.f;
-    }
+    u.lo = Quad<E>::pack(zl);
+    u.hi = Quad<E>::pack(zh);
 }
 
 struct NormRope {
     const void *q, *k;
     void *qo, *ko;
     int64_t q_st, q_sh, k_st, k_sh, qo_st, qo_sh, ko_st, ko_sh;     // elements
-    int32_t T, Hq, H;                                               // H = query and key heads
+    int32_t T, Hq, Hkv;
     const void *qw, *kw;
     int32_t norm;
     float eps;
@@ -140,53 +157,59 @@ struct NormRope {
     int32_t *status;
 };
 
-// Warp: heads [h0, h0 + per) of one token.
+// Block: eight tokens; blockIdx.y = a part of `per` query heads, or (from q_parts on) of key heads.
 template <class E>
 __global__ void __launch_bounds__(kThreads)
-norm_rope_kernel(const NormRope p, const int parts, const int per)
+norm_rope_kernel(const NormRope p, const int q_parts, const int per)
 {
-    const int lane = threadIdx.x & 31, l = lane & 15, half = lane >> 4;
-    const int64_t unit = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const int32_t t = (int32_t)(unit / parts);
-    if (t >= p.T) return;
-    const int h0 = (int)(unit - (int64_t)t * parts) * per, h1 = min(h0 + per, p.H);
+    __shared__ __align__(16) Angles sh;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane & 15, half = lane >> 4;
+    const int32_t t = blockIdx.x * kWarps + warp;
+    const bool is_q = (int)blockIdx.y < q_parts;
+    const int h0 = ((int)blockIdx.y - (is_q ? 0 : q_parts)) * per, h1 = min(h0 + per, is_q ? p.Hq : p.Hkv);
+    const int64_t sh_in = is_q ? p.q_sh : p.k_sh, sh_out = is_q ? p.qo_sh : p.ko_sh;
+    const E *src = static_cast<const E *>(is_q ? p.q : p.k) + t * (is_q ? p.q_st : p.k_st) + (h0 + half) * sh_in;
+    E *dst = static_cast<E *>(is_q ? p.qo : p.ko) + t * (is_q ? p.qo_st : p.ko_st) + (h0 + half) * sh_out;
 
-    auto fetch = [&](int base, Head<E> (&u)[kRows]) {
+    // Loads and stores run over the half warp's heads h0 + half, + 2, ...; `src` and `dst` are at the next one.
+    int left = t < p.T ? (h1 - h0 - half + 1) / 2 : 0;              // heads not yet loaded
+    auto fetch = [&](Head<E> (&u)[kRows]) {
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int h = base + half + 2 * i;
-            if (h < h1)
-                u[i] = load_head(h < p.Hq ? static_cast<const E *>(p.q) + t * p.q_st + h * p.q_sh
-                                          : static_cast<const E *>(p.k) + t * p.k_st + (h - p.Hq) * p.k_sh, l);
+            if (i < left) u[i] = load_head(src, l);
+            src += 2 * sh_in;
         }
+        left -= kRows;
     };
     Head<E> u[kRows] = {};
-    fetch(h0, u);
+    int todo = left;
+    fetch(u);
     // A negative position marks a padding row; one past the table is reported.
-    const int64_t pos = p.positions ? (int64_t)p.positions[t] : p.pos0 + t;
-    if (pos < 0) return;
+    int64_t pos = -1;
+    if (t < p.T) pos = p.positions ? (int64_t)p.positions[t] : p.pos0 + t;
     if (p.turn.table && pos >= p.turn.n_pos) {
         if (lane == 0) raise_status(p.status, PEC_ERR_BAD_INDEX);
-        return;
+        pos = -1;
     }
-    float c[4] = {}, s[4] = {}, ql[4], qh[4], kl[4], kh[4];
-    if (p.turn.table) angles(p.turn, (int32_t)pos, l, c, s);
-    load_weight<E>(p.norm && h0 < p.Hq ? p.qw : nullptr, l, ql, qh);
-    load_weight<E>(p.norm && h1 > p.Hq ? p.kw : nullptr, l, kl, kh);
-    for (int base = h0; base < h1; base += 2 * kRows) {
-        if (base != h0) fetch(base, u);
+    if (p.turn.table) {
+        if (lane == 0) sh.pos[warp] = (int32_t)pos;
+        __syncthreads();
+        angles(p.turn, sh);
+        __syncthreads();
+    }
+    if (pos < 0) return;
+    Map m;
+    make_map<E>(m, p.norm ? (is_q ? p.qw : p.kw) : nullptr, p.turn.table ? sh.cos[warp] : nullptr, sh.sin[warp], l);
+    const int rounds = ((h1 - h0 + 1) / 2 + kRows - 1) / kRows;     // the same for both halves: shuffles stay converged
+    for (int r = 0; r < rounds; ++r) {
+        if (r) fetch(u);
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int h = base + half + 2 * i;
-            const bool is_q = h < p.Hq;
-            float wl[4], wh[4];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) { wl[x] = is_q ? ql[x] : kl[x]; wh[x] = is_q ? qh[x] : kh[x]; }
-            head_math<E>(u[i], p.norm != 0, wl, wh, p.eps, p.turn.table != nullptr, c, s);
-            if (h < h1)
-                store_head(is_q ? static_cast<E *>(p.qo) + t * p.qo_st + h * p.qo_sh
-                                : static_cast<E *>(p.ko) + t * p.ko_st + (h - p.Hq) * p.ko_sh, l, u[i]);
+            head_math<E>(u[i], p.norm != 0, p.eps, m);
+            if (i < todo) store_head(dst, l, u[i]);
+            dst += 2 * sh_out;
         }
+        todo -= kRows;
     }
 }
 
@@ -203,73 +226,79 @@ struct Append {
     int32_t *status;
 };
 
-// As above over a token's key heads and then its value heads.
+// As above: a warp takes `per` key heads of its token and the value heads of the same numbers.
 template <class E>
 __global__ void __launch_bounds__(kThreads)
-kv_append_kernel(const Append p, const int parts, const int per)
+kv_append_kernel(const Append p, const int per)
 {
-    const int lane = threadIdx.x & 31, l = lane & 15, half = lane >> 4;
-    const int64_t unit = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const int32_t t = (int32_t)(unit / parts);
-    if (t >= p.c.T) return;
-    const int H = 2 * p.Hkv, h0 = (int)(unit - (int64_t)t * parts) * per, h1 = min(h0 + per, H);
+    __shared__ __align__(16) Angles sh;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane & 15, half = lane >> 4;
+    const int32_t t = blockIdx.x * kWarps + warp;
+    const int h0 = (int)blockIdx.y * per, h1 = min(h0 + per, p.Hkv);
+    const E *ks = static_cast<const E *>(p.k) + t * p.k_st + (h0 + half) * p.k_sh;
+    const E *vs = static_cast<const E *>(p.v) + t * p.v_st + (h0 + half) * p.v_sh;
 
-    auto fetch = [&](int base, Head<E> (&u)[kRows]) {
+    int left = t < p.c.T ? (h1 - h0 - half + 1) / 2 : 0;
+    auto fetch = [&](Head<E> (&ku)[kRows], Head<E> (&vu)[kRows]) {
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int h = base + half + 2 * i;
-            if (h < h1)
-                u[i] = load_head(h < p.Hkv ? static_cast<const E *>(p.k) + t * p.k_st + h * p.k_sh
-                                           : static_cast<const E *>(p.v) + t * p.v_st + (h - p.Hkv) * p.v_sh, l);
+            if (i < left) { ku[i] = load_head(ks, l); vu[i] = load_head(vs, l); }
+            ks += 2 * p.k_sh;
+            vs += 2 * p.v_sh;
         }
+        left -= kRows;
     };
-    Head<E> u[kRows] = {};
-    fetch(h0, u);
-    float wl[4], wh[4], c[4] = {}, s[4] = {};
-    const bool math = h0 < p.Hkv && (p.norm || p.turn.table);      // values alone, or keys as they are: a copy
-    load_weight<E>(math && p.norm ? p.kw : nullptr, l, wl, wh);
-    int32_t b, end;
-    if (!find_request(p.c, t, p.status, b, end)) return;
-    const int64_t pos = (int64_t)p.c.kv_lens[b] - end + t, nth = pos / p.c.page_size;
-    bool ok = pos >= 0 && nth < p.c.max_pages && (!p.turn.table || pos < p.turn.n_pos);
-    int64_t page = -1;
-    if (ok) {
-        page = p.c.table[b * p.c.table_stride + nth];
-        ok = page >= 0 && page < p.c.num_pages;
+    Head<E> ku[kRows] = {}, vu[kRows] = {};
+    int todo = left;
+    fetch(ku, vu);
+    int32_t b, start, end, kv;
+    int64_t pos = -1, page = 0, slot = 0;
+    if (t < p.c.T && find_request(p.c, t, p.status, b, start, end, kv)) {
+        pos = (int64_t)kv - end + t;
+        const int64_t nth = pos / p.c.page_size;
+        slot = pos - nth * p.c.page_size;
+        bool ok = pos >= 0 && nth < p.c.max_pages && (!p.turn.table || pos < p.turn.n_pos);
+        if (ok) {
+            page = p.c.table[b * p.c.table_stride + nth];
+            ok = page >= 0 && page < p.c.num_pages;
+        }
+        if (!ok) {
+            if (lane == 0) raise_status(p.status, PEC_ERR_BAD_INDEX);
+            pos = -1;
+        }
     }
-    if (!ok) {
-        if (lane == 0) raise_status(p.status, PEC_ERR_BAD_INDEX);
-        return;
+    if (p.turn.table) {
+        if (lane == 0) sh.pos[warp] = (int32_t)pos;
+        __syncthreads();
+        angles(p.turn, sh);
+        __syncthreads();
     }
-    if (math && p.turn.table) angles(p.turn, (int32_t)pos, l, c, s);
-    const int64_t slot = pos - nth * p.c.page_size;
-    E *k_slot = static_cast<E *>(p.k_pages) + page * p.c.k_sp + slot * p.c.k_st;
-    E *v_slot = static_cast<E *>(p.v_pages) + page * p.c.v_sp + slot * p.c.v_st;
-    for (int base = h0; base < h1; base += 2 * kRows) {
-        if (base != h0) fetch(base, u);
+    if (pos < 0) return;
+    const bool math = p.norm || p.turn.table;                       // else the keys are copied
+    Map m;
+    make_map<E>(m, p.norm ? p.kw : nullptr, p.turn.table ? sh.cos[warp] : nullptr, sh.sin[warp], l);
+    E *kd = static_cast<E *>(p.k_pages) + page * p.c.k_sp + slot * p.c.k_st + (h0 + half) * p.c.k_sh;
+    E *vd = static_cast<E *>(p.v_pages) + page * p.c.v_sp + slot * p.c.v_st + (h0 + half) * p.c.v_sh;
+    const int rounds = ((h1 - h0 + 1) / 2 + kRows - 1) / kRows;
+    for (int r = 0; r < rounds; ++r) {
+        if (r) fetch(ku, vu);
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int h = base + half + 2 * i;
-            const bool is_k = h < p.Hkv;
-            if (math) {                                             // uniform over the warp; a pair may be a key and a value
-                Head<E> z = u[i];
-                head_math<E>(z, p.norm != 0, wl, wh, p.eps, p.turn.table != nullptr, c, s);
-                if (is_k) u[i] = z;
+            if (math) head_math<E>(ku[i], p.norm != 0, p.eps, m);
+            if (i < todo) {
+                store_head(kd, l, ku[i]);
+                store_head(vd, l, vu[i]);
             }
-            if (h < h1) store_head(is_k ? k_slot + h * p.c.k_sh : v_slot + (h - p.Hkv) * p.c.v_sh, l, u[i]);
+            kd += 2 * p.c.k_sh;
+            vd += 2 * p.c.v_sh;
         }
+        todo -= kRows;
     }
 }
 
-// Parts that a token's H heads are dealt to, one warp each: 16 heads a warp where there are tokens enough to fill the GPU (the
-// angles are then worked out once for 16 heads), fewer where there are not, down to one pair.
-inline void deal(int64_t T, int64_t H, int &parts, int &per)
-{
-    int64_t n = T * H / (148 * 32);
-    n = n < 2 ? 2 : (n > 16 ? 16 : (n + 1) / 2 * 2);
-    per = (int)(n < H ? n : H);
-    parts = (int)((H + per - 1) / per);
-}
+// Heads of a part: as many as a warp loads at once (8) where the call is too small to fill the GPU otherwise, four times that
+// where it is not, so that the angles are worked out for more heads.
+inline int heads_per_part(int64_t T, int64_t H) { return T * H < (int64_t)148 * 32 * 32 ? 2 * kRows : 8 * kRows; }
 
 }  // namespace heads
 
@@ -369,17 +398,15 @@ extern "C" int pec_qk_norm_rope(const pec_norm_rope_args *a, void *cuda_stream)
     p.q = a->q; p.k = a->k; p.qo = a->q_out; p.ko = a->k_out;
     p.q_st = sq[0]; p.q_sh = sq[1]; p.qo_st = sq[2]; p.qo_sh = sq[3];
     p.k_st = sk[0]; p.k_sh = sk[1]; p.ko_st = sk[2]; p.ko_sh = sk[3];
-    p.T = (int32_t)a->T; p.Hq = a->Hq; p.H = a->Hq + a->Hkv;
+    p.T = (int32_t)a->T; p.Hq = a->Hq; p.Hkv = a->Hkv;
     p.qw = a->q_weight; p.kw = a->k_weight; p.norm = a->norm; p.eps = a->eps;
     p.turn = {a->rope_table, a->n_pos};
     p.positions = a->positions; p.pos0 = a->pos0; p.status = a->status;
-    int parts, per;
-    heads::deal(p.T, p.H, parts, per);
-    const int64_t blocks = ((int64_t)p.T * parts + heads::kWarps - 1) / heads::kWarps;
-    if (blocks > 0x7fffffff) { set_error("%s: grid too large", who); return PEC_ERR_UNSUPPORTED; }
+    const int per = heads::heads_per_part(p.T, p.Hq + p.Hkv), q_parts = (p.Hq + per - 1) / per;
+    const dim3 grid((unsigned)((p.T + heads::kWarps - 1) / heads::kWarps), (unsigned)(q_parts + (p.Hkv + per - 1) / per));
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (esz == 2) heads::norm_rope_kernel<__nv_bfloat16><<<(unsigned)blocks, heads::kThreads, 0, stream>>>(p, parts, per);
-    else          heads::norm_rope_kernel<float><<<(unsigned)blocks, heads::kThreads, 0, stream>>>(p, parts, per);
+    if (esz == 2) heads::norm_rope_kernel<__nv_bfloat16><<<grid, heads::kThreads, 0, stream>>>(p, q_parts, per);
+    else          heads::norm_rope_kernel<float><<<grid, heads::kThreads, 0, stream>>>(p, q_parts, per);
     const cudaError_t err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("%s: launch failed: %s", who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
@@ -406,13 +433,11 @@ extern "C" int pec_kv_append(const pec_kv_append_args *a, void *cuda_stream)
     p.k = a->k; p.v = a->v; p.k_st = s[0]; p.k_sh = s[1]; p.v_st = s[2]; p.v_sh = s[3];
     p.k_pages = a->k_pages; p.v_pages = a->v_pages; p.Hkv = a->Hkv;
     p.kw = a->k_weight; p.norm = a->norm; p.eps = a->eps; p.turn = {a->rope_table, a->n_pos}; p.status = a->status;
-    int parts, per;
-    heads::deal(a->T, 2 * (int64_t)a->Hkv, parts, per);
-    const int64_t blocks = (a->T * parts + heads::kWarps - 1) / heads::kWarps;
-    if (blocks > 0x7fffffff) { set_error("%s: grid too large", who); return PEC_ERR_UNSUPPORTED; }
+    const int per = heads::heads_per_part(a->T, 2 * (int64_t)a->Hkv);
+    const dim3 grid((unsigned)((a->T + heads::kWarps - 1) / heads::kWarps), (unsigned)((a->Hkv + per - 1) / per));
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (esz == 2) heads::kv_append_kernel<__nv_bfloat16><<<(unsigned)blocks, heads::kThreads, 0, stream>>>(p, parts, per);
-    else          heads::kv_append_kernel<float><<<(unsigned)blocks, heads::kThreads, 0, stream>>>(p, parts, per);
+    if (esz == 2) heads::kv_append_kernel<__nv_bfloat16><<<grid, heads::kThreads, 0, stream>>>(p, per);
+    else          heads::kv_append_kernel<float><<<grid, heads::kThreads, 0, stream>>>(p, per);
     const cudaError_t err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("%s: launch failed: %s", who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;

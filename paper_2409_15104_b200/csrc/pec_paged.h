@@ -26,26 +26,35 @@ __device__ __forceinline__ void raise_status(int32_t *status, int32_t code)
     if (status) atomicCAS(status, 0, code);
 }
 
-// The request that owns token row t, searched by one converged warp: lane l looks at cu_q[l + 1], cu_q[l + 33], ... (the
-// loads are independent of one another; a binary search would be a chain of log2(B) dependent ones) and b is the number of
-// requests that end at or before t.  Returns false for padding rows; a table that is not ascending around t raises the
-// status word and returns false.
-__device__ __forceinline__ bool find_request(const PagedCache &c, int32_t t, int32_t *status, int32_t &b, int32_t &end)
+// The request that owns token row t and that request's entry of kv_lens, searched by one converged warp, 32 requests at a
+// time: every lane's loads are independent of one another (a binary search would be a chain of log2(B) dependent ones) and the
+// owner's values come by shuffle.  Returns false for padding rows; offsets that are not ascending around t, or pass T, raise the
+// status word and give false as well.
+__device__ __forceinline__ bool find_request(const PagedCache &c, int32_t t, int32_t *status, int32_t &b, int32_t &start, int32_t &end, int32_t &kv)
 {
     const int lane = threadIdx.x & 31;
-    b = 0;
+    const int32_t first = c.cu_q[0];
+    int32_t prev = first;                                       // the end of the request before this group of 32
     for (int b0 = 0; b0 < c.B; b0 += 32) {
-        const bool past = (b0 + lane < c.B) && c.cu_q[b0 + lane + 1] <= t;
-        b += __popc(__ballot_sync(0xffffffffu, past));
+        int32_t e = INT32_MAX, k = 0;
+        if (b0 + lane < c.B) { e = c.cu_q[b0 + lane + 1]; k = c.kv_lens[b0 + lane]; }
+        const int src = __popc(__ballot_sync(0xffffffffu, e <= t));       // requests of the group that end at or before t
+        if (src < 32) {
+            b = b0 + src;
+            end = __shfl_sync(0xffffffffu, e, src);
+            kv = __shfl_sync(0xffffffffu, k, src);
+            const int32_t before = __shfl_sync(0xffffffffu, e, src > 0 ? src - 1 : 0);
+            start = src > 0 ? before : prev;
+            if (b >= c.B || t < first) return false;
+            if (start < 0 || t < start || t >= end || end > c.T) {
+                if (lane == 0) raise_status(status, PEC_ERR_BAD_INDEX);
+                return false;
+            }
+            return true;
+        }
+        prev = __shfl_sync(0xffffffffu, e, 31);
     }
-    if (b >= c.B) return false;
-    const int32_t start = c.cu_q[b];
-    end = c.cu_q[b + 1];
-    if (t < start || t >= end || end > c.T) {
-        if (lane == 0 && t >= c.cu_q[0]) raise_status(status, PEC_ERR_BAD_INDEX);
-        return false;
-    }
-    return true;
+    return false;
 }
 
 // Host checks common to the entry points; returns a pec_status.

@@ -196,8 +196,8 @@ paged_combine_kernel(const Params p)
     asm volatile("griddepcontrol.wait;" ::: "memory");             // launched ahead of the attention kernels' end
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, kvh = blockIdx.y;
     const int32_t t = blockIdx.x;
-    int32_t b, end;
-    if (!find_request(p.c, t, p.status, b, end)) return;
+    int32_t b, start, end, cached;
+    if (!find_request(p.c, t, p.status, b, start, end, cached)) return;
     const Request r = load_request(p, b);
     if (r.n == 0) return;
     const int32_t tok = t - r.start;
