@@ -226,31 +226,31 @@ struct Append {
     int32_t *status;
 };
 
-// As above: a warp takes `per` key heads of its token and the value heads of the same numbers.
+// As above; blockIdx.y = a part of the key heads, or (from `parts` on) of the value heads, which are copied.
 template <class E>
 __global__ void __launch_bounds__(kThreads)
-kv_append_kernel(const Append p, const int per)
+kv_append_kernel(const Append p, const int parts, const int per)
 {
     __shared__ __align__(16) Angles sh;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane & 15, half = lane >> 4;
     const int32_t t = blockIdx.x * kWarps + warp;
-    const int h0 = (int)blockIdx.y * per, h1 = min(h0 + per, p.Hkv);
-    const E *ks = static_cast<const E *>(p.k) + t * p.k_st + (h0 + half) * p.k_sh;
-    const E *vs = static_cast<const E *>(p.v) + t * p.v_st + (h0 + half) * p.v_sh;
+    const bool is_k = (int)blockIdx.y < parts;
+    const int h0 = ((int)blockIdx.y - (is_k ? 0 : parts)) * per, h1 = min(h0 + per, p.Hkv);
+    const int64_t s_in = is_k ? p.k_sh : p.v_sh, s_out = is_k ? p.c.k_sh : p.c.v_sh;
+    const E *src = static_cast<const E *>(is_k ? p.k : p.v) + t * (is_k ? p.k_st : p.v_st) + (h0 + half) * s_in;
 
     int left = t < p.c.T ? (h1 - h0 - half + 1) / 2 : 0;
-    auto fetch = [&](Head<E> (&ku)[kRows], Head<E> (&vu)[kRows]) {
+    auto fetch = [&](Head<E> (&u)[kRows]) {
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            if (i < left) { ku[i] = load_head(ks, l); vu[i] = load_head(vs, l); }
-            ks += 2 * p.k_sh;
-            vs += 2 * p.v_sh;
+            if (i < left) u[i] = load_head(src, l);
+            src += 2 * s_in;
         }
         left -= kRows;
     };
-    Head<E> ku[kRows] = {}, vu[kRows] = {};
+    Head<E> u[kRows] = {};
     int todo = left;
-    fetch(ku, vu);
+    fetch(u);
     int32_t b, start, end, kv;
     int64_t pos = -1, page = 0, slot = 0;
     if (t < p.c.T && find_request(p.c, t, p.status, b, start, end, kv)) {
@@ -267,30 +267,26 @@ kv_append_kernel(const Append p, const int per)
             pos = -1;
         }
     }
-    if (p.turn.table) {
+    const bool turn = is_k && p.turn.table, math = is_k && (p.norm || p.turn.table);   // uniform over the block
+    if (turn) {
         if (lane == 0) sh.pos[warp] = (int32_t)pos;
         __syncthreads();
         angles(p.turn, sh);
         __syncthreads();
     }
     if (pos < 0) return;
-    const bool math = p.norm || p.turn.table;                       // else the keys are copied
     Map m;
-    make_map<E>(m, p.norm ? p.kw : nullptr, p.turn.table ? sh.cos[warp] : nullptr, sh.sin[warp], l);
-    E *kd = static_cast<E *>(p.k_pages) + page * p.c.k_sp + slot * p.c.k_st + (h0 + half) * p.c.k_sh;
-    E *vd = static_cast<E *>(p.v_pages) + page * p.c.v_sp + slot * p.c.v_st + (h0 + half) * p.c.v_sh;
+    make_map<E>(m, math && p.norm ? p.kw : nullptr, turn ? sh.cos[warp] : nullptr, sh.sin[warp], l);
+    E *dst = static_cast<E *>(is_k ? p.k_pages : p.v_pages) + page * (is_k ? p.c.k_sp : p.c.v_sp) + slot * (is_k ? p.c.k_st : p.c.v_st) +
+             (h0 + half) * s_out;
     const int rounds = ((h1 - h0 + 1) / 2 + kRows - 1) / kRows;
     for (int r = 0; r < rounds; ++r) {
-        if (r) fetch(ku, vu);
+        if (r) fetch(u);
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            if (math) head_math<E>(ku[i], p.norm != 0, p.eps, m);
-            if (i < todo) {
-                store_head(kd, l, ku[i]);
-                store_head(vd, l, vu[i]);
-            }
-            kd += 2 * p.c.k_sh;
-            vd += 2 * p.c.v_sh;
+            if (math) head_math<E>(u[i], p.norm != 0, p.eps, m);
+            if (i < todo) store_head(dst, l, u[i]);
+            dst += 2 * s_out;
         }
         todo -= kRows;
     }
@@ -433,11 +429,11 @@ extern "C" int pec_kv_append(const pec_kv_append_args *a, void *cuda_stream)
     p.k = a->k; p.v = a->v; p.k_st = s[0]; p.k_sh = s[1]; p.v_st = s[2]; p.v_sh = s[3];
     p.k_pages = a->k_pages; p.v_pages = a->v_pages; p.Hkv = a->Hkv;
     p.kw = a->k_weight; p.norm = a->norm; p.eps = a->eps; p.turn = {a->rope_table, a->n_pos}; p.status = a->status;
-    const int per = heads::heads_per_part(a->T, 2 * (int64_t)a->Hkv);
-    const dim3 grid((unsigned)((a->T + heads::kWarps - 1) / heads::kWarps), (unsigned)((a->Hkv + per - 1) / per));
+    const int per = heads::heads_per_part(a->T, 2 * (int64_t)a->Hkv), parts = (a->Hkv + per - 1) / per;
+    const dim3 grid((unsigned)((a->T + heads::kWarps - 1) / heads::kWarps), (unsigned)(2 * parts));
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (esz == 2) heads::kv_append_kernel<__nv_bfloat16><<<grid, heads::kThreads, 0, stream>>>(p, per);
-    else          heads::kv_append_kernel<float><<<grid, heads::kThreads, 0, stream>>>(p, per);
+    if (esz == 2) heads::kv_append_kernel<__nv_bfloat16><<<grid, heads::kThreads, 0, stream>>>(p, parts, per);
+    else          heads::kv_append_kernel<float><<<grid, heads::kThreads, 0, stream>>>(p, parts, per);
     const cudaError_t err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("%s: launch failed: %s", who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
