@@ -185,79 +185,89 @@ paged_simple_kernel(const Params p)
 }
 
 // ------------------------------------------------------------------------------------------ combining partials
-// One CTA = one new token and one KV head; a warp merges the partials of one packed row at a time, a lane owning four
-// channels: the largest LSE first, then the weighted sum, four partials' loads in flight.  Rows whose result is in place
-// already (keys not cut) are left alone.
-constexpr int kCombineWarps = 4;
+// A CTA merges the partial results of eight packed rows (few class) or 64 (many class) of one unit: a (request, KV head) whose
+// tiles cross a cut of the line, or a block of rows whose keys are cut into slices.  Units are enumerated by what splits them -
+// CTA c of the few class looks at cut c and takes the unit around it if this is the unit's first cut - so that the grid has the
+// size of what can be split, not of the batch, and a CTA without a unit ends after one look at the tables.  (A CTA per token and
+// KV head took 66 us to find nothing to do for 2048 tokens.)  All of that runs before the attention kernels end (the tables were
+// complete before they began); the partials are read afterwards, and no CTA ends before that wait, so that whatever follows on
+// the stream follows the attention kernels too.
+// A warp merges one row at a time, a lane owning four channels: the largest LSE first, then the weighted sum.
+constexpr int kCombineWarps = 8, kFewGroup = 8, kManyGroup = 64;
 
-__global__ void __launch_bounds__(kCombineWarps * 32)
-paged_combine_kernel(const Params p)
+__device__ __forceinline__ void combine_row(const Params &p, const float *po, const float *pl, int64_t at0, int64_t shift, int64_t step,
+                                            int count, int64_t item, int lane)
 {
-    asm volatile("griddepcontrol.wait;" ::: "memory");             // launched ahead of the attention kernels' end
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, kvh = blockIdx.y;
-    const int32_t t = blockIdx.x;
-    int32_t b, start, end, cached;
-    if (!find_request(p.c, t, p.status, b, start, end, cached)) return;
-    const Request r = load_request(p, b);
-    if (r.n == 0) return;
-    const int32_t tok = t - r.start;
-    const bool few = is_few(p, r);
-    int64_t first = 0, shift = 0;
-    int32_t count;
-    if (few) {
+    auto place = [&](int s) { return at0 + s * step + (s == 0 ? shift : 0); };     // of partial s, in rows
+    float m = -INFINITY;
+    for (int s = lane; s < count; s += 32) m = fmaxf(m, pl[place(s)]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    float tot = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (m != -INFINITY) {
+#pragma unroll 4
+        for (int s = 0; s < count; ++s) {
+            const int64_t at = place(s);
+            const float l = pl[at], w = (l == -INFINITY) ? 0.f : expf(l - m);
+            const float4 v = *reinterpret_cast<const float4 *>(po + at * kHeadDim + 4 * lane);
+            acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y); acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
+            tot += w;
+        }
+    }
+    const float inv = tot > 0.f ? 1.f / tot : 0.f;
+    acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
+    if (p.o_is_bf16) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
+        *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.o) + item * kHeadDim + 4 * lane) =
+            make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+    } else {
+        *reinterpret_cast<float4 *>(static_cast<float *>(p.o) + item * kHeadDim + 4 * lane) = acc;
+    }
+    if (lane == 0) p.lse[item] = (m == -INFINITY) ? -INFINITY : m + logf(tot);
+}
+
+__global__ void __launch_bounds__(kCombineWarps * 32, 4)
+paged_combine_kernel(const Params p, const int few_groups, const int few_blocks, const int many_groups)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if ((int)blockIdx.x < few_blocks) {
+        const int64_t cut = blockIdx.x / few_groups + 1;
+        const int group = blockIdx.x % few_groups;
         int64_t all, rest;
         batch_tiles(p, all, rest);
-        const int64_t piece = few_piece(p, all), u0 = few_before(p, b) + (int64_t)kvh * r.tiles(), u1 = u0 + r.tiles();
-        first = u0 / piece;
-        count = (int32_t)((u1 - 1) / piece - first) + 1;
-        shift = u0 > first * piece ? 1 : 0;
-    }
-    for (int h = warp; h < p.g; h += kCombineWarps) {
-        int32_t row = tok * p.g + h;
-        const float *po, *pl;
-        int64_t s_row, s_step, s0;
-        if (few) {
-            s_row = p.few_rows; s_step = 2; s0 = 2 * first;
-            po = p.few_o; pl = p.few_lse;
-        } else {
-            const int32_t per = p.many_rows;
-            const Parts parts = parts_many(p, b, r, row / per);
-            count = parts.count;
-            row %= per;
-            s_row = p.many_rows; s_step = p.Hkv; s0 = parts.first * p.Hkv + kvh;
-            po = p.many_o; pl = p.many_lse;
+        const int64_t piece = few_piece(p, all), at = cut * piece;
+        Walk w;
+        w.u0 = at;
+        if (at < all * p.Hkv) walk_to(p, w, at, lane);
+        const bool mine = w.u0 < at && w.u0 >= at - piece;       // else the cut falls between units, or is not the unit's first
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (!mine) return;
+        const int64_t u1 = w.u0 + w.r.tiles();
+        const int64_t first = cut - 1;                           // piece with the unit's first tiles
+        const int count = (int)((u1 - 1) / piece - first) + 1;
+        const int row = group * kFewGroup + warp;
+        if (row >= w.r.n * p.g) return;
+        const int64_t item = (int64_t)(w.r.start + row / p.g) * p.Hq + w.kvh * p.g + row % p.g;
+        combine_row(p, p.few_o, p.few_lse, 2 * first * p.few_rows + row, w.u0 > first * piece ? p.few_rows : 0, 2 * (int64_t)p.few_rows, count,
+                    item, lane);
+    } else {
+        int64_t x = blockIdx.x - few_blocks;
+        const int group = (int)(x % many_groups);
+        x /= many_groups;
+        const int kvh = (int)(x % p.Hkv);
+        SplitBlock sb;
+        const bool mine = locate_split(p, x / p.Hkv, sb);
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (!mine) return;
+        for (int i = warp; i < kManyGroup; i += kCombineWarps) {
+            const int row = group * kManyGroup + i;              // of the block
+            const int64_t packed = (int64_t)sb.block * p.many_rows + row;
+            if (row >= p.many_rows || packed >= (int64_t)sb.r.n * p.g) return;
+            const int64_t item = (sb.r.start + packed / p.g) * p.Hq + kvh * p.g + packed % p.g;
+            combine_row(p, p.many_o, p.many_lse, (sb.first * p.Hkv + kvh) * p.many_rows + row, 0, (int64_t)p.Hkv * p.many_rows, sb.slices, item,
+                        lane);
         }
-        if (count <= 1) continue;
-        auto place = [&](int s) { return (s0 + s * s_step + (s == 0 ? shift : 0)) * s_row + row; };
-        float m = -INFINITY;
-        for (int s = lane; s < count; s += 32) m = fmaxf(m, pl[place(s)]);
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        float tot = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (m != -INFINITY) {
-#pragma unroll 4
-            for (int s = 0; s < count; ++s) {
-                const int64_t at = place(s);
-                const float l = pl[at], w = (l == -INFINITY) ? 0.f : expf(l - m);
-                const float4 v = *reinterpret_cast<const float4 *>(po + at * kHeadDim + 4 * lane);
-                if (w != 0.f) {
-                    acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y); acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
-                    tot += w;
-                }
-            }
-        }
-        const float inv = tot > 0.f ? 1.f / tot : 0.f;
-        acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
-        const int64_t item = (int64_t)t * p.Hq + kvh * p.g + h;
-        if (p.o_is_bf16) {
-            const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
-            *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.o) + item * kHeadDim + 4 * lane) =
-                make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
-        } else {
-            *reinterpret_cast<float4 *>(static_cast<float *>(p.o) + item * kHeadDim + 4 * lane) = acc;
-        }
-        if (lane == 0) p.lse[item] = (m == -INFINITY) ? -INFINITY : m + logf(tot);
     }
 }
 
@@ -284,8 +294,13 @@ int launch_paged_simple(const Params &p, int64_t items, cudaStream_t stream)
 
 int launch_paged_combine(const Params &p, cudaStream_t stream)
 {
+    // Every cut of the line; every block that can be cut: one has two slots or more.
+    const int few_groups = (p.few_rows + kFewGroup - 1) / kFewGroup, few_blocks = p.few ? (p.few_ctas - 1) * few_groups : 0;
+    const int many_groups = (p.many_rows + kManyGroup - 1) / kManyGroup;
+    const int64_t many_blocks = (int64_t)((p.many_cap / 2 + p.Hkv - 1) / p.Hkv) * p.Hkv * many_groups;
+    if (few_blocks + many_blocks == 0) return PEC_OK;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)p.c.T, (unsigned)p.Hkv);
+    cfg.gridDim = dim3((unsigned)(few_blocks + many_blocks));
     cfg.blockDim = dim3(kCombineWarps * 32);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -293,7 +308,7 @@ int launch_paged_combine(const Params &p, cudaStream_t stream)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    cudaError_t err = cudaLaunchKernelEx(&cfg, paged_combine_kernel, p);
+    cudaError_t err = cudaLaunchKernelEx(&cfg, paged_combine_kernel, p, few_groups, few_blocks, many_groups);
     if (err == cudaSuccess) err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;

@@ -66,61 +66,6 @@ __device__ __forceinline__ bool wait_all(uint64_t *bar, uint32_t parity, Shared 
     return __all_sync(0xffffffffu, wait_bar(bar, parity, sh, p));
 }
 
-// The loader's walk along the line.  The 32 requests around the current one sit in the lanes' registers.
-struct Walk {
-    int32_t b0, b;                                         // first request of the lanes' group; current request
-    Request mine, r;                                       // this lane's, the current one
-    int32_t kvh, tile;                                     // current KV head and tile of the request
-    int64_t u0;                                            // the unit's first tile on the line
-};
-__device__ __forceinline__ void walk_take(Walk &w, int src)
-{
-    w.b = w.b0 + src;
-    w.r.start = __shfl_sync(0xffffffffu, w.mine.start, src);
-    w.r.n = __shfl_sync(0xffffffffu, w.mine.n, src);
-    w.r.kv = __shfl_sync(0xffffffffu, w.mine.kv, src);
-}
-__device__ __forceinline__ void walk_group(const Params &p, Walk &w, int lane)
-{
-    w.mine.start = w.mine.n = w.mine.kv = 0;
-    if (w.b0 + lane < p.c.B) w.mine = load_request(p, w.b0 + lane);
-}
-// To place `at` on the line (below its end).
-__device__ __forceinline__ void walk_to(const Params &p, Walk &w, int64_t at, int lane)
-{
-    int64_t before = 0;
-    for (w.b0 = 0; w.b0 < p.c.B; w.b0 += 32) {
-        walk_group(p, w, lane);
-        const int64_t len = is_few(p, w.mine) ? (int64_t)w.mine.tiles() * p.Hkv : 0, incl = warp_prefix(len, lane);
-        const unsigned who = __ballot_sync(0xffffffffu, at >= before + incl - len && at < before + incl);
-        if (who) {
-            const int src = __ffs(who) - 1;
-            walk_take(w, src);
-            const int64_t off = at - __shfl_sync(0xffffffffu, before + incl - len, src);
-            w.kvh = (int32_t)(off / w.r.tiles());
-            w.tile = (int32_t)(off % w.r.tiles());
-            w.u0 = at - w.tile;
-            return;
-        }
-        before += __shfl_sync(0xffffffffu, incl, 31);
-    }
-}
-// To the next unit (there is one).
-__device__ __forceinline__ void walk_next(const Params &p, Walk &w, int lane)
-{
-    w.u0 += w.r.tiles();
-    w.tile = 0;
-    if (++w.kvh < p.Hkv) return;
-    w.kvh = 0;
-    unsigned left = __ballot_sync(0xffffffffu, is_few(p, w.mine) && w.b0 + lane > w.b);
-    while (!left && w.b0 + 32 < p.c.B) {
-        w.b0 += 32;
-        walk_group(p, w, lane);
-        left = __ballot_sync(0xffffffffu, is_few(p, w.mine));
-    }
-    walk_take(w, left ? __ffs(left) - 1 : 0);
-}
-
 __global__ void __launch_bounds__(kThreads, 1)
 paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                  const __grid_constant__ CUtensorMap tm_v, const Params p, const int box, const int q_tokens, const int skip_last)
@@ -134,6 +79,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     // The loader warp works out this CTA's piece of the line while others set up barriers and tensor memory.
     Walk walk;
     if (warp == kLoadWarp) {
+        if (lane == 0) griddep_launch_dependents();        // the combining kernel may be launched; it waits for this one's end
         int64_t all, rest;
         batch_tiles(p, all, rest);
         const int64_t piece = few_piece(p, all), first = blockIdx.x * piece;

@@ -169,43 +169,96 @@ __device__ __forceinline__ bool locate_many(const Params &p, int64_t idx, Item &
     return false;
 }
 
-// Where the partials of a token's request lie, for the combining kernel.  One converged warp.
-struct Parts {
-    int32_t count;                            // 1: the result is in place already
-    // few: slots of KV head kvh are 2 c (+ 1 in the first CTA if its piece began with another unit), c = c0 .. c0 + count - 1
-    // many: slots (first + s) * Hkv + kvh
-    int64_t first;
+// A warp's walk along the few class's line.  The 32 requests around the current one sit in the lanes' registers.
+struct Walk {
+    int32_t b0, b;                                         // first request of the lanes' group; current request
+    Request mine, r;                                       // this lane's, the current one
+    int32_t kvh, tile;                                     // current KV head and tile of the request
+    int64_t u0;                                            // the unit's first tile on the line
 };
-__device__ __forceinline__ Parts parts_many(const Params &p, int b, const Request &r, int32_t block)
+__device__ __forceinline__ void walk_take(Walk &w, int src)
+{
+    w.b = w.b0 + src;
+    w.r.start = __shfl_sync(0xffffffffu, w.mine.start, src);
+    w.r.n = __shfl_sync(0xffffffffu, w.mine.n, src);
+    w.r.kv = __shfl_sync(0xffffffffu, w.mine.kv, src);
+}
+__device__ __forceinline__ void walk_group(const Params &p, Walk &w, int lane)
+{
+    w.mine.start = w.mine.n = w.mine.kv = 0;
+    if (w.b0 + lane < p.c.B) w.mine = load_request(p, w.b0 + lane);
+}
+// To place `at` on the line (below its end).
+__device__ __forceinline__ void walk_to(const Params &p, Walk &w, int64_t at, int lane)
+{
+    int64_t before = 0;
+    for (w.b0 = 0; w.b0 < p.c.B; w.b0 += 32) {
+        walk_group(p, w, lane);
+        const int64_t len = is_few(p, w.mine) ? (int64_t)w.mine.tiles() * p.Hkv : 0, incl = warp_prefix(len, lane);
+        const unsigned who = __ballot_sync(0xffffffffu, at >= before + incl - len && at < before + incl);
+        if (who) {
+            const int src = __ffs(who) - 1;
+            walk_take(w, src);
+            const int64_t off = at - __shfl_sync(0xffffffffu, before + incl - len, src);
+            w.kvh = (int32_t)(off / w.r.tiles());
+            w.tile = (int32_t)(off % w.r.tiles());
+            w.u0 = at - w.tile;
+            return;
+        }
+        before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+}
+// To the next unit (there is one).
+__device__ __forceinline__ void walk_next(const Params &p, Walk &w, int lane)
+{
+    w.u0 += w.r.tiles();
+    w.tile = 0;
+    if (++w.kvh < p.Hkv) return;
+    w.kvh = 0;
+    unsigned left = __ballot_sync(0xffffffffu, is_few(p, w.mine) && w.b0 + lane > w.b);
+    while (!left && w.b0 + 32 < p.c.B) {
+        w.b0 += 32;
+        walk_group(p, w, lane);
+        left = __ballot_sync(0xffffffffu, is_few(p, w.mine));
+    }
+    walk_take(w, left ? __ffs(left) - 1 : 0);
+}
+
+// Block `idx` of the requests of the many class whose keys are cut (in the order of their slots); one converged warp.
+struct SplitBlock {
+    Request r;
+    int32_t block, slices;
+    int64_t first;                            // slots (first + s) * Hkv + kvh
+};
+__device__ __forceinline__ bool locate_split(const Params &p, int64_t idx, SplitBlock &out)
 {
     const int lane = threadIdx.x & 31;
     int64_t few, many;
     batch_tiles(p, few, many);
+    if (many == 0) return false;
     const int64_t slice = many_slice(p, many);
-    Parts out;
-    out.count = slices_of(r, slice);
-    out.first = 0;
-    if (out.count <= 1) return out;
-    int64_t slots = 0;
-    for (int i = lane; i < b; i += 32) {
-        const Request x = load_request(p, i);
-        if (is_many(p, x)) {
-            const int32_t ns = slices_of(x, slice);
-            if (ns > 1) slots += (int64_t)blocks_of(p, x) * ns;
+    int64_t before = 0, slots = 0;
+    for (int b0 = 0; b0 < p.c.B; b0 += 32) {
+        Request r;
+        r.start = r.n = r.kv = 0;
+        if (b0 + lane < p.c.B) r = load_request(p, b0 + lane);
+        const int32_t ns = is_many(p, r) ? slices_of(r, slice) : 0;
+        const int64_t blocks = ns > 1 ? blocks_of(p, r) : 0, incl = warp_prefix(blocks, lane), incl_s = warp_prefix(blocks * ns, lane);
+        const unsigned who = __ballot_sync(0xffffffffu, idx >= before + incl - blocks && idx < before + incl);
+        if (who) {
+            const int src = __ffs(who) - 1;
+            out.r.start = __shfl_sync(0xffffffffu, r.start, src);
+            out.r.n = __shfl_sync(0xffffffffu, r.n, src);
+            out.r.kv = __shfl_sync(0xffffffffu, r.kv, src);
+            out.slices = __shfl_sync(0xffffffffu, ns, src);
+            out.block = (int32_t)(idx - __shfl_sync(0xffffffffu, before + incl - blocks, src));
+            out.first = __shfl_sync(0xffffffffu, slots + incl_s - blocks * ns, src) + (int64_t)out.block * out.slices;
+            return true;
         }
+        before += __shfl_sync(0xffffffffu, incl, 31);
+        slots += __shfl_sync(0xffffffffu, incl_s, 31);
     }
-    out.first = warp_sum(slots) + (int64_t)block * out.count;
-    return out;
-}
-// Tiles on the few class's line before request b.
-__device__ __forceinline__ int64_t few_before(const Params &p, int b)
-{
-    int64_t t = 0;
-    for (int i = threadIdx.x & 31; i < b; i += 32) {
-        const Request x = load_request(p, i);
-        if (is_few(p, x)) t += x.tiles();
-    }
-    return warp_sum(t) * p.Hkv;
+    return false;
 }
 
 }  // namespace paged
