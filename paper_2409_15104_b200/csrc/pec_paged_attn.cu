@@ -11,6 +11,167 @@
 namespace pec {
 namespace paged {
 
+// ------------------------------------------------------------------------------------------ plan
+// Items of the many class (bf16: chunks; fp32: every request), one CTA.
+//
+// Blocks are counted request by request, a request's last block (the one that sees the most keys) first.  A unit of work is a
+// block for one KV head; its length is the number of its request's key tiles.  Units up to the last full wave of many_ctas CTAs stay
+// whole, unless one is longer than an SM's fair share of all tiles (slice0); of the rest, which would leave SMs idle for a whole
+// unit's time, the keys are cut into slices (slice1): as many as fill one, two or three waves, whichever has the shortest
+// estimated time, or none.  The estimate, in times of a tile (1.35 us): a wave of slices takes its tiles and kItemTiles for a CTA's
+// start and end; a slice's partial, written and read once, kMergeTiles / 32 (132 KB both ways).
+// Slots that cut units take: cutting units of length l into slices of S takes less than sum l / S + their number.  slice0 >= all
+// tiles / many_ctas, and units longer than that are fewer than many_ctas: 2 many_ctas.  The tail has less than many_ctas + Hkv
+// units of mean length m and slice1 >= m / cuts with cuts * units <= 3 many_ctas: 4 many_ctas + Hkv.
+// Items go into the list longest first (by 256 classes of visible tiles): an SM that falls free late finds short work.  The order
+// inside a class is whatever the atomics make it; it changes when an item runs, never what it computes.
+constexpr int kPlanThreads = 1024, kClasses = 256;
+constexpr int kItemTiles = 3, kMergeTiles = 1;
+
+__device__ __forceinline__ int64_t block_prefix(int64_t v, int64_t *s_warp, int64_t &total)    // inclusive; one value per thread
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int64_t x = warp_prefix(v, lane);
+    __syncthreads();
+    if (lane == 31) s_warp[warp] = x;
+    __syncthreads();
+    const int64_t w = s_warp[lane], incl = warp_prefix(w, lane);
+    total = __shfl_sync(0xffffffffu, incl, 31);
+    const int64_t before = __shfl_sync(0xffffffffu, incl - w, warp);
+    return x + before;
+}
+
+__global__ void __launch_bounds__(kPlanThreads)
+paged_plan_kernel(const Params p, const int items_cap, const int split_cap)
+{
+    __shared__ int64_t s_warp[32];
+    __shared__ int32_t s_item[kPlanThreads], s_split[kPlanThreads], s_slot[kPlanThreads];   // ends of the requests' ranges
+    __shared__ int32_t s_start[kPlanThreads], s_n[kPlanThreads], s_kv[kPlanThreads], s_n0[kPlanThreads];
+    __shared__ int32_t s_class[kClasses], s_most;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int tid = threadIdx.x;
+    if (tid < kClasses) s_class[tid] = 0;
+    if (tid == 0) s_most = 1;
+    __syncthreads();
+
+    int64_t blocks = 0, tiles = 0;
+    int32_t most = 1;
+    for (int b = tid; b < p.c.B; b += kPlanThreads) {
+        const Request r = load_request(p, b);
+        if (is_many(p, r)) { const int64_t nb = blocks_of(p, r); blocks += nb; tiles += nb * r.tiles(); most = max(most, r.tiles()); }
+    }
+    atomicMax(&s_most, most);
+    int64_t all_blocks, all_tiles;
+    block_prefix(blocks, s_warp, all_blocks);
+    block_prefix(tiles, s_warp, all_tiles);
+    most = s_most;
+    const int32_t tail_at = (int32_t)(all_blocks * p.Hkv / p.many_ctas * p.many_ctas / p.Hkv);
+    const int64_t tail_blocks = all_blocks - tail_at, units = tail_blocks * p.Hkv;
+    const int32_t slice0 = (int32_t)max((all_tiles * p.Hkv + p.many_ctas - 1) / p.many_ctas, (int64_t)kMinSliceTiles);
+    int32_t slice1 = slice0;
+    if (units > 0) {
+        int64_t tail = 0, before = 0, part;
+        for (int b0 = 0; b0 < p.c.B; b0 += kPlanThreads) {
+            Request r;
+            r.start = r.n = r.kv = 0;
+            if (b0 + tid < p.c.B) r = load_request(p, b0 + tid);
+            const int64_t nb = is_many(p, r) ? blocks_of(p, r) : 0, end = before + block_prefix(nb, s_warp, part);
+            tail += min(nb, max(end - tail_at, (int64_t)0)) * r.tiles();
+            before += part;
+        }
+        block_prefix(tail, s_warp, part);
+        tail = part;
+        const int64_t mean = (tail + tail_blocks - 1) / tail_blocks;
+        int64_t best = 32 * ((units + p.many_ctas - 1) / p.many_ctas) * (mean + kItemTiles), len = mean;
+        for (int w = 1; w <= 3; ++w) {
+            const int64_t cuts = (int64_t)w * p.many_ctas / units;   // slices of a unit of mean length that w waves have room for
+            if (cuts < 2) continue;
+            const int64_t l = max((mean + cuts - 1) / cuts, (int64_t)kMinSliceTiles);
+            const int64_t time = 32 * w * (l + kItemTiles) + kMergeTiles * cuts * units / 16 + 64;
+            if (time < best) { best = time; len = l; }
+        }
+        if (len < mean) slice1 = (int32_t)min(len, (int64_t)slice0);
+    }
+
+    int64_t n_items = 0, n_split = 0;
+    for (int pass = 0; pass < 2; ++pass) {                          // count the classes; write the items
+        int64_t places = 0, slots = 0;
+        n_items = n_split = 0;
+        for (int b0 = 0; b0 < p.c.B; b0 += kPlanThreads) {
+            Request r;
+            r.start = r.n = r.kv = 0;
+            if (b0 + tid < p.c.B) r = load_request(p, b0 + tid);
+            const int32_t nb = is_many(p, r) ? blocks_of(p, r) : 0;
+            int64_t part;
+            const int64_t place = places + block_prefix(nb, s_warp, part) - nb;
+            places += part;
+            const int32_t n0 = (int32_t)min(max(tail_at - place, (int64_t)0), (int64_t)nb), n1 = nb - n0;
+            const int32_t c0 = (r.tiles() + slice0 - 1) / slice0, c1 = (r.tiles() + slice1 - 1) / slice1;
+            const int64_t items = (int64_t)n0 * c0 + (int64_t)n1 * c1, split = (c0 > 1 ? n0 : 0) + (c1 > 1 ? n1 : 0);
+            const int64_t mine = (c0 > 1 ? (int64_t)n0 * c0 : 0) + (c1 > 1 ? (int64_t)n1 * c1 : 0);
+            int64_t chunk_items, chunk_split, chunk_slots;
+            s_item[tid] = (int32_t)block_prefix(items, s_warp, chunk_items);
+            s_split[tid] = (int32_t)block_prefix(split, s_warp, chunk_split);
+            s_slot[tid] = (int32_t)(slots + block_prefix(mine, s_warp, chunk_slots) - mine);
+            s_start[tid] = r.start; s_n[tid] = r.n; s_kv[tid] = r.kv; s_n0[tid] = n0;
+            __syncthreads();
+            for (int i = tid; i < (int)chunk_items; i += kPlanThreads) {
+                int lo = 0, hi = kPlanThreads - 1;                  // the first request whose range ends past i
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (s_item[mid] > i) hi = mid; else lo = mid + 1;
+                }
+                Item it;
+                it.r.start = s_start[lo]; it.r.n = s_n[lo]; it.r.kv = s_kv[lo];
+                it.b = b0 + lo;
+                const int32_t t = it.r.tiles(), d0 = (t + slice0 - 1) / slice0, d1 = (t + slice1 - 1) / slice1, m0 = s_n0[lo];
+                const int32_t nbl = blocks_of(p, it.r);
+                int32_t at = i - (lo > 0 ? s_item[lo - 1] : 0), split_at = lo > 0 ? s_split[lo - 1] : 0, blk, sl;
+                it.slot = s_slot[lo];
+                if (at < m0 * d0) {
+                    blk = at / d0; sl = at - blk * d0;
+                    it.slices = d0; it.slot += at; split_at += blk;
+                } else {
+                    at -= m0 * d0;
+                    blk = at / d1; sl = at - blk * d1;
+                    it.slices = d1; it.slot += (d0 > 1 ? m0 * d0 : 0) + at; split_at += (d0 > 1 ? m0 : 0) + blk;
+                    blk += m0;
+                }
+                it.block = nbl - 1 - blk;
+                const int32_t per = (t + it.slices - 1) / it.slices;
+                it.key_lo = (int32_t)min((int64_t)sl * per * kKeyTile, (int64_t)it.r.kv);
+                it.key_hi = (int32_t)min((int64_t)(sl + 1) * per * kKeyTile, (int64_t)it.r.kv);
+                // Visible tiles: the block's last token sees up to its own position.
+                const int64_t last = min((int64_t)it.r.n, (int64_t)(it.block + 1) * p.blk_div / p.blk_mul + 1);
+                const int64_t see = p.causal ? min((int64_t)it.key_hi, it.r.pos0() + last) : it.key_hi;
+                const int32_t w = see > it.key_lo ? (int32_t)((see - it.key_lo + kKeyTile - 1) / kKeyTile) : 0;
+                const int32_t cls = kClasses - 1 - (int32_t)((int64_t)w * (kClasses - 1) / most);
+                if (pass == 0) {
+                    atomicAdd(&s_class[cls], 1);
+                } else {
+                    const int to = atomicAdd(&s_class[cls], 1);
+                    it.pad[0] = it.pad[1] = it.pad[2] = 0;
+                    if (to < items_cap) p.many_items[to] = it;
+                    if (it.slices > 1 && sl == 0 && n_split + split_at < split_cap) p.many_split[n_split + split_at] = it;
+                }
+            }
+            n_items += chunk_items; n_split += chunk_split; slots += chunk_slots;
+            __syncthreads();
+        }
+        if (pass == 0) {                                            // ends of the classes -> their starts
+            const int32_t mine = tid < kClasses ? s_class[tid] : 0;
+            int64_t sum;
+            const int64_t end = block_prefix(mine, s_warp, sum);
+            if (tid < kClasses) s_class[tid] = (int32_t)(end - mine);
+            __syncthreads();
+        }
+    }
+    if (tid == 0) {
+        p.many_count[0] = (int32_t)min(n_items, (int64_t)items_cap);   // (the caps are never reached, see above)
+        p.many_count[1] = (int32_t)min(n_split, (int64_t)split_cap);
+    }
+}
+
 // ------------------------------------------------------------------------------------------ FMA kernel
 // One CTA = 64 packed rows of one KV head against one slice of the request's keys, 64 keys at a time.  256 threads as 16 x 16:
 // thread (ty, tx) owns score rows 4 ty .. + 3 and keys tx + 16 j, and output rows 4 ty .. + 3 with channels 4 tx .. + 3 and
@@ -30,18 +191,11 @@ paged_simple_kernel(const Params p)
     float *sK = sQ + kBM * kLd;             // [kBN][kLd]
     float *sV = sK + kBN * kLd;             // [kBN][kHeadDim]
     float *sP = sV + kBN * kHeadDim;        // [kBM][kLdP]
-    __shared__ Item s_item;
-    __shared__ int s_found;
     __shared__ int32_t s_page[kBN];
-    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, kvh = blockIdx.y;
-    if (tid < 32) {
-        Item it;
-        const bool found = locate_many(p, blockIdx.x, it);
-        if (tid == 0) { s_found = found; if (found) s_item = it; }
-    }
-    __syncthreads();
-    if (!s_found) return;
-    const Item it = s_item;
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, kvh = blockIdx.x % p.Hkv;
+    asm volatile("griddepcontrol.wait;" ::: "memory");              // launched ahead of the plan's end
+    if ((int)(blockIdx.x / p.Hkv) >= p.many_count[0]) return;
+    const Item it = p.many_items[blockIdx.x / p.Hkv];
     const int32_t row0 = it.block * kBM, rows = min(kBM, it.r.n * p.g - row0);
 
     for (int i = tid; i < kBM * (kHeadDim / 4); i += kThreads) {
@@ -158,8 +312,8 @@ paged_simple_kernel(const Params p)
         }
     }
 
-    const int64_t slot = it.slot * p.Hkv + kvh;
-    if (it.slices > 1 && slot >= p.many_cap) return;               // cannot happen (see many_slice); never write past the scratch
+    const int64_t slot = (int64_t)it.slot * p.Hkv + kvh;
+    if (it.slices > 1 && slot >= p.many_cap) return;               // cannot happen (see many_plan); never write past the scratch
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int32_t r = ty * 4 + i;
@@ -185,15 +339,14 @@ paged_simple_kernel(const Params p)
 }
 
 // ------------------------------------------------------------------------------------------ combining partials
-// A CTA merges the partial results of eight packed rows (few class) or 64 (many class) of one unit: a (request, KV head) whose
-// tiles cross a cut of the line, or a block of rows whose keys are cut into slices.  Units are enumerated by what splits them -
-// CTA c of the few class looks at cut c and takes the unit around it if this is the unit's first cut - so that the grid has the
-// size of what can be split, not of the batch, and a CTA without a unit ends after one look at the tables.  (A CTA per token and
-// KV head took 66 us to find nothing to do for 2048 tokens.)  All of that runs before the attention kernels end (the tables were
-// complete before they began); the partials are read afterwards, and no CTA ends before that wait, so that whatever follows on
-// the stream follows the attention kernels too.
+// A CTA merges the partial results of eight packed rows (few class) or 32 (many class) of one unit: a (request, KV head) whose
+// tiles cross a cut of the line, or a block of rows whose keys are cut into slices (listed by the plan).  Units are enumerated by
+// what splits them - CTA c of the few class looks at cut c and takes the unit around it if this is the unit's first cut - so that
+// the grid has the size of what can be split, not of the batch.  (A CTA per token and KV head took 66 us to find nothing to do for
+// 2048 tokens.)  The few class looks its unit up before the attention kernels end (the tables were complete before they began);
+// partials are read afterwards, and no CTA ends before that wait, so that whatever follows on the stream follows those kernels too.
 // A warp merges one row at a time, a lane owning four channels: the largest LSE first, then the weighted sum.
-constexpr int kCombineWarps = 8, kFewGroup = 8, kManyGroup = 64;
+constexpr int kCombineWarps = 8, kFewGroup = 8, kManyGroup = 32;
 
 __device__ __forceinline__ void combine_row(const Params &p, const float *po, const float *pl, int64_t at0, int64_t shift, int64_t step,
                                             int count, int64_t item, int lane)
@@ -227,15 +380,14 @@ __device__ __forceinline__ void combine_row(const Params &p, const float *po, co
     if (lane == 0) p.lse[item] = (m == -INFINITY) ? -INFINITY : m + logf(tot);
 }
 
-__global__ void __launch_bounds__(kCombineWarps * 32, 4)
+__global__ void __launch_bounds__(kCombineWarps * 32, 3)
 paged_combine_kernel(const Params p, const int few_groups, const int few_blocks, const int many_groups)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((int)blockIdx.x < few_blocks) {
         const int64_t cut = blockIdx.x / few_groups + 1;
         const int group = blockIdx.x % few_groups;
-        int64_t all, rest;
-        batch_tiles(p, all, rest);
+        const int64_t all = few_tiles(p);
         const int64_t piece = few_piece(p, all), at = cut * piece;
         Walk w;
         w.u0 = at;
@@ -252,21 +404,20 @@ paged_combine_kernel(const Params p, const int few_groups, const int few_blocks,
         combine_row(p, p.few_o, p.few_lse, 2 * first * p.few_rows + row, w.u0 > first * piece ? p.few_rows : 0, 2 * (int64_t)p.few_rows, count,
                     item, lane);
     } else {
-        int64_t x = blockIdx.x - few_blocks;
-        const int group = (int)(x % many_groups);
-        x /= many_groups;
-        const int kvh = (int)(x % p.Hkv);
-        SplitBlock sb;
-        const bool mine = locate_split(p, x / p.Hkv, sb);
+        // The blocks that are cut, from the plan's list.
         asm volatile("griddepcontrol.wait;" ::: "memory");
-        if (!mine) return;
-        for (int i = warp; i < kManyGroup; i += kCombineWarps) {
-            const int row = group * kManyGroup + i;              // of the block
-            const int64_t packed = (int64_t)sb.block * p.many_rows + row;
-            if (row >= p.many_rows || packed >= (int64_t)sb.r.n * p.g) return;
-            const int64_t item = (sb.r.start + packed / p.g) * p.Hq + kvh * p.g + packed % p.g;
-            combine_row(p, p.many_o, p.many_lse, (sb.first * p.Hkv + kvh) * p.many_rows + row, 0, (int64_t)p.Hkv * p.many_rows, sb.slices, item,
-                        lane);
+        const int64_t n = (int64_t)p.many_count[1] * p.Hkv * many_groups;
+        for (int64_t x = blockIdx.x - few_blocks; x < n; x += gridDim.x - few_blocks) {
+            const int group = (int)(x % many_groups), kvh = (int)(x / many_groups % p.Hkv);
+            const Item it = p.many_split[x / many_groups / p.Hkv];
+            for (int i = warp; i < kManyGroup; i += kCombineWarps) {
+                const int row = group * kManyGroup + i;          // of the block
+                const int32_t packed = it.block * p.many_rows + row;
+                if (row >= p.many_rows || packed >= it.r.n * p.g) break;
+                const int64_t item = (int64_t)(it.r.start + packed / p.g) * p.Hq + kvh * p.g + packed % p.g;
+                combine_row(p, p.many_o, p.many_lse, ((int64_t)it.slot * p.Hkv + kvh) * p.many_rows + row, 0, (int64_t)p.Hkv * p.many_rows,
+                            it.slices, item, lane);
+            }
         }
     }
 }
@@ -274,6 +425,15 @@ paged_combine_kernel(const Params p, const int few_groups, const int few_blocks,
 }  // namespace paged
 
 using namespace paged;
+
+// The kernel that follows starts as this one does and waits for its end before it reads the list.
+int launch_paged_plan(const Params &p, cudaStream_t stream)
+{
+    paged_plan_kernel<<<1, kPlanThreads, 0, stream>>>(p, p.items_cap, p.many_cap / 2);
+    const cudaError_t err = cudaGetLastError();
+    if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
+    return PEC_OK;
+}
 
 int launch_paged_simple(const Params &p, int64_t items, cudaStream_t stream)
 {
@@ -285,9 +445,9 @@ int launch_paged_simple(const Params &p, int64_t items, cudaStream_t stream)
         set_error("pec_paged_attn: cannot raise the shared-memory limit");
         return PEC_ERR_CUDA;
     }
-    if (items > 0x7fffffff) { set_error("pec_paged_attn: grid too large"); return PEC_ERR_UNSUPPORTED; }
-    paged_simple_kernel<<<dim3((unsigned)items, (unsigned)p.Hkv), kThreads, kSimpleSmem, stream>>>(p);
-    const cudaError_t err = cudaGetLastError();
+    if (items * p.Hkv > 0x7fffffff) { set_error("pec_paged_attn: grid too large"); return PEC_ERR_UNSUPPORTED; }
+    cudaError_t err = launch_dependent(paged_simple_kernel, dim3((unsigned)(items * p.Hkv)), kThreads, kSimpleSmem, stream, true, p);
+    if (err == cudaSuccess) err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
 }
@@ -297,18 +457,11 @@ int launch_paged_combine(const Params &p, cudaStream_t stream)
     // Every cut of the line; every block that can be cut: one has two slots or more.
     const int few_groups = (p.few_rows + kFewGroup - 1) / kFewGroup, few_blocks = p.few ? (p.few_ctas - 1) * few_groups : 0;
     const int many_groups = (p.many_rows + kManyGroup - 1) / kManyGroup;
-    const int64_t many_blocks = (int64_t)((p.many_cap / 2 + p.Hkv - 1) / p.Hkv) * p.Hkv * many_groups;
+    const int64_t most = (int64_t)p.many_cap / 2 * many_groups;      // a block that is cut has two slots or more
+    const int many_blocks = (int)(most < 4 * p.many_ctas ? most : 4 * p.many_ctas);
     if (few_blocks + many_blocks == 0) return PEC_OK;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(few_blocks + many_blocks));
-    cfg.blockDim = dim3(kCombineWarps * 32);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaError_t err = cudaLaunchKernelEx(&cfg, paged_combine_kernel, p, few_groups, few_blocks, many_groups);
+    cudaError_t err = launch_dependent(paged_combine_kernel, dim3((unsigned)(few_blocks + many_blocks)), kCombineWarps * 32, 0, stream, true,
+                                       p, few_groups, few_blocks, many_groups);
     if (err == cudaSuccess) err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
@@ -355,6 +508,7 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
         set_error("%s: q and o must be 16-byte aligned (lse 4-byte)", who);
         return PEC_ERR_ALIGNMENT;
     }
+    if (a->T * (a->Hq / a->Hkv) >= ((int64_t)1 << 31)) { set_error("%s: T * Hq / Hkv of 2^31 or more unsupported", who); return PEC_ERR_UNSUPPORTED; }
     p.q = a->q; p.k_pages = a->k_pages; p.v_pages = a->v_pages;
     p.q_st = a->q_stride_t; p.q_sh = a->q_stride_h;
     p.o = a->o; p.lse = a->lse; p.o_is_bf16 = a->o_dtype == PEC_BF16;
@@ -380,29 +534,36 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
         floats = 2 * (size_t)p.few_ctas * p.few_rows * (kHeadDim + 1);
         floats = (floats + 3) & ~(size_t)3;
     }
-    // Blocks of the many class, the grid bound and the partial slots it may take (see many_slice).
+    // Blocks of the many class, the grid bound and the partial slots it may take (see many_plan).
     const int tps = kFewRows / p.g;           // tensor cores: two stages of whole tokens; FMA: 64 packed rows
     p.blk_mul = tensor ? 1 : p.g; p.blk_div = tensor ? 2 * tps : kBM;
     p.many_rows = tensor ? 2 * tps * p.g : kBM;
-    p.many_slots = 2 * sms;
+    p.many_ctas = sms;
     c.many_items = 0;
     if (!p.few || (int64_t)p.max_q * p.g > kFewRows) {
         const int64_t shortest = p.few ? kFewRows / p.g + 1 : 1, most = a->T / shortest;       // new tokens of such a request; how many there can be
         const int64_t blocks = a->T * p.blk_mul / p.blk_div + (a->B < most ? a->B : most);
-        c.many_items = blocks + ceil_div(p.many_slots, p.Hkv);
+        c.many_items = blocks + ceil_div(6 * (int64_t)p.many_ctas, p.Hkv) + 2;                 // whole blocks and slots
         const int64_t most_slices = ceil_div(ceil_div((int64_t)a->max_pages * a->page_size, kKeyTile), kMinSliceTiles);
-        int64_t cap = 2 * (int64_t)p.many_slots;
+        int64_t cap = 6 * (int64_t)p.many_ctas + p.Hkv;
         if (most_slices <= 1) cap = 0;
         else if (blocks * most_slices * p.Hkv < cap) cap = blocks * most_slices * p.Hkv;
         p.many_cap = (int32_t)cap;
     }
-    c.bytes = (floats + (size_t)p.many_cap * p.many_rows * (kHeadDim + 1)) * sizeof(float);
+    if (c.many_items > ((int64_t)1 << 26)) { set_error("%s: more than 2^26 blocks of rows unsupported", who); return PEC_ERR_UNSUPPORTED; }
+    p.items_cap = (int32_t)c.many_items;
+    const size_t slots = (((size_t)p.many_cap * p.many_rows * (kHeadDim + 1)) + 3) & ~(size_t)3;
+    const size_t list = c.many_items > 0 ? 4 + (c.many_items + p.many_cap / 2) * sizeof(Item) / sizeof(float) : 0;
+    c.bytes = (floats + slots + list) * sizeof(float);
     if (a->workspace) {
         float *ws = static_cast<float *>(a->workspace);
         p.few_o = ws;
         p.few_lse = ws + 2 * (size_t)p.few_ctas * p.few_rows * kHeadDim;
         p.many_o = ws + floats;
         p.many_lse = p.many_o + (size_t)p.many_cap * p.many_rows * kHeadDim;
+        p.many_count = reinterpret_cast<int32_t *>(ws + floats + slots);
+        p.many_items = reinterpret_cast<Item *>(p.many_count + 4);
+        p.many_split = p.many_items + p.items_cap;
     }
     return PEC_OK;
 }
@@ -431,8 +592,9 @@ extern "C" int pec_paged_attn(const pec_paged_args *args, void *cuda_stream)
     }
     if (args->T == 0) return PEC_OK;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (c.many_items > 0) rc = args->dtype == PEC_BF16 ? launch_paged_many(c.p, c.many_items, stream) : launch_paged_simple(c.p, c.many_items, stream);
-    if (rc == PEC_OK && c.p.few) rc = launch_paged_few(c.p, stream);
+    if (c.many_items > 0) rc = launch_paged_plan(c.p, stream);
+    if (rc == PEC_OK && c.many_items > 0) rc = args->dtype == PEC_BF16 ? launch_paged_many(c.p, c.many_items, stream) : launch_paged_simple(c.p, c.many_items, stream);
+    if (rc == PEC_OK && c.p.few) rc = launch_paged_few(c.p, c.many_items > 0, stream);
     if (rc != PEC_OK || c.bytes == 0) return rc;
     return launch_paged_combine(c.p, stream);
 }

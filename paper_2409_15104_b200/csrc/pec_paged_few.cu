@@ -80,8 +80,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     Walk walk;
     if (warp == kLoadWarp) {
         if (lane == 0) griddep_launch_dependents();        // the combining kernel may be launched; it waits for this one's end
-        int64_t all, rest;
-        batch_tiles(p, all, rest);
+        const int64_t all = few_tiles(p);
         const int64_t piece = few_piece(p, all), first = blockIdx.x * piece;
         const int64_t count = all * p.Hkv - first;
         const int32_t n = (int32_t)(count < 0 ? 0 : (count < piece ? count : piece));
@@ -105,7 +104,10 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     }
     __syncthreads();
     const int32_t count = sh->count;
-    if (count == 0) return;
+    if (count == 0) {
+        griddep_wait();
+        return;
+    }
     if (warp == 4) {
         tmem_alloc(smem_u32(&sh->tmem_base), kTmemCols);
         tmem_relinquish();
@@ -404,12 +406,14 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     tc_fence_before();
     __syncthreads();
     if (warp == 4) tmem_dealloc(tmem, kTmemCols);
+    // Beside the last CTAs of the kernel for many rows, which write other rows; but whoever waits for this kernel waits for that one.
+    griddep_wait();
 }
 
 }  // namespace few
 }  // namespace paged
 
-int launch_paged_few(const paged::Params &p, cudaStream_t stream)
+int launch_paged_few(const paged::Params &p, bool after_many, cudaStream_t stream)
 {
     using namespace paged;
     const int box = host_map::box_rows(p.c.page_size);
@@ -431,8 +435,9 @@ int launch_paged_few(const paged::Params &p, cudaStream_t stream)
         set_error("pec_paged_attn: kernel set-up failed (shared-memory limit, or the register allocation does not cover the warp-role split)");
         return PEC_ERR_CUDA;
     }
-    few::paged_few_kernel<<<p.few_ctas, few::kThreads, few::kSmemBytes, stream>>>(tm_q, tm_k, tm_v, p, box, q_tokens, test_skip_last_load());
-    const cudaError_t err = cudaGetLastError();
+    cudaError_t err = launch_dependent(few::paged_few_kernel, dim3((unsigned)p.few_ctas), few::kThreads, few::kSmemBytes, stream, after_many,
+                                       tm_q, tm_k, tm_v, p, box, q_tokens, (int)test_skip_last_load());
+    if (err == cudaSuccess) err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
 }

@@ -60,13 +60,17 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t sQ = (raw + 1023u) & ~1023u, sRing = sQ + 2 * kTileBytes;
     Shared *sh = reinterpret_cast<Shared *>(smem_raw + (sQ - raw) + (2 + kSlots) * kTileBytes);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, kvh = blockIdx.y;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, kvh = blockIdx.x % p.Hkv;
     const int tps = kTile / p.g, srows = tps * p.g;        // tokens and packed rows of a stage
 
     if (warp == kLoadWarp) {
-        Item it;
-        const bool found = locate_many(p, blockIdx.x, it);
+        // The kernel for few rows may start on SMs that this grid leaves.  The plan has to be complete before its list is read.
+        if (lane == 0) griddep_launch_dependents();
+        griddep_wait();
         if (lane == 0) {
+            const bool found = (int)(blockIdx.x / p.Hkv) < p.many_count[0];
+            Item it;
+            if (found) it = p.many_items[blockIdx.x / p.Hkv];
             Geom g = {};
             g.found = found;
             if (found) {
@@ -74,7 +78,7 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 g.b = it.b; g.kv = it.r.kv; g.key_lo = it.key_lo; g.key_hi = it.key_hi;
                 g.tok_row = it.r.start + tok0;
                 g.slices = it.slices;
-                g.slot = it.slot * p.Hkv + kvh;
+                g.slot = (int64_t)it.slot * p.Hkv + kvh;
 #pragma unroll
                 for (int st = 0; st < 2; ++st) {
                     int32_t nt = it.r.n - tok0 - st * tps;
@@ -86,7 +90,7 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     g.n[st] = (nt > 0 && end > it.key_lo) ? (end - it.key_lo + kTile - 1) / kTile : 0;
                 }
                 g.n_max = g.n[0] > g.n[1] ? g.n[0] : g.n[1];
-                if (g.slices > 1 && g.slot >= p.many_cap) g.found = 0;     // cannot happen (see many_slice); never write past the scratch
+                if (g.slices > 1 && g.slot >= p.many_cap) g.found = 0;     // cannot happen (see many_plan); never write past the scratch
             }
             sh->g = g;
             // P is handed over by the warps that have rows only.  (Those without would run ahead: S(j + 1) may be complete before
@@ -444,9 +448,10 @@ int launch_paged_many(const paged::Params &p, int64_t items, cudaStream_t stream
         set_error("pec_paged_attn: kernel set-up failed (shared-memory limit, or the register allocation does not cover the warp-role split)");
         return PEC_ERR_CUDA;
     }
-    if (items > 0x7fffffff) { set_error("pec_paged_attn: grid too large"); return PEC_ERR_UNSUPPORTED; }
-    many::paged_many_kernel<<<dim3((unsigned)items, (unsigned)p.Hkv), many::kThreads, many::kSmemBytes, stream>>>(tm_q, tm_k, tm_v, p, box, test_skip_last_load());
-    const cudaError_t err = cudaGetLastError();
+    if (items * p.Hkv > 0x7fffffff) { set_error("pec_paged_attn: grid too large"); return PEC_ERR_UNSUPPORTED; }
+    cudaError_t err = launch_dependent(many::paged_many_kernel, dim3((unsigned)(items * p.Hkv)), many::kThreads, many::kSmemBytes, stream, true,
+                                       tm_q, tm_k, tm_v, p, box, (int)test_skip_last_load());
+    if (err == cudaSuccess) err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
 }

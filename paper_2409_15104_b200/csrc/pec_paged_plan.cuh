@@ -1,5 +1,5 @@
-// How a batch's work is cut for the kernels behind pec_paged_attn, worked out on the device by every CTA from the tables
-// themselves (no host plan: a captured graph replays with whatever lengths the tables then hold).
+// How a batch's work is cut for the kernels behind pec_paged_attn, worked out on the device from the tables themselves (no host
+// plan: a captured graph replays with whatever lengths the tables then hold).
 //
 // Query rows are packed: the g = Hq / Hkv heads of a KV head and the new tokens of a request are the rows of one matrix,
 // row = token * g + head of the group, so that a key tile read once serves all of them.
@@ -7,8 +7,9 @@
 // Two classes of requests, by their packed rows n * g:
 //   few  (at most 128: decode steps)  worked on by a persistent grid.  The key tiles of all (request, KV head) pairs lie on
 //        one line that is cut into equal pieces, one per CTA; a pair that crosses a cut leaves one partial result per piece.
-//   many (chunks)                     blocks of rows, each block's keys cut into slices where a unit of work would be longer
-//        than an SM's fair share of the whole.
+//   many (chunks)                     items of one block of rows against all or a slice of its keys, listed longest first by a
+//        kernel of one CTA ahead of the attention kernel, which has one CTA per (item, KV head).  (With every CTA working out
+//        its own item from the tables a CTA spent 4-6 us on it: five waves of 64-token blocks lost 20 of 210 us.)
 // Partials are merged by their LSE by one kernel for both classes (combine), which finds them by the same arithmetic.
 #pragma once
 #include "pec_internal.h"
@@ -19,8 +20,7 @@ namespace paged {
 
 constexpr int kKeyTile = 128;                 // keys per tile
 constexpr int kFewRows = 128;                 // packed rows of the few class
-constexpr int kMinSliceTiles = 4;             // shortest slice of the many class: its partial costs as much traffic as 1-2 tiles
-constexpr int64_t kNoSplit = (int64_t)1 << 40;
+constexpr int kMinSliceTiles = 2;             // shortest slice of the many class
 
 // Device-side description of one call, passed to the kernels by value.
 struct Params {
@@ -43,10 +43,12 @@ struct Params {
     float *few_o, *few_lse;                   // [2 * few_ctas][few_rows][128], [..][few_rows]
     // many class: blocks of a request = ceil(n * blk_mul / blk_div)
     int32_t blk_mul, blk_div;
-    int32_t many_slots;                       // fair share = all tiles / many_slots
+    int32_t many_ctas;                        // CTAs of the many class that run at a time
     int32_t many_rows;                        // rows of a partial slot
-    int32_t many_cap;                         // slots that the workspace holds
+    int32_t many_cap, items_cap;              // slots and items that the workspace holds
     float *many_o, *many_lse;
+    int32_t *many_count;                      // [2]: items, blocks that are cut
+    struct Item *many_items, *many_split;     // the items, longest first; slice 0 of each block that is cut
 };
 
 struct Request {
@@ -70,7 +72,7 @@ __device__ __forceinline__ Request load_request(const Params &p, int b)
 }
 __device__ __forceinline__ bool is_few(const Params &p, const Request &r) { return p.few && r.n > 0 && (int64_t)r.n * p.g <= kFewRows; }
 __device__ __forceinline__ bool is_many(const Params &p, const Request &r) { return r.n > 0 && !is_few(p, r); }
-__device__ __forceinline__ int32_t blocks_of(const Params &p, const Request &r) { return (int32_t)(((int64_t)r.n * p.blk_mul + p.blk_div - 1) / p.blk_div); }
+__device__ __forceinline__ int32_t blocks_of(const Params &p, const Request &r) { return (r.n * p.blk_mul + p.blk_div - 1) / p.blk_div; }   // T * g < 2^31
 
 __device__ __forceinline__ int64_t warp_sum(int64_t v)
 {
@@ -88,86 +90,31 @@ __device__ __forceinline__ int64_t warp_prefix(int64_t v, int lane)    // inclus
     return v;
 }
 
-// Key tiles of the whole batch, per KV head.  One converged warp.
-__device__ __forceinline__ void batch_tiles(const Params &p, int64_t &few, int64_t &many)
+// Tiles on the few class's line per KV head.  One converged warp.
+__device__ __forceinline__ int64_t few_tiles(const Params &p)
 {
-    const int lane = threadIdx.x & 31;
-    few = many = 0;
-    for (int b = lane; b < p.c.B; b += 32) {
+    int64_t few = 0;
+    for (int b = threadIdx.x & 31; b < p.c.B; b += 32) {
         const Request r = load_request(p, b);
         if (is_few(p, r)) few += r.tiles();
-        else if (is_many(p, r)) many += (int64_t)blocks_of(p, r) * r.tiles();
     }
-    few = warp_sum(few);
-    many = warp_sum(many);
+    return warp_sum(few);
 }
-// few: tiles per CTA.  many: tiles per slice; a request is cut into ceil(tiles / slice) slices of equal length.
-// Slots that split requests take: each has tiles > S, so ceil(tiles / S) < 2 tiles / S, and S >= many * Hkv / many_slots makes
-// the sum over all of them, times Hkv, less than 2 * many_slots.
+// Tiles per CTA.
 __device__ __forceinline__ int64_t few_piece(const Params &p, int64_t few)
 {
     const int64_t all = few * p.Hkv;
     return all > 0 ? (all + p.few_ctas - 1) / p.few_ctas : 1;
 }
-__device__ __forceinline__ int64_t many_slice(const Params &p, int64_t many)
-{
-    const int64_t s = (many * p.Hkv + p.many_slots - 1) / p.many_slots;
-    return s < kMinSliceTiles ? kMinSliceTiles : s;
-}
-__device__ __forceinline__ int32_t slices_of(const Request &r, int64_t slice) { return (int32_t)((r.tiles() + slice - 1) / slice); }
 
-// One item of the many class: rows of one request's block against one slice of its keys (for one KV head, the grid's y).
-struct Item {
+// One item of the many class: rows of one request's block against one slice of its keys, for every KV head.
+struct __align__(16) Item {
     Request r;
     int32_t b, block, slices;
     int32_t key_lo, key_hi;                   // key positions of the slice
-    int64_t slot;                             // partial slot of KV head 0 (slot * Hkv + kvh), where slices > 1
+    int32_t slot;                             // partial slot of KV head 0 (slot * Hkv + kvh), where slices > 1
+    int32_t pad[3];
 };
-// Item `idx`; one converged warp, every lane returns the same.  False past the last item.
-__device__ __forceinline__ bool locate_many(const Params &p, int64_t idx, Item &it)
-{
-    const int lane = threadIdx.x & 31;
-    int64_t few, many;
-    batch_tiles(p, few, many);
-    if (many == 0) return false;
-    const int64_t slice = many_slice(p, many);
-    int64_t before = 0, slots = 0;            // items and partial slots of earlier groups of 32 requests
-    for (int b0 = 0; b0 < p.c.B; b0 += 32) {
-        Request r;
-        r.start = r.n = r.kv = 0;
-        if (b0 + lane < p.c.B) r = load_request(p, b0 + lane);
-        int64_t items = 0, mine = 0;
-        int32_t ns = 0;
-        if (is_many(p, r)) {
-            ns = slices_of(r, slice);
-            items = (int64_t)blocks_of(p, r) * ns;
-            mine = ns > 1 ? items : 0;
-        }
-        const int64_t incl = warp_prefix(items, lane), incl_s = warp_prefix(mine, lane);
-        const unsigned who = __ballot_sync(0xffffffffu, idx >= before + incl - items && idx < before + incl);
-        if (who) {
-            const int src = __ffs(who) - 1;
-            it.b = b0 + src;
-            it.r.start = __shfl_sync(0xffffffffu, r.start, src);
-            it.r.n = __shfl_sync(0xffffffffu, r.n, src);
-            it.r.kv = __shfl_sync(0xffffffffu, r.kv, src);
-            it.slices = __shfl_sync(0xffffffffu, ns, src);
-            const int64_t at = idx - __shfl_sync(0xffffffffu, before + incl - items, src);
-            const int64_t first_slot = __shfl_sync(0xffffffffu, slots + incl_s - mine, src);
-            // The last block sees the most keys: it goes first.
-            const int32_t nb = blocks_of(p, it.r), blk = (int32_t)(at / it.slices), sl = (int32_t)(at % it.slices);
-            it.block = nb - 1 - blk;
-            const int32_t per = (it.r.tiles() + it.slices - 1) / it.slices;
-            it.key_lo = min((int64_t)sl * per * kKeyTile, (int64_t)it.r.kv);
-            it.key_hi = min((int64_t)(sl + 1) * per * kKeyTile, (int64_t)it.r.kv);
-            it.slot = first_slot + (int64_t)it.block * it.slices + sl;
-            return true;
-        }
-        before += __shfl_sync(0xffffffffu, incl, 31);
-        slots += __shfl_sync(0xffffffffu, incl_s, 31);
-    }
-    return false;
-}
 
 // A warp's walk along the few class's line.  The 32 requests around the current one sit in the lanes' registers.
 struct Walk {
@@ -224,49 +171,30 @@ __device__ __forceinline__ void walk_next(const Params &p, Walk &w, int lane)
     walk_take(w, left ? __ffs(left) - 1 : 0);
 }
 
-// Block `idx` of the requests of the many class whose keys are cut (in the order of their slots); one converged warp.
-struct SplitBlock {
-    Request r;
-    int32_t block, slices;
-    int64_t first;                            // slots (first + s) * Hkv + kvh
-};
-__device__ __forceinline__ bool locate_split(const Params &p, int64_t idx, SplitBlock &out)
-{
-    const int lane = threadIdx.x & 31;
-    int64_t few, many;
-    batch_tiles(p, few, many);
-    if (many == 0) return false;
-    const int64_t slice = many_slice(p, many);
-    int64_t before = 0, slots = 0;
-    for (int b0 = 0; b0 < p.c.B; b0 += 32) {
-        Request r;
-        r.start = r.n = r.kv = 0;
-        if (b0 + lane < p.c.B) r = load_request(p, b0 + lane);
-        const int32_t ns = is_many(p, r) ? slices_of(r, slice) : 0;
-        const int64_t blocks = ns > 1 ? blocks_of(p, r) : 0, incl = warp_prefix(blocks, lane), incl_s = warp_prefix(blocks * ns, lane);
-        const unsigned who = __ballot_sync(0xffffffffu, idx >= before + incl - blocks && idx < before + incl);
-        if (who) {
-            const int src = __ffs(who) - 1;
-            out.r.start = __shfl_sync(0xffffffffu, r.start, src);
-            out.r.n = __shfl_sync(0xffffffffu, r.n, src);
-            out.r.kv = __shfl_sync(0xffffffffu, r.kv, src);
-            out.slices = __shfl_sync(0xffffffffu, ns, src);
-            out.block = (int32_t)(idx - __shfl_sync(0xffffffffu, before + incl - blocks, src));
-            out.first = __shfl_sync(0xffffffffu, slots + incl_s - blocks * ns, src) + (int64_t)out.block * out.slices;
-            return true;
-        }
-        before += __shfl_sync(0xffffffffu, incl, 31);
-        slots += __shfl_sync(0xffffffffu, incl_s, 31);
-    }
-    return false;
-}
-
 }  // namespace paged
 
+// Launch that may (`dependent`) start before the preceding kernel of the stream has ended, where that kernel says so.
+template <class... A, class... B>
+inline cudaError_t launch_dependent(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cudaStream_t stream, bool dependent, B... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = dependent ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, (A)args...);
+}
+
 // Launchers (each returns a pec_status).
+int launch_paged_plan(const paged::Params &p, cudaStream_t stream);                        // items of the many class
 int launch_paged_simple(const paged::Params &p, int64_t items, cudaStream_t stream);       // fp32
 int launch_paged_many(const paged::Params &p, int64_t items, cudaStream_t stream);         // bf16
-int launch_paged_few(const paged::Params &p, cudaStream_t stream);
+int launch_paged_few(const paged::Params &p, bool after_many, cudaStream_t stream);         // bf16; after_many: overlaps that kernel's end
 int launch_paged_combine(const paged::Params &p, cudaStream_t stream);
 
 }  // namespace pec
