@@ -177,20 +177,30 @@ paged_plan_kernel(const Params p, const int items_cap, const int split_cap)
 // thread (ty, tx) owns score rows 4 ty .. + 3 and keys tx + 16 j, and output rows 4 ty .. + 3 with channels 4 tx .. + 3 and
 // 64 + 4 tx .. + 3.  Rows, keys and values past their ends are zero in shared memory, so that what a page holds past the
 // request's end never meets a product.
+// Bound by the FMA pipe: per four channels a warp's 16 + 16 micro-tile takes 64 FMA instructions and 12 shared-memory
+// wavefronts, per four keys of P V 128 and 20.  The probabilities take the place of the key tile, which keeps a CTA at 100 KB
+// and two of them on an SM: one's loads and barriers run under the other's arithmetic.  Tiles come by asynchronous copies, the
+// values' while the scores are worked out.
 constexpr int kBM = 64, kBN = 64, kThreads = 256;
 constexpr int kLd = kHeadDim + 4, kLdP = kBN + 4;
-constexpr size_t kSimpleSmem = sizeof(float) * (2 * kBM * kLd + kBN * kHeadDim + kBM * kLdP);
+constexpr size_t kSimpleSmem = sizeof(float) * (2 * kBM * kLd + kBN * kHeadDim);
 
-__device__ __forceinline__ float4 load4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+// 16 bytes to shared memory, zeros where !ok (nothing is read then).
+__device__ __forceinline__ void copy16(float *dst, const float *src, bool ok)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 2)
 paged_simple_kernel(const Params p)
 {
     extern __shared__ __align__(16) float smem[];
     float *sQ = smem;                       // [kBM][kLd]
     float *sK = sQ + kBM * kLd;             // [kBN][kLd]
     float *sV = sK + kBN * kLd;             // [kBN][kHeadDim]
-    float *sP = sV + kBN * kHeadDim;        // [kBM][kLdP]
+    float *sP = sK;                         // [kBM][kLdP], once the scores are done with the keys
     __shared__ int32_t s_page[kBN];
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, kvh = blockIdx.x % p.Hkv;
     asm volatile("griddepcontrol.wait;" ::: "memory");              // launched ahead of the plan's end
@@ -200,12 +210,8 @@ paged_simple_kernel(const Params p)
 
     for (int i = tid; i < kBM * (kHeadDim / 4); i += kThreads) {
         const int r = i / (kHeadDim / 4), c = (i % (kHeadDim / 4)) * 4;
-        float4 val = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r < rows) {
-            const int32_t t = (row0 + r) / p.g, h = kvh * p.g + (row0 + r) % p.g;
-            val = load4(static_cast<const float *>(p.q) + (int64_t)(it.r.start + t) * p.q_st + (int64_t)h * p.q_sh + c);
-        }
-        *reinterpret_cast<float4 *>(sQ + r * kLd + c) = val;
+        const int32_t rr = min(r, rows - 1), t = (row0 + rr) / p.g, h = kvh * p.g + (row0 + rr) % p.g;
+        copy16(sQ + r * kLd + c, static_cast<const float *>(p.q) + (int64_t)(it.r.start + t) * p.q_st + (int64_t)h * p.q_sh + c, r < rows);
     }
 
     float m_run[4], l_run[4], acc[4][8];
@@ -222,7 +228,6 @@ paged_simple_kernel(const Params p)
     const int32_t end = p.causal ? min(it.key_hi, last + 1) : it.key_hi;
 
     for (int32_t k0 = it.key_lo; k0 < end; k0 += kBN) {
-        __syncthreads();                     // the previous tile's reads are done (also orders the Q stores)
         if (tid < kBN) {                     // page of each key of the tile; -1: past the end, or a bad page number
             int32_t page = -1;
             if (k0 + tid < it.key_hi) {
@@ -231,19 +236,30 @@ paged_simple_kernel(const Params p)
             }
             s_page[tid] = page;
         }
-        __syncthreads();
-        for (int i = tid; i < kBN * (kHeadDim / 4); i += kThreads) {
-            const int r = i / (kHeadDim / 4), c = (i % (kHeadDim / 4)) * 4;
-            float4 kk = make_float4(0.f, 0.f, 0.f, 0.f), vv = kk;
-            const int64_t page = s_page[r];
-            if (page >= 0) {
-                const int64_t slot = (k0 + r) % p.c.page_size;
-                kk = load4(static_cast<const float *>(p.k_pages) + page * p.c.k_sp + slot * p.c.k_st + (int64_t)kvh * p.c.k_sh + c);
-                vv = load4(static_cast<const float *>(p.v_pages) + page * p.c.v_sp + slot * p.c.v_st + (int64_t)kvh * p.c.v_sh + c);
-            }
-            *reinterpret_cast<float4 *>(sK + r * kLd + c) = kk;
-            *reinterpret_cast<float4 *>(sV + r * kHeadDim + c) = vv;
+        __syncthreads();                     // ... and the previous tile's reads are done
+        // A warp copies whole rows of 512 bytes, eight of each tile: warp w rows w, w + 8, ...
+        const int c4 = (tid & 31) * 4;
+        int64_t page[8];
+        int32_t slot[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = (tid >> 5) + 8 * i;
+            page[i] = s_page[r];
+            slot[i] = (k0 + r) % p.c.page_size;
+            const bool ok = page[i] >= 0;
+            const float *src = static_cast<const float *>(p.k_pages) + (ok ? page[i] * p.c.k_sp + slot[i] * p.c.k_st : 0) + (int64_t)kvh * p.c.k_sh + c4;
+            copy16(sK + r * kLd + c4, src, ok);
         }
+        copy_commit();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = (tid >> 5) + 8 * i;
+            const bool ok = page[i] >= 0;
+            const float *src = static_cast<const float *>(p.v_pages) + (ok ? page[i] * p.c.v_sp + slot[i] * p.c.v_st : 0) + (int64_t)kvh * p.c.v_sh + c4;
+            copy16(sV + r * kHeadDim + c4, src, ok);
+        }
+        copy_commit();
+        copy_wait<1>();                      // the keys (and Q)
         __syncthreads();
 
         float s[4][4];
@@ -268,6 +284,7 @@ paged_simple_kernel(const Params p)
                     s[i][j] = fmaf(qa[i].w, kb[j].w, s[i][j]);
                 }
         }
+        __syncthreads();                     // every warp is done with the keys: P may take their place
         // Mask by choice, not by adding -inf: a masked score may be anything.  State replicated over a row's 16 threads.
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -296,21 +313,29 @@ paged_simple_kernel(const Params p)
 #pragma unroll
             for (int c = 0; c < 8; ++c) acc[i][c] *= alpha;
         }
+        copy_wait<0>();                      // the values
         __syncthreads();
-#pragma unroll 4
-        for (int j = 0; j < kBN; ++j) {
-            const float4 v0 = *reinterpret_cast<const float4 *>(sV + j * kHeadDim + tx * 4);
-            const float4 v1 = *reinterpret_cast<const float4 *>(sV + j * kHeadDim + 64 + tx * 4);
+#pragma unroll 2
+        for (int j = 0; j < kBN; j += 4) {
+            float pr[4][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float pij = sP[(ty * 4 + i) * kLdP + j];
-                acc[i][0] = fmaf(pij, v0.x, acc[i][0]); acc[i][1] = fmaf(pij, v0.y, acc[i][1]);
-                acc[i][2] = fmaf(pij, v0.z, acc[i][2]); acc[i][3] = fmaf(pij, v0.w, acc[i][3]);
-                acc[i][4] = fmaf(pij, v1.x, acc[i][4]); acc[i][5] = fmaf(pij, v1.y, acc[i][5]);
-                acc[i][6] = fmaf(pij, v1.z, acc[i][6]); acc[i][7] = fmaf(pij, v1.w, acc[i][7]);
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(pr[i]) = *reinterpret_cast<const float4 *>(sP + (ty * 4 + i) * kLdP + j);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const float4 v0 = *reinterpret_cast<const float4 *>(sV + (j + x) * kHeadDim + tx * 4);
+                const float4 v1 = *reinterpret_cast<const float4 *>(sV + (j + x) * kHeadDim + 64 + tx * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w = pr[i][x];
+                    acc[i][0] = fmaf(w, v0.x, acc[i][0]); acc[i][1] = fmaf(w, v0.y, acc[i][1]);
+                    acc[i][2] = fmaf(w, v0.z, acc[i][2]); acc[i][3] = fmaf(w, v0.w, acc[i][3]);
+                    acc[i][4] = fmaf(w, v1.x, acc[i][4]); acc[i][5] = fmaf(w, v1.y, acc[i][5]);
+                    acc[i][6] = fmaf(w, v1.z, acc[i][6]); acc[i][7] = fmaf(w, v1.w, acc[i][7]);
+                }
             }
         }
     }
+    copy_wait<0>();                          // Q's copies, where there was no tile
 
     const int64_t slot = (int64_t)it.slot * p.Hkv + kvh;
     if (it.slices > 1 && slot >= p.many_cap) return;               // cannot happen (see many_plan); never write past the scratch
@@ -339,14 +364,14 @@ paged_simple_kernel(const Params p)
 }
 
 // ------------------------------------------------------------------------------------------ combining partials
-// A CTA merges the partial results of eight packed rows (few class) or 32 (many class) of one unit: a (request, KV head) whose
+// A CTA merges the partial results of some packed rows of one unit: a (request, KV head) whose
 // tiles cross a cut of the line, or a block of rows whose keys are cut into slices (listed by the plan).  Units are enumerated by
 // what splits them - CTA c of the few class looks at cut c and takes the unit around it if this is the unit's first cut - so that
 // the grid has the size of what can be split, not of the batch.  (A CTA per token and KV head took 66 us to find nothing to do for
 // 2048 tokens.)  The few class looks its unit up before the attention kernels end (the tables were complete before they began);
 // partials are read afterwards, and no CTA ends before that wait, so that whatever follows on the stream follows those kernels too.
 // A warp merges one row at a time, a lane owning four channels: the largest LSE first, then the weighted sum.
-constexpr int kCombineWarps = 8, kFewGroup = 8, kManyGroup = 32;
+constexpr int kCombineWarps = 8, kManyGroup = 32;
 
 __device__ __forceinline__ void combine_row(const Params &p, const float *po, const float *pl, int64_t at0, int64_t shift, int64_t step,
                                             int count, int64_t item, int lane)
@@ -398,11 +423,11 @@ paged_combine_kernel(const Params p, const int few_groups, const int few_blocks,
         const int64_t u1 = w.u0 + w.r.tiles();
         const int64_t first = cut - 1;                           // piece with the unit's first tiles
         const int count = (int)((u1 - 1) / piece - first) + 1;
-        const int row = group * kFewGroup + warp;
-        if (row >= w.r.n * p.g) return;
-        const int64_t item = (int64_t)(w.r.start + row / p.g) * p.Hq + w.kvh * p.g + row % p.g;
-        combine_row(p, p.few_o, p.few_lse, 2 * first * p.few_rows + row, w.u0 > first * piece ? p.few_rows : 0, 2 * (int64_t)p.few_rows, count,
-                    item, lane);
+        for (int row = group * kCombineWarps + warp; row < w.r.n * p.g; row += few_groups * kCombineWarps) {
+            const int64_t item = (int64_t)(w.r.start + row / p.g) * p.Hq + w.kvh * p.g + row % p.g;
+            combine_row(p, p.few_o, p.few_lse, 2 * first * p.few_rows + row, w.u0 > first * piece ? p.few_rows : 0, 2 * (int64_t)p.few_rows,
+                        count, item, lane);
+        }
     } else {
         // The blocks that are cut, from the plan's list.
         asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -455,7 +480,7 @@ int launch_paged_simple(const Params &p, int64_t items, cudaStream_t stream)
 int launch_paged_combine(const Params &p, cudaStream_t stream)
 {
     // Every cut of the line; every block that can be cut: one has two slots or more.
-    const int few_groups = (p.few_rows + kFewGroup - 1) / kFewGroup, few_blocks = p.few ? (p.few_ctas - 1) * few_groups : 0;
+    const int few_groups = p.few_rows > 3 * kCombineWarps ? 4 : (p.few_rows + kCombineWarps - 1) / kCombineWarps, few_blocks = p.few ? (p.few_ctas - 1) * few_groups : 0;
     const int many_groups = (p.many_rows + kManyGroup - 1) / kManyGroup;
     const int64_t most = (int64_t)p.many_cap / 2 * many_groups;      // a block that is cut has two slots or more
     const int many_blocks = (int)(most < 4 * p.many_ctas ? most : 4 * p.many_ctas);
@@ -538,7 +563,7 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
     const int tps = kFewRows / p.g;           // tensor cores: two stages of whole tokens; FMA: 64 packed rows
     p.blk_mul = tensor ? 1 : p.g; p.blk_div = tensor ? 2 * tps : kBM;
     p.many_rows = tensor ? 2 * tps * p.g : kBM;
-    p.many_ctas = sms;
+    p.many_ctas = tensor ? sms : 2 * sms;
     c.many_items = 0;
     if (!p.few || (int64_t)p.max_q * p.g > kFewRows) {
         const int64_t shortest = p.few ? kFewRows / p.g + 1 : 1, most = a->T / shortest;       // new tokens of such a request; how many there can be
