@@ -18,104 +18,121 @@ namespace paged {
 // block for one KV head; its length is the number of its request's key tiles.  Units up to the last full wave of many_ctas CTAs stay
 // whole, unless one is longer than an SM's fair share of all tiles (slice0); of the rest, which would leave SMs idle for a whole
 // unit's time, the keys are cut into slices (slice1): as many as fill one, two or three waves, whichever has the shortest
-// estimated time, or none.  The estimate, in times of a tile (1.35 us): a wave of slices takes its tiles and kItemTiles for a CTA's
-// start and end; a slice's partial, written and read once, kMergeTiles / 32 (132 KB both ways).
+// estimated time, or none.  The estimate, in 1/32 of a tile's time: a wave of slices takes its tiles and item_cost for a CTA's
+// start and end; a slice's partial, written and read once, merge_cost.  On the tensor cores a tile takes 1.35 us, start and end 4
+// us, a partial of 132 KB 0.04 us both ways; with the FMA kernel, 17 us a tile, both are next to nothing.
 // Slots that cut units take: cutting units of length l into slices of S takes less than sum l / S + their number.  slice0 >= all
 // tiles / many_ctas, and units longer than that are fewer than many_ctas: 2 many_ctas.  The tail has less than many_ctas + Hkv
 // units of mean length m and slice1 >= m / cuts with cuts * units <= 3 many_ctas: 4 many_ctas + Hkv.
 // Items go into the list longest first (by 256 classes of visible tiles): an SM that falls free late finds short work.  The order
 // inside a class is whatever the atomics make it; it changes when an item runs, never what it computes.
-constexpr int kPlanThreads = 1024, kClasses = 256;
-constexpr int kItemTiles = 3, kMergeTiles = 1;
+constexpr int kPlanThreads = 256, kClasses = 256;
 
-__device__ __forceinline__ int64_t block_prefix(int64_t v, int64_t *s_warp, int64_t &total)    // inclusive; one value per thread
+// Inclusive prefix sums of two values per thread over the block, and their totals.
+struct Pair { int64_t x, y; };
+__device__ __forceinline__ Pair block_prefix(int64_t x, int64_t y, Pair *s_warp, Pair &total)
 {
+    constexpr int kWarps = kPlanThreads / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t x = warp_prefix(v, lane);
+    Pair v = {warp_prefix(x, lane), warp_prefix(y, lane)};
+    __syncthreads();                                                // the previous call's reads are done
+    if (lane == 31) s_warp[warp] = v;
     __syncthreads();
-    if (lane == 31) s_warp[warp] = x;
-    __syncthreads();
-    const int64_t w = s_warp[lane], incl = warp_prefix(w, lane);
-    total = __shfl_sync(0xffffffffu, incl, 31);
-    const int64_t before = __shfl_sync(0xffffffffu, incl - w, warp);
-    return x + before;
+    total = {0, 0};
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        const Pair o = s_warp[w];
+        if (w < warp) { v.x += o.x; v.y += o.y; }
+        total.x += o.x; total.y += o.y;
+    }
+    return v;
 }
 
 __global__ void __launch_bounds__(kPlanThreads)
 paged_plan_kernel(const Params p, const int items_cap, const int split_cap)
 {
-    __shared__ int64_t s_warp[32];
-    __shared__ int32_t s_item[kPlanThreads], s_split[kPlanThreads], s_slot[kPlanThreads];   // ends of the requests' ranges
+    __shared__ Pair s_warp[kPlanThreads / 32];
+    __shared__ int32_t s_item[kPlanThreads], s_split[kPlanThreads], s_slot[kPlanThreads];   // ends (s_slot: starts) of the requests' ranges
     __shared__ int32_t s_start[kPlanThreads], s_n[kPlanThreads], s_kv[kPlanThreads], s_n0[kPlanThreads];
     __shared__ int32_t s_class[kClasses], s_most;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x;
-    if (tid < kClasses) s_class[tid] = 0;
+    const bool one = p.c.B <= kPlanThreads;                         // a request per thread: looked up once
+    s_class[tid] = 0;
     if (tid == 0) s_most = 1;
-    __syncthreads();
+    Request r;
+    int32_t nb = 0;
+    auto take = [&](int b0) {                                       // this thread's request of the group from b0 on
+        r.start = r.n = r.kv = 0;
+        if (b0 + tid < p.c.B) r = load_request(p, b0 + tid);
+        nb = is_many(p, r) ? blocks_of(p, r) : 0;
+    };
 
-    int64_t blocks = 0, tiles = 0;
+    // Blocks and tiles of the whole batch; with one group, the place of this thread's first block too.
+    int64_t blocks = 0, tiles = 0, place = 0;
     int32_t most = 1;
-    for (int b = tid; b < p.c.B; b += kPlanThreads) {
-        const Request r = load_request(p, b);
-        if (is_many(p, r)) { const int64_t nb = blocks_of(p, r); blocks += nb; tiles += nb * r.tiles(); most = max(most, r.tiles()); }
+    for (int b0 = 0; b0 < p.c.B; b0 += kPlanThreads) {
+        take(b0);
+        blocks += nb; tiles += (int64_t)nb * r.tiles();
+        if (nb > 0) most = max(most, r.tiles());
     }
+    Pair all;
+    place = block_prefix(blocks, tiles, s_warp, all).x - blocks;
     atomicMax(&s_most, most);
-    int64_t all_blocks, all_tiles;
-    block_prefix(blocks, s_warp, all_blocks);
-    block_prefix(tiles, s_warp, all_tiles);
-    most = s_most;
-    const int32_t tail_at = (int32_t)(all_blocks * p.Hkv / p.many_ctas * p.many_ctas / p.Hkv);
-    const int64_t tail_blocks = all_blocks - tail_at, units = tail_blocks * p.Hkv;
-    const int32_t slice0 = (int32_t)max((all_tiles * p.Hkv + p.many_ctas - 1) / p.many_ctas, (int64_t)kMinSliceTiles);
+    const int32_t tail_at = (int32_t)(all.x * p.Hkv / p.many_ctas * p.many_ctas / p.Hkv);
+    const int64_t tail_blocks = all.x - tail_at, units = tail_blocks * p.Hkv;
+    const int32_t slice0 = (int32_t)max((all.y * p.Hkv + p.many_ctas - 1) / p.many_ctas, (int64_t)p.min_slice);
     int32_t slice1 = slice0;
+    Pair sum;
     if (units > 0) {
-        int64_t tail = 0, before = 0, part;
+        int64_t tail = 0, before = 0;
         for (int b0 = 0; b0 < p.c.B; b0 += kPlanThreads) {
-            Request r;
-            r.start = r.n = r.kv = 0;
-            if (b0 + tid < p.c.B) r = load_request(p, b0 + tid);
-            const int64_t nb = is_many(p, r) ? blocks_of(p, r) : 0, end = before + block_prefix(nb, s_warp, part);
-            tail += min(nb, max(end - tail_at, (int64_t)0)) * r.tiles();
-            before += part;
+            if (!one) {
+                take(b0);
+                place = before + block_prefix(nb, 0, s_warp, sum).x - nb;
+                before += sum.x;
+            }
+            tail += min((int64_t)nb, max(place + nb - tail_at, (int64_t)0)) * r.tiles();
         }
-        block_prefix(tail, s_warp, part);
-        tail = part;
+        block_prefix(tail, 0, s_warp, sum);
+        tail = sum.x;
         const int64_t mean = (tail + tail_blocks - 1) / tail_blocks;
-        int64_t best = 32 * ((units + p.many_ctas - 1) / p.many_ctas) * (mean + kItemTiles), len = mean;
+        int64_t best = (units + p.many_ctas - 1) / p.many_ctas * (32 * mean + p.item_cost), len = mean;
         for (int w = 1; w <= 3; ++w) {
-            const int64_t cuts = (int64_t)w * p.many_ctas / units;   // slices of a unit of mean length that w waves have room for
+            const int32_t cuts = w * p.many_ctas / (int32_t)units;  // slices of a unit of mean length that w waves have room for
             if (cuts < 2) continue;
-            const int64_t l = max((mean + cuts - 1) / cuts, (int64_t)kMinSliceTiles);
-            const int64_t time = 32 * w * (l + kItemTiles) + kMergeTiles * cuts * units / 16 + 64;
+            const int64_t l = max((mean + cuts - 1) / cuts, (int64_t)p.min_slice);
+            const int64_t time = w * (32 * l + p.item_cost) + p.merge_cost * cuts * units;
             if (time < best) { best = time; len = l; }
         }
         if (len < mean) slice1 = (int32_t)min(len, (int64_t)slice0);
     }
+    __syncthreads();
+    most = s_most;
 
     int64_t n_items = 0, n_split = 0;
     for (int pass = 0; pass < 2; ++pass) {                          // count the classes; write the items
         int64_t places = 0, slots = 0;
         n_items = n_split = 0;
         for (int b0 = 0; b0 < p.c.B; b0 += kPlanThreads) {
-            Request r;
-            r.start = r.n = r.kv = 0;
-            if (b0 + tid < p.c.B) r = load_request(p, b0 + tid);
-            const int32_t nb = is_many(p, r) ? blocks_of(p, r) : 0;
-            int64_t part;
-            const int64_t place = places + block_prefix(nb, s_warp, part) - nb;
-            places += part;
+            if (!one) {
+                take(b0);
+                place = places + block_prefix(nb, 0, s_warp, sum).x - nb;
+                places += sum.x;
+            }
             const int32_t n0 = (int32_t)min(max(tail_at - place, (int64_t)0), (int64_t)nb), n1 = nb - n0;
             const int32_t c0 = (r.tiles() + slice0 - 1) / slice0, c1 = (r.tiles() + slice1 - 1) / slice1;
             const int64_t items = (int64_t)n0 * c0 + (int64_t)n1 * c1, split = (c0 > 1 ? n0 : 0) + (c1 > 1 ? n1 : 0);
             const int64_t mine = (c0 > 1 ? (int64_t)n0 * c0 : 0) + (c1 > 1 ? (int64_t)n1 * c1 : 0);
-            int64_t chunk_items, chunk_split, chunk_slots;
-            s_item[tid] = (int32_t)block_prefix(items, s_warp, chunk_items);
-            s_split[tid] = (int32_t)block_prefix(split, s_warp, chunk_split);
-            s_slot[tid] = (int32_t)(slots + block_prefix(mine, s_warp, chunk_slots) - mine);
+            Pair chunk;                                             // items with split blocks above them; slots
+            const Pair end = block_prefix(items | split << 32, mine, s_warp, chunk);
+            const int32_t chunk_items = (int32_t)chunk.x;
+            s_item[tid] = (int32_t)end.x;
+            s_split[tid] = (int32_t)(end.x >> 32);
+            s_slot[tid] = (int32_t)(slots + end.y - mine);
             s_start[tid] = r.start; s_n[tid] = r.n; s_kv[tid] = r.kv; s_n0[tid] = n0;
             __syncthreads();
-            for (int i = tid; i < (int)chunk_items; i += kPlanThreads) {
+            for (int i = tid; i < chunk_items; i += kPlanThreads) {
                 int lo = 0, hi = kPlanThreads - 1;                  // the first request whose range ends past i
                 while (lo < hi) {
                     const int mid = (lo + hi) >> 1;
@@ -125,7 +142,6 @@ paged_plan_kernel(const Params p, const int items_cap, const int split_cap)
                 it.r.start = s_start[lo]; it.r.n = s_n[lo]; it.r.kv = s_kv[lo];
                 it.b = b0 + lo;
                 const int32_t t = it.r.tiles(), d0 = (t + slice0 - 1) / slice0, d1 = (t + slice1 - 1) / slice1, m0 = s_n0[lo];
-                const int32_t nbl = blocks_of(p, it.r);
                 int32_t at = i - (lo > 0 ? s_item[lo - 1] : 0), split_at = lo > 0 ? s_split[lo - 1] : 0, blk, sl;
                 it.slot = s_slot[lo];
                 if (at < m0 * d0) {
@@ -137,15 +153,15 @@ paged_plan_kernel(const Params p, const int items_cap, const int split_cap)
                     it.slices = d1; it.slot += (d0 > 1 ? m0 * d0 : 0) + at; split_at += (d0 > 1 ? m0 : 0) + blk;
                     blk += m0;
                 }
-                it.block = nbl - 1 - blk;
+                it.block = blocks_of(p, it.r) - 1 - blk;
                 const int32_t per = (t + it.slices - 1) / it.slices;
                 it.key_lo = (int32_t)min((int64_t)sl * per * kKeyTile, (int64_t)it.r.kv);
                 it.key_hi = (int32_t)min((int64_t)(sl + 1) * per * kKeyTile, (int64_t)it.r.kv);
                 // Visible tiles: the block's last token sees up to its own position.
-                const int64_t last = min((int64_t)it.r.n, (int64_t)(it.block + 1) * p.blk_div / p.blk_mul + 1);
-                const int64_t see = p.causal ? min((int64_t)it.key_hi, it.r.pos0() + last) : it.key_hi;
-                const int32_t w = see > it.key_lo ? (int32_t)((see - it.key_lo + kKeyTile - 1) / kKeyTile) : 0;
-                const int32_t cls = kClasses - 1 - (int32_t)((int64_t)w * (kClasses - 1) / most);
+                const int32_t last = (int32_t)min((int64_t)it.r.n, (int64_t)(it.block + 1) * p.blk_div / p.blk_mul + 1);
+                const int32_t see = p.causal ? min(it.key_hi, it.r.pos0() + last) : it.key_hi;
+                const int32_t w = see > it.key_lo ? (see - it.key_lo + kKeyTile - 1) / kKeyTile : 0;
+                const int32_t cls = kClasses - 1 - (int32_t)((float)w / (float)most * (kClasses - 1));
                 if (pass == 0) {
                     atomicAdd(&s_class[cls], 1);
                 } else {
@@ -155,14 +171,13 @@ paged_plan_kernel(const Params p, const int items_cap, const int split_cap)
                     if (it.slices > 1 && sl == 0 && n_split + split_at < split_cap) p.many_split[n_split + split_at] = it;
                 }
             }
-            n_items += chunk_items; n_split += chunk_split; slots += chunk_slots;
+            n_items += chunk_items; n_split += chunk.x >> 32; slots += chunk.y;
             __syncthreads();
         }
-        if (pass == 0) {                                            // ends of the classes -> their starts
-            const int32_t mine = tid < kClasses ? s_class[tid] : 0;
-            int64_t sum;
-            const int64_t end = block_prefix(mine, s_warp, sum);
-            if (tid < kClasses) s_class[tid] = (int32_t)(end - mine);
+        if (pass == 0) {                                            // sizes of the classes -> their starts
+            const int32_t size = s_class[tid];
+            const int64_t end = block_prefix(size, 0, s_warp, sum).x;
+            s_class[tid] = (int32_t)end - size;
             __syncthreads();
         }
     }
@@ -171,14 +186,15 @@ paged_plan_kernel(const Params p, const int items_cap, const int split_cap)
         p.many_count[1] = (int32_t)min(n_split, (int64_t)split_cap);
     }
 }
+static_assert(kClasses == kPlanThreads, "a class per thread");
 
 // ------------------------------------------------------------------------------------------ FMA kernel
 // One CTA = 64 packed rows of one KV head against one slice of the request's keys, 64 keys at a time.  256 threads as 16 x 16:
 // thread (ty, tx) owns score rows 4 ty .. + 3 and keys tx + 16 j, and output rows 4 ty .. + 3 with channels 4 tx .. + 3 and
 // 64 + 4 tx .. + 3.  Rows, keys and values past their ends are zero in shared memory, so that what a page holds past the
 // request's end never meets a product.
-// Bound by the FMA pipe: per four channels a warp's 16 + 16 micro-tile takes 64 FMA instructions and 12 shared-memory
-// wavefronts, per four keys of P V 128 and 20.  The probabilities take the place of the key tile, which keeps a CTA at 100 KB
+// Bound by the FMA pipe: per four channels a warp's 16 + 16 micro-tile takes 32 packed FMA instructions (64 issue slots of the
+// pipe) and 12 shared-memory wavefronts, per four keys of P V 64 (128) and 20; packed, they leave issue slots for the rest.  The probabilities take the place of the key tile, which keeps a CTA at 100 KB
 // and two of them on an SM: one's loads and barriers run under the other's arithmetic.  Tiles come by asynchronous copies, the
 // values' while the scores are worked out.
 constexpr int kBM = 64, kBN = 64, kThreads = 256;
@@ -214,7 +230,8 @@ paged_simple_kernel(const Params p)
         copy16(sQ + r * kLd + c, static_cast<const float *>(p.q) + (int64_t)(it.r.start + t) * p.q_st + (int64_t)h * p.q_sh + c, r < rows);
     }
 
-    float m_run[4], l_run[4], acc[4][8];
+    float m_run[4], l_run[4];
+    float2 acc[4][4];                        // channels 4 tx .. + 3, 64 + 4 tx .. + 3
     int32_t lim[4];                          // keys below it are visible to the row
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -222,7 +239,7 @@ paged_simple_kernel(const Params p)
         const int32_t r = row0 + ty * 4 + i, pos = it.r.pos0() + r / p.g;
         lim[i] = p.causal ? min(it.key_hi, pos + 1) : it.key_hi;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) acc[i][c] = 0.f;
+        for (int c = 0; c < 4; ++c) acc[i][c] = make_float2(0.f, 0.f);
     }
     const int32_t last = it.r.pos0() + (row0 + rows - 1) / p.g;
     const int32_t end = p.causal ? min(it.key_hi, last + 1) : it.key_hi;
@@ -262,12 +279,13 @@ paged_simple_kernel(const Params p)
         copy_wait<1>();                      // the keys (and Q)
         __syncthreads();
 
-        float s[4][4];
+        // Packed FMAs: each half of s2 sums every second channel.
+        float2 s2[4][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
-#pragma unroll 4
+            for (int j = 0; j < 4; ++j) s2[i][j] = make_float2(0.f, 0.f);
+#pragma unroll 2
         for (int d = 0; d < kHeadDim; d += 4) {
             float4 qa[4], kb[4];
 #pragma unroll
@@ -278,21 +296,19 @@ paged_simple_kernel(const Params p)
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    s[i][j] = fmaf(qa[i].x, kb[j].x, s[i][j]);
-                    s[i][j] = fmaf(qa[i].y, kb[j].y, s[i][j]);
-                    s[i][j] = fmaf(qa[i].z, kb[j].z, s[i][j]);
-                    s[i][j] = fmaf(qa[i].w, kb[j].w, s[i][j]);
+                    s2[i][j] = __ffma2_rn(make_float2(qa[i].x, qa[i].y), make_float2(kb[j].x, kb[j].y), s2[i][j]);
+                    s2[i][j] = __ffma2_rn(make_float2(qa[i].z, qa[i].w), make_float2(kb[j].z, kb[j].w), s2[i][j]);
                 }
         }
         __syncthreads();                     // every warp is done with the keys: P may take their place
         // Mask by choice, not by adding -inf: a masked score may be anything.  State replicated over a row's 16 threads.
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float mx = -INFINITY;
+            float mx = -INFINITY, s[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                s[i][j] = (k0 + tx + 16 * j < lim[i]) ? s[i][j] * p.scale_log2 : -INFINITY;
-                mx = fmaxf(mx, s[i][j]);
+                s[j] = (k0 + tx + 16 * j < lim[i]) ? (s2[i][j].x + s2[i][j].y) * p.scale_log2 : -INFINITY;
+                mx = fmaxf(mx, s[j]);
             }
 #pragma unroll
             for (int o = 8; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -302,7 +318,7 @@ paged_simple_kernel(const Params p)
             float rs = 0.f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float pj = exp2f(s[i][j] - m_use);
+                const float pj = exp2f(s[j] - m_use);
                 rs += pj;
                 sP[(ty * 4 + i) * kLdP + tx + 16 * j] = pj;
             }
@@ -311,7 +327,7 @@ paged_simple_kernel(const Params p)
             l_run[i] = l_run[i] * alpha + rs;
             m_run[i] = m_new;
 #pragma unroll
-            for (int c = 0; c < 8; ++c) acc[i][c] *= alpha;
+            for (int c = 0; c < 4; ++c) acc[i][c] = __fmul2_rn(acc[i][c], make_float2(alpha, alpha));
         }
         copy_wait<0>();                      // the values
         __syncthreads();
@@ -326,11 +342,11 @@ paged_simple_kernel(const Params p)
                 const float4 v1 = *reinterpret_cast<const float4 *>(sV + (j + x) * kHeadDim + 64 + tx * 4);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float w = pr[i][x];
-                    acc[i][0] = fmaf(w, v0.x, acc[i][0]); acc[i][1] = fmaf(w, v0.y, acc[i][1]);
-                    acc[i][2] = fmaf(w, v0.z, acc[i][2]); acc[i][3] = fmaf(w, v0.w, acc[i][3]);
-                    acc[i][4] = fmaf(w, v1.x, acc[i][4]); acc[i][5] = fmaf(w, v1.y, acc[i][5]);
-                    acc[i][6] = fmaf(w, v1.z, acc[i][6]); acc[i][7] = fmaf(w, v1.w, acc[i][7]);
+                    const float2 w = make_float2(pr[i][x], pr[i][x]);
+                    acc[i][0] = __ffma2_rn(w, make_float2(v0.x, v0.y), acc[i][0]);
+                    acc[i][1] = __ffma2_rn(w, make_float2(v0.z, v0.w), acc[i][1]);
+                    acc[i][2] = __ffma2_rn(w, make_float2(v1.x, v1.y), acc[i][2]);
+                    acc[i][3] = __ffma2_rn(w, make_float2(v1.z, v1.w), acc[i][3]);
                 }
             }
         }
@@ -347,7 +363,7 @@ paged_simple_kernel(const Params p)
         const float lse = l_run[i] > 0.f ? m_run[i] * 0.6931471805599453f + logf(l_run[i]) : -INFINITY;
         float out[8];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) out[c] = l_run[i] > 0.f ? acc[i][c] * inv : 0.f;
+        for (int c = 0; c < 8; ++c) out[c] = l_run[i] > 0.f ? (c & 1 ? acc[i][c / 2].y : acc[i][c / 2].x) * inv : 0.f;
         if (it.slices > 1) {
             float *o = p.many_o + (slot * p.many_rows + r) * kHeadDim;
             *reinterpret_cast<float4 *>(o + tx * 4) = make_float4(out[0], out[1], out[2], out[3]);
@@ -412,9 +428,8 @@ paged_combine_kernel(const Params p, const int few_groups, const int few_blocks,
     if ((int)blockIdx.x < few_blocks) {
         const int64_t cut = blockIdx.x / few_groups + 1;
         const int group = blockIdx.x % few_groups;
-        const int64_t all = few_tiles(p);
-        const int64_t piece = few_piece(p, all), at = cut * piece;
         Walk w;
+        const int64_t all = walk_tiles(p, w, lane), piece = few_piece(p, all), at = cut * piece;
         w.u0 = at;
         if (at < all * p.Hkv) walk_to(p, w, at, lane);
         const bool mine = w.u0 < at && w.u0 >= at - piece;       // else the cut falls between units, or is not the unit's first
@@ -564,12 +579,15 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
     p.blk_mul = tensor ? 1 : p.g; p.blk_div = tensor ? 2 * tps : kBM;
     p.many_rows = tensor ? 2 * tps * p.g : kBM;
     p.many_ctas = tensor ? sms : 2 * sms;
+    p.min_slice = tensor ? 2 : 1;
+    p.item_cost = tensor ? 96 : 8;
+    p.merge_cost = tensor ? 1 : 0;
     c.many_items = 0;
     if (!p.few || (int64_t)p.max_q * p.g > kFewRows) {
         const int64_t shortest = p.few ? kFewRows / p.g + 1 : 1, most = a->T / shortest;       // new tokens of such a request; how many there can be
         const int64_t blocks = a->T * p.blk_mul / p.blk_div + (a->B < most ? a->B : most);
         c.many_items = blocks + ceil_div(6 * (int64_t)p.many_ctas, p.Hkv) + 2;                 // whole blocks and slots
-        const int64_t most_slices = ceil_div(ceil_div((int64_t)a->max_pages * a->page_size, kKeyTile), kMinSliceTiles);
+        const int64_t most_slices = ceil_div(ceil_div((int64_t)a->max_pages * a->page_size, kKeyTile), p.min_slice);
         int64_t cap = 6 * (int64_t)p.many_ctas + p.Hkv;
         if (most_slices <= 1) cap = 0;
         else if (blocks * most_slices * p.Hkv < cap) cap = blocks * most_slices * p.Hkv;

@@ -80,8 +80,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     Walk walk;
     if (warp == kLoadWarp) {
         if (lane == 0) griddep_launch_dependents();        // the combining kernel may be launched; it waits for this one's end
-        const int64_t all = few_tiles(p);
-        const int64_t piece = few_piece(p, all), first = blockIdx.x * piece;
+        const int64_t all = walk_tiles(p, walk, lane), piece = few_piece(p, all), first = blockIdx.x * piece;
         const int64_t count = all * p.Hkv - first;
         const int32_t n = (int32_t)(count < 0 ? 0 : (count < piece ? count : piece));
         if (n > 0) walk_to(p, walk, first, lane);
@@ -101,28 +100,29 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&sh->kv_full[s]), 1); mbar_init(smem_u32(&sh->kv_empty[s]), 1); }
         mbar_init_fence();
         prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
-    }
-    __syncthreads();
-    const int32_t count = sh->count;
-    if (count == 0) {
-        griddep_wait();
-        return;
-    }
-    if (warp == 4) {
+    } else if (warp == 4) {
         tmem_alloc(smem_u32(&sh->tmem_base), kTmemCols);
         tmem_relinquish();
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    const int32_t count = sh->count;
     const uint32_t tmem = sh->tmem_base;
+    if (count == 0) {
+        if (warp == 4) tmem_dealloc(tmem, kTmemCols);
+        griddep_wait();
+        return;
+    }
 
     if (warp == kLoadWarp) {
         // ------------------------------------------------------------------ loader
         reg_dealloc<kLightRegs>();
         const BoxLane bl = box_lane(box, lane);
         const int64_t first = sh->first, end = first + count;
-        int32_t page = box_page(p, walk.b, walk.tile * kKeyTile, walk.r.kv, bl);
+        const BoxStep step = box_step(p.c.page_size);
+        BoxPlace at = box_place(p.c.page_size, walk.tile * kKeyTile, bl);      // this lane's box of the current tile, and its page
+        int32_t page = box_page(p, walk.b, walk.tile * kKeyTile, walk.r.kv, bl, at);
         int segs = 0, n = 0;
         uint32_t issued = 0, q_issued = 0;                 // ring items and segments whose loads are under way
         bool ok = true;
@@ -157,10 +157,14 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             if (n + tiles < count) walk_next(p, walk, lane);
             for (int j = 0; j < tiles && ok; ++j, ++n, k0 += kKeyTile) {
                 int32_t page_next = 0;
-                if (j + 1 < tiles) page_next = box_page(p, b, k0 + kKeyTile, kv, bl);
-                else if (n + 1 < count) page_next = box_page(p, walk.b, walk.tile * kKeyTile, walk.r.kv, bl);
+                BoxPlace at_next = box_next(at, step);
+                if (j + 1 < tiles) {
+                    page_next = box_page(p, b, k0 + kKeyTile, kv, bl, at_next);
+                } else if (n + 1 < count) {                // the next unit, from its first tile
+                    at_next = box_place(p.c.page_size, 0, bl);
+                    page_next = box_page(p, walk.b, 0, walk.r.kv, bl, at_next);
+                }
                 const uint32_t bytes = tile_bytes(k0, kv, box);
-                const int32_t row = (k0 + bl.first) % p.c.page_size;
 #pragma unroll
                 for (int which = 0; which < 2; ++which) {  // K, V
                     const int item = 2 * n + which, slot = item % kSlots, fill = item / kSlots;
@@ -172,10 +176,11 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     __syncwarp();
                     if (bl.used && k0 + bl.first < kv)
                         tma_load_4d(sRing + (uint32_t)slot * kTileBytes + bl.offset, which ? (const void *)&tm_v : (const void *)&tm_k, bar,
-                                    bl.half * 64, kvh, row, page);
+                                    bl.half * 64, kvh, at.row, page);
                     ++issued;
                 }
                 page = page_next;
+                at = at_next;
             }
         }
         // No more segments for either group.

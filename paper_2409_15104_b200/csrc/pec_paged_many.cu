@@ -63,56 +63,91 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, kvh = blockIdx.x % p.Hkv;
     const int tps = kTile / p.g, srows = tps * p.g;        // tokens and packed rows of a stage
 
+    // The loader warp reads the CTA's item, works out the geometry and starts the first loads (Q, K(0), V(0)) before the CTA-wide
+    // sync; meanwhile others set up the remaining barriers and the tensor memory.
+    const BoxLane bl = box_lane(box, lane);
+    const BoxStep step = box_step(p.c.page_size);
+    BoxPlace at = {0, 0};                                  // this lane's box of the next tile, and its page
+    int32_t page = 0;
+    bool found = false;
+    // This lane's box (if it is one to load) of K (which = 0) or V into the ring's slot.
+    auto load_tile = [&](int which, int slot, uint32_t bytes, bool mine) {
+        const uint32_t bar = smem_u32(&sh->kv_full[slot]);
+        if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
+        __syncwarp();
+        if (mine)
+            tma_load_4d(sRing + (uint32_t)slot * kTileBytes + bl.offset, which ? (const void *)&tm_v : (const void *)&tm_k, bar, bl.half * 64, kvh,
+                        at.row, page);
+    };
     if (warp == kLoadWarp) {
         // The kernel for few rows may start on SMs that this grid leaves.  The plan has to be complete before its list is read.
-        if (lane == 0) griddep_launch_dependents();
-        griddep_wait();
         if (lane == 0) {
-            const bool found = (int)(blockIdx.x / p.Hkv) < p.many_count[0];
-            Item it;
-            if (found) it = p.many_items[blockIdx.x / p.Hkv];
-            Geom g = {};
-            g.found = found;
-            if (found) {
-                const int32_t tok0 = it.block * 2 * tps;
-                g.b = it.b; g.kv = it.r.kv; g.key_lo = it.key_lo; g.key_hi = it.key_hi;
-                g.tok_row = it.r.start + tok0;
-                g.slices = it.slices;
-                g.slot = (int64_t)it.slot * p.Hkv + kvh;
+            griddep_launch_dependents();
+            sh->abort_flag = 0;
+            for (int st = 0; st < 2; ++st) mbar_init(smem_u32(&sh->bar_q[st]), 1);
+            for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&sh->kv_full[s]), 1); mbar_init(smem_u32(&sh->kv_empty[s]), 2); }
+        }
+        griddep_wait();
+        const Item it = p.many_items[blockIdx.x / p.Hkv];  // (inside the list's room, filled or not)
+        found = (int)(blockIdx.x / p.Hkv) < p.many_count[0];
+        Geom g = {};
+        if (found) {
+            const int32_t tok0 = it.block * 2 * tps;
+            g.b = it.b; g.kv = it.r.kv; g.key_lo = it.key_lo; g.key_hi = it.key_hi;
+            g.tok_row = it.r.start + tok0;
+            g.slices = it.slices;
+            g.slot = (int64_t)it.slot * p.Hkv + kvh;
 #pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    int32_t nt = it.r.n - tok0 - st * tps;
-                    nt = nt < 0 ? 0 : (nt > tps ? tps : nt);
-                    g.rows[st] = nt * p.g;
-                    g.pos0[st] = it.r.pos0() + tok0 + st * tps;
-                    int32_t end = it.key_hi;
-                    if (p.causal && end > g.pos0[st] + nt) end = g.pos0[st] + nt;
-                    g.n[st] = (nt > 0 && end > it.key_lo) ? (end - it.key_lo + kTile - 1) / kTile : 0;
-                }
-                g.n_max = g.n[0] > g.n[1] ? g.n[0] : g.n[1];
-                if (g.slices > 1 && g.slot >= p.many_cap) g.found = 0;     // cannot happen (see many_plan); never write past the scratch
+            for (int st = 0; st < 2; ++st) {
+                int32_t nt = it.r.n - tok0 - st * tps;
+                nt = nt < 0 ? 0 : (nt > tps ? tps : nt);
+                g.rows[st] = nt * p.g;
+                g.pos0[st] = it.r.pos0() + tok0 + st * tps;
+                int32_t end = it.key_hi;
+                if (p.causal && end > g.pos0[st] + nt) end = g.pos0[st] + nt;
+                g.n[st] = (nt > 0 && end > it.key_lo) ? (end - it.key_lo + kTile - 1) / kTile : 0;
             }
+            g.n_max = g.n[0] > g.n[1] ? g.n[0] : g.n[1];
+            if (g.slices > 1 && g.slot >= p.many_cap) found = false;       // cannot happen (see the plan); never write past the scratch
+        }
+        g.found = found;
+        if (lane == 0) {
             sh->g = g;
             // P is handed over by the warps that have rows only.  (Those without would run ahead: S(j + 1) may be complete before
             // P(j) is, and their arrivals for j + 1 would then complete phase j.)
             for (int st = 0; st < 2; ++st) mbar_init(smem_u32(&sh->p_ready[st]), g.rows[st] > 32 ? (uint32_t)(g.rows[st] + 31) / 32 : 1);
             mbar_init_fence();
         }
-    } else if (tid == 0) {
-        sh->abort_flag = 0;
+        __syncwarp();
+        if (found && g.n_max > 0) {
+
+            at = box_place(p.c.page_size, g.key_lo, bl);
+            page = box_page(p, g.b, g.key_lo, g.kv, bl, at);
+            if (lane == 0) {
+                // The second stage's tokens may lie past the request's, or past q (zero fill): those rows are not used.
+                for (int st = 0; st < 2; ++st) {
+                    const uint32_t bar = smem_u32(&sh->bar_q[st]), dst = sQ + st * kTileBytes;
+                    mbar_arrive_expect_tx(bar, (uint32_t)srows * 256u);
+                    tma_load_4d(dst, &tm_q, bar, 0, 0, kvh, g.tok_row + st * tps);
+                    tma_load_4d(dst + kHalfTileBytes, &tm_q, bar, 64, 0, kvh, g.tok_row + st * tps);
+                }
+            }
+            const uint32_t bytes = tile_bytes(g.key_lo, g.kv, box);
+            const bool mine = bl.used && g.key_lo + bl.first < g.kv;
+            load_tile(0, 0, bytes, mine);
+            load_tile(1, 1, bytes, mine);
+            at = box_next(at, step);
+            if (g.n_max > 1) page = box_page(p, g.b, g.key_lo + kTile, g.kv, bl, at);
+        }
+    } else if (tid == kMmaWarp0 * 32) {
         for (int st = 0; st < 2; ++st) {
-            mbar_init(smem_u32(&sh->bar_q[st]), 1);
             mbar_init(smem_u32(&sh->s_full[st]), 1);
             mbar_init(smem_u32(&sh->s_taken[st]), 4);      // one arrival per softmax warp
             mbar_init(smem_u32(&sh->pv_done[st]), 1);
         }
-        for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&sh->kv_full[s]), 1); mbar_init(smem_u32(&sh->kv_empty[s]), 2); }
         mbar_init_fence();
         prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
-    }
-    __syncthreads();
-    if (!sh->g.found) return;
-    if (warp == 4) {
+    } else if (warp == 4) {
         tmem_alloc(smem_u32(&sh->tmem_base), kTmemCols);
         tmem_relinquish();
     }
@@ -121,44 +156,35 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     tc_fence_after();
     const int n_max = sh->g.n_max;
     const uint32_t tmem = sh->tmem_base;
+    if (!sh->g.found) {
+        if (warp == 4) tmem_dealloc(tmem, kTmemCols);
+        return;
+    }
 
     if (warp == kLoadWarp) {
-        // ------------------------------------------------------------------ TMA loader (one box per lane)
+        // ------------------------------------------------------------------ TMA loader (one box per lane); tile 0 is under way
         reg_dealloc<kLightRegs>();
         if (n_max > 0) {
-            const BoxLane bl = box_lane(box, lane);
             const int32_t b = sh->g.b, kv = sh->g.kv;
-            int32_t k0 = sh->g.key_lo, page = box_page(p, b, k0, kv, bl);
-            if (lane == 0) {
-                // The second stage's tokens may lie past the request's, or past q (zero fill): those rows are not used.
-                for (int st = 0; st < 2; ++st) {
-                    const uint32_t bar = smem_u32(&sh->bar_q[st]), dst = sQ + st * kTileBytes;
-                    mbar_arrive_expect_tx(bar, (uint32_t)srows * 256u);
-                    tma_load_4d(dst, &tm_q, bar, 0, 0, kvh, sh->g.tok_row + st * tps);
-                    tma_load_4d(dst + kHalfTileBytes, &tm_q, bar, 64, 0, kvh, sh->g.tok_row + st * tps);
-                }
-            }
-            int issued = 0;
+            int32_t k0 = sh->g.key_lo + kTile;
+            int issued = 2;
             bool ok = true;
-            for (int j = 0; j < n_max && ok; ++j, k0 += kTile) {
-                const int32_t page_next = j + 1 < n_max ? box_page(p, b, k0 + kTile, kv, bl) : 0;
+            for (int j = 1; j < n_max && ok; ++j, k0 += kTile) {
+                const BoxPlace at_next = box_next(at, step);
+                const int32_t page_next = j + 1 < n_max ? box_page(p, b, k0 + kTile, kv, bl, at_next) : 0;
                 const uint32_t bytes = tile_bytes(k0, kv, box);
-                const int32_t row = (k0 + bl.first) % p.c.page_size;
+                const bool mine = bl.used && k0 + bl.first < kv;
 #pragma unroll
                 for (int which = 0; which < 2; ++which) {  // K, V
                     const int item = 2 * j + which, slot = item % kSlots, fill = item / kSlots;
-                    if (skip_last && n_max > 1 && item == 2 * n_max - 1) { ok = false; break; }   // test hook: the wait for it runs out
+                    if (skip_last && item == 2 * n_max - 1) { ok = false; break; }   // test hook: the wait for it runs out
                     if (fill > 0) ok = wait_all(&sh->kv_empty[slot], (fill - 1) & 1, sh, p);
                     if (!ok) break;
-                    const uint32_t bar = smem_u32(&sh->kv_full[slot]);
-                    if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
-                    __syncwarp();
-                    if (bl.used && k0 + bl.first < kv)
-                        tma_load_4d(sRing + (uint32_t)slot * kTileBytes + bl.offset, which ? (const void *)&tm_v : (const void *)&tm_k, bar,
-                                    bl.half * 64, kvh, row, page);
+                    load_tile(which, slot, bytes, mine);
                     ++issued;
                 }
                 page = page_next;
+                at = at_next;
             }
             if (!ok && lane == 0) {
                 // Given up: the copies under way must land before the CTA may leave (each wait with the usual limit).

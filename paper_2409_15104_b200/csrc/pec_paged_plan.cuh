@@ -20,8 +20,6 @@ namespace paged {
 
 constexpr int kKeyTile = 128;                 // keys per tile
 constexpr int kFewRows = 128;                 // packed rows of the few class
-constexpr int kMinSliceTiles = 2;             // shortest slice of the many class
-
 // Device-side description of one call, passed to the kernels by value.
 struct Params {
     const void *q, *k_pages, *v_pages;
@@ -44,6 +42,8 @@ struct Params {
     // many class: blocks of a request = ceil(n * blk_mul / blk_div)
     int32_t blk_mul, blk_div;
     int32_t many_ctas;                        // CTAs of the many class that run at a time
+    int32_t min_slice;                        // key tiles of the shortest slice
+    int32_t item_cost, merge_cost;            // start and end of a CTA, a slice's partial: 1/32 of a tile's time (see paged_plan_kernel)
     int32_t many_rows;                        // rows of a partial slot
     int32_t many_cap, items_cap;              // slots and items that the workspace holds
     float *many_o, *many_lse;
@@ -90,16 +90,6 @@ __device__ __forceinline__ int64_t warp_prefix(int64_t v, int lane)    // inclus
     return v;
 }
 
-// Tiles on the few class's line per KV head.  One converged warp.
-__device__ __forceinline__ int64_t few_tiles(const Params &p)
-{
-    int64_t few = 0;
-    for (int b = threadIdx.x & 31; b < p.c.B; b += 32) {
-        const Request r = load_request(p, b);
-        if (is_few(p, r)) few += r.tiles();
-    }
-    return warp_sum(few);
-}
 // Tiles per CTA.
 __device__ __forceinline__ int64_t few_piece(const Params &p, int64_t few)
 {
@@ -135,12 +125,22 @@ __device__ __forceinline__ void walk_group(const Params &p, Walk &w, int lane)
     w.mine.start = w.mine.n = w.mine.kv = 0;
     if (w.b0 + lane < p.c.B) w.mine = load_request(p, w.b0 + lane);
 }
-// To place `at` on the line (below its end).
+// Tiles on the line per KV head; leaves the walk's first group of requests in the lanes.
+__device__ __forceinline__ int64_t walk_tiles(const Params &p, Walk &w, int lane)
+{
+    int64_t few = 0;
+    for (w.b0 = (p.c.B - 1) & ~31; w.b0 >= 0; w.b0 -= 32) {
+        walk_group(p, w, lane);
+        if (is_few(p, w.mine)) few += w.mine.tiles();
+    }
+    return warp_sum(few);
+}
+// To place `at` on the line (below its end), from the state that walk_tiles leaves.
 __device__ __forceinline__ void walk_to(const Params &p, Walk &w, int64_t at, int lane)
 {
     int64_t before = 0;
     for (w.b0 = 0; w.b0 < p.c.B; w.b0 += 32) {
-        walk_group(p, w, lane);
+        if (w.b0 > 0) walk_group(p, w, lane);
         const int64_t len = is_few(p, w.mine) ? (int64_t)w.mine.tiles() * p.Hkv : 0, incl = warp_prefix(len, lane);
         const unsigned who = __ballot_sync(0xffffffffu, at >= before + incl - len && at < before + incl);
         if (who) {

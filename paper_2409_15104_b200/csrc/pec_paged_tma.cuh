@@ -34,21 +34,37 @@ __device__ __forceinline__ BoxLane box_lane(int box, int lane)
     l.offset = (uint32_t)l.half * kHalfTileBytes + (uint32_t)l.first * 128u;
     return l;
 }
+// Where this lane's box of a key tile lies: the number in the request's list of pages and the row of the page.  Walked from tile
+// to tile without divisions, which would sit between a free slot and its next load.
+struct BoxPlace { int32_t nth, row; };
+struct BoxStep { int32_t nth, row, page_size; };
+__device__ __forceinline__ BoxStep box_step(int32_t page_size) { return {kKeyTile / page_size, kKeyTile % page_size, page_size}; }
+__device__ __forceinline__ BoxPlace box_place(int32_t page_size, int32_t k0, const BoxLane &l)
+{
+    const int32_t nth = (k0 + l.first) / page_size;
+    return {nth, k0 + l.first - nth * page_size};
+}
+__device__ __forceinline__ BoxPlace box_next(const BoxPlace &b, const BoxStep &s)
+{
+    BoxPlace n = {b.nth + s.nth, b.row + s.row};
+    if (n.row >= s.page_size) { n.row -= s.page_size; ++n.nth; }
+    return n;
+}
 // Page of this lane's box of the key tile that begins at position k0 (0 where the box is not loaded, or the number is bad).
-__device__ __forceinline__ int32_t box_page(const Params &p, int b, int32_t k0, int32_t kv, const BoxLane &l)
+__device__ __forceinline__ int32_t box_page(const Params &p, int b, int32_t k0, int32_t kv, const BoxLane &l, const BoxPlace &at)
 {
     if (!l.used || k0 + l.first >= kv) return 0;
-    const int32_t page = __ldg(p.c.table + b * p.c.table_stride + (k0 + l.first) / p.c.page_size);
+    const int32_t page = __ldg(p.c.table + b * p.c.table_stride + at.nth);
     if (page >= 0 && page < p.c.num_pages) return page;
     raise_status(p.status, PEC_ERR_BAD_INDEX);
     return 0;
 }
-// Bytes of the tile's boxes that are loaded.
+// Bytes of the tile's boxes that are loaded (box is a power of two).
 __device__ __forceinline__ uint32_t tile_bytes(int32_t k0, int32_t kv, int box)
 {
     int32_t n = kv - k0;
     n = n < 0 ? 0 : (n > kKeyTile ? kKeyTile : n);
-    return (uint32_t)((n + box - 1) / box * box) * 256u;
+    return (uint32_t)((n + box - 1) & -box) * 256u;
 }
 // What a page holds past the request's end may be anything; 0 * NaN would reach every row's output.  The whole warp that issues
 // the product P V clears those rows of the V tile first (once per request: only its last tile has such rows).
