@@ -386,29 +386,41 @@ paged_simple_kernel(const Params p)
 // the grid has the size of what can be split, not of the batch.  (A CTA per token and KV head took 66 us to find nothing to do for
 // 2048 tokens.)  The few class looks its unit up before the attention kernels end (the tables were complete before they began);
 // partials are read afterwards, and no CTA ends before that wait, so that whatever follows on the stream follows those kernels too.
-// A warp merges one row at a time, a lane owning four channels: the largest LSE first, then the weighted sum.
+// A warp merges one row at a time, a lane owning four channels: the largest LSE first, then the weighted sum, sixteen partials'
+// loads in flight.
 constexpr int kCombineWarps = 8, kManyGroup = 32;
 
 __device__ __forceinline__ void combine_row(const Params &p, const float *po, const float *pl, int64_t at0, int64_t shift, int64_t step,
                                             int count, int64_t item, int lane)
 {
+    constexpr int kBatch = 16;                                    // partials' rows in flight
     auto place = [&](int s) { return at0 + s * step + (s == 0 ? shift : 0); };     // of partial s, in rows
-    float m = -INFINITY;
-    for (int s = lane; s < count; s += 32) m = fmaxf(m, pl[place(s)]);
+    float l = lane < count ? pl[place(lane)] : -INFINITY, m = l;   // lane s: the LSE of partial s of the current 32
+    for (int s = lane + 32; s < count; s += 32) m = fmaxf(m, pl[place(s)]);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     float tot = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (m != -INFINITY) {
-#pragma unroll 4
-        for (int s = 0; s < count; ++s) {
-            const int64_t at = place(s);
-            const float l = pl[at], w = (l == -INFINITY) ? 0.f : expf(l - m);
-            const float4 v = *reinterpret_cast<const float4 *>(po + at * kHeadDim + 4 * lane);
-            acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y); acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
-            tot += w;
+    for (int s0 = 0; s0 < count && m != -INFINITY; s0 += 32) {
+        if (s0 > 0) l = s0 + lane < count ? pl[place(s0 + lane)] : -INFINITY;
+        const float w = l == -INFINITY ? 0.f : expf(l - m);
+        tot += w;
+        for (int b = 0; b < 32 && s0 + b < count; b += kBatch) {
+            float4 v[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (s0 + b + i < count) v[i] = *reinterpret_cast<const float4 *>(po + place(s0 + b + i) * kHeadDim + 4 * lane);
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const float x = __shfl_sync(0xffffffffu, w, b + i);
+                acc.x = fmaf(x, v[i].x, acc.x); acc.y = fmaf(x, v[i].y, acc.y); acc.z = fmaf(x, v[i].z, acc.z); acc.w = fmaf(x, v[i].w, acc.w);
+            }
         }
     }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) tot += __shfl_xor_sync(0xffffffffu, tot, d);
     const float inv = tot > 0.f ? 1.f / tot : 0.f;
     acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
     if (p.o_is_bf16) {
@@ -421,7 +433,7 @@ __device__ __forceinline__ void combine_row(const Params &p, const float *po, co
     if (lane == 0) p.lse[item] = (m == -INFINITY) ? -INFINITY : m + logf(tot);
 }
 
-__global__ void __launch_bounds__(kCombineWarps * 32, 3)
+__global__ void __launch_bounds__(kCombineWarps * 32, 2)
 paged_combine_kernel(const Params p, const int few_groups, const int few_blocks, const int many_groups)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
