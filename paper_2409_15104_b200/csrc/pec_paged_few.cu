@@ -49,6 +49,7 @@ struct Shared {
     uint64_t kv_full[kSlots], kv_empty[kSlots];
     uint64_t s_full[2][2], p_ready[2][2];                  // [group][TMEM buffer]
     uint64_t pv_done[2], o_free[2];                        // [group]
+    uint64_t drained;
     Segment seg[2];
     int64_t first;                                         // this CTA's piece of the line
     int32_t count;
@@ -98,6 +99,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             mbar_init(smem_u32(&sh->o_free[g]), 4);
         }
         for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&sh->kv_full[s]), 1); mbar_init(smem_u32(&sh->kv_empty[s]), 1); }
+        mbar_init(smem_u32(&sh->drained), 1);
         mbar_init_fence();
         prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
     } else if (warp == 4) {
@@ -190,11 +192,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             if (ok && lane == 0) { sh->seg[g].tiles = 0; mbar_arrive(smem_u32(&sh->q_full[g])); }
         }
         if (!ok && lane == 0) {
-            // Given up: the copies under way must land before the CTA may leave (each wait with the usual limit).
-            auto landed = [&](uint64_t *bar, uint32_t parity) {
-                const long long t0 = clock64();
-                while (!mbar_try_wait_suspend(smem_u32(bar), parity, 2000u) && clock64() - t0 < p.wait_cycles) {}
-            };
+            // Given up: the copies under way must land before the CTA may leave.
+            auto landed = [&](uint64_t *bar, uint32_t parity) { wait_quietly(bar, parity, p); };
             for (uint32_t i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i) landed(&sh->kv_full[i % kSlots], (i / kSlots) & 1);
             for (uint32_t i = q_issued > 2 ? q_issued - 2 : 0; i < q_issued; ++i) landed(&sh->q_full[i & 1], (i >> 1) & 1);
         }
@@ -267,6 +266,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             cur = next;
             ++segs;
         }
+        if (!ok) drain_products(&sh->drained, leader, p);
         __syncwarp();
     } else if (warp > kLoadWarp) {
         reg_dealloc<kLightRegs>();

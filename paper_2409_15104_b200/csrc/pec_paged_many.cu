@@ -41,6 +41,7 @@ struct Shared {
     uint64_t kv_full[kSlots], kv_empty[kSlots];
     uint64_t s_full[2], s_taken[2], p_ready[2];            // [stage], one phase per key tile
     uint64_t pv_done[2];
+    uint64_t drained[2];
     Geom g;
     uint32_t tmem_base;
     volatile int abort_flag;
@@ -144,6 +145,7 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             mbar_init(smem_u32(&sh->s_full[st]), 1);
             mbar_init(smem_u32(&sh->s_taken[st]), 4);      // one arrival per softmax warp
             mbar_init(smem_u32(&sh->pv_done[st]), 1);
+            mbar_init(smem_u32(&sh->drained[st]), 1);
         }
         mbar_init_fence();
         prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
@@ -187,11 +189,8 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 at = at_next;
             }
             if (!ok && lane == 0) {
-                // Given up: the copies under way must land before the CTA may leave (each wait with the usual limit).
-                auto landed = [&](uint64_t *bar, uint32_t parity) {
-                    const long long t0 = clock64();
-                    while (!mbar_try_wait_suspend(smem_u32(bar), parity, 2000u) && clock64() - t0 < p.wait_cycles) {}
-                };
+                // Given up: the copies under way must land before the CTA may leave.
+                auto landed = [&](uint64_t *bar, uint32_t parity) { wait_quietly(bar, parity, p); };
                 landed(&sh->bar_q[0], 0); landed(&sh->bar_q[1], 0);
                 for (int i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i) landed(&sh->kv_full[i % kSlots], (i / kSlots) & 1);
             }
@@ -273,6 +272,7 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 }
                 kv_release(2 * j + 1);
             }
+            if (!ok) drain_products(&sh->drained[st], leader, p);
         }
         __syncwarp();
     } else if (warp > kMmaWarp1) {

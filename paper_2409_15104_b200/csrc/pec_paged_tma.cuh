@@ -79,6 +79,21 @@ __device__ __forceinline__ void clear_tail(uint32_t tile, int32_t valid, int lan
     __syncwarp();
 }
 
+// Ends of a CTA that gives up (a wait of its own or of an earlier CTA has run out): a wait with the usual limit that raises
+// nothing and does not look at the abort flag, for copies and products under way.
+__device__ __forceinline__ void wait_quietly(uint64_t *bar, uint32_t parity, const Params &p)
+{
+    const long long t0 = clock64();
+    while (!mbar_try_wait_suspend(smem_u32(bar), parity, 2000u) && clock64() - t0 < p.wait_cycles) {}
+}
+// Until the products that the calling warp's `leader` lane has issued are complete: tensor memory may not be given back before.
+__device__ __forceinline__ void drain_products(uint64_t *bar, bool leader, const Params &p)
+{
+    if (leader) tc_commit(smem_u32(bar));
+    __syncwarp();
+    wait_quietly(bar, 0, p);
+}
+
 namespace host_map {
 // bf16, 128-byte swizzle, rank 4.  Encoded for every call (well under a microsecond each).
 inline bool encode(CUtensorMap *map, const void *base, const uint64_t (&dims)[4], const int64_t (&strides)[3], const uint32_t (&box)[4])

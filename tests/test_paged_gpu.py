@@ -396,3 +396,101 @@ def test_calls_without_tokens(pec):
     pec.pec_paged_attn(q, kp, vp, table, dev([0, 0]), dev([20]), o=o)
     pec.check_status()
     assert (o == 7.0).all()
+
+
+def test_a_request_per_row_of_a_large_batch(pec):
+    """More requests than a warp, a plan group (256) or a block looks at once, of both classes, some empty, with room before the
+    first and after the last row."""
+    g = np.random.RandomState(4)
+    for B, pick in ((1500, [0, 1, 1, 2]), (300, [0, 1, 130, 200])):
+        n = [int(x) for x in g.choice(pick, B)]
+        kv = [m + int(x) for m, x in zip(n, g.choice([0, 1, 30, 200], B))]
+        kp, vp, table = ref.make_cache(B, kv, 16, 1, BF16, DEV)
+        cu = [c + 3 for c in ref.offsets(n)]                          # three rows that belong to no request
+        T = cu[-1] + 2
+        q = torch.randn((T, 1, 128), device=DEV).to(BF16)
+        o, lse = torch.full((T, 1, 128), 7.0, dtype=BF16, device=DEV), torch.full((T, 1), 7.0, device=DEV)
+        pec.pec_paged_attn(q, kp, vp, table, dev(cu), dev(kv), o=o, lse=lse)
+        pec.check_status()
+        for rows in (slice(0, 3), slice(cu[-1], T)):
+            assert (o[rows] == 7.0).all() and (lse[rows] == 7.0).all()
+        ref.check_attend(o, lse, ref.attend(q, kp, vp, table, cu, kv), BF16, f"{B} requests")
+        k, v = torch.randn((T, 1, 128), device=DEV).to(BF16), torch.randn((T, 1, 128), device=DEV).to(BF16)
+        pec.pec_kv_append(k, v, kp, vp, table, dev(cu), dev(kv))
+        pec.check_status()
+        last = [b for b in range(B) if n[b]][-1]
+        assert torch.equal(kp[int(table[last, (kv[last] - 1) // 16]), (kv[last] - 1) % 16], k[cu[last + 1] - 1])
+
+
+def test_two_calls_at_once(pec):
+    """Two batches on two streams with workspaces of their own, many times: the same bits as one after the other."""
+    cases = []
+    for seed, n, kv in ((51, [1] * 20, [700 + 31 * i for i in range(20)]), (52, [200, 1, 70], [900, 4000, 70])):
+        kp, vp, table = ref.make_cache(seed, kv, 16, 2, BF16, DEV)
+        q = torch.randn((sum(n), 8, 128), device=DEV).to(BF16)
+        args = (q, kp, vp, table, dev(ref.offsets(n)), dev(kv))
+        cases.append((args, max(n), pec.pec_paged_attn(*args, max_q_len=max(n))))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(20):
+        got = [pec.pec_paged_attn(*args, max_q_len=most, stream=s) for (args, most, _), s in zip(cases, streams)]
+        torch.cuda.synchronize()
+        for (_, _, want), have in zip(cases, got):
+            assert torch.equal(want[0], have[0]) and torch.equal(want[1], have[1])
+    pec.check_status()
+
+
+def test_requests_that_share_pages(pec):
+    """A common prefix in the same pages of two requests, each with its own last page."""
+    kp, vp, table = ref.make_cache(61, [333, 333], 16, 2, BF16, DEV)
+    table[1, :20] = table[0, :20]
+    for n in ([1, 1], [100, 13]):
+        q = torch.randn((sum(n), 8, 128), device=DEV).to(BF16)
+        cu = ref.offsets(n)
+        o, lse = pec.pec_paged_attn(q, kp, vp, table, dev(cu), dev([333, 333]), max_q_len=max(n))
+        pec.check_status()
+        ref.check_attend(o, lse, ref.attend(q, kp, vp, table, cu, [333, 333]), BF16, f"shared pages {n}")
+
+
+@pytest.mark.parametrize("page,total", [(1024, 5000), (65536, 70000), (512, 512), (8, 3000)])
+def test_page_sizes_and_a_cache_of_one_page(pec, page, total):
+    for n in (1, 140):
+        attend(pec, page + n, [n], [total], 4, 1, page, BF16, known=n == 1, what=f"pages of {page}, {n} new")
+
+
+def test_partials_of_two_caches_merge(pec):
+    """A long request's cache on two holders (Section 5.2): the new token's fp32 partials over either part, merged."""
+    kp, vp, table = ref.make_cache(71, [900, 500], 16, 2, BF16, DEV)
+    q = torch.randn((1, 8, 128), device=DEV).to(BF16)
+    parts = []
+    for b, kv in ((0, 900), (1, 500)):
+        parts.append(pec.pec_paged_attn(q, kp, vp, table[b:b + 1], dev([0, 1]), dev([kv]), max_q_len=1, causal=False, out_dtype=F32))
+    o, lse = pec.pec_attn_merge(*parts[0], *parts[1])
+    pec.check_status()
+    both = torch.cat([kp[table[0, :57].long()].reshape(-1, 2, 128)[:900], kp[table[1, :32].long()].reshape(-1, 2, 128)[:500]]).view(1, 1400, 2, 128)
+    bothv = torch.cat([vp[table[0, :57].long()].reshape(-1, 2, 128)[:900], vp[table[1, :32].long()].reshape(-1, 2, 128)[:500]]).view(1, 1400, 2, 128)
+    want = ref.attend(q, both, bothv, torch.zeros((1, 1), dtype=torch.int32), [0, 1], [1400])
+    ref.check_attend(o, lse, want, BF16, "two partials merged")
+
+
+@pytest.mark.parametrize("n,kv", [([1] * 40, [2500] * 40), ([300, 300], [2500, 2500])])
+def test_a_wait_that_runs_out_is_reported(pec, n, kv):
+    """The loader of each CTA leaves its last value tile out: the waits for it run out within the limit, the status word says so,
+    and the next launch is right."""
+    kp, vp, table = ref.make_cache(81, kv, 16, 2, BF16, DEV)
+    q = torch.randn((sum(n), 8, 128), device=DEV).to(BF16)
+    cu = ref.offsets(n)
+    args = (q, kp, vp, table, dev(cu), dev(kv))
+    try:
+        pec.pec_control(binding.PEC_CTL_WAIT_LIMIT_CYCLES, 4_000_000)
+        pec.pec_control(binding.PEC_CTL_TEST_SKIP_LAST_LOAD, 1)
+        pec.pec_paged_attn(*args, max_q_len=max(n))
+        with pytest.raises(binding.PecError) as e:
+            pec.check_status()
+        assert e.value.code == binding.PEC_ERR_TIMEOUT
+    finally:
+        pec.pec_control(binding.PEC_CTL_TEST_SKIP_LAST_LOAD, 0)
+        pec.pec_control(binding.PEC_CTL_WAIT_LIMIT_CYCLES, 2_000_000_000)
+    o, lse = pec.pec_paged_attn(*args, max_q_len=max(n))
+    pec.check_status()
+    ref.check_attend(o, lse, ref.attend(q, kp, vp, table, cu, kv), BF16, "after a wait that ran out")
