@@ -7,17 +7,26 @@
 // per piece for the combining kernel.  A unit's part in a piece is a "segment".
 //
 // Warp roles (three warpgroups):
-//   warps 0-3, 4-7  softmax and epilogue of even and odd segments (a thread = a packed row = a TMEM lane); with two groups the
-//                   epilogue of one segment runs beside the first tiles of the next.  Warps whose 32 rows are all past the
-//                   segment's rows only keep the barriers in step (they never look at PV's).
-//   warp 8          MMA issuer       warp 9  TMA loader: segment descriptors, Q (two buffers), K and V tiles (a ring of five)
-//   warps 10-11     idle (they complete the third warpgroup, which hands its registers over)
+//   warps 0-3, 4-7  softmax and epilogue of even and odd segments; with two groups the epilogue of one segment runs beside the
+//                   first tiles of the next
+//   warp 8          MMA issuer       warp 9  TMA loader: segment descriptors, Q (two buffers), K and V tiles (a ring)
+//   warps 10-11     idle
 // The loader runs through segment borders, so the stream from memory does not stop at them.
 //
-// Per tile: S(n) = Q K^T into one of two TMEM buffers; the softmax warps read their rows, and write P (bf16) over the same
-// buffer; O += P V.  The issuer's order S(n + 1), PV(n) has the next scores ready when the softmax comes back for them; S(n + 2)
-// may overwrite P(n) because the issuing thread's products execute in order.  O has one accumulator per group.
-// TMEM columns: S [0, 256), two buffers; O [256, 512), one per group.
+// Two forms of the products, by the number of packed rows that a request can have:
+//   wide    S = Q K^T and O = P V with the rows as the 128 rows of the product (a thread = a row = a TMEM lane; warps whose 32
+//           rows are all past the segment's only keep the barriers in step).  P (bf16) is written over S.
+//           TMEM columns: S [0, 256), two buffers; O [256, 512), one per group.
+//   narrow  up to 16 rows: S^T = K Q^T and O^T = V^T P^T with the rows as 16 columns (a thread = a key, then a channel).  A row's
+//           maximum and sum run across threads, but a tile costs 1/8 of the tensor work and 1/16 of the exponentials, and P
+//           goes through 4 KB of shared memory.  Not needed for the rate of a short run - the wide form streams 6.37 TB/s as
+//           well - but a long run of it draws the 1 kW limit, the SM clock falls to 1.5 GHz and the rate with it, to 5.55 TB/s
+//           (three requests of 131072 keys, 64 / 8 heads).
+//           TMEM columns: S^T [0, 32), two buffers; O^T [32, 64), one per group.
+//
+// Per tile: S(n) into one of two TMEM buffers, P(n) into its place or one of two shared buffers, O += P V.  The issuer's order
+// S(n + 1), PV(n) has the next scores ready when the softmax comes back for them; S(n + 2) may overwrite S(n) or P(n) because
+// the issuing thread's products execute in order.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -28,11 +37,17 @@ using namespace sm100;
 namespace paged {
 namespace few {
 
-constexpr int kSlots = 5;                                  // K/V ring
 constexpr int kThreads = 384;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kSpareWarp = 10;
 constexpr int kLightRegs = 56, kSoftmaxRegs = 224;         // 256 * 224 + 128 * 56 = 384 * 168 (the launch allocation)
-constexpr uint32_t kTmemCols = 512, kColO = 256;
+constexpr int kNarrowRows = 16;
+// Shared memory: two Q buffers (and two P buffers), then the ring.
+template <bool kNarrow> struct Cfg {
+    static constexpr int kSlots = kNarrow ? 6 : 5;
+    static constexpr uint32_t kHalfQ = kNarrow ? kNarrowRows * 128u : kHalfTileBytes, kQBytes = 2 * kHalfQ;   // 64 channels of the rows; both halves
+    static constexpr uint32_t kRing = kNarrow ? 4 * kQBytes : 2 * kQBytes;                                    // P buffers are as large as Q's
+    static constexpr uint32_t kTmemCols = kNarrow ? 64 : 512, kCols = kNarrow ? kNarrowRows : 128, kColO = 2 * kCols;
+};
 constexpr float kRescaleThreshold = 8.0f;                  // log2 units
 
 struct Segment {
@@ -46,17 +61,18 @@ struct Segment {
 
 struct Shared {
     uint64_t q_full[2], q_empty[2];                        // per group: descriptor and Q of its next segment
-    uint64_t kv_full[kSlots], kv_empty[kSlots];
+    uint64_t kv_full[6], kv_empty[6];
     uint64_t s_full[2][2], p_ready[2][2];                  // [group][TMEM buffer]
     uint64_t pv_done[2], o_free[2];                        // [group]
     uint64_t drained;
     Segment seg[2];
+    float red[2][4][kNarrowRows];                          // [group][warp][row]
     int64_t first;                                         // this CTA's piece of the line
     int32_t count;
     uint32_t tmem_base;
     volatile int abort_flag;
 };
-constexpr size_t kSmemBytes = (2 + kSlots) * kTileBytes + 1024 /*alignment slack*/ + sizeof(Shared);
+template <bool kNarrow> constexpr size_t smem_bytes() { return Cfg<kNarrow>::kRing + Cfg<kNarrow>::kSlots * kTileBytes + 1024 /*alignment slack*/ + sizeof(Shared); }
 
 __device__ __forceinline__ bool wait_bar(uint64_t *bar, uint32_t parity, Shared *sh, const Params &p)
 {
@@ -67,14 +83,88 @@ __device__ __forceinline__ bool wait_all(uint64_t *bar, uint32_t parity, Shared 
     return __all_sync(0xffffffffu, wait_bar(bar, parity, sh, p));
 }
 
+// Eight K steps of D (+)= A B as one statement: descriptors are the first one's plus constants (in 16-byte units).  kA: 0 = a
+// K-major 128-row tile whose second 64 channels lie kHalfTileBytes on; 1 = an M-major tile, 2048 bytes a step.  B: K-major, 16
+// rows, its second 64 columns 2048 bytes on.
+template <int kA>
+__device__ __forceinline__ void mma_narrow(uint32_t d, uint64_t a0, uint64_t b0, uint32_t idesc, uint32_t accumulate)
+{
+    constexpr int a1 = kA ? 128 : 2, a2 = kA ? 256 : 4, a3 = kA ? 384 : 6, h = kHalfTileBytes >> 4;
+    constexpr int a4 = kA ? 512 : h, a5 = kA ? 640 : h + 2, a6 = kA ? 768 : h + 4, a7 = kA ? 896 : h + 6;
+    asm volatile(
+        "{\n\t.reg .pred p0, pt;\n\t.reg .b64 da, db;\n\t"
+        "setp.ne.u32 p0, %4, 0;\n\t"
+        "setp.eq.u32 pt, %0, %0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p0;\n\t"
+        "add.s64 da, %1, %5;\n\tadd.s64 db, %2, 2;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, pt;\n\t"
+        "add.s64 da, %1, %6;\n\tadd.s64 db, %2, 4;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, pt;\n\t"
+        "add.s64 da, %1, %7;\n\tadd.s64 db, %2, 6;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, pt;\n\t"
+        "add.s64 da, %1, %8;\n\tadd.s64 db, %2, 128;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, pt;\n\t"
+        "add.s64 da, %1, %9;\n\tadd.s64 db, %2, 130;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, pt;\n\t"
+        "add.s64 da, %1, %10;\n\tadd.s64 db, %2, 132;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, pt;\n\t"
+        "add.s64 da, %1, %11;\n\tadd.s64 db, %2, 134;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, pt;\n\t}"
+        ::"r"(d), "l"(a0), "l"(b0), "r"(idesc), "r"(accumulate), "n"(a1), "n"(a2), "n"(a3), "n"(a4), "n"(a5), "n"(a6), "n"(a7) : "memory");
+}
+// 16 consecutive columns of this warp's 32 TMEM lanes, and back.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n\t"
+        "tcgen05.wait::st.sync.aligned;"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+// Barrier of the 128 threads of a softmax group that also tells whether any of them says so.  It has no limit of its own, so the
+// four warps of a group reach every one of them together: whether to go on is always decided by such a vote.
+__device__ __forceinline__ bool group_any(int g, bool say)
+{
+    uint32_t any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %2, 0;\n\t"
+        "barrier.cta.red.or.pred q, %1, 128, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(any) : "r"(1 + g), "r"((uint32_t)say) : "memory");
+    return any != 0;
+}
+// For each of 16 values the result over the warp's lanes; every lane gets all of them.
+template <class F>
+__device__ __forceinline__ void warp_reduce16(float (&x)[kNarrowRows], F f)
+{
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1)
+#pragma unroll
+        for (int c = 0; c < kNarrowRows; ++c) x[c] = f(x[c], __shfl_xor_sync(0xffffffffu, x[c], d));
+}
+
+template <bool kNarrow>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                  const __grid_constant__ CUtensorMap tm_v, const Params p, const int box, const int q_tokens, const int skip_last)
 {
+    typedef Cfg<kNarrow> C;
+    constexpr int kSlots = C::kSlots;
+    constexpr uint32_t kTmemCols = C::kTmemCols, kColO = C::kColO;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
-    const uint32_t sQ = (raw + 1023u) & ~1023u, sRing = sQ + 2 * kTileBytes;
-    Shared *sh = reinterpret_cast<Shared *>(smem_raw + (sQ - raw) + (2 + kSlots) * kTileBytes);
+    const uint32_t sQ = (raw + 1023u) & ~1023u, sRing = sQ + C::kRing;
+    Shared *sh = reinterpret_cast<Shared *>(smem_raw + (sQ - raw) + C::kRing + kSlots * kTileBytes);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     // The loader warp works out this CTA's piece of the line while others set up barriers and tensor memory.
@@ -119,7 +209,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 
     if (warp == kLoadWarp) {
         // ------------------------------------------------------------------ loader
-        reg_dealloc<kLightRegs>();
+        if (!kNarrow) reg_dealloc<kLightRegs>();
         const BoxLane bl = box_lane(box, lane);
         const int64_t first = sh->first, end = first + count;
         const BoxStep step = box_step(p.c.page_size);
@@ -146,10 +236,10 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 s.out = s.whole ? (int64_t)walk.r.start * p.Hq + (int64_t)walk.kvh * p.g
                                 : (2 * (int64_t)blockIdx.x + (walk.u0 > first ? 1 : 0)) * p.few_rows;
                 sh->seg[g] = s;
-                const uint32_t bar = smem_u32(&sh->q_full[g]), dst = sQ + (uint32_t)g * kTileBytes;
+                const uint32_t bar = smem_u32(&sh->q_full[g]), dst = sQ + (uint32_t)g * C::kQBytes;
                 mbar_arrive_expect_tx(bar, (uint32_t)(q_tokens * p.g) * 256u);
                 tma_load_4d(dst, &tm_q, bar, 0, 0, walk.kvh, walk.r.start);
-                tma_load_4d(dst + kHalfTileBytes, &tm_q, bar, 64, 0, walk.kvh, walk.r.start);
+                tma_load_4d(dst + C::kHalfQ, &tm_q, bar, 64, 0, walk.kvh, walk.r.start);
             }
             __syncwarp();
             ++segs; ++q_issued;
@@ -200,8 +290,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         __syncwarp();
     } else if (warp == kMmaWarp) {
         // ------------------------------------------------------------------ MMA issuer (the whole warp walks, one lane issues)
-        reg_dealloc<kLightRegs>();
+        if (!kNarrow) reg_dealloc<kLightRegs>();
         const bool leader = elect_one();
+        constexpr uint32_t narrow_qk = idesc_bf16_f32(128, kNarrowRows, 0, 0), narrow_pv = idesc_bf16_f32(kHeadDim, kNarrowRows, 1, 0);
         constexpr uint32_t idesc_qk = idesc_bf16_f32(128, 128, 0, 0), idesc_pv = idesc_bf16_f32(128, kHeadDim, 0, 1);
         constexpr uint32_t kBox16 = kHalfTileBytes >> 4;
         const uint64_t k_ring = smem_desc_sw128(sRing, 16, 1024), v_ring = smem_desc_sw128(sRing, kHalfTileBytes, 1024);
@@ -212,12 +303,17 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         auto issue_qk = [&](int n, int g, bool last) {
             if (!kv_wait(2 * n)) return false;
             if (leader) {
-                uint64_t a[8];
+                const uint64_t k0 = k_ring + (uint32_t)(((2 * n) % kSlots) * (kTileBytes >> 4));
+                if constexpr (kNarrow) {
+                    mma_narrow<0>(tmem + (uint32_t)(n & 1) * C::kCols, k0, smem_desc_sw128(sQ + (uint32_t)g * C::kQBytes, 16, 1024), narrow_qk, 0u);
+                    tc_commit(smem_u32(&sh->s_full[g][n & 1]));
+                } else {
+                    uint64_t a[8];
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                    a[ks] = smem_desc_sw128(sQ + (uint32_t)g * kTileBytes + (uint32_t)(ks >> 2) * kHalfTileBytes + (uint32_t)(ks & 3) * 32u, 16, 1024);
-                mma_ss_k128_commit<kBox16>(tmem + (uint32_t)(n & 1) * 128u, a, k_ring + (uint32_t)(((2 * n) % kSlots) * (kTileBytes >> 4)),
-                                           idesc_qk, smem_u32(&sh->s_full[g][n & 1]));
+                    for (int ks = 0; ks < 8; ++ks)
+                        a[ks] = smem_desc_sw128(sQ + (uint32_t)g * kTileBytes + (uint32_t)(ks >> 2) * kHalfTileBytes + (uint32_t)(ks & 3) * 32u, 16, 1024);
+                    mma_ss_k128_commit<kBox16>(tmem + (uint32_t)(n & 1) * C::kCols, a, k0, idesc_qk, smem_u32(&sh->s_full[g][n & 1]));
+                }
                 if (last) tc_commit(smem_u32(&sh->q_empty[g]));
             }
             kv_release(2 * n);
@@ -255,9 +351,13 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 tc_fence_after();
                 if (leader) {
                     const uint64_t v0 = v_ring + slot * (kTileBytes >> 4);
-                    const uint32_t tO = tmem + kColO + (uint32_t)g * 128u, tP = tmem + (uint32_t)(n & 1) * 128u;
-                    mma_ts_k64(tO, tP, v0, idesc_pv, j > 0 ? 1u : 0u);
-                    mma_ts_k64(tO, tP + 32, v0 + (64 * 128 >> 4), idesc_pv, 1u);
+                    const uint32_t tO = tmem + kColO + (uint32_t)g * C::kCols, tP = tmem + (uint32_t)(n & 1) * C::kCols;
+                    if constexpr (kNarrow) {
+                        mma_narrow<1>(tO, v0, smem_desc_sw128(sQ + (uint32_t)(2 + (n & 1)) * C::kQBytes, 16, 1024), narrow_pv, j > 0 ? 1u : 0u);
+                    } else {
+                        mma_ts_k64(tO, tP, v0, idesc_pv, j > 0 ? 1u : 0u);
+                        mma_ts_k64(tO, tP + 32, v0 + (64 * 128 >> 4), idesc_pv, 1u);
+                    }
                     tc_commit(smem_u32(&sh->pv_done[g]));
                 }
                 kv_release(2 * n + 1);
@@ -269,15 +369,147 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         if (!ok) drain_products(&sh->drained, leader, p);
         __syncwarp();
     } else if (warp > kLoadWarp) {
-        reg_dealloc<kLightRegs>();
+        if (!kNarrow) reg_dealloc<kLightRegs>();
         // An earlier CTA's wait has run out: the launch is lost, every wait of this CTA gives up at its next try.
         if (warp == kSpareWarp && lane == 0 && *reinterpret_cast<volatile int32_t *>(p.status) == PEC_ERR_TIMEOUT) sh->abort_flag = 1;
+    } else if constexpr (kNarrow) {
+        // ------------------------------------------------------------------ softmax and epilogue, narrow form
+        const int g = warp >> 2, quarter = warp & 3, key = quarter * 32 + lane;      // and channel `key` of the accumulator
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const uint32_t tO = tmem + lane_base + kColO + (uint32_t)g * C::kCols;
+        // P^T as the K-major operand: row c at 128 c, 64 keys a row (the second 64 in a second half), 16-byte chunks XOR-swizzled by row.
+        const uint32_t p_half = (uint32_t)(key >> 6) * C::kHalfQ + (uint32_t)(key & 7) * 2u, p_chunk = (uint32_t)(key & 63) >> 3;
+        uint32_t s_phase = 0, pv = 0;
+        for (int k = 0;; ++k) {
+            bool ok = wait_all(&sh->q_full[g], k & 1, sh, p);
+            if (group_any(g, !ok)) break;
+            const Segment s = sh->seg[g];
+            __syncwarp();
+            if (s.tiles == 0) break;
+            if (lane == 0) mbar_arrive(smem_u32(&sh->q_empty[g]));
+            const bool wide = s.rows > 8;                  // columns 8 - 15 are used
+            const int32_t see_all = (p.causal && s.pos0 + 1 < s.kv) ? s.pos0 + 1 : s.kv;           // keys below it are visible to every row
+            float m[kNarrowRows], l[kNarrowRows];          // per row: reference maximum (log2 units, the same in all threads), this thread's sum
+#pragma unroll
+            for (int c = 0; c < kNarrowRows; ++c) { m[c] = -INFINITY; l[c] = 0.f; }
+            int32_t k0 = s.key0;
+            bool stop = false;
+            for (int j = 0; j < s.tiles; ++j, k0 += kKeyTile) {
+                const int buf = (s.tile0 + j) & 1;
+                ok = wait_all(&sh->s_full[g][buf], (s_phase >> buf) & 1, sh, p);
+                s_phase ^= 1u << buf;
+                tc_fence_after();
+                uint32_t r[kNarrowRows];
+                tmem_ld16(tmem + lane_base + (uint32_t)buf * C::kCols, r);
+                tc_fence_before();
+                float x[kNarrowRows];
+#pragma unroll
+                for (int c = 0; c < kNarrowRows; ++c) x[c] = __uint_as_float(r[c]);
+                if (k0 + kKeyTile > see_all) {             // by choice, not by arithmetic: a masked score may be anything
+#pragma unroll
+                    for (int c = 0; c < kNarrowRows; ++c) {
+                        const int32_t see = p.causal ? min(s.kv, s.pos0 + c / p.g + 1) : s.kv;
+                        x[c] = k0 + key < see ? x[c] : -INFINITY;
+                    }
+                }
+                bool grow = false;
+#pragma unroll
+                for (int c = 0; c < kNarrowRows; ++c) {
+                    if (c < s.rows) grow = grow || x[c] * p.scale_log2 > m[c] + kRescaleThreshold;
+                }
+                // The reference maxima move only when one is outgrown by 2^8 (and from -inf); O then waits for its product in flight.
+                if (group_any(g, grow || !ok)) {
+                    if (j > 0 && ok) ok = wait_all(&sh->pv_done[g], (pv + j - 1) & 1, sh, p);
+                    stop = group_any(g, !ok);
+                    if (stop) break;
+                    float t[kNarrowRows];
+#pragma unroll
+                    for (int c = 0; c < kNarrowRows; ++c) t[c] = x[c];
+                    warp_reduce16(t, [](float a, float b) { return fmaxf(a, b); });
+                    if (lane < kNarrowRows) {
+                        float mine = t[0];
+#pragma unroll
+                        for (int c = 1; c < kNarrowRows; ++c) mine = lane == c ? t[c] : mine;
+                        sh->red[g][quarter][lane] = mine;
+                    }
+                    group_any(g, false);
+                    float alpha[kNarrowRows];
+#pragma unroll
+                    for (int c = 0; c < kNarrowRows; ++c) {
+                        const float top = fmaxf(fmaxf(sh->red[g][0][c], sh->red[g][1][c]), fmaxf(sh->red[g][2][c], sh->red[g][3][c])) * p.scale_log2;
+                        alpha[c] = 1.f;
+                        if (c < s.rows && top > m[c] + kRescaleThreshold) {
+                            alpha[c] = ex2(m[c] - top);    // 0 when the row had no key so far
+                            m[c] = top;
+                            l[c] *= alpha[c];
+                        }
+                    }
+                    group_any(g, false);                   // the exchange may be used again
+                    if (j > 0) {
+                        tc_fence_after();
+                        uint32_t o[kNarrowRows];
+                        tmem_ld16(tO, o);
+#pragma unroll
+                        for (int c = 0; c < kNarrowRows; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha[c]);
+                        tmem_st16(tO, o);
+                        tc_fence_before();
+                    }
+                } else if (j > 0) {
+                    // Waited for in every tile (see the wide form); what it says is voted on with the next tile.
+                    if (!wait_all(&sh->pv_done[g], (pv + j - 1) & 1, sh, p)) sh->abort_flag = 1;
+                }
+                // p = 2^(s scale - m), rounded to bf16 as the product's operand; the row's sum takes p before it is rounded.  S(n) is
+                // complete, and with it PV(n - 2), which read this P buffer.
+                const uint32_t dst = sQ + (uint32_t)(2 + buf) * C::kQBytes + p_half;
+#pragma unroll
+                for (int c = 0; c < kNarrowRows; ++c) {
+                    if (c < 8 || wide) {
+                        const float e = ex2(fmaf(x[c], p.scale_log2, m[c] == -INFINITY ? 0.f : -m[c]));
+                        l[c] += e;
+                        const __nv_bfloat16 h = __float2bfloat16_rn(e);
+                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(dst + (uint32_t)c * 128u + ((p_chunk ^ (uint32_t)(c & 7)) << 4)),
+                                     "h"(*reinterpret_cast<const unsigned short *>(&h)) : "memory");
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh->p_ready[g][buf]));
+            }
+            if (stop) break;
+            pv += s.tiles;
+            ok = wait_all(&sh->pv_done[g], (pv - 1) & 1, sh, p);
+            warp_reduce16(l, [](float a, float b) { return a + b; });
+            if (lane < kNarrowRows) {
+                float mine = l[0];
+#pragma unroll
+                for (int c = 1; c < kNarrowRows; ++c) mine = lane == c ? l[c] : mine;
+                sh->red[g][quarter][lane] = mine;
+            }
+            if (group_any(g, !ok)) break;
+            tc_fence_after();
+            uint32_t o[kNarrowRows];
+            tmem_ld16(tO, o);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->o_free[g]));
+#pragma unroll
+            for (int c = 0; c < kNarrowRows; ++c) {
+                if (c >= s.rows) continue;
+                const float sum = (sh->red[g][0][c] + sh->red[g][1][c]) + (sh->red[g][2][c] + sh->red[g][3][c]);
+                const float f = sum == 0.f ? 0.f : __uint_as_float(o[c]) * (1.f / sum);
+                const int64_t at = s.whole ? s.out + (int64_t)(c / p.g) * p.Hq + c % p.g : s.out + c;
+                if (s.whole && p.o_is_bf16) static_cast<__nv_bfloat16 *>(p.o)[at * kHeadDim + key] = __float2bfloat16_rn(f);
+                else (s.whole ? static_cast<float *>(p.o) : p.few_o)[at * kHeadDim + key] = f;
+                if (key == 0) (s.whole ? p.lse : p.few_lse)[at] = sum == 0.f ? -INFINITY : m[c] * 0.6931471805599453f + logf(sum);
+            }
+            if (group_any(g, false)) break;                // the exchange may be used again
+        }
     } else {
-        // ------------------------------------------------------------------ softmax and epilogue
+        // ------------------------------------------------------------------ softmax and epilogue, wide form
         reg_alloc<kSoftmaxRegs>();
         const int g = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
-        const uint32_t tO = tmem + lane_base + kColO + (uint32_t)g * 128u;
+        const uint32_t tO = tmem + lane_base + kColO + (uint32_t)g * C::kCols;
         const int32_t tok = row / p.g, head = row - tok * p.g;
         uint32_t s_phase = 0;                              // bit: parity of the buffer's next s_full
         uint32_t pv = 0;                                   // the group's PV products before this segment
@@ -295,7 +527,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             int32_t k0 = s.key0;
             for (int j = 0; j < s.tiles; ++j, k0 += kKeyTile) {
                 const int buf = (s.tile0 + j) & 1;
-                const uint32_t tS = tmem + lane_base + (uint32_t)buf * 128u;
+                const uint32_t tS = tmem + lane_base + (uint32_t)buf * C::kCols;
                 ok = wait_all(&sh->s_full[g][buf], (s_phase >> buf) & 1, sh, p);
                 if (!ok) break;
                 s_phase ^= 1u << buf;
@@ -433,15 +665,21 @@ int launch_paged_few(const paged::Params &p, bool after_many, cudaStream_t strea
     static std::mutex ready_mutex;
     if (!host::once_per_device(ready, ready_mutex, [] {
             cudaFuncAttributes attr;
-            return cudaFuncSetAttribute(few::paged_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few::kSmemBytes) == cudaSuccess &&
-                   cudaFuncGetAttributes(&attr, few::paged_few_kernel) == cudaSuccess &&
+            return cudaFuncSetAttribute(few::paged_few_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few::smem_bytes<true>()) == cudaSuccess &&
+                   cudaFuncSetAttribute(few::paged_few_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few::smem_bytes<false>()) == cudaSuccess &&
+                   cudaFuncGetAttributes(&attr, few::paged_few_kernel<false>) == cudaSuccess &&
                    attr.numRegs * few::kThreads >= 256 * few::kSoftmaxRegs + 128 * few::kLightRegs; })) {
         (void)cudaGetLastError();
         set_error("pec_paged_attn: kernel set-up failed (shared-memory limit, or the register allocation does not cover the warp-role split)");
         return PEC_ERR_CUDA;
     }
-    cudaError_t err = launch_dependent(few::paged_few_kernel, dim3((unsigned)p.few_ctas), few::kThreads, few::kSmemBytes, stream, after_many,
-                                       tm_q, tm_k, tm_v, p, box, q_tokens, (int)test_skip_last_load());
+    // The narrow form where no request can have more than 16 rows (p.few_rows is the most any can have).
+    const dim3 grid((unsigned)p.few_ctas);
+    const int skip = test_skip_last_load();
+    cudaError_t err =
+        p.few_rows <= few::kNarrowRows
+            ? launch_dependent(few::paged_few_kernel<true>, grid, few::kThreads, few::smem_bytes<true>(), stream, after_many, tm_q, tm_k, tm_v, p, box, q_tokens, skip)
+            : launch_dependent(few::paged_few_kernel<false>, grid, few::kThreads, few::smem_bytes<false>(), stream, after_many, tm_q, tm_k, tm_v, p, box, q_tokens, skip);
     if (err == cudaSuccess) err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
