@@ -438,18 +438,17 @@ paged_combine_kernel(const Params p, const int few_groups, const int few_blocks,
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((int)blockIdx.x < few_blocks) {
-        const int64_t cut = blockIdx.x / few_groups + 1;
+        const int32_t cut = blockIdx.x / few_groups + 1;
         const int group = blockIdx.x % few_groups;
         Walk w;
-        const int64_t all = walk_tiles(p, w, lane), piece = few_piece(p, all), at = cut * piece;
+        const int32_t all = walk_tiles(p, w, lane), piece = few_piece(p, all), at = cut * piece;   // few_ctas * 2^23 at most
         w.u0 = at;
-        if (at < all * p.Hkv) walk_to(p, w, at, lane);
+        if (at < all) walk_to(p, w, at, lane);
         const bool mine = w.u0 < at && w.u0 >= at - piece;       // else the cut falls between units, or is not the unit's first
         asm volatile("griddepcontrol.wait;" ::: "memory");
         if (!mine) return;
-        const int64_t u1 = w.u0 + w.r.tiles();
         const int64_t first = cut - 1;                           // piece with the unit's first tiles
-        const int count = (int)((u1 - 1) / piece - first) + 1;
+        const int count = (w.u0 + w.r.tiles() - 1) / piece - (cut - 1) + 1;
         for (int row = group * kCombineWarps + warp; row < w.r.n * p.g; row += few_groups * kCombineWarps) {
             const int64_t item = (int64_t)(w.r.start + row / p.g) * p.Hq + w.kvh * p.g + row % p.g;
             combine_row(p, p.few_o, p.few_lse, 2 * first * p.few_rows + row, w.u0 > first * piece ? p.few_rows : 0, 2 * (int64_t)p.few_rows,

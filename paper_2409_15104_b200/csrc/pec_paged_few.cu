@@ -66,9 +66,8 @@ struct Shared {
     uint64_t pv_done[2], o_free[2];                        // [group]
     uint64_t drained;
     Segment seg[2];
-    float red[2][4][kNarrowRows];                          // [group][warp][row]
-    int64_t first;                                         // this CTA's piece of the line
-    int32_t count;
+    float4 red[2][2][kNarrowRows];                         // [group][every other exchange][row], one component per warp
+    int32_t count;                                         // tiles of this CTA's piece of the line
     uint32_t tmem_base;
     volatile int abort_flag;
 };
@@ -143,14 +142,23 @@ __device__ __forceinline__ bool group_any(int g, bool say)
         : "=r"(any) : "r"(1 + g), "r"((uint32_t)say) : "memory");
     return any != 0;
 }
-// For each of 16 values the result over the warp's lanes; every lane gets all of them.
+// Lane c (and c + 16) gets the result over the warp's lanes of value c: each step halves the values a lane is in charge of.
 template <class F>
-__device__ __forceinline__ void warp_reduce16(float (&x)[kNarrowRows], F f)
+__device__ __forceinline__ float warp_reduce16(const float (&x)[kNarrowRows], int lane, F f)
 {
+    float y[kNarrowRows];
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1)
+    for (int c = 0; c < kNarrowRows; ++c) y[c] = x[c];
 #pragma unroll
-        for (int c = 0; c < kNarrowRows; ++c) x[c] = f(x[c], __shfl_xor_sync(0xffffffffu, x[c], d));
+    for (int d = 8; d > 0; d >>= 1) {
+        const bool upper = lane & d;
+#pragma unroll
+        for (int i = 0; i < d; ++i) {
+            const float keep = upper ? y[i + d] : y[i], send = upper ? y[i] : y[i + d];
+            y[i] = f(keep, __shfl_xor_sync(0xffffffffu, send, d));
+        }
+    }
+    return f(y[0], __shfl_xor_sync(0xffffffffu, y[0], 16));
 }
 
 template <bool kNarrow>
@@ -167,51 +175,63 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     Shared *sh = reinterpret_cast<Shared *>(smem_raw + (sQ - raw) + C::kRing + kSlots * kTileBytes);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
-    // The loader warp works out this CTA's piece of the line while others set up barriers and tensor memory.
+    // The loader warp sets up the barriers and works out this CTA's piece of the line; it does not wait for the tensor memory and
+    // goes on to the first loads while the others gather.
     Walk walk;
+    int32_t first = 0, n_tiles = 0;
     if (warp == kLoadWarp) {
-        if (lane == 0) griddep_launch_dependents();        // the combining kernel may be launched; it waits for this one's end
-        const int64_t all = walk_tiles(p, walk, lane), piece = few_piece(p, all), first = blockIdx.x * piece;
-        const int64_t count = all * p.Hkv - first;
-        const int32_t n = (int32_t)(count < 0 ? 0 : (count < piece ? count : piece));
-        if (n > 0) walk_to(p, walk, first, lane);
-        if (lane == 0) { sh->first = first; sh->count = n; }
-    } else if (tid == 0) {
-        sh->abort_flag = 0;
-        for (int g = 0; g < 2; ++g) {
-            mbar_init(smem_u32(&sh->q_full[g]), 1);
-            mbar_init(smem_u32(&sh->q_empty[g]), 5);       // four softmax warps, the issuer's commit
-            for (int i = 0; i < 2; ++i) {
-                mbar_init(smem_u32(&sh->s_full[g][i]), 1);
-                mbar_init(smem_u32(&sh->p_ready[g][i]), 4);
+        if (lane == 0) {
+            griddep_launch_dependents();                   // the combining kernel may be launched; it waits for this one's end
+            sh->abort_flag = 0;
+            for (int g = 0; g < 2; ++g) {
+                mbar_init(smem_u32(&sh->q_full[g]), 1);
+                mbar_init(smem_u32(&sh->q_empty[g]), 5);   // four softmax warps, the issuer's commit
+                for (int i = 0; i < 2; ++i) {
+                    mbar_init(smem_u32(&sh->s_full[g][i]), 1);
+                    mbar_init(smem_u32(&sh->p_ready[g][i]), 4);
+                }
+                mbar_init(smem_u32(&sh->pv_done[g]), 1);
+                mbar_init(smem_u32(&sh->o_free[g]), 4);
             }
-            mbar_init(smem_u32(&sh->pv_done[g]), 1);
-            mbar_init(smem_u32(&sh->o_free[g]), 4);
+            for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&sh->kv_full[s]), 1); mbar_init(smem_u32(&sh->kv_empty[s]), 1); }
+            mbar_init(smem_u32(&sh->drained), 1);
+            mbar_init_fence();
         }
-        for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&sh->kv_full[s]), 1); mbar_init(smem_u32(&sh->kv_empty[s]), 1); }
-        mbar_init(smem_u32(&sh->drained), 1);
-        mbar_init_fence();
-        prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
-    } else if (warp == 4) {
-        tmem_alloc(smem_u32(&sh->tmem_base), kTmemCols);
-        tmem_relinquish();
+        const int32_t all = walk_tiles(p, walk, lane), piece = few_piece(p, all);
+        first = (int32_t)blockIdx.x * piece;
+        n_tiles = min(max(all - first, 0), piece);
+        if (n_tiles > 0) walk_to(p, walk, first, lane);
+        if (lane == 0) sh->count = n_tiles;
+        __syncwarp();
+        asm volatile("barrier.cta.arrive 3, %0;" ::"n"(kThreads) : "memory");
+        if (n_tiles == 0) {
+            griddep_wait();
+            return;
+        }
+    } else {
+        if (warp == 4) {
+            tmem_alloc(smem_u32(&sh->tmem_base), kTmemCols);
+            tmem_relinquish();
+        } else if (tid == 0) {
+            prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
+        }
+        tc_fence_before();
+        asm volatile("barrier.cta.sync 3, %0;" ::"n"(kThreads) : "memory");
+        tc_fence_after();
+        n_tiles = sh->count;
+        if (n_tiles == 0) {
+            if (warp == 4) tmem_dealloc(sh->tmem_base, kTmemCols);
+            return;
+        }
     }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    const int32_t count = sh->count;
-    const uint32_t tmem = sh->tmem_base;
-    if (count == 0) {
-        if (warp == 4) tmem_dealloc(tmem, kTmemCols);
-        griddep_wait();
-        return;
-    }
+    const int32_t count = n_tiles;
+    const uint32_t tmem = warp == kLoadWarp ? 0 : sh->tmem_base;
 
     if (warp == kLoadWarp) {
         // ------------------------------------------------------------------ loader
         if (!kNarrow) reg_dealloc<kLightRegs>();
         const BoxLane bl = box_lane(box, lane);
-        const int64_t first = sh->first, end = first + count;
+        const int32_t end = first + count;
         const BoxStep step = box_step(p.c.page_size);
         BoxPlace at = box_place(p.c.page_size, walk.tile * kKeyTile, bl);      // this lane's box of the current tile, and its page
         int32_t page = box_page(p, walk.b, walk.tile * kKeyTile, walk.r.kv, bl, at);
@@ -221,9 +241,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         while (n < count && ok) {
             // a segment: descriptor and Q
             const int g = segs & 1;
-            const int64_t lo = walk.u0 > first ? walk.u0 : first;
-            const int64_t hi = walk.u0 + walk.r.tiles() < end ? walk.u0 + walk.r.tiles() : end;
-            const int32_t tiles = (int32_t)(hi - lo);
+            const int32_t tiles = min(walk.u0 + walk.r.tiles(), end) - max(walk.u0, first);
             if (segs >= 2) ok = wait_all(&sh->q_empty[g], ((segs >> 1) - 1) & 1, sh, p);
             if (!ok) break;
             if (lane == 0) {
@@ -380,6 +398,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         // P^T as the K-major operand: row c at 128 c, 64 keys a row (the second 64 in a second half), 16-byte chunks XOR-swizzled by row.
         const uint32_t p_half = (uint32_t)(key >> 6) * C::kHalfQ + (uint32_t)(key & 7) * 2u, p_chunk = (uint32_t)(key & 63) >> 3;
         uint32_t s_phase = 0, pv = 0;
+        // Exchanges between the group's warps take turns in two buffers: whoever writes one has passed the vote of the exchange
+        // after its last use, which its readers reached after reading.
+        int turn = 0;
         for (int k = 0;; ++k) {
             bool ok = wait_all(&sh->q_full[g], k & 1, sh, p);
             if (group_any(g, !ok)) break;
@@ -392,6 +413,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             float m[kNarrowRows], l[kNarrowRows];          // per row: reference maximum (log2 units, the same in all threads), this thread's sum
 #pragma unroll
             for (int c = 0; c < kNarrowRows; ++c) { m[c] = -INFINITY; l[c] = 0.f; }
+            float m_row = -INFINITY;                       // m of row lane % 16
             int32_t k0 = s.key0;
             bool stop = false;
             for (int j = 0; j < s.tiles; ++j, k0 += kKeyTile) {
@@ -418,33 +440,31 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     if (c < s.rows) grow = grow || x[c] * p.scale_log2 > m[c] + kRescaleThreshold;
                 }
                 // The reference maxima move only when one is outgrown by 2^8 (and from -inf); O then waits for its product in flight.
-                if (group_any(g, grow || !ok)) {
+                if (j == 0 || group_any(g, grow || !ok)) {
                     if (j > 0 && ok) ok = wait_all(&sh->pv_done[g], (pv + j - 1) & 1, sh, p);
                     stop = group_any(g, !ok);
                     if (stop) break;
-                    float t[kNarrowRows];
-#pragma unroll
-                    for (int c = 0; c < kNarrowRows; ++c) t[c] = x[c];
-                    warp_reduce16(t, [](float a, float b) { return fmaxf(a, b); });
-                    if (lane < kNarrowRows) {
-                        float mine = t[0];
-#pragma unroll
-                        for (int c = 1; c < kNarrowRows; ++c) mine = lane == c ? t[c] : mine;
-                        sh->red[g][quarter][lane] = mine;
-                    }
+                    const float most = warp_reduce16(x, lane, [](float a, float b) { return fmaxf(a, b); });
+                    float4 *red = sh->red[g][turn ^= 1];
+                    if (lane < kNarrowRows) reinterpret_cast<float *>(red + lane)[quarter] = most;
                     group_any(g, false);
+                    // Lane c works out row c's new reference; the others get it by shuffle.
+                    const float4 t = red[lane & (kNarrowRows - 1)];
+                    const float top = fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w)) * p.scale_log2;
+                    const bool move = (lane & (kNarrowRows - 1)) < s.rows && top > m_row + kRescaleThreshold;
+                    const float a_row = move ? ex2(m_row - top) : 1.f;     // 0 when the row had no key so far
+                    if (move) m_row = top;
                     float alpha[kNarrowRows];
 #pragma unroll
                     for (int c = 0; c < kNarrowRows; ++c) {
-                        const float top = fmaxf(fmaxf(sh->red[g][0][c], sh->red[g][1][c]), fmaxf(sh->red[g][2][c], sh->red[g][3][c])) * p.scale_log2;
-                        alpha[c] = 1.f;
-                        if (c < s.rows && top > m[c] + kRescaleThreshold) {
-                            alpha[c] = ex2(m[c] - top);    // 0 when the row had no key so far
-                            m[c] = top;
+                        if (c < 8 || wide) {
+                            m[c] = __shfl_sync(0xffffffffu, m_row, c);
+                            alpha[c] = __shfl_sync(0xffffffffu, a_row, c);
                             l[c] *= alpha[c];
+                        } else {
+                            alpha[c] = 1.f;
                         }
                     }
-                    group_any(g, false);                   // the exchange may be used again
                     if (j > 0) {
                         tc_fence_after();
                         uint32_t o[kNarrowRows];
@@ -478,13 +498,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             if (stop) break;
             pv += s.tiles;
             ok = wait_all(&sh->pv_done[g], (pv - 1) & 1, sh, p);
-            warp_reduce16(l, [](float a, float b) { return a + b; });
-            if (lane < kNarrowRows) {
-                float mine = l[0];
-#pragma unroll
-                for (int c = 1; c < kNarrowRows; ++c) mine = lane == c ? l[c] : mine;
-                sh->red[g][quarter][lane] = mine;
-            }
+            const float part = warp_reduce16(l, lane, [](float a, float b) { return a + b; });
+            float4 *red = sh->red[g][turn ^= 1];
+            if (lane < kNarrowRows) reinterpret_cast<float *>(red + lane)[quarter] = part;
             if (group_any(g, !ok)) break;
             tc_fence_after();
             uint32_t o[kNarrowRows];
@@ -492,17 +508,23 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->o_free[g]));
+            // Lane c works out row c's factor, place and LSE.
+            const int row = lane & (kNarrowRows - 1);
+            const float4 t = red[row];
+            const float sum = (t.x + t.y) + (t.z + t.w);
+            const int64_t at = s.whole ? s.out + (int64_t)(row / p.g) * p.Hq + row % p.g : s.out + row;
+            const float f_row = sum == 0.f ? 0.f : 1.f / sum;
+            if (quarter == 0 && lane < s.rows && lane < kNarrowRows)
+                (s.whole ? p.lse : p.few_lse)[at] = sum == 0.f ? -INFINITY : m_row * 0.6931471805599453f + logf(sum);
 #pragma unroll
             for (int c = 0; c < kNarrowRows; ++c) {
-                if (c >= s.rows) continue;
-                const float sum = (sh->red[g][0][c] + sh->red[g][1][c]) + (sh->red[g][2][c] + sh->red[g][3][c]);
-                const float f = sum == 0.f ? 0.f : __uint_as_float(o[c]) * (1.f / sum);
-                const int64_t at = s.whole ? s.out + (int64_t)(c / p.g) * p.Hq + c % p.g : s.out + c;
-                if (s.whole && p.o_is_bf16) static_cast<__nv_bfloat16 *>(p.o)[at * kHeadDim + key] = __float2bfloat16_rn(f);
-                else (s.whole ? static_cast<float *>(p.o) : p.few_o)[at * kHeadDim + key] = f;
-                if (key == 0) (s.whole ? p.lse : p.few_lse)[at] = sum == 0.f ? -INFINITY : m[c] * 0.6931471805599453f + logf(sum);
+                if (c >= s.rows) break;
+                const float f = __shfl_sync(0xffffffffu, f_row, c);
+                const int64_t to = __shfl_sync(0xffffffffu, at, c) * kHeadDim + key;
+                const float y = f == 0.f ? 0.f : __uint_as_float(o[c]) * f;
+                if (s.whole && p.o_is_bf16) static_cast<__nv_bfloat16 *>(p.o)[to] = __float2bfloat16_rn(y);
+                else (s.whole ? static_cast<float *>(p.o) : p.few_o)[to] = y;
             }
-            if (group_any(g, false)) break;                // the exchange may be used again
         }
     } else {
         // ------------------------------------------------------------------ softmax and epilogue, wide form

@@ -90,13 +90,6 @@ __device__ __forceinline__ int64_t warp_prefix(int64_t v, int lane)    // inclus
     return v;
 }
 
-// Tiles per CTA.
-__device__ __forceinline__ int64_t few_piece(const Params &p, int64_t few)
-{
-    const int64_t all = few * p.Hkv;
-    return all > 0 ? (all + p.few_ctas - 1) / p.few_ctas : 1;
-}
-
 // One item of the many class: rows of one request's block against one slice of its keys, for every KV head.
 struct __align__(16) Item {
     Request r;
@@ -106,13 +99,23 @@ struct __align__(16) Item {
     int32_t pad[3];
 };
 
-// A warp's walk along the few class's line.  The 32 requests around the current one sit in the lanes' registers.
+// A warp's walk along the few class's line.  The 32 requests around the current one sit in the lanes' registers.  Places on the
+// line fit in 32 bits (walk_tiles).
 struct Walk {
     int32_t b0, b;                                         // first request of the lanes' group; current request
     Request mine, r;                                       // this lane's, the current one
     int32_t kvh, tile;                                     // current KV head and tile of the request
-    int64_t u0;                                            // the unit's first tile on the line
+    int32_t u0;                                            // the unit's first tile on the line
 };
+__device__ __forceinline__ int32_t warp_prefix32(int32_t v, int lane)    // inclusive
+{
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t up = __shfl_up_sync(0xffffffffu, v, d);
+        if (lane >= d) v += up;
+    }
+    return v;
+}
 __device__ __forceinline__ void walk_take(Walk &w, int src)
 {
     w.b = w.b0 + src;
@@ -125,34 +128,42 @@ __device__ __forceinline__ void walk_group(const Params &p, Walk &w, int lane)
     w.mine.start = w.mine.n = w.mine.kv = 0;
     if (w.b0 + lane < p.c.B) w.mine = load_request(p, w.b0 + lane);
 }
-// Tiles on the line per KV head; leaves the walk's first group of requests in the lanes.
-__device__ __forceinline__ int64_t walk_tiles(const Params &p, Walk &w, int lane)
+// Tiles of the whole line; leaves the walk's first group of requests in the lanes.  A batch of 2^30 tiles or more (a tile of one
+// head is 64 KB: no cache holds as much, but requests may share pages) is reported and given none.
+__device__ __forceinline__ int32_t walk_tiles(const Params &p, Walk &w, int lane)
 {
     int64_t few = 0;
     for (w.b0 = (p.c.B - 1) & ~31; w.b0 >= 0; w.b0 -= 32) {
         walk_group(p, w, lane);
         if (is_few(p, w.mine)) few += w.mine.tiles();
     }
-    return warp_sum(few);
+    few = warp_sum(few) * p.Hkv;
+    if (few >= 1 << 30) {
+        raise_status(p.status, PEC_ERR_BAD_INDEX);
+        few = 0;
+    }
+    return (int32_t)few;
 }
+// Tiles per CTA.
+__device__ __forceinline__ int32_t few_piece(const Params &p, int32_t all) { return all > 0 ? (all + p.few_ctas - 1) / p.few_ctas : 1; }
 // To place `at` on the line (below its end), from the state that walk_tiles leaves.
-__device__ __forceinline__ void walk_to(const Params &p, Walk &w, int64_t at, int lane)
+__device__ __forceinline__ void walk_to(const Params &p, Walk &w, int32_t at, int lane)
 {
-    int64_t before = 0;
+    int32_t before = 0;
     for (w.b0 = 0; w.b0 < p.c.B; w.b0 += 32) {
         if (w.b0 > 0) walk_group(p, w, lane);
-        const int64_t len = is_few(p, w.mine) ? (int64_t)w.mine.tiles() * p.Hkv : 0, incl = warp_prefix(len, lane);
-        const unsigned who = __ballot_sync(0xffffffffu, at >= before + incl - len && at < before + incl);
+        const int32_t len = is_few(p, w.mine) ? w.mine.tiles() * p.Hkv : 0, end = before + warp_prefix32(len, lane);
+        const unsigned who = __ballot_sync(0xffffffffu, at >= end - len && at < end);
         if (who) {
             const int src = __ffs(who) - 1;
             walk_take(w, src);
-            const int64_t off = at - __shfl_sync(0xffffffffu, before + incl - len, src);
-            w.kvh = (int32_t)(off / w.r.tiles());
-            w.tile = (int32_t)(off % w.r.tiles());
+            const int32_t off = at - __shfl_sync(0xffffffffu, end - len, src), t = w.r.tiles();
+            w.kvh = off / t;
+            w.tile = off - w.kvh * t;
             w.u0 = at - w.tile;
             return;
         }
-        before += __shfl_sync(0xffffffffu, incl, 31);
+        before = __shfl_sync(0xffffffffu, end, 31);
     }
 }
 // To the next unit (there is one).
