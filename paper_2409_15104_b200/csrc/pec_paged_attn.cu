@@ -506,10 +506,10 @@ int launch_paged_simple(const Params &p, int64_t items, cudaStream_t stream)
 int launch_paged_combine(const Params &p, cudaStream_t stream)
 {
     // Every cut of the line; every block that can be cut: one has two slots or more.
-    const int few_groups = p.few_rows > 3 * kCombineWarps ? 4 : (p.few_rows + kCombineWarps - 1) / kCombineWarps, few_blocks = p.few ? (p.few_ctas - 1) * few_groups : 0;
+    const int few_groups = p.few_rows > kCombineWarps ? 2 : 1, few_blocks = p.few ? (p.few_ctas - 1) * few_groups : 0;
     const int many_groups = (p.many_rows + kManyGroup - 1) / kManyGroup;
     const int64_t most = (int64_t)p.many_cap / 2 * many_groups;      // a block that is cut has two slots or more
-    const int many_blocks = (int)(most < 4 * p.many_ctas ? most : 4 * p.many_ctas);
+    const int many_blocks = (int)(most < 2 * p.many_ctas ? most : 2 * p.many_ctas);
     if (few_blocks + many_blocks == 0) return PEC_OK;
     cudaError_t err = launch_dependent(paged_combine_kernel, dim3((unsigned)(few_blocks + many_blocks)), kCombineWarps * 32, 0, stream, true,
                                        p, few_groups, few_blocks, many_groups);
