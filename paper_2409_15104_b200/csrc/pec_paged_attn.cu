@@ -559,7 +559,7 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
         set_error("%s: q and o must be 16-byte aligned (lse 4-byte)", who);
         return PEC_ERR_ALIGNMENT;
     }
-    if (a->T * (a->Hq / a->Hkv) >= ((int64_t)1 << 31)) { set_error("%s: T * Hq / Hkv of 2^31 or more unsupported", who); return PEC_ERR_UNSUPPORTED; }
+    if (a->T * (a->Hq / a->Hkv) > ((int64_t)1 << 31) - 1024) { set_error("%s: T * Hq / Hkv near 2^31 or above unsupported", who); return PEC_ERR_UNSUPPORTED; }
     p.q = a->q; p.k_pages = a->k_pages; p.v_pages = a->v_pages;
     p.q_st = a->q_stride_t; p.q_sh = a->q_stride_h;
     p.o = a->o; p.lse = a->lse; p.o_is_bf16 = a->o_dtype == PEC_BF16;
