@@ -199,7 +199,7 @@ static_assert(kClasses == kPlanThreads, "a class per thread");
 // values' while the scores are worked out.
 constexpr int kBM = 64, kBN = 64, kThreads = 256;
 constexpr int kLd = kHeadDim + 4, kLdP = kBN + 4;
-constexpr size_t kSimpleSmem = sizeof(float) * (2 * kBM * kLd + kBN * kHeadDim);
+constexpr size_t kF32Smem = sizeof(float) * (2 * kBM * kLd + kBN * kHeadDim);
 
 // 16 bytes to shared memory, zeros where !ok (nothing is read then).
 __device__ __forceinline__ void copy16(float *dst, const float *src, bool ok)
@@ -210,7 +210,7 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int kLeft> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
 __global__ void __launch_bounds__(kThreads, 2)
-paged_simple_kernel(const Params p)
+paged_f32_kernel(const Params p)
 {
     extern __shared__ __align__(16) float smem[];
     float *sQ = smem;                       // [kBM][kLd]
@@ -382,8 +382,8 @@ paged_simple_kernel(const Params p)
 // ------------------------------------------------------------------------------------------ combining partials
 // A CTA merges the partial results of some packed rows of one unit: a (request, KV head) whose
 // tiles cross a cut of the line, or a block of rows whose keys are cut into slices (listed by the plan).  Units are enumerated by
-// what splits them - CTA c of the few class looks at cut c and takes the unit around it if this is the unit's first cut - so that
-// the grid has the size of what can be split, not of the batch.  (A CTA per token and KV head took 66 us to find nothing to do for
+// what splits them - CTA c of the few class looks at cut c and takes the unit around it if this is the unit's first cut - or, where
+// there are fewer units than cuts, one by one, so that the grid has the size of what can be split, not of the batch.  (A CTA per token and KV head took 66 us to find nothing to do for
 // 2048 tokens.)  The few class looks its unit up before the attention kernels end (the tables were complete before they began);
 // partials are read afterwards, and no CTA ends before that wait, so that whatever follows on the stream follows those kernels too.
 // A warp merges one row at a time, a lane owning four channels: the largest LSE first, then the weighted sum, sixteen partials'
@@ -434,21 +434,28 @@ __device__ __forceinline__ void combine_row(const Params &p, const float *po, co
 }
 
 __global__ void __launch_bounds__(kCombineWarps * 32, 2)
-paged_combine_kernel(const Params p, const int few_groups, const int few_blocks, const int many_groups)
+paged_combine_kernel(const Params p, const int by_unit, const int few_groups, const int few_blocks, const int many_groups)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if ((int)blockIdx.x < few_blocks) {
-        const int32_t cut = blockIdx.x / few_groups + 1;
+        const int32_t nth = blockIdx.x / few_groups;
         const int group = blockIdx.x % few_groups;
         Walk w;
-        const int32_t all = walk_tiles(p, w, lane), piece = few_piece(p, all), at = cut * piece;   // few_ctas * 2^23 at most
-        w.u0 = at;
-        if (at < all) walk_to(p, w, at, lane);
-        const bool mine = w.u0 < at && w.u0 >= at - piece;       // else the cut falls between units, or is not the unit's first
+        const int32_t all = walk_tiles(p, w, lane), piece = few_piece(p, all);
+        bool mine;
+        if (by_unit) {
+            mine = all > 0 && walk_unit(p, w, nth, lane);
+        } else {
+            const int32_t at = (nth + 1) * piece;                // few_ctas * 2^23 at most
+            mine = at < all;
+            if (mine) walk_to(p, w, at, lane);
+            mine = mine && w.u0 < at && w.u0 >= at - piece;      // else the cut falls between units, or is not the unit's first
+        }
         asm volatile("griddepcontrol.wait;" ::: "memory");
         if (!mine) return;
-        const int64_t first = cut - 1;                           // piece with the unit's first tiles
-        const int count = (w.u0 + w.r.tiles() - 1) / piece - (cut - 1) + 1;
+        const int64_t first = w.u0 / piece;                      // piece with the unit's first tiles
+        const int count = (w.u0 + w.r.tiles() - 1) / piece - (int)first + 1;
+        if (count == 1) return;
         for (int row = group * kCombineWarps + warp; row < w.r.n * p.g; row += few_groups * kCombineWarps) {
             const int64_t item = (int64_t)(w.r.start + row / p.g) * p.Hq + w.kvh * p.g + row % p.g;
             combine_row(p, p.few_o, p.few_lse, 2 * first * p.few_rows + row, w.u0 > first * piece ? p.few_rows : 0, 2 * (int64_t)p.few_rows,
@@ -486,18 +493,18 @@ int launch_paged_plan(const Params &p, cudaStream_t stream)
     return PEC_OK;
 }
 
-int launch_paged_simple(const Params &p, int64_t items, cudaStream_t stream)
+int launch_paged_f32(const Params &p, int64_t items, cudaStream_t stream)
 {
     static unsigned char ready[host::kMaxDevices] = {};
     static std::mutex ready_mutex;
     if (!host::once_per_device(ready, ready_mutex, [] {
-            return cudaFuncSetAttribute(paged_simple_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSimpleSmem) == cudaSuccess; })) {
+            return cudaFuncSetAttribute(paged_f32_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kF32Smem) == cudaSuccess; })) {
         (void)cudaGetLastError();
         set_error("pec_paged_attn: cannot raise the shared-memory limit");
         return PEC_ERR_CUDA;
     }
     if (items * p.Hkv > 0x7fffffff) { set_error("pec_paged_attn: grid too large"); return PEC_ERR_UNSUPPORTED; }
-    cudaError_t err = launch_dependent(paged_simple_kernel, dim3((unsigned)(items * p.Hkv)), kThreads, kSimpleSmem, stream, true, p);
+    cudaError_t err = launch_dependent(paged_f32_kernel, dim3((unsigned)(items * p.Hkv)), kThreads, kF32Smem, stream, true, p);
     if (err == cudaSuccess) err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
@@ -506,13 +513,18 @@ int launch_paged_simple(const Params &p, int64_t items, cudaStream_t stream)
 int launch_paged_combine(const Params &p, cudaStream_t stream)
 {
     // Every cut of the line; every block that can be cut: one has two slots or more.
-    const int few_groups = p.few_rows > kCombineWarps ? 2 : 1, few_blocks = p.few ? (p.few_ctas - 1) * few_groups : 0;
+    // One row a warp where the units are so few that this takes no more than two CTAs per SM.
+    const int64_t units = (int64_t)(p.c.B < p.c.T ? p.c.B : p.c.T) * p.Hkv;
+    const int by_unit = units < p.few_ctas, most_groups = (p.few_rows + kCombineWarps - 1) / kCombineWarps;
+    int few_groups = by_unit ? (int)(2 * p.few_ctas / units) : 2, few_blocks = 0;
+    if (few_groups > most_groups) few_groups = most_groups;
+    if (p.few) few_blocks = (by_unit ? (int)units : p.few_ctas - 1) * few_groups;
     const int many_groups = (p.many_rows + kManyGroup - 1) / kManyGroup;
     const int64_t most = (int64_t)p.many_cap / 2 * many_groups;      // a block that is cut has two slots or more
     const int many_blocks = (int)(most < 2 * p.many_ctas ? most : 2 * p.many_ctas);
     if (few_blocks + many_blocks == 0) return PEC_OK;
     cudaError_t err = launch_dependent(paged_combine_kernel, dim3((unsigned)(few_blocks + many_blocks)), kCombineWarps * 32, 0, stream, true,
-                                       p, few_groups, few_blocks, many_groups);
+                                       p, by_unit, few_groups, few_blocks, many_groups);
     if (err == cudaSuccess) err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
@@ -647,7 +659,7 @@ extern "C" int pec_paged_attn(const pec_paged_args *args, void *cuda_stream)
     if (args->T == 0) return PEC_OK;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (c.many_items > 0) rc = launch_paged_plan(c.p, stream);
-    if (rc == PEC_OK && c.many_items > 0) rc = args->dtype == PEC_BF16 ? launch_paged_many(c.p, c.many_items, stream) : launch_paged_simple(c.p, c.many_items, stream);
+    if (rc == PEC_OK && c.many_items > 0) rc = args->dtype == PEC_BF16 ? launch_paged_many(c.p, c.many_items, stream) : launch_paged_f32(c.p, c.many_items, stream);
     if (rc == PEC_OK && c.p.few) rc = launch_paged_few(c.p, c.many_items > 0, stream);
     if (rc != PEC_OK || c.bytes == 0) return rc;
     return launch_paged_combine(c.p, stream);

@@ -18,10 +18,11 @@
 //           rows are all past the segment's only keep the barriers in step).  P (bf16) is written over S.
 //           TMEM columns: S [0, 256), two buffers; O [256, 512), one per group.
 //   narrow  up to 16 rows: S^T = K Q^T and O^T = V^T P^T with the rows as 16 columns (a thread = a key, then a channel).  A row's
-//           maximum and sum run across threads, but a tile costs 1/8 of the tensor work and 1/16 of the exponentials, and P
-//           goes through 4 KB of shared memory.  Not needed for the rate of a short run - the wide form streams 6.37 TB/s as
-//           well - but a long run of it draws the 1 kW limit, the SM clock falls to 1.5 GHz and the rate with it, to 5.55 TB/s
-//           (three requests of 131072 keys, 64 / 8 heads).
+//           maximum and sum run across threads, but a tile costs 3/16 of the tensor work and 1/16 of the exponentials.  P goes
+//           through 8 KB of shared memory, as two bf16 parts: 0 to 2.5 % slower than as one, and a bf16 result errs by its own
+//           rounding alone.  What it is for is a long run: the wide form draws the 1 kW limit, the SM clock falls to 1.5 GHz and
+//           the stream with it - three requests of 131072 keys, 64 / 8 heads, 5.55 TB/s for seconds (6.37 in a short run)
+//           against 6.46 (6.65); 64 requests of 2400 keys on average, 32 / 8 heads, 4.88 against 5.65.
 //           TMEM columns: S^T [0, 32), two buffers; O^T [32, 64), one per group.
 //
 // Per tile: S(n) into one of two TMEM buffers, P(n) into its place or one of two shared buffers, O += P V.  The issuer's order
@@ -45,7 +46,7 @@ constexpr int kNarrowRows = 16;
 template <bool kNarrow> struct Cfg {
     static constexpr int kSlots = kNarrow ? 6 : 5;
     static constexpr uint32_t kHalfQ = kNarrow ? kNarrowRows * 128u : kHalfTileBytes, kQBytes = 2 * kHalfQ;   // 64 channels of the rows; both halves
-    static constexpr uint32_t kRing = kNarrow ? 4 * kQBytes : 2 * kQBytes;                                    // P buffers are as large as Q's
+    static constexpr uint32_t kRing = kNarrow ? 6 * kQBytes : 2 * kQBytes;   // two P buffers of two parts, each as large as Q's
     static constexpr uint32_t kTmemCols = kNarrow ? 64 : 512, kCols = kNarrow ? kNarrowRows : 128, kColO = 2 * kCols;
 };
 constexpr float kRescaleThreshold = 8.0f;                  // log2 units
@@ -371,7 +372,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     const uint64_t v0 = v_ring + slot * (kTileBytes >> 4);
                     const uint32_t tO = tmem + kColO + (uint32_t)g * C::kCols, tP = tmem + (uint32_t)(n & 1) * C::kCols;
                     if constexpr (kNarrow) {
-                        mma_narrow<1>(tO, v0, smem_desc_sw128(sQ + (uint32_t)(2 + (n & 1)) * C::kQBytes, 16, 1024), narrow_pv, j > 0 ? 1u : 0u);
+                        const uint64_t p0 = smem_desc_sw128(sQ + (uint32_t)(2 + 2 * (n & 1)) * C::kQBytes, 16, 1024);
+                        mma_narrow<1>(tO, v0, p0, narrow_pv, j > 0 ? 1u : 0u);
+                        mma_narrow<1>(tO, v0, p0 + (C::kQBytes >> 4), narrow_pv, 1u);
                     } else {
                         mma_ts_k64(tO, tP, v0, idesc_pv, j > 0 ? 1u : 0u);
                         mma_ts_k64(tO, tP + 32, v0 + (64 * 128 >> 4), idesc_pv, 1u);
@@ -478,17 +481,18 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     // Waited for in every tile (see the wide form); what it says is voted on with the next tile.
                     if (!wait_all(&sh->pv_done[g], (pv + j - 1) & 1, sh, p)) sh->abort_flag = 1;
                 }
-                // p = 2^(s scale - m), rounded to bf16 as the product's operand; the row's sum takes p before it is rounded.  S(n) is
-                // complete, and with it PV(n - 2), which read this P buffer.
-                const uint32_t dst = sQ + (uint32_t)(2 + buf) * C::kQBytes + p_half;
+                // p = 2^(s scale - m) as the sum of two bf16 operands (16 bits of it; the second product costs next to nothing at
+                // 16 columns); the row's sum takes p itself.  S(n) is complete, and with it PV(n - 2), which read this P buffer.
+                const uint32_t dst = sQ + (uint32_t)(2 + 2 * buf) * C::kQBytes + p_half;
 #pragma unroll
                 for (int c = 0; c < kNarrowRows; ++c) {
                     if (c < 8 || wide) {
                         const float e = ex2(fmaf(x[c], p.scale_log2, m[c] == -INFINITY ? 0.f : -m[c]));
                         l[c] += e;
-                        const __nv_bfloat16 h = __float2bfloat16_rn(e);
-                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(dst + (uint32_t)c * 128u + ((p_chunk ^ (uint32_t)(c & 7)) << 4)),
-                                     "h"(*reinterpret_cast<const unsigned short *>(&h)) : "memory");
+                        const __nv_bfloat16 hi = __float2bfloat16_rn(e), lo = __float2bfloat16_rn(e - __bfloat162float(hi));
+                        const uint32_t to = dst + (uint32_t)c * 128u + ((p_chunk ^ (uint32_t)(c & 7)) << 4);
+                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"(*reinterpret_cast<const unsigned short *>(&hi)) : "memory");
+                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + C::kQBytes), "h"(*reinterpret_cast<const unsigned short *>(&lo)) : "memory");
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

@@ -5,11 +5,13 @@
 // row = token * g + head of the group, so that a key tile read once serves all of them.
 //
 // Two classes of requests, by their packed rows n * g:
-//   few  (at most 128: decode steps)  worked on by a persistent grid.  The key tiles of all (request, KV head) pairs lie on
+//   few  (at most 128: decode steps; fp32 has none)  worked on by a persistent grid.  The key tiles of all (request, KV head) pairs lie on
 //        one line that is cut into equal pieces, one per CTA; a pair that crosses a cut leaves one partial result per piece.
 //   many (chunks)                     items of one block of rows against all or a slice of its keys, listed longest first by a
 //        kernel of one CTA ahead of the attention kernel, which has one CTA per (item, KV head).  (With every CTA working out
 //        its own item from the tables a CTA spent 4-6 us on it: five waves of 64-token blocks lost 20 of 210 us.)
+// Both sides of 128 rows, measured (64 requests of 3000 keys, 8 KV heads, few / many): 4 rows a request 128 / 163 us, 32 138 / 174,
+// 128 160 / 181; 200 requests of 132 keys, 64 rows 49 / 99; one request of 32000 keys, 128 rows 40 / 55.
 // Partials are merged by their LSE by one kernel for both classes (combine), which finds them by the same arithmetic.
 #pragma once
 #include "pec_internal.h"
@@ -166,6 +168,29 @@ __device__ __forceinline__ void walk_to(const Params &p, Walk &w, int32_t at, in
         before = __shfl_sync(0xffffffffu, end, 31);
     }
 }
+// To the first tile of unit `u` in line order; false where there are not so many.
+__device__ __forceinline__ bool walk_unit(const Params &p, Walk &w, int32_t u, int lane)
+{
+    int32_t before = 0, tiles = 0;
+    for (w.b0 = 0; w.b0 < p.c.B; w.b0 += 32) {
+        if (w.b0 > 0) walk_group(p, w, lane);
+        const bool few = is_few(p, w.mine);
+        const int32_t units = few ? p.Hkv : 0, len = few ? w.mine.tiles() * p.Hkv : 0;
+        const int32_t end = before + warp_prefix32(units, lane), t_end = tiles + warp_prefix32(len, lane);
+        const unsigned who = __ballot_sync(0xffffffffu, u >= end - units && u < end);
+        if (who) {
+            const int src = __ffs(who) - 1;
+            walk_take(w, src);
+            w.kvh = u - __shfl_sync(0xffffffffu, end - units, src);
+            w.tile = 0;
+            w.u0 = __shfl_sync(0xffffffffu, t_end - len, src) + w.kvh * w.r.tiles();
+            return true;
+        }
+        before = __shfl_sync(0xffffffffu, end, 31);
+        tiles = __shfl_sync(0xffffffffu, t_end, 31);
+    }
+    return false;
+}
 // To the next unit (there is one).
 __device__ __forceinline__ void walk_next(const Params &p, Walk &w, int lane)
 {
@@ -203,7 +228,7 @@ inline cudaError_t launch_dependent(void (*kernel)(A...), dim3 grid, int threads
 
 // Launchers (each returns a pec_status).
 int launch_paged_plan(const paged::Params &p, cudaStream_t stream);                        // items of the many class
-int launch_paged_simple(const paged::Params &p, int64_t items, cudaStream_t stream);       // fp32
+int launch_paged_f32(const paged::Params &p, int64_t items, cudaStream_t stream);       // fp32
 int launch_paged_many(const paged::Params &p, int64_t items, cudaStream_t stream);         // bf16
 int launch_paged_few(const paged::Params &p, bool after_many, cudaStream_t stream);         // bf16; after_many: overlaps that kernel's end
 int launch_paged_combine(const paged::Params &p, cudaStream_t stream);

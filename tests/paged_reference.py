@@ -72,11 +72,12 @@ def attend(q, k_pages, v_pages, block_table, cu_q, kv_lens, causal=True, scale=N
     return o, lse, A, B
 
 
-def check_attend(got_o, got_l, want, dtype, what=""):
+def check_attend(got_o, got_l, want, dtype, what="", p_error=None):
     """Bounds: a score is a sum of 128 products in fp32, off by at most 128 * 2^-23 * B (each addition to a full ulp, which
     covers truncating adders), and so is the scaling's rounding; e^x turns that into a relative error of p, twice (p and the
     sum).  2^x is approximated to 2^-21.  bf16 rounds p by 2^-8 of itself; fp32 sums of up to 2^18 terms in pieces and
-    merges stay below 2e-6 of A.  The output is rounded once to its type."""
+    merges stay below 2e-6 of A.  The output is rounded once to its type.  p_error: another relative error of p than a bf16
+    rounding's."""
     o, lse, A, B = want
     got_o, got_l = got_o.detach(), got_l.detach()
     out_t = got_o.dtype
@@ -88,7 +89,9 @@ def check_attend(got_o, got_l, want, dtype, what=""):
     delta = 130 * 2.0 ** -23 * B
     full = real & ~empty
     assert np.isfinite(go[real]).all() and np.isfinite(gl[full]).all(), f"{what}: not finite"
-    bound = (2 * delta[..., None] + 2.0 ** -20 + 2e-6 + (HALF[torch.bfloat16] if dtype == torch.bfloat16 else 0.0)) * A + HALF[out_t] * np.abs(o) + 1e-30
+    if p_error is None:
+        p_error = HALF[torch.bfloat16] if dtype == torch.bfloat16 else 0.0
+    bound = (2 * delta[..., None] + 2.0 ** -20 + 2e-6 + p_error) * A + HALF[out_t] * np.abs(o) + 1e-30
     off = np.abs(go - o)[full] / bound[full]
     bl = (delta + 2.0 ** -20 + 2e-6 + 2.0 ** -23 * np.abs(np.where(full, lse, 0.0)))[full]
     off_l = np.abs(gl[full] - lse[full]) / bl

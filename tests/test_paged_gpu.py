@@ -494,3 +494,16 @@ def test_a_wait_that_runs_out_is_reported(pec, n, kv):
     o, lse = pec.pec_paged_attn(*args, max_q_len=max(n))
     pec.check_status()
     ref.check_attend(o, lse, ref.attend(q, kp, vp, table, cu, kv), BF16, "after a wait that ran out")
+
+
+@pytest.mark.parametrize("n,kv,hq,hkv", [([1], [3000], 8, 1), ([1] * 9, [5, 128, 700, 129, 1, 2000, 64, 300, 1111], 32, 8), ([2, 1, 2], [900, 40, 2], 16, 2),
+                                         ([16], [333], 1, 1), ([5, 3], [4000, 3], 3, 1)])
+def test_few_rows_keep_more_of_the_probabilities(pec, n, kv, hq, hkv):
+    """At most 16 packed rows: p is the sum of two bf16 values, each rounded to half a step: 2^-8 of what the first left, 2^-16
+    of p."""
+    kp, vp, table = ref.make_cache(91, kv, 16, hkv, BF16, DEV)
+    cu = ref.offsets(n)
+    q = torch.randn((sum(n), hq, 128), device=DEV).to(BF16)
+    o, lse = pec.pec_paged_attn(q, kp, vp, table, dev(cu), dev(kv), max_q_len=max(n), out_dtype=F32)
+    pec.check_status()
+    ref.check_attend(o, lse, ref.attend(q, kp, vp, table, cu, kv), BF16, f"fp32 output, {n} of {kv}"[:100], p_error=2.0 ** -16)
