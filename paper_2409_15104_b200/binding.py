@@ -2,10 +2,10 @@
 
 Function names mirror the C ABI (include/pec.h).  torch provides device memory and streams.
 The library is loaded on first use; a missing or unloadable library raises - there is no
-fallback implementation.
+fallback implementation.  The paged serving calls, which take microseconds, are marshalled by a
+compiled module (_pec_torch.so, csrc/pec_torch.cpp) instead of ctypes.
 """
 import ctypes
-import functools
 import os
 
 import torch
@@ -512,166 +512,66 @@ def pec_linear_merged(o_parts, lse_parts, w, y=None, stream=None):
     return y
 
 
-def _need(ok, text):
-    if not ok:
-        raise ValueError(text)
+_NO_TABLE = (None, 0)
+_torch_module = None
 
 
-# The paged calls are a few microseconds of device work in a decode step, and these checks - those that the library cannot
-# make - are most of what the host does for one.  So they take each attribute once and build text only when they fail.
-def _refuse(t, what, dims, dtype, index):
-    raise ValueError(f"{what}: need a {dims}-dimensional {dtype} tensor on cuda:{index} with a contiguous innermost dimension, "
-                     f"got {tuple(t.shape)} with strides {t.stride()}, {t.dtype} on {t.device}")
+def _marshal():
+    """The compiled marshalling of the paged calls (_pec_torch.so, csrc/pec_torch.cpp), bound to the library."""
+    global _torch_module
+    if _torch_module is None:
+        lib = load()
+        try:
+            from . import _pec_torch
+        except ImportError as e:
+            raise RuntimeError("_pec_torch.so is missing or unloadable: build it with `python -m paper_2409_15104_b200.build`") from e
+        _pec_torch.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
+                          (lib.pec_qk_norm_rope, lib.pec_kv_append, lib.pec_paged_attn, lib.pec_paged_workspace_size)))
+        _torch_module = _pec_torch
+    return _torch_module
 
 
-def _vector(t, what, dtype, index):
-    """Address and length of a contiguous vector of this type on this device."""
-    if t.dtype is not dtype or t.get_device() != index or t.dim() != 1 or not t.is_contiguous():
-        _refuse(t, what, 1, dtype, index)
-    return t.data_ptr(), t.shape[0]
-
-
-def _rows(t, what, dtype, index):
-    """Token and head strides of [T, H, D] of this type on this device; a dimension of one entry has no stride of its own,
-    whatever torch says."""
-    if t.dtype is not dtype or t.get_device() != index or t.dim() != 3:
-        _refuse(t, what, 3, dtype, index)
-    st, sh, sd = t.stride()
-    if sd != 1 or st < 128 or sh < 128 or (st | sh) & 7:
-        n, h, d = t.shape
-        if sd != 1 and d > 1:
-            _refuse(t, what, 3, dtype, index)
-        st, sh = st if n > 1 else 128, sh if h > 1 else 128
-    return st, sh
-
-
-def _pages(t, what, dtype, index):
-    """Page, token and head strides of [pages, page_size, Hkv, D]."""
-    if t.dtype is not dtype or t.get_device() != index or t.dim() != 4:
-        _refuse(t, what, 4, dtype, index)
-    sp, st, sh, sd = t.stride()
-    if sd != 1 or sp < 128 or sh < 128 or (sp | sh) & 7:
-        n, _, h, d = t.shape
-        if sd != 1 and d > 1:
-            _refuse(t, what, 4, dtype, index)
-        sp, sh = sp if n > 1 else 128, sh if h > 1 else 128
-    return sp, st, sh
-
-
-def _ready_status(index):
-    """Address of the status word; the word must exist before a capture, where its zeroing would become part of the graph."""
-    word = _status_words.get(index)
+def _call_status(t):
+    """The status word of a call's device; it must exist before a capture, where its zeroing would become part of the graph."""
+    word = _status_words.get(t.get_device())
     if word is None:
-        _need(not torch.cuda.is_current_stream_capturing(), "call status_word() once on this device before capturing")
-        word = status_word(torch.device("cuda", index))
-    return word.data_ptr()
-
-
-def _launching(call):
-    """The call with its first tensor's device current and, where `stream` is given, that stream, so that what it allocates
-    belongs to them; the call gets the device's index and the stream's handle as `on`."""
-
-    @functools.wraps(call)
-    def run(x, *args, stream=None, **kw):
-        index = x.get_device()
-        if index < 0:
-            _dtype_code(x.dtype)
+        if not t.is_cuda:
+            _dtype_code(t.dtype)
             raise ValueError("tensors must be on a CUDA device")
-        if stream is None and index == torch.cuda.current_device():
-            return call(x, *args, on=(index, torch._C._cuda_getCurrentRawStream(index)), **kw)
-        _need(stream is None or stream.device == x.device, "the stream belongs to another device")
-        with torch.cuda.device(index), torch.cuda.stream(stream):
-            return call(x, *args, on=(index, torch._C._cuda_getCurrentRawStream(index)), **kw)
-
-    return run
+        if torch.cuda.is_current_stream_capturing():
+            raise ValueError("call status_word() once on this device before capturing")
+        word = status_word(t.device)
+    return word
 
 
-def _rope(tables, index):
-    if tables is None:
-        return None, 0
-    table, n_pos = tables
-    at, n = _vector(table, "tables", torch.float32, index)
-    if n < 8192 + (n_pos + 63) // 64 * 128:                    # pec_rope_table_floats
-        raise ValueError("tables: the table is shorter than n_pos asks for")
-    return at, n_pos
+def _on_stream(call, t, stream):
+    """`call` with `stream` (of the tensor's device) current, so that what it allocates belongs to that stream."""
+    if stream.device != t.device:
+        raise ValueError("the stream belongs to another device")
+    with torch.cuda.stream(stream):
+        return call()
 
 
-def _weight(w, norm, dtype, index):
-    if w is None:
-        return None
-    at, n = _vector(w, "weight", dtype, index)
-    _need(norm and n == 128, "a weight needs norm=True and 128 entries")
-    return at
-
-
-@_launching
 def pec_qk_norm_rope(q, k=None, *, norm=True, q_weight=None, k_weight=None, eps=1e-6, tables=None, positions=None, pos0=0,
-                     q_out=None, k_out=None, inplace=False, on=None):
+                     q_out=None, k_out=None, inplace=False, stream=None):
     """RMS norm of every head (norm=True) and rotary encoding (tables = pec_rope_table(...)) in one pass; returns (q_out, k_out).
 
     q [T, Hq, 128], k [T, Hkv, 128] or None: CUDA tensors of one type (bf16 or fp32), last dimension contiguous (column slices
     of a fused projection are fine).  Token t is at positions[t] (int32 CUDA tensor; negative: padding, its rows are not
     written) or at pos0 + t.  inplace=True writes into q and k.  stream: a torch stream other than the current one.
     """
-    index, handle = on
-    dt = q.dtype
-    code = _dtype_code(dt)
-    qst, qsh = _rows(q, "q", dt, index)
-    T, Hq, D = q.shape
-    if q_out is None:
-        q_out = q if inplace else q.new_empty((T, Hq, D))
-    else:
-        _need(q_out.shape == q.shape, "q_out: need q's shape")
-    qost, qosh = _rows(q_out, "q_out", dt, index)
-    kp = kop = None
-    kst = ksh = kost = kosh = Hkv = 0
-    if k is not None:
-        kst, ksh = _rows(k, "k", dt, index)
-        Tk, Hkv, Dk = k.shape
-        if Tk != T or Dk != D:
-            raise ValueError("k: need q's tokens and head dimension")
-        if k_out is None:
-            k_out = k if inplace else k.new_empty((T, Hkv, D))
-        else:
-            _need(k_out.shape == k.shape, "k_out: need k's shape")
-        kost, kosh = _rows(k_out, "k_out", dt, index)
-        kp, kop = k.data_ptr(), k_out.data_ptr()
-    pos = None
-    if positions is not None:
-        pos, n = _vector(positions, "positions", torch.int32, index)
-        if n != T:
-            raise ValueError("positions: need one per token")
-    table, n_pos = _rope(tables, index)
-    if T == 0 or Hq + Hkv == 0:                               # tensors without elements have no address
-        return q_out, k_out
-    a = pec_norm_rope_args(q.data_ptr(), kp, qst, qsh, kst, ksh, q_out.data_ptr(), kop, qost, qosh, kost, kosh, code, Hq, Hkv, D, T,
-                           _weight(q_weight, norm, dt, index), _weight(k_weight, norm, dt, index), 1 if norm else 0, eps,
-                           table, n_pos, pos, pos0, _ready_status(index))
-    rc = (_lib or load()).pec_qk_norm_rope(a, handle)
+    if stream is not None:
+        return _on_stream(lambda: pec_qk_norm_rope(q, k, norm=norm, q_weight=q_weight, k_weight=k_weight, eps=eps, tables=tables,
+                                                   positions=positions, pos0=pos0, q_out=q_out, k_out=k_out, inplace=inplace), q, stream)
+    rc, q_out, k_out = (_torch_module or _marshal()).norm_rope(q, k, q_out, k_out, inplace, norm, q_weight, k_weight, eps,
+                                                               *(tables or _NO_TABLE), positions, pos0, _call_status(q))
     if rc:
         _check(rc)
     return q_out, k_out
 
 
-def _paged(k_pages, v_pages, block_table, cu_q, kv_lens, T, dtype, index):
-    """The checked cache and batch fields of the paged calls, in the order of _PAGED_FIELDS, and the cache's shape."""
-    ks, vs = _pages(k_pages, "k_pages", dtype, index), _pages(v_pages, "v_pages", dtype, index)
-    cu, n = _vector(cu_q, "cu_q", torch.int32, index)
-    lens, B = _vector(kv_lens, "kv_lens", torch.int32, index)
-    shape = k_pages.shape
-    if block_table.dtype is not torch.int32 or block_table.get_device() != index or block_table.dim() != 2:
-        _refuse(block_table, "block_table", 2, torch.int32, index)
-    (rows, width), (step, inner) = block_table.shape, block_table.stride()
-    if inner != 1 and width > 1:
-        _refuse(block_table, "block_table", 2, torch.int32, index)
-    if v_pages.shape != shape or n != B + 1 or rows != B:
-        raise ValueError("need v_pages of k_pages' shape, cu_q [B + 1], kv_lens [B] and block_table [B, pages]")
-    return (k_pages.data_ptr(), v_pages.data_ptr(), *ks, *vs, shape[1], shape[0], block_table.data_ptr(), step if B > 1 else width, width,
-            cu, lens, B, T), shape
-
-
-@_launching
-def pec_kv_append(k, v, k_pages, v_pages, block_table, cu_q, kv_lens, *, norm=False, k_weight=None, eps=1e-6, tables=None, on=None):
+def pec_kv_append(k, v, k_pages, v_pages, block_table, cu_q, kv_lens, *, norm=False, k_weight=None, eps=1e-6, tables=None,
+                  stream=None):
     """Appends a batch's new keys (normalised with norm=True, rotated with tables) and values to a paged cache.
 
     k, v [T, Hkv, 128]; k_pages, v_pages [pages, page_size, Hkv, 128] (any strides but the last: transpose head-major pages
@@ -679,27 +579,17 @@ def pec_kv_append(k, v, k_pages, v_pages, block_table, cu_q, kv_lens, *, norm=Fa
     kv_lens int32 [B] cached tokens including the new ones.  All CUDA tensors; the tables are read when the kernel runs.
     stream: a torch stream other than the current one.
     """
-    index, handle = on
-    dt = k.dtype
-    code = _dtype_code(dt)
-    strides = *_rows(k, "k", dt, index), *_rows(v, "v", dt, index)
-    T, Hkv, D = k.shape
-    cache, shape = _paged(k_pages, v_pages, block_table, cu_q, kv_lens, T, dt, index)
-    if v.shape != k.shape or shape[2] != Hkv or shape[3] != D:
-        raise ValueError("need v of k's shape and a cache of k's heads and head dimension")
-    table, n_pos = _rope(tables, index)
-    if T == 0:                                                # tensors without elements have no address
-        return
-    a = pec_kv_append_args(k.data_ptr(), v.data_ptr(), *strides, code, *cache, Hkv, D, _weight(k_weight, norm, dt, index),
-                           1 if norm else 0, eps, table, n_pos, _ready_status(index))
-    rc = (_lib or load()).pec_kv_append(a, handle)
+    if stream is not None:
+        return _on_stream(lambda: pec_kv_append(k, v, k_pages, v_pages, block_table, cu_q, kv_lens, norm=norm, k_weight=k_weight,
+                                                eps=eps, tables=tables), k, stream)
+    rc = (_torch_module or _marshal()).kv_append(k, v, k_pages, v_pages, block_table, cu_q, kv_lens, norm, k_weight, eps,
+                                                 *(tables or _NO_TABLE), _call_status(k))
     if rc:
         _check(rc)
 
 
-@_launching
 def pec_paged_attn(q, k_pages, v_pages, block_table, cu_q, kv_lens, *, max_q_len=0, causal=True, softmax_scale=0.0,
-                   out_dtype=None, o=None, lse=None, workspace=None, on=None):
+                   out_dtype=None, o=None, lse=None, workspace=None, stream=None):
     """Attention of a batch's new tokens q [T, Hq, 128] over a paged cache that holds their keys and values already (see
     pec_kv_append for the cache and the tables); returns (o [T, Hq, 128], lse [T, Hq]).
 
@@ -707,38 +597,12 @@ def pec_paged_attn(q, k_pages, v_pages, block_table, cu_q, kv_lens, *, max_q_len
     tensor of at least the size the library asks for, allocated here when not given.  stream: a torch stream other than the
     current one.
     """
-    index, handle = on
-    lib = _lib or load()
-    dt = q.dtype
-    code = ocode = _dtype_code(dt)
-    qst, qsh = _rows(q, "q", dt, index)
-    T, Hq, D = q.shape
-    cache, shape = _paged(k_pages, v_pages, block_table, cu_q, kv_lens, T, dt, index)
-    if shape[3] != D:
-        raise ValueError("k_pages: need q's head dimension")
-    if o is None:
-        o = q.new_empty((T, Hq, D), dtype=out_dtype)
-    elif o.get_device() != index or not o.is_contiguous() or o.shape != q.shape or (out_dtype is not None and o.dtype is not out_dtype):
-        raise ValueError("o: need a contiguous tensor of q's shape")
-    if o.dtype is not dt:
-        ocode = _dtype_code(o.dtype)
-    if lse is None:
-        lse = q.new_empty((T, Hq), dtype=torch.float32)
-    elif lse.get_device() != index or not lse.is_contiguous() or lse.dtype is not torch.float32 or lse.shape != (T, Hq):
-        raise ValueError("lse: need a contiguous fp32 tensor [T, Hq]")
-    if T == 0:                                                # tensors without elements have no address
-        return o, lse
-    a = pec_paged_args(q.data_ptr(), qst, qsh, code, *cache, max_q_len, o.data_ptr(), ocode, lse.data_ptr(), Hq, shape[2], D,
-                       1 if causal else 0, softmax_scale, None, 0, _ready_status(index))
-    if workspace is None:
-        size = lib.pec_paged_workspace_size(a)
-        if size:
-            workspace = q.new_empty((size,), dtype=torch.uint8)
-            a.workspace, a.workspace_bytes = workspace.data_ptr(), size
-    else:
-        _need(workspace.get_device() == index and workspace.is_contiguous(), "workspace: need a contiguous tensor on q's device")
-        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    rc = lib.pec_paged_attn(a, handle)
+    if stream is not None:
+        return _on_stream(lambda: pec_paged_attn(q, k_pages, v_pages, block_table, cu_q, kv_lens, max_q_len=max_q_len, causal=causal,
+                                                 softmax_scale=softmax_scale, out_dtype=out_dtype, o=o, lse=lse, workspace=workspace),
+                          q, stream)
+    rc, o, lse = (_torch_module or _marshal()).paged_attn(q, k_pages, v_pages, block_table, cu_q, kv_lens, max_q_len, causal,
+                                                          softmax_scale, out_dtype, o, lse, workspace, _call_status(q))
     if rc:
         _check(rc)
     return o, lse

@@ -507,3 +507,35 @@ def test_few_rows_keep_more_of_the_probabilities(pec, n, kv, hq, hkv):
     o, lse = pec.pec_paged_attn(q, kp, vp, table, dev(cu), dev(kv), max_q_len=max(n), out_dtype=F32)
     pec.check_status()
     ref.check_attend(o, lse, ref.attend(q, kp, vp, table, cu, kv), BF16, f"fp32 output, {n} of {kv}"[:100], p_error=2.0 ** -16)
+
+
+def test_the_binding_refuses_what_the_library_cannot_see(pec):
+    kp, vp, table = ref.make_cache(1, [20, 20], 16, 2, BF16, DEV, wild=False)
+    q, k = torch.zeros((2, 4, 128), dtype=BF16, device=DEV), torch.zeros((2, 2, 128), dtype=BF16, device=DEV)
+    cu, kv = dev([0, 1, 2]), dev([20, 20])
+    wide = torch.zeros((2, 4, 256), dtype=BF16, device=DEV)[:, :, ::2]
+    attn = dict(q=q, k_pages=kp, v_pages=vp, block_table=table, cu_q=cu, kv_lens=kv)
+    for over in (dict(q=q.cpu()), dict(q=q[0]), dict(q=wide), dict(q=q[..., :64]), dict(k_pages=kp.float()), dict(v_pages=vp[:-1]), dict(k_pages=kp.cpu()),
+                 dict(block_table=table.long()), dict(block_table=table[:1]), dict(cu_q=cu[:2]), dict(cu_q=cu.float()), dict(kv_lens=kv.cpu()),
+                 dict(o=torch.zeros((2, 4, 64), dtype=BF16, device=DEV)), dict(o=torch.zeros_like(q), out_dtype=F32), dict(lse=torch.zeros((2, 4), dtype=BF16, device=DEV)),
+                 dict(max_q_len=-1), dict(workspace=torch.zeros(64, dtype=torch.uint8))):
+        with pytest.raises(ValueError):
+            pec.pec_paged_attn(**{**attn, **over})
+    for over in (dict(q=q.half()), dict(k_pages=None), dict(out_dtype=torch.float16), dict(max_q_len="many")):
+        with pytest.raises(TypeError):
+            pec.pec_paged_attn(**{**attn, **over})
+    with pytest.raises(binding.PecError) as e:
+        pec.pec_paged_attn(**attn, workspace=torch.zeros(64, dtype=torch.uint8, device=DEV))
+    assert e.value.code == -4
+    append = dict(k=k, v=k, k_pages=kp, v_pages=vp, block_table=table, cu_q=cu, kv_lens=kv)
+    w = torch.ones(128, dtype=BF16, device=DEV)
+    for over in (dict(v=k[:1]), dict(k=q, v=q), dict(k_weight=w), dict(norm=True, k_weight=w[:64]), dict(norm=True, k_weight=w.float()),
+                 dict(tables=(torch.zeros(100, device=DEV), 10)), dict(v=k.cpu())):
+        with pytest.raises(ValueError):
+            pec.pec_kv_append(**{**append, **over})
+    for over in (dict(k=k[:1]), dict(positions=dev([1])), dict(positions=torch.zeros(2, device=DEV)), dict(q_out=k), dict(norm=False, q_weight=w)):
+        with pytest.raises(ValueError):
+            pec.pec_qk_norm_rope(**{**dict(q=q, k=k), **over})
+    with pytest.raises(binding.PecError):
+        pec.pec_qk_norm_rope(q, eps=0.0)
+    pec.check_status()
