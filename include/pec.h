@@ -496,7 +496,7 @@ int pec_qk_norm_rope(const pec_norm_rope_args *args, void *cuda_stream);
  * Entries of block_table that a request does not reach are not read.  What a page holds past the request's end may be
  * anything, NaN included.  A page number outside [0, num_pages), a position outside the table's row and offsets that are not
  * ascending store PEC_ERR_BAD_INDEX in *status; no access leaves the cache, and the outputs of the requests concerned are
- * undefined.
+ * undefined.  (So does a batch of 2^30 or more pairs of a 128-key tile and a KV head, which only shared pages can amount to.)
  */
 
 /*
@@ -567,7 +567,7 @@ typedef struct {
     void *o;                    /* device; [T, Hq, D] contiguous, 16-byte aligned               */
     int32_t o_dtype;
     float *lse;                 /* device; [T, Hq]                                              */
-    int32_t Hq, Hkv, D;         /* D must be 128; Hkv | Hq; Hq / Hkv <= 128                     */
+    int32_t Hq, Hkv, D;         /* D must be 128; Hkv | Hq; g = Hq / Hkv <= 128, T g < 2^31 - 1024 */
     int32_t causal;
     float softmax_scale;        /* 0 selects 1/sqrt(D)                                          */
     void *workspace;
@@ -578,7 +578,8 @@ typedef struct {
 int pec_paged_attn(const pec_paged_args *args, void *cuda_stream);
 
 /* Bytes of workspace pec_paged_attn needs for these arguments (0 if they are invalid): a function of T, B, Hq, Hkv, dtype,
- * max_q_len, the causal flag and the current device's SM count, not of what the tables hold. */
+ * max_q_len, max_pages, page_size and the current device's SM count, not of what the tables hold; on 148 SMs at most 140 MB
+ * and the list of row blocks (48 bytes for every 256 packed rows and request). */
 size_t pec_paged_workspace_size(const pec_paged_args *args);
 
 /*

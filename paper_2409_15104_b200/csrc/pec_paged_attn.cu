@@ -18,7 +18,9 @@ namespace paged {
 // block for one KV head; its length is the number of its request's key tiles.  Units up to the last full wave of many_ctas CTAs stay
 // whole, unless one is longer than an SM's fair share of all tiles (slice0); of the rest, which would leave SMs idle for a whole
 // unit's time, the keys are cut into slices (slice1): as many as fill one, two or three waves, whichever has the shortest
-// estimated time, or none.  The estimate, in 1/32 of a tile's time: a wave of slices takes its tiles and item_cost for a CTA's
+// estimated time, or none.  That holds for units of nearly one length, or for a batch of less than a wave; units of all lengths fill
+// the SMs by going longest first, and cutting some of them only adds work (24 requests of 4 to 30 tiles, 4.2 waves: 207 us cut, 193
+// not).  The estimate, in 1/32 of a tile's time: a wave of slices takes its tiles and item_cost for a CTA's
 // start and end; a slice's partial, written and read once, merge_cost.  On the tensor cores a tile takes 1.35 us, start and end 4
 // us, a partial of 132 KB 0.04 us both ways; with the FMA kernel, 17 us a tile, both are next to nothing.
 // Slots that cut units take: cutting units of length l into slices of S takes less than sum l / S + their number.  slice0 >= all
@@ -54,12 +56,12 @@ paged_plan_kernel(const Params p, const int items_cap, const int split_cap)
     __shared__ Pair s_warp[kPlanThreads / 32];
     __shared__ int32_t s_item[kPlanThreads], s_split[kPlanThreads], s_slot[kPlanThreads];   // ends (s_slot: starts) of the requests' ranges
     __shared__ int32_t s_start[kPlanThreads], s_n[kPlanThreads], s_kv[kPlanThreads], s_n0[kPlanThreads];
-    __shared__ int32_t s_class[kClasses], s_most;
+    __shared__ int32_t s_class[kClasses], s_most, s_least;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x;
     const bool one = p.c.B <= kPlanThreads;                         // a request per thread: looked up once
     s_class[tid] = 0;
-    if (tid == 0) s_most = 1;
+    if (tid == 0) { s_most = 1; s_least = INT32_MAX; }
     Request r;
     int32_t nb = 0;
     auto take = [&](int b0) {                                       // this thread's request of the group from b0 on
@@ -70,15 +72,20 @@ paged_plan_kernel(const Params p, const int items_cap, const int split_cap)
 
     // Blocks and tiles of the whole batch; with one group, the place of this thread's first block too.
     int64_t blocks = 0, tiles = 0, place = 0;
-    int32_t most = 1;
+    int32_t most = 1, least = INT32_MAX;                            // visible tiles of any block
     for (int b0 = 0; b0 < p.c.B; b0 += kPlanThreads) {
         take(b0);
         blocks += nb; tiles += (int64_t)nb * r.tiles();
-        if (nb > 0) most = max(most, r.tiles());
+        if (nb > 0) {
+            most = max(most, r.tiles());
+            const int32_t see = p.causal ? min(r.kv, r.pos0() + p.blk_div / p.blk_mul + 1) : r.kv;   // the first block's
+            least = min(least, see > 0 ? (see + kKeyTile - 1) / kKeyTile : 1);
+        }
     }
     Pair all;
     place = block_prefix(blocks, tiles, s_warp, all).x - blocks;
     atomicMax(&s_most, most);
+    atomicMin(&s_least, least);
     const int32_t tail_at = (int32_t)(all.x * p.Hkv / p.many_ctas * p.many_ctas / p.Hkv);
     const int64_t tail_blocks = all.x - tail_at, units = tail_blocks * p.Hkv;
     const int32_t slice0 = (int32_t)max((all.y * p.Hkv + p.many_ctas - 1) / p.many_ctas, (int64_t)p.min_slice);
@@ -98,7 +105,8 @@ paged_plan_kernel(const Params p, const int items_cap, const int split_cap)
         tail = sum.x;
         const int64_t mean = (tail + tail_blocks - 1) / tail_blocks;
         int64_t best = (units + p.many_ctas - 1) / p.many_ctas * (32 * mean + p.item_cost), len = mean;
-        for (int w = 1; w <= 3; ++w) {
+        const bool even = 3LL * s_least >= 2LL * s_most;            // (block_prefix has synchronised the block)
+        for (int w = 1; w <= 3 && (even || tail_at == 0); ++w) {
             const int32_t cuts = w * p.many_ctas / (int32_t)units;  // slices of a unit of mean length that w waves have room for
             if (cuts < 2) continue;
             const int64_t l = max((mean + cuts - 1) / cuts, (int64_t)p.min_slice);
