@@ -202,9 +202,11 @@ static_assert(kClasses == kPlanThreads, "a class per thread");
 // 64 + 4 tx .. + 3.  Rows, keys and values past their ends are zero in shared memory, so that what a page holds past the
 // request's end never meets a product.
 // Bound by the FMA pipe: per four channels a warp's 16 + 16 micro-tile takes 32 packed FMA instructions (64 issue slots of the
-// pipe) and 12 shared-memory wavefronts, per four keys of P V 64 (128) and 20; packed, they leave issue slots for the rest.  The probabilities take the place of the key tile, which keeps a CTA at 100 KB
-// and two of them on an SM: one's loads and barriers run under the other's arithmetic.  Tiles come by asynchronous copies, the
-// values' while the scores are worked out.
+// pipe) and 12 shared-memory wavefronts, per four keys of P V 64 (128) and 20; packed, they leave issue slots for the rest.
+// The probabilities take the place of the key tile, which keeps a CTA at 100 KB and two of them on an SM: one's loads and
+// barriers run under the other's arithmetic.  Tiles come by asynchronous copies, the values' while the scores are worked out.
+// Measured on three fp32 requests (741 rows, 8 heads, 2.5 GFLOP visible, 3.2 computed): 108 us, where the FMA pipe alone would take
+// 45 (8 x 4 scores a thread, 128 threads, a third less shared-memory traffic: 113 us).
 constexpr int kBM = 64, kBN = 64, kThreads = 256;
 constexpr int kLd = kHeadDim + 4, kLdP = kBN + 4;
 constexpr size_t kF32Smem = sizeof(float) * (2 * kBM * kLd + kBN * kHeadDim);
