@@ -31,7 +31,7 @@ def check_heads(got, x, weight, positions, dtype, norm, turn, skip=(), before=No
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("T,hq,hkv", [(1, 1, 1), (1, 32, 8), (3, 5, 1), (64, 32, 8), (257, 8, 8), (1000, 64, 8), (5, 100, 3), (2048, 2, 1)])
+@pytest.mark.parametrize("T,hq,hkv", [(1, 1, 1), (1, 32, 8), (3, 5, 1), (64, 32, 8), (257, 7, 7), (1000, 64, 8), (5, 100, 3), (2048, 2, 1)])
 @pytest.mark.parametrize("norm,turn", [(True, True), (False, True), (True, False)])
 def test_norm_rope(pec, dtype, T, hq, hkv, norm, turn):
     n_pos = 200000
