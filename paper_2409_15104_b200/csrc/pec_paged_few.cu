@@ -23,6 +23,8 @@
 //           rounding alone.  What it is for is a long run: the wide form draws the 1 kW limit, the SM clock falls to 1.5 GHz and
 //           the stream with it - three requests of 131072 keys, 64 / 8 heads, 5.55 TB/s for seconds (6.37 in a short run)
 //           against 6.46 (6.65); 64 requests of 2400 keys on average, 32 / 8 heads, 4.88 against 5.65.
+//           Both sides of 16 rows, short runs, 64 requests of 3000 keys: 16 rows 131 us against the wide form's 135; 32 rows in 32
+//           columns 260 against 138, the exponentials and stores of P per key no longer fit under the stream.
 //           TMEM columns: S^T [0, 32), two buffers; O^T [32, 64), one per group.
 //
 // Per tile: S(n) into one of two TMEM buffers, P(n) into its place or one of two shared buffers, O += P V.  The issuer's order
