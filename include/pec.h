@@ -452,7 +452,7 @@ int pec_linear_merged(const void *const *o_parts, const float *const *lse_parts,
  *     y = x / sqrt(mean(x^2) + eps) * w                                     if norm, else y = x
  *     z[i] = y[i] cos a - y[i + 64] sin a,  z[i + 64] = y[i + 64] cos a + y[i] sin a,  a = p * theta^(-2 i / 128)
  *                                                                            if rope_table, else z = y
- * in fp32, rounded once to the type of the output (that of the input).
+ * in fp32 (a head whose sum of squares passes 3.4e38 becomes 0), rounded once to the type of the output (that of the input).
  * q [T, Hq, D], k [T, Hkv, D], channel-contiguous with free token and head strides (column slices of a fused QKV tensor);
  * q_out, k_out likewise; q_out may be q (k_out k) with the same strides, any other overlap is not allowed.  Hq or Hkv may
  * be 0: that side's pointers are then not used.  q_weight, k_weight: [D] of the same type, or NULL for 1; used with norm.

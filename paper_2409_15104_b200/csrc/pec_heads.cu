@@ -257,12 +257,9 @@ kv_append_kernel(const Append p, const int parts, const int per)
         pos = (int64_t)kv - end + t;
         const int64_t nth = pos / p.c.page_size;
         slot = pos - nth * p.c.page_size;
-        bool ok = pos >= 0 && nth < p.c.max_pages && (!p.turn.table || pos < p.turn.n_pos);
-        if (ok) {
-            page = p.c.table[b * p.c.table_stride + nth];
-            ok = page >= 0 && page < p.c.num_pages;
-        }
-        if (!ok) {
+        if (pos >= 0 && nth < p.c.max_pages && (!p.turn.table || pos < p.turn.n_pos)) {
+            page = p.c.table[b * p.c.table_stride + nth];           // looked at when the angles are done
+        } else {
             if (lane == 0) raise_status(p.status, PEC_ERR_BAD_INDEX);
             pos = -1;
         }
@@ -275,6 +272,10 @@ kv_append_kernel(const Append p, const int parts, const int per)
         __syncthreads();
     }
     if (pos < 0) return;
+    if (page < 0 || page >= p.c.num_pages) {
+        if (lane == 0) raise_status(p.status, PEC_ERR_BAD_INDEX);
+        return;
+    }
     Map m;
     make_map<E>(m, math && p.norm ? p.kw : nullptr, turn ? sh.cos[warp] : nullptr, sh.sin[warp], l);
     E *dst = static_cast<E *>(is_k ? p.k_pages : p.v_pages) + page * (is_k ? p.c.k_sp : p.c.v_sp) + slot * (is_k ? p.c.k_st : p.c.v_st) +
