@@ -539,3 +539,80 @@ def test_the_binding_refuses_what_the_library_cannot_see(pec):
     with pytest.raises(binding.PecError):
         pec.pec_qk_norm_rope(q, eps=0.0)
     pec.check_status()
+
+
+def _chain(pec, hq, hkv, page, S, seed):
+    """State and one step of a decode chain whose kernels follow each other without a pause: projection output -> norm and rotation ->
+    append -> attention -> the next step's input."""
+    torch.manual_seed(seed)
+    num = -(-S // page)
+    st = dict(kp=torch.zeros((num, page, hkv, 128), dtype=BF16, device=DEV), vp=torch.zeros((num, page, hkv, 128), dtype=BF16, device=DEV),
+              ids=torch.randperm(num, device=DEV)[None].int(), cu=dev([0, 1]), kv=dev([0]), pos=dev([0]), tables=pec.pec_rope_table(THETA, S, DEV),
+              x=torch.randn((1, hq * 128), device=DEV).to(BF16), w=(torch.randn(((hq + 2 * hkv) * 128, hq * 128), device=DEV) / 30).to(BF16))
+
+    def step():
+        st["kv"] += 1                                             # torch kernels, copies and a GEMM in between
+        st["pos"].copy_(st["kv"])
+        st["pos"] -= 1
+        qkv = pec.pec_linear(st["x"], st["w"]).view(1, hq + 2 * hkv, 128)
+        q, _ = pec.pec_qk_norm_rope(qkv[:, :hq], tables=st["tables"], positions=st["pos"])
+        pec.pec_kv_append(qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], st["kp"], st["vp"], st["ids"], st["cu"], st["kv"], norm=True, tables=st["tables"])
+        o, _ = pec.pec_paged_attn(q, st["kp"], st["vp"], st["ids"], st["cu"], st["kv"], max_q_len=1)
+        st["x"].copy_(o.view(1, hq * 128))
+
+    return st, step
+
+
+def test_steps_without_a_pause_give_the_bits_of_steps_with_one(pec):
+    """300 decode steps back to back, with a synchronisation after every kernel's step, and replayed from a graph."""
+    ends = []
+    for mode in ("paused", "flowing", "graph"):
+        st, step = _chain(pec, 8, 2, 16, 400, 5)
+        graph = None
+        for i in range(300):
+            if mode == "graph" and i == 10:
+                graph = torch.cuda.CUDAGraph()
+                kept = {k: st[k].clone() for k in ("kv", "pos", "x", "kp", "vp")}
+                with torch.cuda.graph(graph):
+                    step()
+                for k, v in kept.items():
+                    st[k].copy_(v)
+            graph.replay() if graph else step()
+            if mode == "paused":
+                torch.cuda.synchronize()
+        pec.check_status()
+        assert int(st["kv"]) == 300
+        ends.append((st["x"].clone(), st["kp"].clone(), st["vp"].clone()))
+    for other in ends[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(ends[0], other))
+
+
+def test_a_capture_with_other_nodes_and_a_fork(pec):
+    """Captured behind copies, fills, torch kernels and a joined side stream; replays read what those nodes wrote."""
+    binding.status_word(torch.device(DEV))
+    kv = [700, 300]
+    kp, vp, table = ref.make_cache(95, kv, 16, 2, BF16, DEV, poison=False, wild=False)
+    for n in ([1, 1], [150, 2]):
+        cu, lens, true_lens, src = dev(ref.offsets(n)), dev(kv), dev(kv), torch.randn((sum(n), 8, 128), device=DEV).to(BF16)
+        q = torch.empty_like(src)
+        o, lse = torch.empty_like(src), torch.empty(src.shape[:2], device=DEV)
+        call = lambda: pec.pec_paged_attn(q, kp, vp, table, cu, lens, max_q_len=max(n), o=o, lse=lse)
+        q.copy_(src)
+        call()
+        g = torch.cuda.CUDAGraph()
+        side = torch.cuda.Stream()
+        with torch.cuda.graph(g):
+            q.zero_()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                lens.fill_(0)
+                lens.add_(true_lens)
+            q.copy_(src)
+            torch.cuda.current_stream().wait_stream(side)
+            call()
+        for _ in range(3):
+            src.normal_()
+            o.fill_(7.0)
+            g.replay()
+            pec.check_status()
+            ref.check_attend(o, lse, ref.attend(src, kp, vp, table, cu.tolist(), kv), BF16, f"captured behind other nodes {n}")
