@@ -34,7 +34,7 @@ def _build_torch_module(force: bool) -> None:
     for d in includes:
         cmd += ["-isystem" if d != INCLUDE else "-I", d]
     cmd += [os.path.join(CSRC, TORCH_SOURCE), "-o", TORCH_MODULE, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu",
-            "-lc10", "-lc10_cuda"]
+            "-ltorch_cuda", "-lc10", "-lc10_cuda"]
     subprocess.run(cmd, check=True)
 
 
