@@ -364,7 +364,7 @@ paged_f32_kernel(const Params p)
     copy_wait<0>();                          // Q's copies, where there was no tile
 
     const int64_t slot = (int64_t)it.slot * p.Hkv + kvh;
-    if (it.slices > 1 && slot >= p.many_cap) return;               // cannot happen (see many_plan); never write past the scratch
+    if (it.slices > 1 && slot >= p.many_cap) return;               // cannot happen (see paged_plan_kernel); never write past the scratch
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int32_t r = ty * 4 + i;
@@ -390,14 +390,15 @@ paged_f32_kernel(const Params p)
 }
 
 // ------------------------------------------------------------------------------------------ combining partials
-// A CTA merges the partial results of some packed rows of one unit: a (request, KV head) whose
-// tiles cross a cut of the line, or a block of rows whose keys are cut into slices (listed by the plan).  Units are enumerated by
-// what splits them - CTA c of the few class looks at cut c and takes the unit around it if this is the unit's first cut - or, where
-// there are fewer units than cuts, one by one, so that the grid has the size of what can be split, not of the batch.  (A CTA per token and KV head took 66 us to find nothing to do for
-// 2048 tokens.)  The few class looks its unit up before the attention kernels end (the tables were complete before they began);
-// partials are read afterwards, and no CTA ends before that wait, so that whatever follows on the stream follows those kernels too.
+// A CTA merges the partial results of some packed rows of one unit: a (request, KV head) whose tiles cross a cut of the line, or a
+// block of rows whose keys are cut into slices (listed by the plan).  Units are enumerated by what splits them - CTA c of the few
+// class looks at cut c and takes the unit around it if this is the unit's first cut - or, where there are fewer units than cuts, one
+// by one, so that the grid has the size of what can be split, not of the batch.  (A CTA per token and KV head took 66 us to find
+// nothing to do for 2048 tokens; 32 tokens over 32000, 8 units: 61 us by cut, 40 by unit.)  The few class looks its unit up before
+// the attention kernels end (the tables were complete before they began); partials are read afterwards, and no CTA ends before that
+// wait, so that whatever follows on the stream follows those kernels too.
 // A warp merges one row at a time, a lane owning four channels: the largest LSE first, then the weighted sum, sixteen partials'
-// loads in flight.
+// loads in flight.  Bound by latency: two dependent reads, 3 to 4 us with the launch.
 constexpr int kCombineWarps = 8, kManyGroup = 32;
 
 __device__ __forceinline__ void combine_row(const Params &p, const float *po, const float *pl, int64_t at0, int64_t shift, int64_t step,
@@ -607,7 +608,7 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
         floats = 2 * (size_t)p.few_ctas * p.few_rows * (kHeadDim + 1);
         floats = (floats + 3) & ~(size_t)3;
     }
-    // Blocks of the many class, the grid bound and the partial slots it may take (see many_plan).
+    // Blocks of the many class, the grid bound and the partial slots it may take (see paged_plan_kernel).
     const int tps = kFewRows / p.g;           // tensor cores: two stages of whole tokens; FMA: 64 packed rows
     p.blk_mul = tensor ? 1 : p.g; p.blk_div = tensor ? 2 * tps : kBM;
     p.many_rows = tensor ? 2 * tps * p.g : kBM;
