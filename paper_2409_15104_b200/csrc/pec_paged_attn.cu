@@ -2,6 +2,7 @@
 // kernel that merges partial results.
 #include <cuda_bf16.h>
 #include <cmath>
+#include <numeric>
 #include <cuda_runtime.h>
 #include "pec_host.h"
 #include "pec_internal.h"
@@ -553,6 +554,19 @@ struct Call {
 inline bool aligned16(const void *x) { return (reinterpret_cast<uintptr_t>(x) & 15u) == 0; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// false: the numbers do not fit a tensor map's 32-bit coordinate.
+static bool fold_pages(int64_t sp, int64_t sh, int64_t num_pages, int64_t Hkv, FoldedPages &f)
+{
+    if (num_pages == 1) sp = 0;               // strides that no address uses
+    if (Hkv == 1) sh = 0;
+    const int64_t unit = std::gcd(sp, sh), most = ((int64_t)1 << 31) - 1;
+    f = {unit > 0 ? unit : kHeadDim, 0, 0};
+    const int64_t page = sp / f.unit, head = sh / f.unit;
+    if (page > most || head > most || (num_pages - 1) * page > most || (num_pages - 1) * page + (Hkv - 1) * head > most) return false;
+    f.page = (int32_t)page; f.head = (int32_t)head;
+    return true;
+}
+
 // Checks the arguments and works out the launch.
 static int resolve(const char *who, const pec_paged_args *a, Call &c)
 {
@@ -583,6 +597,10 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
         return PEC_ERR_ALIGNMENT;
     }
     if (a->T * (a->Hq / a->Hkv) > ((int64_t)1 << 31) - 1024) { set_error("%s: T * Hq / Hkv near 2^31 or above unsupported", who); return PEC_ERR_UNSUPPORTED; }
+    if (a->dtype == PEC_BF16 && !(fold_pages(p.c.k_sp, p.c.k_sh, p.c.num_pages, a->Hkv, p.fk) && fold_pages(p.c.v_sp, p.c.v_sh, p.c.num_pages, a->Hkv, p.fv))) {
+        set_error("%s: the pages reach over 2^31 times the greatest common divisor of their page and head strides", who);
+        return PEC_ERR_UNSUPPORTED;
+    }
     p.q = a->q; p.k_pages = a->k_pages; p.v_pages = a->v_pages;
     p.q_st = a->q_stride_t; p.q_sh = a->q_stride_h;
     p.o = a->o; p.lse = a->lse; p.o_is_bf16 = a->o_dtype == PEC_BF16;

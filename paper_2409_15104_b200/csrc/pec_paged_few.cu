@@ -85,14 +85,15 @@ __device__ __forceinline__ bool wait_all(uint64_t *bar, uint32_t parity, Shared 
     return __all_sync(0xffffffffu, wait_bar(bar, parity, sh, p));
 }
 
-// Eight K steps of D (+)= A B as one statement: descriptors are the first one's plus constants (in 16-byte units).  kA: 0 = a
-// K-major 128-row tile whose second 64 channels lie kHalfTileBytes on; 1 = an M-major tile, 2048 bytes a step.  B: K-major, 16
+// Eight K steps of D (+)= A B as one statement: descriptors are the first one's plus constants (in 16-byte units).  A: a tile of the
+// ring, kA = 0 K-major (K: 16 channels a step, the second 64 in the groups' second halves), 1 M-major (V: two groups a step).  B: K-major, 16
 // rows, its second 64 columns 2048 bytes on.
 template <int kA>
 __device__ __forceinline__ void mma_narrow(uint32_t d, uint64_t a0, uint64_t b0, uint32_t idesc, uint32_t accumulate)
 {
-    constexpr int a1 = kA ? 128 : 2, a2 = kA ? 256 : 4, a3 = kA ? 384 : 6, h = kHalfTileBytes >> 4;
-    constexpr int a4 = kA ? 512 : h, a5 = kA ? 640 : h + 2, a6 = kA ? 768 : h + 4, a7 = kA ? 896 : h + 6;
+    constexpr int h = kGroupHalf >> 4, s = 2 * kGroupBytes >> 4;
+    constexpr int a1 = kA ? s : 2, a2 = kA ? 2 * s : 4, a3 = kA ? 3 * s : 6, a4 = kA ? 4 * s : h, a5 = kA ? 5 * s : h + 2;
+    constexpr int a6 = kA ? 6 * s : h + 4, a7 = kA ? 7 * s : h + 6;
     asm volatile(
         "{\n\t.reg .pred p0, pt;\n\t.reg .b64 da, db;\n\t"
         "setp.ne.u32 p0, %4, 0;\n\t"
@@ -288,8 +289,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
                     __syncwarp();
                     if (bl.used && k0 + bl.first < kv)
-                        tma_load_4d(sRing + (uint32_t)slot * kTileBytes + bl.offset, which ? (const void *)&tm_v : (const void *)&tm_k, bar,
-                                    bl.half * 64, kvh, at.row, page);
+                        load_box(sRing + (uint32_t)slot * kTileBytes, which ? (const void *)&tm_v : (const void *)&tm_k, bar, bl, which ? p.fv : p.fk,
+                                 kvh, at.row, page);
                     ++issued;
                 }
                 page = page_next;
@@ -315,8 +316,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         const bool leader = elect_one();
         constexpr uint32_t narrow_qk = idesc_bf16_f32(128, kNarrowRows, 0, 0), narrow_pv = idesc_bf16_f32(kHeadDim, kNarrowRows, 1, 0);
         constexpr uint32_t idesc_qk = idesc_bf16_f32(128, 128, 0, 0), idesc_pv = idesc_bf16_f32(128, kHeadDim, 0, 1);
-        constexpr uint32_t kBox16 = kHalfTileBytes >> 4;
-        const uint64_t k_ring = smem_desc_sw128(sRing, 16, 1024), v_ring = smem_desc_sw128(sRing, kHalfTileBytes, 1024);
+        const uint64_t k_ring = smem_desc_sw128(sRing, 16, kGroupBytes), v_ring = smem_desc_sw128(sRing, kGroupHalf, kGroupBytes);
         uint32_t p_phase = 0;                              // bit 2 g + buffer: parity of the next p_ready
         auto kv_wait = [&](int item) { return wait_all(&sh->kv_full[item % kSlots], (item / kSlots) & 1, sh, p); };
         auto kv_release = [&](int item) { if (leader) tc_commit(smem_u32(&sh->kv_empty[item % kSlots])); };
@@ -333,7 +333,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)
                         a[ks] = smem_desc_sw128(sQ + (uint32_t)g * kTileBytes + (uint32_t)(ks >> 2) * kHalfTileBytes + (uint32_t)(ks & 3) * 32u, 16, 1024);
-                    mma_ss_k128_commit<kBox16>(tmem + (uint32_t)(n & 1) * C::kCols, a, k0, idesc_qk, smem_u32(&sh->s_full[g][n & 1]));
+                    mma_ss_k128_commit<(kGroupHalf >> 4)>(tmem + (uint32_t)(n & 1) * C::kCols, a, k0, idesc_qk, smem_u32(&sh->s_full[g][n & 1]));
                 }
                 if (last) tc_commit(smem_u32(&sh->q_empty[g]));
             }
@@ -378,8 +378,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                         mma_narrow<1>(tO, v0, p0, narrow_pv, j > 0 ? 1u : 0u);
                         mma_narrow<1>(tO, v0, p0 + (C::kQBytes >> 4), narrow_pv, 1u);
                     } else {
-                        mma_ts_k64(tO, tP, v0, idesc_pv, j > 0 ? 1u : 0u);
-                        mma_ts_k64(tO, tP + 32, v0 + (64 * 128 >> 4), idesc_pv, 1u);
+                        mma_pv_k64(tO, tP, v0, idesc_pv, j > 0 ? 1u : 0u);
+                        mma_pv_k64(tO, tP + 32, v0 + (8 * kGroupBytes >> 4), idesc_pv, 1u);
                     }
                     tc_commit(smem_u32(&sh->pv_done[g]));
                 }
@@ -684,8 +684,8 @@ int launch_paged_few(const paged::Params &p, bool after_many, cudaStream_t strea
     const int box = host_map::box_rows(p.c.page_size);
     const int tps = kFewRows / p.g, q_tokens = tps < p.max_q ? tps : p.max_q;
     CUtensorMap tm_q, tm_k, tm_v;
-    if (!host_map::queries(&tm_q, p, q_tokens) || !host_map::pages(&tm_k, p, p.k_pages, p.c.k_sp, p.c.k_st, p.c.k_sh, box) ||
-        !host_map::pages(&tm_v, p, p.v_pages, p.c.v_sp, p.c.v_st, p.c.v_sh, box)) {
+    if (!host_map::queries(&tm_q, p, q_tokens) || !host_map::pages(&tm_k, p, p.k_pages, p.c.k_st, p.fk, box) ||
+        !host_map::pages(&tm_v, p, p.v_pages, p.c.v_st, p.fv, box)) {
         set_error("pec_paged_attn: cuTensorMapEncodeTiled failed (driver too old, or strides/addresses not encodable)");
         return PEC_ERR_CUDA;
     }

@@ -77,8 +77,7 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
         __syncwarp();
         if (mine)
-            tma_load_4d(sRing + (uint32_t)slot * kTileBytes + bl.offset, which ? (const void *)&tm_v : (const void *)&tm_k, bar, bl.half * 64, kvh,
-                        at.row, page);
+            load_box(sRing + (uint32_t)slot * kTileBytes, which ? (const void *)&tm_v : (const void *)&tm_k, bar, bl, which ? p.fv : p.fk, kvh, at.row, page);
     };
     if (warp == kLoadWarp) {
         // The kernel for few rows may start on SMs that this grid leaves.  The plan has to be complete before its list is read.
@@ -206,23 +205,22 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             auto kv_wait = [&](int item) { return wait_all(&sh->kv_full[item % kSlots], (item / kSlots) & 1, sh, p); };
             auto kv_release = [&](int item) { if (leader) tc_commit(smem_u32(&sh->kv_empty[item % kSlots])); };
             const uint32_t tS = tmem + kColS, tP = tmem + kColP + st * 64, tO = tmem + kColO + st * kTile;
-            constexpr uint32_t kBox16 = kHalfTileBytes >> 4;
             uint64_t a_desc[8];
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks)
                 a_desc[ks] = smem_desc_sw128(sQ + st * kTileBytes + (uint32_t)(ks >> 2) * kHalfTileBytes + (uint32_t)(ks & 3) * 32u, 16, 1024);
-            const uint64_t k_ring = smem_desc_sw128(sRing, 16, 1024), v_ring = smem_desc_sw128(sRing, kHalfTileBytes, 1024);
+            const uint64_t k_ring = smem_desc_sw128(sRing, 16, kGroupBytes), v_ring = smem_desc_sw128(sRing, kGroupHalf, kGroupBytes);
             const int n_st = sh->g.n[st], n_ot = sh->g.n[st ^ 1];
             const int32_t key_lo = sh->g.key_lo, kv = sh->g.kv;
             auto issue_qk = [&](int j) {
                 const uint64_t k0 = k_ring + (uint32_t)((((2 * j) % kSlots) * kTileBytes) >> 4);
-                if (leader) mma_ss_k128_commit<kBox16>(tS, a_desc, k0, idesc_qk, smem_u32(&sh->s_full[st]));
+                if (leader) mma_ss_k128_commit<(kGroupHalf >> 4)>(tS, a_desc, k0, idesc_qk, smem_u32(&sh->s_full[st]));
             };
             auto issue_pv = [&](int j) {
                 const uint64_t v0 = v_ring + (uint32_t)((((2 * j + 1) % kSlots) * kTileBytes) >> 4);
                 if (leader) {
-                    mma_ts_k64(tO, tP, v0, idesc_pv, j > 0 ? 1u : 0u);
-                    mma_ts_k64(tO, tP + 32, v0 + (64 * 128 >> 4), idesc_pv, 1u);
+                    mma_pv_k64(tO, tP, v0, idesc_pv, j > 0 ? 1u : 0u);
+                    mma_pv_k64(tO, tP + 32, v0 + (8 * kGroupBytes >> 4), idesc_pv, 1u);
                     tc_commit(smem_u32(&sh->pv_done[st]));
                 }
             };
@@ -458,8 +456,8 @@ int launch_paged_many(const paged::Params &p, int64_t items, cudaStream_t stream
     using namespace paged;
     const int box = host_map::box_rows(p.c.page_size);
     CUtensorMap tm_q, tm_k, tm_v;
-    if (!host_map::queries(&tm_q, p, kFewRows / p.g) || !host_map::pages(&tm_k, p, p.k_pages, p.c.k_sp, p.c.k_st, p.c.k_sh, box) ||
-        !host_map::pages(&tm_v, p, p.v_pages, p.c.v_sp, p.c.v_st, p.c.v_sh, box)) {
+    if (!host_map::queries(&tm_q, p, kFewRows / p.g) || !host_map::pages(&tm_k, p, p.k_pages, p.c.k_st, p.fk, box) ||
+        !host_map::pages(&tm_v, p, p.v_pages, p.c.v_st, p.fv, box)) {
         set_error("pec_paged_attn: cuTensorMapEncodeTiled failed (driver too old, or strides/addresses not encodable)");
         return PEC_ERR_CUDA;
     }

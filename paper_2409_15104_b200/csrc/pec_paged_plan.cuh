@@ -23,10 +23,15 @@ namespace paged {
 constexpr int kKeyTile = 128;                 // keys per tile
 constexpr int kFewRows = 128;                 // packed rows of the few class
 // Device-side description of one call, passed to the kernels by value.
+// Where the rows of a page's head begin, as one number for the tensor maps, whose five dimensions a box of both channel halves
+// takes up: (page * .page + head * .head) units of `unit` elements, the greatest common divisor of the two strides.
+struct FoldedPages { int64_t unit; int32_t page, head; };
+
 struct Params {
     const void *q, *k_pages, *v_pages;
     int64_t q_st, q_sh;
     PagedCache c;
+    FoldedPages fk, fv;                       // bf16
     void *o;
     float *lse;
     int32_t o_is_bf16;

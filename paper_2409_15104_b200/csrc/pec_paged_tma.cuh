@@ -21,18 +21,38 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, uint
         ::"r"(dst), "l"(tmap), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
 }
 
-// A 128-key tile comes in boxes of `box` = gcd(page_size, 128) rows x 64 channels: such a box never crosses a page, whatever the
-// page size (a multiple of 8, so that a box is whole 8-row swizzle groups and lands on a 1024-byte boundary).  Lane i of the
-// loading warp takes rows (i / 2) * box .. of channel half i % 2; boxes past the request's end are not loaded.
-struct BoxLane { int32_t first; uint32_t offset; int half; bool used; };
+// 5-D tiled load, coordinates innermost first.
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const void *tmap, uint32_t bar, int c0, int c1, int c2, int c3, int c4)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+        ::"r"(dst), "l"(tmap), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4) : "memory");
+}
+
+// A 128-key tile lies in shared memory as 16 groups of eight keys, a group as its two channel halves of eight 128-byte rows
+// (128-byte swizzle): groups 2048 bytes apart, halves 1024.  It comes in boxes of `box` = gcd(page_size, 128) keys, both halves at
+// once: such a box never crosses a page, whatever the page size (a multiple of 8, so that a box is whole groups).  Lane i of the
+// loading warp takes keys i * box ..; boxes past the request's end are not loaded.
+// The copy unit takes 85 to 110 cycles a box whatever its size, and a tile of K and V has 2800 at the rate of HBM: with a box per
+// half (the halves 16 KB apart) pages of 16 tokens took 244 us where pages of 64 took 191 (three requests of 131072 keys), pages of
+// 8 tokens 381; with both halves in one box 198, 190 and 246.
+constexpr uint32_t kGroupBytes = 2048, kGroupHalf = 1024;
+struct BoxLane { int32_t first; uint32_t offset; bool used; };
 __device__ __forceinline__ BoxLane box_lane(int box, int lane)
 {
-    BoxLane l;
-    l.half = lane & 1;
-    l.first = (lane >> 1) * box;
-    l.used = l.first < kKeyTile;
-    l.offset = (uint32_t)l.half * kHalfTileBytes + (uint32_t)l.first * 128u;
-    return l;
+    const int32_t first = lane * box;
+    return {first, (uint32_t)(first >> 3) * kGroupBytes, first < kKeyTile};
+}
+__device__ __forceinline__ void load_box(uint32_t tile, const void *tmap, uint32_t bar, const BoxLane &l, const FoldedPages &f, int kvh, int row, int page)
+{
+    tma_load_5d(tile + l.offset, tmap, bar, 0, 0, 0, row >> 3, page * f.page + kvh * f.head);
+}
+// Four K steps (16 keys each) of D (+)= A B with A in tensor memory (8 columns per step) and B the N-major V tile.
+__device__ __forceinline__ void mma_pv_k64(uint32_t d_tmem, uint32_t a_tmem, uint64_t b0, uint32_t idesc, uint32_t accumulate)
+{
+    mma_ts(d_tmem, a_tmem, b0, idesc, accumulate);
+#pragma unroll
+    for (uint32_t ks = 1; ks < 4; ++ks) mma_ts(d_tmem, a_tmem + 8 * ks, b0 + (2 * kGroupBytes >> 4) * ks, idesc, 1u);
 }
 // Where this lane's box of a key tile lies: the number in the request's list of pages and the row of the page.  Walked from tile
 // to tile without divisions, which would sit between a free slot and its next load.
@@ -72,7 +92,7 @@ __device__ __forceinline__ void clear_tail(uint32_t tile, int32_t valid, int lan
 {
     if (valid < 0) valid = 0;
     for (int i = valid * 16 + lane; i < kKeyTile * 16; i += 32) {
-        const uint32_t a = tile + (uint32_t)(i & 8 ? kHalfTileBytes : 0u) + (uint32_t)(i >> 4) * 128u + (uint32_t)(i & 7) * 16u;
+        const uint32_t a = tile + (uint32_t)(i >> 7) * kGroupBytes + (i & 8 ? kGroupHalf : 0u) + (uint32_t)((i >> 4) & 7) * 128u + (uint32_t)(i & 7) * 16u;
         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(a), "r"(0) : "memory");
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -112,11 +132,17 @@ inline bool queries(CUtensorMap *map, const Params &p, int tokens)
     return encode(map, p.q, {(uint64_t)kHeadDim, (uint64_t)p.g, (uint64_t)p.Hkv, (uint64_t)p.c.T}, {p.q_sh, p.q_sh * p.g, p.q_st},
                   {64u, (uint32_t)p.g, 1u, (uint32_t)tokens});
 }
-// Pages: channel, KV head, token of the page, page.
-inline bool pages(CUtensorMap *map, const Params &p, const void *base, int64_t sp, int64_t st, int64_t sh, int box)
+// Pages: 64 channels, eight tokens, channel half, eight-token groups of a page, page and head (FoldedPages).
+inline bool pages(CUtensorMap *map, const Params &p, const void *base, int64_t st, const FoldedPages &f, int box)
 {
-    return encode(map, base, {(uint64_t)kHeadDim, (uint64_t)p.Hkv, (uint64_t)p.c.page_size, (uint64_t)p.c.num_pages}, {sh, st, sp},
-                  {64u, 1u, (uint32_t)box, 1u});
+    const host::EncodeTiledFn fn = host::encode_fn();
+    if (!fn) return false;
+    const cuuint64_t last = (cuuint64_t)(p.c.num_pages - 1) * f.page + (cuuint64_t)(p.Hkv - 1) * f.head;
+    const cuuint64_t d[5] = {64, 8, 2, (cuuint64_t)p.c.page_size / 8, last + 1};
+    const cuuint64_t s[4] = {(cuuint64_t)st * 2, 128, (cuuint64_t)st * 16, (cuuint64_t)f.unit * 2};
+    const cuuint32_t b[5] = {64, 8, 2, (cuuint32_t)box / 8, 1}, e[5] = {1, 1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), d, s, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 inline int box_rows(int page_size)
 {

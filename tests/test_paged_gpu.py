@@ -458,6 +458,42 @@ def test_page_sizes_and_a_cache_of_one_page(pec, page, total):
         attend(pec, page + n, [n], [total], 4, 1, page, BF16, known=n == 1, what=f"pages of {page}, {n} new")
 
 
+def _other_order(pages, order):
+    """The same pages [P, page, Hkv, 128] behind other strides; what lies between them is NaN."""
+    P, page, hkv, d = pages.shape
+    if order == "heads first":
+        return pages.permute(2, 0, 1, 3).contiguous().permute(1, 2, 0, 3)
+    if order == "between a token's others":
+        full = torch.full((P, page, hkv, 2, d), float("nan"), dtype=pages.dtype, device=DEV)
+        full[:, :, :, 1] = pages
+        return full[:, :, :, 1]
+    if order == "a layer's pages":
+        full = torch.full((P, 3, page, hkv, d), float("nan"), dtype=pages.dtype, device=DEV)
+        full[:, 1] = pages
+        return full[:, 1]
+    st = hkv * 136 + 8                                             # strides whose greatest common divisor is 8 elements
+    full = torch.full((P * (page * st + 24),), float("nan"), dtype=pages.dtype, device=DEV)
+    out = full.as_strided(pages.shape, (page * st + 24, st, 136, 1))
+    out.copy_(pages)
+    return out
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k_order,v_order", [("heads first", "heads first"), ("between a token's others", "a layer's pages"),
+                                             ("a layer's pages", "odd strides"), ("odd strides", "heads first")])
+@pytest.mark.parametrize("n,kv,hq,hkv,page", [([1, 1, 1], [700, 130, 33], 8, 2, 16), ([3, 20], [900, 260], 6, 3, 24),
+                                              ([200, 1], [500, 300], 8, 1, 64), ([1], [200], 4, 4, 256)])
+def test_orders_of_the_cache(pec, dtype, k_order, v_order, n, kv, hq, hkv, page):
+    kp, vp, table = ref.make_cache(71, kv, page, hkv, dtype, DEV)
+    cu = ref.offsets(n)
+    q = torch.randn((cu[-1], hq, 128), generator=torch.Generator().manual_seed(72)).to(dtype).to(DEV)
+    plain = pec.pec_paged_attn(q, kp, vp, table, dev(cu), dev(kv), max_q_len=max(n))
+    o, lse = pec.pec_paged_attn(q, _other_order(kp, k_order), _other_order(vp, v_order), table, dev(cu), dev(kv), max_q_len=max(n))
+    pec.check_status()
+    ref.check_attend(o, lse, ref.attend(q, kp, vp, table, cu, kv), dtype, f"{k_order}, {v_order}")
+    assert torch.equal(o, plain[0]) and torch.equal(lse, plain[1]), "the order of the cache changed bits"
+
+
 def test_partials_of_two_caches_merge(pec):
     """A long request's cache on two holders (Section 5.2): the new token's fp32 partials over either part, merged."""
     kp, vp, table = ref.make_cache(71, [900, 500], 16, 2, BF16, DEV)

@@ -103,6 +103,19 @@ def test_paged_attn_validates_on_the_host(over, code):
     assert lib.pec_paged_attn(None, None) == -1
 
 
+@pytest.mark.parametrize("over,bf16", [
+    (dict(k_pages_stride_p=16 * 8 * 128 + 8, num_pages=(1 << 31) - 1), -2),          # common divisor 8: page numbers times 2049
+    (dict(k_pages_stride_p=16 * 8 * 128 + 8, num_pages=1 << 20), -2), (dict(k_pages_stride_p=16 * 8 * 128 + 8, num_pages=1 << 19), 0),
+    (dict(num_pages=(1 << 24) - 1), 0), (dict(v_pages_stride_h=1 << 45), -2),
+    (dict(v_pages_stride_h=1 << 45, Hkv=1), 0), (dict(v_pages_stride_p=(1 << 45) + 8, num_pages=1), 0), (dict(v_pages_stride_p=(1 << 45) + 8), -2),
+])
+def test_strides_that_the_tensor_maps_cannot_hold(over, bf16):
+    lib = binding.load()
+    for dtype, code in ((binding.PEC_BF16, bf16), (binding.PEC_F32, 0)):
+        a = _paged(dtype=dtype, o_dtype=binding.PEC_F32, **over)
+        assert lib.pec_paged_attn(ctypes.byref(a), None) == code, binding.pec_last_error()
+
+
 def test_paged_attn_asks_for_its_workspace():
     lib = binding.load()
     a = _paged(T=64, max_q_len=1, max_pages=1000, table_stride=1000, num_pages=100000, B=64)
