@@ -27,6 +27,8 @@ namespace paged {
 // Slots that cut units take: cutting units of length l into slices of S takes less than sum l / S + their number.  slice0 >= all
 // tiles / many_ctas, and units longer than that are fewer than many_ctas: 2 many_ctas.  The tail has less than many_ctas + Hkv
 // units of mean length m and slice1 >= m / cuts with cuts * units <= 3 many_ctas: 4 many_ctas + Hkv.
+// Items that cutting adds (the grid has a CTA for each, used or not, and one that finds nothing takes its SM 1.4 us: 888 more of them
+// cost 24 requests of 300 tokens 9 us of 195, 296 fewer saved 1.2 of 174.9): ceil(l / S) - 1 < l / S of a unit, in all many_ctas for slice0 and 3 many_ctas for slice1.
 // Items go into the list longest first (by 256 classes of visible tiles): an SM that falls free late finds short work.  The order
 // inside a class is whatever the atomics make it; it changes when an item runs, never what it computes.
 constexpr int kPlanThreads = 256, kClasses = 256;
@@ -638,7 +640,7 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
     if (!p.few || (int64_t)p.max_q * p.g > kFewRows) {
         const int64_t shortest = p.few ? kFewRows / p.g + 1 : 1, most = a->T / shortest;       // new tokens of such a request; how many there can be
         const int64_t blocks = a->T * p.blk_mul / p.blk_div + (a->B < most ? a->B : most);
-        c.many_items = blocks + ceil_div(6 * (int64_t)p.many_ctas, p.Hkv) + 2;                 // whole blocks and slots
+        c.many_items = blocks + ceil_div(4 * (int64_t)p.many_ctas, p.Hkv) + 2;                 // blocks and what cutting adds to them
         const int64_t most_slices = ceil_div(ceil_div((int64_t)a->max_pages * a->page_size, kKeyTile), p.min_slice);
         int64_t cap = 6 * (int64_t)p.many_ctas + p.Hkv;
         if (most_slices <= 1) cap = 0;
