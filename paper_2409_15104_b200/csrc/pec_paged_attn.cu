@@ -87,6 +87,15 @@ paged_plan_kernel(const Params p, const int items_cap, const int split_cap)
     }
     Pair all;
     place = block_prefix(blocks, tiles, s_warp, all).x - blocks;
+    // Offsets that go back and forth make requests whose tokens overlap, each fine by itself: more blocks than T tokens can have,
+    // and with them more items and slots than the workspace holds.  Such a batch gets no items.
+    if (all.x > p.many_blocks) {
+        if (tid == 0) {
+            raise_status(p.status, PEC_ERR_BAD_INDEX);
+            p.many_count[0] = p.many_count[1] = 0;
+        }
+        return;
+    }
     atomicMax(&s_most, most);
     atomicMin(&s_least, least);
     const int32_t tail_at = (int32_t)(all.x * p.Hkv / p.many_ctas * p.many_ctas / p.Hkv);
@@ -646,8 +655,9 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
         if (most_slices <= 1) cap = 0;
         else if (blocks * most_slices * p.Hkv < cap) cap = blocks * most_slices * p.Hkv;
         p.many_cap = (int32_t)cap;
+        if (c.many_items > ((int64_t)1 << 26)) { set_error("%s: more than 2^26 blocks of rows unsupported", who); return PEC_ERR_UNSUPPORTED; }
+        p.many_blocks = (int32_t)blocks;
     }
-    if (c.many_items > ((int64_t)1 << 26)) { set_error("%s: more than 2^26 blocks of rows unsupported", who); return PEC_ERR_UNSUPPORTED; }
     p.items_cap = (int32_t)c.many_items;
     const size_t slots = (((size_t)p.many_cap * p.many_rows * (kHeadDim + 1)) + 3) & ~(size_t)3;
     const size_t list = c.many_items > 0 ? 4 + (c.many_items + p.many_cap / 2) * sizeof(Item) / sizeof(float) : 0;

@@ -52,6 +52,7 @@ struct Params {
     int32_t min_slice;                        // key tiles of the shortest slice
     int32_t item_cost, merge_cost;            // start and end of a CTA, a slice's partial: 1/32 of a tile's time (see paged_plan_kernel)
     int32_t many_rows;                        // rows of a partial slot
+    int32_t many_blocks;                      // bound of the batch's blocks, from which many_cap and items_cap follow
     int32_t many_cap, items_cap;              // slots and items that the workspace holds
     float *many_o, *many_lse;
     int32_t *many_count;                      // [2]: items, blocks that are cut

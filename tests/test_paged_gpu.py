@@ -652,3 +652,31 @@ def test_a_capture_with_other_nodes_and_a_fork(pec):
             g.replay()
             pec.check_status()
             ref.check_attend(o, lse, ref.attend(src, kp, vp, table, cu.tolist(), kv), BF16, f"captured behind other nodes {n}")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cu", [[0, 200] * 32 + [0], [200, 0] * 32 + [200], [0, 200, 200, 0] * 16 + [200]])
+def test_overlapping_offsets_stay_inside_the_workspace(pec, dtype, cu):
+    """Offsets that go back and forth: every second request is in order by itself, together they have many times the blocks of
+    T tokens.  The workspace has exactly the size asked for; what lies around it is neither written nor merged into a result."""
+    kp, vp, table = ref.make_cache(26, [1024] * 64, 128, 1, dtype, DEV)
+    q = torch.randn((200, 1, 128), device=DEV).to(dtype)
+    a = binding.pec_paged_args()
+    a.q, a.k_pages, a.v_pages, a.block_table, a.cu_q, a.kv_lens, a.o, a.lse, a.status = [1 << 20] * 9
+    a.q_stride_t = a.q_stride_h = a.k_pages_stride_h = a.v_pages_stride_h = a.k_pages_stride_t = a.v_pages_stride_t = 128
+    a.k_pages_stride_p = a.v_pages_stride_p = 128 * 128
+    a.dtype = a.o_dtype = binding.PEC_BF16 if dtype == BF16 else binding.PEC_F32
+    a.page_size, a.num_pages, a.table_stride, a.max_pages, a.B, a.T = 128, kp.shape[0], table.shape[1], table.shape[1], 64, 200
+    a.Hq, a.Hkv, a.D, a.causal = 1, 1, 128, 1
+    need = binding.pec_paged_workspace_size(a)
+    guard = 4 << 20
+    room = torch.full(((need + 2 * guard) // 4 + 4,), 1000.0, device=DEV)
+    bytes_ = room.view(torch.uint8)
+    ws = bytes_[guard:guard + need]
+    o, lse = torch.full((200, 1, 128), 7.0, dtype=dtype, device=DEV), torch.full((200, 1), 7.0, device=DEV)
+    pec.pec_paged_attn(q, kp, vp, table, dev(cu), dev([1024] * 64), o=o, lse=lse, workspace=ws)
+    with pytest.raises(binding.PecError) as e:
+        pec.check_status()
+    assert e.value.code == binding.PEC_ERR_BAD_INDEX
+    assert (bytes_[:guard].view(torch.float32) == 1000.0).all() and (room[(guard + need + 3) // 4:] == 1000.0).all()
+    assert o.float().abs().max() < 100 and lse.abs().max() < 100
