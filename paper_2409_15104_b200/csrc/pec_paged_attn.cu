@@ -381,11 +381,12 @@ paged_f32_kernel(const Params p)
     for (int i = 0; i < 4; ++i) {
         const int32_t r = ty * 4 + i;
         if (r >= rows) continue;
-        const float inv = l_run[i] > 0.f ? 1.f / l_run[i] : 0.f;
-        const float lse = l_run[i] > 0.f ? m_run[i] * 0.6931471805599453f + logf(l_run[i]) : -INFINITY;
+        const bool empty = l_run[i] == 0.f;                          // a NaN sum is not: it reaches o and lse
+        const float inv = empty ? 0.f : 1.f / l_run[i];
+        const float lse = empty ? -INFINITY : m_run[i] * 0.6931471805599453f + logf(l_run[i]);
         float out[8];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) out[c] = l_run[i] > 0.f ? (c & 1 ? acc[i][c / 2].y : acc[i][c / 2].x) * inv : 0.f;
+        for (int c = 0; c < 8; ++c) out[c] = empty ? 0.f : (c & 1 ? acc[i][c / 2].y : acc[i][c / 2].x) * inv;
         if (it.slices > 1) {
             float *o = p.many_o + (slot * p.many_rows + r) * kHeadDim;
             *reinterpret_cast<float4 *>(o + tx * 4) = make_float4(out[0], out[1], out[2], out[3]);

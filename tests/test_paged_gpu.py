@@ -680,3 +680,25 @@ def test_overlapping_offsets_stay_inside_the_workspace(pec, dtype, cu):
     assert e.value.code == binding.PEC_ERR_BAD_INDEX
     assert (bytes_[:guard].view(torch.float32) == 1000.0).all() and (room[(guard + need + 3) // 4:] == 1000.0).all()
     assert o.float().abs().max() < 100 and lse.abs().max() < 100
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,kv", [(1, 100), (20, 100), (1, 3000), (20, 3000), (200, 3000)])
+@pytest.mark.parametrize("bad", ["nan", "inf"])
+def test_rows_that_see_a_key_that_is_not_finite_say_so(pec, dtype, n, kv, bad):
+    """A NaN score, or one of +inf (exp(inf - inf)), makes a row's sum NaN: that is not "sees no key" (0 and -inf), in a request of
+    one tile (kv = 100) as in one whose keys are cut (a part that were left out would give a plausible result).  The rows before
+    the key do not see it and keep their values."""
+    kp, vp, table = ref.make_cache(22, [kv], 16, 2, dtype, DEV)
+    q = torch.randn((n, 8, 128), generator=torch.Generator().manual_seed(23))
+    q[..., 5] = q[..., 5].abs() + 0.1                             # the score of a key with +inf there is +inf
+    q = q.to(dtype).to(DEV)
+    want = ref.attend(q, kp, vp, table, [0, n], [kv])
+    at = kv - (n + 1) // 2
+    kp[int(table[0, at // 16]), at % 16, :, 5] = float(bad)
+    o, lse = pec.pec_paged_attn(q, kp, vp, table, dev([0, n]), dev([kv]), max_q_len=n)
+    pec.check_status()
+    sees = n - (kv - at)
+    assert not torch.isfinite(o[sees:]).any()
+    assert not torch.isfinite(lse[sees:]).any() and not torch.isneginf(lse[sees:]).any()
+    ref.check_attend(o[:sees], lse[:sees], [x[:sees] for x in want], dtype, f"rows before a key with {bad}")
