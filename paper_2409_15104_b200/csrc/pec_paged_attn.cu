@@ -420,12 +420,18 @@ __device__ __forceinline__ void combine_row(const Params &p, const float *po, co
     constexpr int kBatch = 16;                                    // partials' rows in flight
     auto place = [&](int s) { return at0 + s * step + (s == 0 ? shift : 0); };     // of partial s, in rows
     float l = lane < count ? pl[place(lane)] : -INFINITY, m = l;   // lane s: the LSE of partial s of the current 32
-    for (int s = lane + 32; s < count; s += 32) m = fmaxf(m, pl[place(s)]);
+    bool some = l != -INFINITY;                                   // a partial with keys, NaN among them (which the maximum passes over)
+    for (int s = lane + 32; s < count; s += 32) {
+        const float x = pl[place(s)];
+        some = some || x != -INFINITY;
+        m = fmaxf(m, x);
+    }
+    some = __any_sync(0xffffffffu, some);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     float tot = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < count && m != -INFINITY; s0 += 32) {
+    for (int s0 = 0; s0 < count && some; s0 += 32) {
         if (s0 > 0) l = s0 + lane < count ? pl[place(s0 + lane)] : -INFINITY;
         const float w = l == -INFINITY ? 0.f : expf(l - m);
         tot += w;
@@ -445,7 +451,7 @@ __device__ __forceinline__ void combine_row(const Params &p, const float *po, co
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) tot += __shfl_xor_sync(0xffffffffu, tot, d);
-    const float inv = tot > 0.f ? 1.f / tot : 0.f;
+    const float inv = some ? 1.f / tot : 0.f;
     acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
     if (p.o_is_bf16) {
         const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
@@ -454,7 +460,7 @@ __device__ __forceinline__ void combine_row(const Params &p, const float *po, co
     } else {
         *reinterpret_cast<float4 *>(static_cast<float *>(p.o) + item * kHeadDim + 4 * lane) = acc;
     }
-    if (lane == 0) p.lse[item] = (m == -INFINITY) ? -INFINITY : m + logf(tot);
+    if (lane == 0) p.lse[item] = some ? m + logf(tot) : -INFINITY;
 }
 
 __global__ void __launch_bounds__(kCombineWarps * 32, 2)

@@ -702,3 +702,19 @@ def test_rows_that_see_a_key_that_is_not_finite_say_so(pec, dtype, n, kv, bad):
     assert not torch.isfinite(o[sees:]).any()
     assert not torch.isfinite(lse[sees:]).any() and not torch.isneginf(lse[sees:]).any()
     ref.check_attend(o[:sees], lse[:sees], [x[:sees] for x in want], dtype, f"rows before a key with {bad}")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,kv", [(1, 100), (1, 3000), (1, 40000), (13, 3000), (200, 3000)])
+def test_a_query_that_is_not_finite_stays_so_when_its_parts_are_merged(pec, dtype, n, kv):
+    """Every partial of such a row has a NaN for its LSE; the merge must not take that for parts without keys.  The other rows of
+    the same tile keep their values."""
+    kp, vp, table = ref.make_cache(24, [kv], 16, 2, dtype, DEV)
+    q = torch.randn((n, 8, 128), generator=torch.Generator().manual_seed(25)).to(dtype).to(DEV)
+    q[n // 2, 3, 7] = float("nan")
+    o, lse = pec.pec_paged_attn(q, kp, vp, table, dev([0, n]), dev([kv]), max_q_len=n)
+    pec.check_status()
+    assert torch.isnan(o[n // 2, 3]).all() and torch.isnan(lse[n // 2, 3])
+    want = ref.attend(q, kp, vp, table, [0, n], [kv])
+    assert np.isnan(want[1]).sum() == 1                           # that row's LSE: left out by the comparison
+    ref.check_attend(o, lse, want, dtype, f"beside a query that is not finite, {n} of {kv}")
