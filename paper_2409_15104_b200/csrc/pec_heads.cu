@@ -112,8 +112,9 @@ __device__ __forceinline__ void make_map(Map &m, const void *w, const float *cos
     m.hs[0] = make_float2(-wh[0] * s.x, -wh[1] * s.y); m.hs[1] = make_float2(-wh[2] * s.z, -wh[3] * s.w);
 }
 
-// Norm and rotation of one head held by a half warp.
-template <class E>
+// Norm and rotation of one head held by a half warp.  Without a rotation a pair's channels do not meet: 0 times a partner that is not
+// finite would be NaN.  (kTurn is the kernels' parameter because a choice here takes ten registers more and a block less per SM.)
+template <class E, bool kTurn>
 __device__ __forceinline__ void head_math(Head<E> &u, bool norm, float eps, const Map &m)
 {
     float a[4], b[4];
@@ -136,7 +137,8 @@ __device__ __forceinline__ void head_math(Head<E> &u, bool norm, float eps, cons
     float zl[4], zh[4];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const float2 x = __ffma2_rn(lo[i], m.lc[i], __fmul2_rn(hi[i], m.hs[i])), y = __ffma2_rn(hi[i], m.hc[i], __fmul2_rn(lo[i], m.ls[i]));
+        const float2 x = kTurn ? __ffma2_rn(lo[i], m.lc[i], __fmul2_rn(hi[i], m.hs[i])) : __fmul2_rn(lo[i], m.lc[i]);
+        const float2 y = kTurn ? __ffma2_rn(hi[i], m.hc[i], __fmul2_rn(lo[i], m.ls[i])) : __fmul2_rn(hi[i], m.hc[i]);
         zl[2 * i] = x.x; zl[2 * i + 1] = x.y; zh[2 * i] = y.x; zh[2 * i + 1] = y.y;
     }
     u.lo = Quad<E>::pack(zl);
@@ -158,7 +160,7 @@ struct NormRope {
 };
 
 // Block: eight tokens; blockIdx.y = a part of `per` query heads, or (from q_parts on) of key heads.
-template <class E>
+template <class E, bool kTurn>
 __global__ void __launch_bounds__(kThreads)
 norm_rope_kernel(const NormRope p, const int q_parts, const int per)
 {
@@ -187,11 +189,11 @@ norm_rope_kernel(const NormRope p, const int q_parts, const int per)
     // A negative position marks a padding row; one past the table is reported.
     int64_t pos = -1;
     if (t < p.T) pos = p.positions ? (int64_t)p.positions[t] : p.pos0 + t;
-    if (p.turn.table && pos >= p.turn.n_pos) {
+    if (kTurn && pos >= p.turn.n_pos) {
         if (lane == 0) raise_status(p.status, PEC_ERR_BAD_INDEX);
         pos = -1;
     }
-    if (p.turn.table) {
+    if (kTurn) {
         if (lane == 0) sh.pos[warp] = (int32_t)pos;
         __syncthreads();
         angles(p.turn, sh);
@@ -199,13 +201,13 @@ norm_rope_kernel(const NormRope p, const int q_parts, const int per)
     }
     if (pos < 0) return;
     Map m;
-    make_map<E>(m, p.norm ? (is_q ? p.qw : p.kw) : nullptr, p.turn.table ? sh.cos[warp] : nullptr, sh.sin[warp], l);
+    make_map<E>(m, p.norm ? (is_q ? p.qw : p.kw) : nullptr, kTurn ? sh.cos[warp] : nullptr, sh.sin[warp], l);
     const int rounds = ((h1 - h0 + 1) / 2 + kRows - 1) / kRows;     // the same for both halves: shuffles stay converged
     for (int r = 0; r < rounds; ++r) {
         if (r) fetch(u);
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            head_math<E>(u[i], p.norm != 0, p.eps, m);
+            head_math<E, kTurn>(u[i], p.norm != 0, p.eps, m);
             if (i < todo) store_head(dst, l, u[i]);
             dst += 2 * sh_out;
         }
@@ -227,7 +229,7 @@ struct Append {
 };
 
 // As above; blockIdx.y = a part of the key heads, or (from `parts` on) of the value heads, which are copied.
-template <class E>
+template <class E, bool kTurn>
 __global__ void __launch_bounds__(kThreads)
 kv_append_kernel(const Append p, const int parts, const int per)
 {
@@ -257,14 +259,14 @@ kv_append_kernel(const Append p, const int parts, const int per)
         pos = (int64_t)kv - end + t;
         const int64_t nth = pos / p.c.page_size;
         slot = pos - nth * p.c.page_size;
-        if (pos >= 0 && nth < p.c.max_pages && (!p.turn.table || pos < p.turn.n_pos)) {
+        if (pos >= 0 && nth < p.c.max_pages && (!kTurn || pos < p.turn.n_pos)) {
             page = p.c.table[b * p.c.table_stride + nth];           // looked at when the angles are done
         } else {
             if (lane == 0) raise_status(p.status, PEC_ERR_BAD_INDEX);
             pos = -1;
         }
     }
-    const bool turn = is_k && p.turn.table, math = is_k && (p.norm || p.turn.table);   // uniform over the block
+    const bool turn = is_k && kTurn, math = is_k && (p.norm || kTurn);   // uniform over the block
     if (turn) {
         if (lane == 0) sh.pos[warp] = (int32_t)pos;
         __syncthreads();
@@ -285,7 +287,7 @@ kv_append_kernel(const Append p, const int parts, const int per)
         if (r) fetch(u);
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            if (math) head_math<E>(u[i], p.norm != 0, p.eps, m);
+            if (math) head_math<E, kTurn>(u[i], p.norm != 0, p.eps, m);
             if (i < todo) store_head(dst, l, u[i]);
             dst += 2 * s_out;
         }
@@ -402,8 +404,10 @@ extern "C" int pec_qk_norm_rope(const pec_norm_rope_args *a, void *cuda_stream)
     const int per = heads::heads_per_part(p.T, p.Hq + p.Hkv), q_parts = (p.Hq + per - 1) / per;
     const dim3 grid((unsigned)((p.T + heads::kWarps - 1) / heads::kWarps), (unsigned)(q_parts + (p.Hkv + per - 1) / per));
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (esz == 2) heads::norm_rope_kernel<__nv_bfloat16><<<grid, heads::kThreads, 0, stream>>>(p, q_parts, per);
-    else          heads::norm_rope_kernel<float><<<grid, heads::kThreads, 0, stream>>>(p, q_parts, per);
+    const bool turn = p.turn.table != nullptr;
+    const auto kernel = esz == 2 ? (turn ? heads::norm_rope_kernel<__nv_bfloat16, true> : heads::norm_rope_kernel<__nv_bfloat16, false>)
+                                 : (turn ? heads::norm_rope_kernel<float, true> : heads::norm_rope_kernel<float, false>);
+    kernel<<<grid, heads::kThreads, 0, stream>>>(p, q_parts, per);
     const cudaError_t err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("%s: launch failed: %s", who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
@@ -433,8 +437,10 @@ extern "C" int pec_kv_append(const pec_kv_append_args *a, void *cuda_stream)
     const int per = heads::heads_per_part(a->T, 2 * (int64_t)a->Hkv), parts = (a->Hkv + per - 1) / per;
     const dim3 grid((unsigned)((a->T + heads::kWarps - 1) / heads::kWarps), (unsigned)(2 * parts));
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (esz == 2) heads::kv_append_kernel<__nv_bfloat16><<<grid, heads::kThreads, 0, stream>>>(p, parts, per);
-    else          heads::kv_append_kernel<float><<<grid, heads::kThreads, 0, stream>>>(p, parts, per);
+    const bool turn = p.turn.table != nullptr;
+    const auto kernel = esz == 2 ? (turn ? heads::kv_append_kernel<__nv_bfloat16, true> : heads::kv_append_kernel<__nv_bfloat16, false>)
+                                 : (turn ? heads::kv_append_kernel<float, true> : heads::kv_append_kernel<float, false>);
+    kernel<<<grid, heads::kThreads, 0, stream>>>(p, parts, per);
     const cudaError_t err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("%s: launch failed: %s", who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;

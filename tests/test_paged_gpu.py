@@ -718,3 +718,57 @@ def test_a_query_that_is_not_finite_stays_so_when_its_parts_are_merged(pec, dtyp
     want = ref.attend(q, kp, vp, table, [0, n], [kv])
     assert np.isnan(want[1]).sum() == 1                           # that row's LSE: left out by the comparison
     ref.check_attend(o, lse, want, dtype, f"beside a query that is not finite, {n} of {kv}")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("norm", [False, True])
+def test_without_a_table_channels_do_not_meet(pec, dtype, norm):
+    """No rotation: z = y.  What is not finite in channel i stays there (a rotation by zero would bring inf * 0 into channel
+    i + 64 or i - 64), and without a norm the heads are copied."""
+    x = torch.randn((5, 3, 128), generator=torch.Generator().manual_seed(8)).to(dtype).to(DEV)
+    x[1, 0, 5], x[2, 1, 100], x[3, 2, 64], x[4, 0, 0] = float("inf"), float("-inf"), float("nan"), -0.0
+    kp, vp, table = ref.make_cache(14, [5], 16, 3, dtype, DEV, poison=False)
+    v = torch.randn((5, 3, 128), device=DEV).to(dtype)
+    pec.pec_kv_append(x, v, kp, vp, table, dev([0, 5]), dev([5]), norm=norm)
+    outs = [*pec.pec_qk_norm_rope(x, x.clone(), norm=norm), kp[int(table[0, 0]), :5]]
+    pec.check_status()
+    for out in outs:
+        if not norm:
+            assert torch.equal(out.isnan(), x.isnan())
+            assert torch.equal(out.nan_to_num(nan=9.0), x.nan_to_num(nan=9.0)) and torch.equal(torch.signbit(out[4]), torch.signbit(x[4]))
+            continue
+        for t, h, c in ((1, 0, 5), (2, 1, 100)):                  # x / sqrt(inf): 0, and NaN where x is inf
+            rest = [i for i in range(128) if i != c]
+            assert torch.isnan(out[t, h, c]) and (out[t, h, rest] == 0).all()
+        assert torch.isnan(out[3, 2]).all()
+        for t in range(5):
+            for h in range(3):
+                if (t, h) not in ((1, 0), (2, 1), (3, 2)):
+                    check_heads(out[t:t + 1, h:h + 1], x[t:t + 1, h:h + 1], None, [0], dtype, True, False)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("norm", [False, True])
+def test_without_a_table_channels_do_not_meet(pec, dtype, norm):
+    """No rotation: z = y.  What is not finite in channel i stays there (a rotation by zero would bring inf * 0 into channel
+    i + 64 or i - 64), and without a norm the heads are copied."""
+    x = torch.randn((5, 3, 128), generator=torch.Generator().manual_seed(8)).to(dtype).to(DEV)
+    x[1, 0, 5], x[2, 1, 100], x[3, 2, 64], x[4, 0, 0] = float("inf"), float("-inf"), float("nan"), -0.0
+    kp, vp, table = ref.make_cache(14, [5], 16, 3, dtype, DEV, poison=False)
+    v = torch.randn((5, 3, 128), device=DEV).to(dtype)
+    pec.pec_kv_append(x, v, kp, vp, table, dev([0, 5]), dev([5]), norm=norm)
+    outs = [*pec.pec_qk_norm_rope(x, x.clone(), norm=norm), kp[int(table[0, 0]), :5]]
+    pec.check_status()
+    for out in outs:
+        if not norm:
+            assert torch.equal(out.isnan(), x.isnan())
+            assert torch.equal(out.nan_to_num(nan=9.0), x.nan_to_num(nan=9.0)) and torch.equal(torch.signbit(out[4]), torch.signbit(x[4]))
+            continue
+        for t, h, c in ((1, 0, 5), (2, 1, 100)):                  # x / sqrt(inf): 0, and NaN where x is inf
+            rest = [i for i in range(128) if i != c]
+            assert torch.isnan(out[t, h, c]) and (out[t, h, rest] == 0).all()
+        assert torch.isnan(out[3, 2]).all()
+        for t in range(5):
+            for h in range(3):
+                if (t, h) not in ((1, 0), (2, 1), (3, 2)):
+                    check_heads(out[t:t + 1, h:h + 1], x[t:t + 1, h:h + 1], None, [0], dtype, True, False)
