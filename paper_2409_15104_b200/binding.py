@@ -263,7 +263,11 @@ def status_word(device=None) -> torch.Tensor:
     dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
     key = dev.index if dev.index is not None else torch.cuda.current_device()
     if key not in _status_words:
-        _status_words[key] = torch.zeros(1, dtype=torch.int32, device=dev)
+        word = torch.zeros(1, dtype=torch.int32, device=dev)
+        with torch.cuda.device(key):
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream().synchronize()          # other streams' kernels may report from now on
+        _status_words[key] = word
     return _status_words[key]
 
 

@@ -772,3 +772,20 @@ def test_without_a_table_channels_do_not_meet(pec, dtype, norm):
             for h in range(3):
                 if (t, h) not in ((1, 0), (2, 1), (3, 2)):
                     check_heads(out[t:t + 1, h:h + 1], x[t:t + 1, h:h + 1], None, [0], dtype, True, False)
+
+
+def test_a_status_word_made_on_a_busy_stream_loses_no_report(pec, monkeypatch):
+    """The device's word is zeroed on the stream of whoever asks first; a call on another stream may not run before that."""
+    tables = pec.pec_rope_table(THETA, 100, DEV)
+    q, at = torch.randn((1, 2, 128), device=DEV), dev([100])
+    torch.cuda.synchronize()
+    monkeypatch.setattr(binding, "_status_words", {})
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)                            # 0.2 s
+        binding.status_word(DEV)
+    pec.pec_qk_norm_rope(q, tables=tables, positions=at)          # a position past the table
+    torch.cuda.synchronize()
+    with pytest.raises(binding.PecError) as e:
+        pec.check_status()
+    assert e.value.code == binding.PEC_ERR_BAD_INDEX
