@@ -272,11 +272,13 @@ def status_word(device=None) -> torch.Tensor:
 
 
 def check_status(device=None):
-    """Synchronise and raise if a kernel recorded an expired wait; clears the word."""
+    """Synchronise the device, all its streams, and raise if a kernel recorded an expired wait or a bad index; clears the word."""
     w = status_word(device)
+    torch.cuda.synchronize(w.device)
     code = int(w.item())
     if code != 0:
         w.zero_()
+        torch.cuda.synchronize(w.device)                           # no later call on another stream loses its report to this
         raise PecError(code, {PEC_ERR_TIMEOUT: "a kernel's bounded wait expired",
                               PEC_ERR_BAD_INDEX: "a kernel met a page number, position or offset out of range"}.get(code, "kernel status"))
 

@@ -789,3 +789,22 @@ def test_a_status_word_made_on_a_busy_stream_loses_no_report(pec, monkeypatch):
     with pytest.raises(binding.PecError) as e:
         pec.check_status()
     assert e.value.code == binding.PEC_ERR_BAD_INDEX
+
+
+def test_check_status_waits_for_calls_on_other_streams(pec):
+    tables = pec.pec_rope_table(THETA, 100, DEV)
+    q, at = torch.randn((1, 2, 128), device=DEV), dev([100])
+    pec.check_status()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)                            # 0.2 s
+        pec.pec_qk_norm_rope(q, tables=tables, positions=at)      # a position past the table
+    try:
+        with pytest.raises(binding.PecError) as e:
+            pec.check_status()
+        assert e.value.code == binding.PEC_ERR_BAD_INDEX
+    finally:
+        torch.cuda.synchronize()
+        binding.status_word(DEV).zero_()
+    pec.check_status()
