@@ -80,6 +80,12 @@ void same(const Tensor &t, const char *what, const Like &l, at::ScalarType type,
         fail(PyExc_ValueError, "%s: need a %d-dimensional %s tensor on %s with a contiguous innermost dimension", what, dims, c10::toString(type),
                                 l.device.str().c_str());
 }
+// These dimensions go through the C ABI in 32 bits.
+int32_t narrow(int64_t size, const char *what)
+{
+    if (size > INT32_MAX) refuse(what, "dimensions below 2^31");
+    return (int32_t)size;
+}
 // A dimension of one entry has no stride of its own, whatever torch says.
 int64_t stride(const Tensor &t, int i) { return t.size(i) > 1 ? t.stride(i) : 128; }
 
@@ -124,19 +130,17 @@ void paged(A &a, PyObject *const *o, int64_t T, const Like &l)
     same(lens, "kv_lens", l, at::kInt, 1);
     const int64_t B = lens.size(0);
     if (cu.size(0) != B + 1 || table.size(0) != B) fail(PyExc_ValueError, "need cu_q [B + 1], kv_lens [B] and block_table [B, pages]");
-    if (k.size(1) > INT32_MAX || table.size(1) > INT32_MAX || B > INT32_MAX || k.size(2) > INT32_MAX || k.size(3) > INT32_MAX)
-        fail(PyExc_ValueError, "a dimension of 2^31 or more");
     if (!cu.is_contiguous() || !lens.is_contiguous()) fail(PyExc_ValueError, "need contiguous cu_q and kv_lens");
     a.k_pages = k.data_ptr(); a.v_pages = v.data_ptr();
     a.k_pages_stride_p = stride(k, 0); a.k_pages_stride_t = stride(k, 1); a.k_pages_stride_h = stride(k, 2);
     a.v_pages_stride_p = stride(v, 0); a.v_pages_stride_t = stride(v, 1); a.v_pages_stride_h = stride(v, 2);
-    a.num_pages = k.size(0); a.page_size = (int32_t)k.size(1); a.Hkv = (int32_t)k.size(2); a.D = (int32_t)k.size(3);
+    a.num_pages = k.size(0); a.page_size = narrow(k.size(1), "k_pages"); a.Hkv = narrow(k.size(2), "k_pages"); a.D = narrow(k.size(3), "k_pages");
     a.block_table = static_cast<const int32_t *>(table.data_ptr());
-    a.max_pages = (int32_t)table.size(1);
+    a.max_pages = narrow(table.size(1), "block_table");
     a.table_stride = B > 1 ? table.stride(0) : table.size(1);
     a.cu_q = static_cast<const int32_t *>(cu.data_ptr());
     a.kv_lens = static_cast<const int32_t *>(lens.data_ptr());
-    a.B = (int32_t)B; a.T = T;
+    a.B = narrow(B, "kv_lens"); a.T = T;
 }
 
 // (straight from the CUDA allocator, 0.3 us a tensor less than through the dispatcher)
@@ -166,7 +170,7 @@ PyObject *norm_rope(PyObject *, PyObject *const *o, Py_ssize_t n)
     const bool inplace = truth(o[4]), norm = truth(o[5]), has_k = o[1] != Py_None;
     pec_norm_rope_args a{};
     a.dtype = type_code(l.type);
-    a.T = q.size(0); a.Hq = (int32_t)q.size(1); a.D = (int32_t)q.size(2);
+    a.T = q.size(0); a.Hq = narrow(q.size(1), "q"); a.D = narrow(q.size(2), "q");
     a.q = q.data_ptr(); a.q_stride_t = stride(q, 0); a.q_stride_h = stride(q, 1);
     // The output of one side: the tensor given, the input itself, or a new one.
     auto out = [&](PyObject *given, PyObject *input, const char *what) -> PyObject * {
@@ -183,7 +187,7 @@ PyObject *norm_rope(PyObject *, PyObject *const *o, Py_ssize_t n)
         const Tensor &k = tensor(o[1], "k");
         same(k, "k", l, l.type, 3);
         if (k.size(0) != a.T || k.size(2) != q.size(2)) refuse("k", "q's tokens and head dimension");
-        a.Hkv = (int32_t)k.size(1);
+        a.Hkv = narrow(k.size(1), "k");
         a.k = k.data_ptr(); a.k_stride_t = stride(k, 0); a.k_stride_h = stride(k, 1);
     }
     a.norm = norm; a.eps = real(o[8]);
@@ -250,7 +254,7 @@ PyObject *paged_attn(PyObject *, PyObject *const *o, Py_ssize_t n)
     if (a.D != q.size(2)) refuse("k_pages", "q's head dimension");
     a.dtype = type_code(l.type);
     a.q = q.data_ptr(); a.q_stride_t = stride(q, 0); a.q_stride_h = stride(q, 1);
-    a.Hq = (int32_t)q.size(1);
+    a.Hq = narrow(q.size(1), "q");
     const int64_t most = integer(o[6]);
     if (most < 0 || most > INT32_MAX) refuse("max_q_len", "0 <= max_q_len < 2^31");
     a.max_q_len = (int32_t)most;

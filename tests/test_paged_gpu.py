@@ -808,3 +808,13 @@ def test_check_status_waits_for_calls_on_other_streams(pec):
         torch.cuda.synchronize()
         binding.status_word(DEV).zero_()
     pec.check_status()
+
+
+def test_a_dimension_past_32_bits_is_refused(pec):
+    """A head dimension of 2^32 + 128 is not one of 128."""
+    q = torch.empty((1, 1, (1 << 32) + 128), dtype=BF16, device=DEV)
+    for args in ((q,), (q[..., :128], q)):
+        with pytest.raises(ValueError):
+            pec.pec_qk_norm_rope(*args, norm=False)
+    del q
+    torch.cuda.empty_cache()
