@@ -372,7 +372,7 @@ extern "C" int pec_qk_norm_rope(const pec_norm_rope_args *a, void *cuda_stream)
     int rc = check_norm_rope(who, a->norm, a->eps, a->rope_table, a->n_pos);
     if (rc != PEC_OK) return rc;
     if (!a->status) { set_error("%s: the status word must be non-NULL", who); return PEC_ERR_INVALID_ARG; }
-    if (!a->positions && (a->pos0 < 0 || (a->rope_table && a->pos0 + a->T > a->n_pos))) {
+    if (!a->positions && (a->pos0 < 0 || (a->rope_table && a->pos0 > a->n_pos - a->T))) {
         set_error("%s: positions pos0 .. pos0 + T - 1 must lie inside the table", who);
         return PEC_ERR_INVALID_ARG;
     }
@@ -400,7 +400,7 @@ extern "C" int pec_qk_norm_rope(const pec_norm_rope_args *a, void *cuda_stream)
     p.T = (int32_t)a->T; p.Hq = a->Hq; p.Hkv = a->Hkv;
     p.qw = a->q_weight; p.kw = a->k_weight; p.norm = a->norm; p.eps = a->eps;
     p.turn = {a->rope_table, a->n_pos};
-    p.positions = a->positions; p.pos0 = a->pos0; p.status = a->status;
+    p.positions = a->positions; p.pos0 = a->rope_table ? a->pos0 : 0; p.status = a->status;      // (no position matters without a table)
     const int per = heads::heads_per_part(p.T, p.Hq + p.Hkv), q_parts = (p.Hq + per - 1) / per;
     const dim3 grid((unsigned)((p.T + heads::kWarps - 1) / heads::kWarps), (unsigned)(q_parts + (p.Hkv + per - 1) / per));
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);

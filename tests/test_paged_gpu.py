@@ -818,3 +818,12 @@ def test_a_dimension_past_32_bits_is_refused(pec):
             pec.pec_qk_norm_rope(*args, norm=False)
     del q
     torch.cuda.empty_cache()
+
+
+def test_norm_rope_without_a_table_at_any_first_position(pec):
+    """Positions pos0 + t past 2^63 are not padding."""
+    q = torch.randn((20, 2, 128), device=DEV).to(BF16)
+    out = torch.full_like(q, 7.0)
+    pec.pec_qk_norm_rope(q, pos0=(1 << 63) - 1, q_out=out)
+    pec.check_status()
+    assert torch.equal(out, pec.pec_qk_norm_rope(q)[0])

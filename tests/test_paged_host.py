@@ -152,3 +152,10 @@ def test_reference_agrees_with_the_oracle():
     pos = [0, 17, 40000]
     want = oracle.rope(x.double().numpy().reshape(3, 256), pos, 1e4, 256).reshape(3, 2, 128)
     assert np.abs(ref.rope(x.double().numpy(), pos, 1e4) - want).max() < 1e-9
+
+
+@pytest.mark.parametrize("n_pos", [10, (1 << 31) - 1])
+def test_norm_rope_refuses_positions_that_wrap(n_pos):
+    """pos0 + T past 2^63 is past the table, not before it."""
+    for pos0 in ((1 << 63) - 1, (1 << 63) - 2):
+        assert binding.load().pec_qk_norm_rope(ctypes.byref(_norm_rope(rope_table=BIG, n_pos=n_pos, pos0=pos0, T=2)), None) == -1, binding.pec_last_error()
