@@ -1,6 +1,7 @@
 """Build libpec.so (the C-ABI library) for sm_100a with nvcc, and _pec_torch.so (tensor marshalling for binding.py), in-tree."""
 import os
 import subprocess
+import sys
 import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -22,10 +23,16 @@ def _stale() -> bool:
 
 
 def _build_torch_module(force: bool) -> None:
+    import torch
+    # Beside the module: what it was built for.  One built for another torch or Python does not load, whatever its age.
+    mark = os.path.join(os.path.dirname(TORCH_MODULE), "_pec_torch.built_for")
+    built_for = f"torch {torch.__version__}, Python {sys.version}"
     deps = [os.path.join(CSRC, TORCH_SOURCE), os.path.join(INCLUDE, "pec.h")]
     if not force and os.path.exists(TORCH_MODULE) and all(os.path.getmtime(d) <= os.path.getmtime(TORCH_MODULE) for d in deps):
-        return
-    import torch
+        if os.path.exists(mark):
+            with open(mark) as f:
+                if f.read() == built_for:
+                    return
     root = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
     includes = [INCLUDE, os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
@@ -36,12 +43,11 @@ def _build_torch_module(force: bool) -> None:
     cmd += [os.path.join(CSRC, TORCH_SOURCE), "-o", TORCH_MODULE, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu",
             "-ltorch_cuda", "-lc10", "-lc10_cuda"]
     subprocess.run(cmd, check=True)
+    with open(mark, "w") as f:
+        f.write(built_for)
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    _build_torch_module(force)
-    if not force and not _stale():
-        return LIB
+def _build_library(verbose: bool) -> None:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
            "-shared", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC, "-o", LIB]
@@ -49,6 +55,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
         cmd += ["-Xptxas", "-v"]
     cmd += [os.path.join(CSRC, s) for s in SOURCES]
     subprocess.run(cmd, check=True)
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    # The C library first: it needs neither torch nor g++, and is there for C callers where the module cannot be built.
+    if force or _stale():
+        _build_library(verbose)
+    _build_torch_module(force)
     return LIB
 
 
