@@ -580,8 +580,9 @@ typedef struct {
 int pec_paged_attn(const pec_paged_args *args, void *cuda_stream);
 
 /* Bytes of workspace pec_paged_attn needs for these arguments (0 if they are invalid): a function of T, B, Hq, Hkv, dtype,
- * max_q_len, max_pages, page_size and the current device's SM count, not of what the tables hold; on 148 SMs at most 140 MB
- * and the list of row blocks (48 bytes for every 256 packed rows and request). */
+ * max_q_len, max_pages, page_size and the current device's SM count, not of what the tables hold; on 148 SMs at most 137.1 MB,
+ * 0.133 MB for every KV head, and 48 bytes for every request and every block of rows (of 2 * floor(128 / g) tokens, fp32: of 64
+ * packed rows). */
 size_t pec_paged_workspace_size(const pec_paged_args *args);
 
 /*

@@ -159,3 +159,19 @@ def test_norm_rope_refuses_positions_that_wrap(n_pos):
     """pos0 + T past 2^63 is past the table, not before it."""
     for pos0 in ((1 << 63) - 1, (1 << 63) - 2):
         assert binding.load().pec_qk_norm_rope(ctypes.byref(_norm_rope(rope_table=BIG, n_pos=n_pos, pos0=pos0, T=2)), None) == -1, binding.pec_last_error()
+
+
+@pytest.mark.parametrize("dtype", [binding.PEC_BF16, binding.PEC_F32])
+@pytest.mark.parametrize("hkv,g", [(1, 1), (1, 128), (8, 4), (24, 1), (64, 8), (128, 5), (1024, 67), (65535, 1)])
+@pytest.mark.parametrize("T,B,most", [(1, 1, 1), (64, 64, 1), (4096, 1, 0), (8192, 300, 2048)])
+def test_workspace_stays_below_its_documented_bound(dtype, hkv, g, T, B, most):
+    """148 SMs: 137 MB and 0.133 MB for every KV head, and the list of row blocks."""
+    a = _paged(T=T, B=B, max_q_len=most, max_pages=8192, table_stride=8192, num_pages=1000, Hkv=hkv, Hq=hkv * g, dtype=dtype,
+               o_dtype=binding.PEC_F32, q_stride_t=hkv * g * 128)
+    for side in "kv":
+        setattr(a, f"{side}_pages_stride_t", hkv * 128)
+        setattr(a, f"{side}_pages_stride_p", 16 * hkv * 128)
+    need = binding.load().pec_paged_workspace_size(ctypes.byref(a))
+    block = 2 * (128 // g) * g if dtype == binding.PEC_BF16 else 64                # packed rows
+    lists = 48 * (T * g / block + min(T, B) + 1100 + hkv)
+    assert 0 < need <= 137e6 + 0.133e6 * hkv + lists, (need, binding.pec_last_error())
