@@ -827,3 +827,20 @@ def test_norm_rope_without_a_table_at_any_first_position(pec):
     pec.pec_qk_norm_rope(q, pos0=(1 << 63) - 1, q_out=out)
     pec.check_status()
     assert torch.equal(out, pec.pec_qk_norm_rope(q)[0])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,hq", [(1, 4), (3, 16), (130, 4)])
+def test_scores_of_ten_thousand(pec, dtype, n, hq):
+    """Scores past +-1e4 in natural units (the narrow, the wide and the chunk form), where the maximum's subtraction and the LSE
+    lose the most bits: the bound's score term grows with sum |q k| and covers them."""
+    kp, vp, table = ref.make_cache(9, [1500], 16, 1, dtype, DEV)
+    q = torch.randn((n, hq, 128), generator=torch.Generator().manual_seed(10)).to(dtype).to(DEV)
+    ids = table[0, :94].long()
+    ramp = torch.linspace(0.1, 40.0, 94 * 16, device=DEV).view(94, 16, 1, 1)
+    kp[ids] = (kp[ids].float() * ramp).to(dtype)
+    o, lse = pec.pec_paged_attn(q, kp, vp, table, dev([0, n]), dev([1500]), max_q_len=n, softmax_scale=20.0)
+    pec.check_status()
+    want = ref.attend(q, kp, vp, table, [0, n], [1500], scale=20.0)
+    assert want[1].max() > 1e4
+    ref.check_attend(o, lse, want, dtype, f"scores to {want[1].max():.0f}, {n} tokens")
