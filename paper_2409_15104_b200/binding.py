@@ -550,12 +550,24 @@ def _call_status(t):
     return word
 
 
-def _on_stream(call, t, stream):
-    """`call` with `stream` (of the tensor's device) current, so that what it allocates belongs to that stream."""
+def _on_stream(call, t, stream, *others):
+    """`call` with `stream` (of the tensor's device) current, so that what it allocates belongs to that stream.
+
+    The allocator is told that `stream` uses the call's tensors and the caller's stream its results: either side may drop them
+    at once.  (Waiting for one another is the caller's business.)
+    """
     if stream.device != t.device:
         raise ValueError("the stream belongs to another device")
+    caller = torch.cuda.current_stream(t.device)
     with torch.cuda.stream(stream):
-        return call()
+        results = call()
+    for x in (t, *others):
+        if isinstance(x, torch.Tensor):
+            x.record_stream(stream)
+    for x in results or ():
+        if x is not None:
+            x.record_stream(caller)
+    return results
 
 
 def pec_qk_norm_rope(q, k=None, *, norm=True, q_weight=None, k_weight=None, eps=1e-6, tables=None, positions=None, pos0=0,
@@ -568,7 +580,8 @@ def pec_qk_norm_rope(q, k=None, *, norm=True, q_weight=None, k_weight=None, eps=
     """
     if stream is not None:
         return _on_stream(lambda: pec_qk_norm_rope(q, k, norm=norm, q_weight=q_weight, k_weight=k_weight, eps=eps, tables=tables,
-                                                   positions=positions, pos0=pos0, q_out=q_out, k_out=k_out, inplace=inplace), q, stream)
+                                                   positions=positions, pos0=pos0, q_out=q_out, k_out=k_out, inplace=inplace),
+                          q, stream, k, q_weight, k_weight, *(tables or ()), positions, q_out, k_out)
     rc, q_out, k_out = (_torch_module or _marshal()).norm_rope(q, k, q_out, k_out, inplace, norm, q_weight, k_weight, eps,
                                                                *(tables or _NO_TABLE), positions, pos0, _call_status(q))
     if rc:
@@ -587,7 +600,8 @@ def pec_kv_append(k, v, k_pages, v_pages, block_table, cu_q, kv_lens, *, norm=Fa
     """
     if stream is not None:
         return _on_stream(lambda: pec_kv_append(k, v, k_pages, v_pages, block_table, cu_q, kv_lens, norm=norm, k_weight=k_weight,
-                                                eps=eps, tables=tables), k, stream)
+                                                eps=eps, tables=tables),
+                          k, stream, v, k_pages, v_pages, block_table, cu_q, kv_lens, k_weight, *(tables or ()))
     rc = (_torch_module or _marshal()).kv_append(k, v, k_pages, v_pages, block_table, cu_q, kv_lens, norm, k_weight, eps,
                                                  *(tables or _NO_TABLE), _call_status(k))
     if rc:
@@ -606,7 +620,7 @@ def pec_paged_attn(q, k_pages, v_pages, block_table, cu_q, kv_lens, *, max_q_len
     if stream is not None:
         return _on_stream(lambda: pec_paged_attn(q, k_pages, v_pages, block_table, cu_q, kv_lens, max_q_len=max_q_len, causal=causal,
                                                  softmax_scale=softmax_scale, out_dtype=out_dtype, o=o, lse=lse, workspace=workspace),
-                          q, stream)
+                          q, stream, k_pages, v_pages, block_table, cu_q, kv_lens, o, lse, workspace)
     rc, o, lse = (_torch_module or _marshal()).paged_attn(q, k_pages, v_pages, block_table, cu_q, kv_lens, max_q_len, causal,
                                                           softmax_scale, out_dtype, o, lse, workspace, _call_status(q))
     if rc:

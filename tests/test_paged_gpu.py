@@ -844,3 +844,50 @@ def test_scores_of_ten_thousand(pec, dtype, n, hq):
     want = ref.attend(q, kp, vp, table, [0, n], [1500], scale=20.0)
     assert want[1].max() > 1e4
     ref.check_attend(o, lse, want, dtype, f"scores to {want[1].max():.0f}, {n} tokens")
+
+
+def test_calls_on_another_stream_keep_their_tensors(pec):
+    """Inputs of the current stream that are dropped as soon as the call returns, while the call's stream is still busy: their memory
+    may not be handed out before the call has read it.  The same for a result that is dropped while the current stream reads it."""
+    kp, vp, table = ref.make_cache(27, [600], 16, 2, BF16, DEV)
+    q = torch.randn((64, 8, 128), device=DEV).to(BF16)
+    tables = pec.pec_rope_table(THETA, 1000, DEV)
+    want_h, _ = pec.pec_qk_norm_rope(q, tables=tables)
+    want, want_l = pec.pec_paged_attn(q, kp, vp, table, dev([0, 64]), dev([600]), max_q_len=64)
+    k2, v2 = kp.clone(), vp.clone()
+    pec.pec_kv_append(q[:, :2], q[:, 2:4], k2, v2, table, dev([0, 64]), dev([600]), tables=tables)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    k3, v3 = kp.clone(), vp.clone()
+
+    def overwrite():                                              # whatever small blocks are free now
+        for _ in range(20):
+            torch.full((64, 8, 128), 100.0, dtype=BF16, device=DEV)
+            torch.full((64,), 99, dtype=torch.int32, device=DEV)
+
+    for call in (lambda: pec.pec_qk_norm_rope(q.clone(), tables=tables, stream=side)[0],
+                 lambda: pec.pec_paged_attn(q.clone(), kp, vp, table.clone(), dev([0, 64]), dev([600]), max_q_len=64, stream=side),
+                 lambda: pec.pec_kv_append(q.clone()[:, :2], q.clone()[:, 2:4], k3, v3, table.clone(), dev([0, 64]), dev([600]), tables=tables, stream=side)):
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)                        # 50 ms
+        out = call()
+        overwrite()
+        torch.cuda.synchronize()
+        if isinstance(out, tuple):
+            assert torch.equal(out[0], want) and torch.equal(out[1], want_l)
+        elif out is not None:
+            assert torch.equal(out, want_h)
+    assert torch.equal(k3.view(torch.int16), k2.view(torch.int16)) and torch.equal(v3.view(torch.int16), v2.view(torch.int16))
+    # A result read by the current stream and dropped; the call's stream takes the next result's memory.
+    out = pec.pec_qk_norm_rope(q, tables=tables, stream=side)[0]
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda._sleep(100_000_000)
+    kept = out.clone()
+    del out
+    for _ in range(5):
+        other = pec.pec_qk_norm_rope(q + 1, tables=tables, stream=side)[0]
+        del other
+    torch.cuda.synchronize()
+    assert torch.equal(kept, want_h)
+    pec.check_status()
