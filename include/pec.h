@@ -538,11 +538,13 @@ int pec_kv_append(const pec_kv_append_args *args, void *cuda_stream);
  * kv_lens[b] of them (causal = 0).  One token per request is a decode step, many a chunk of a prefill resumed on its stored
  * prefix (Section 5.1); both kinds may be in one batch.  o [T, Hq, D] and lse [T, Hq] as in pec_prefill_attn: a row that
  * sees no key gets 0 and -inf; fp32 o is a partial fit for pec_attn_merge.  dtype PEC_BF16 runs the tensor cores (bf16 products,
- * fp32 accumulation, probabilities rounded to bf16 - to 16 bits where Hq / Hkv * max_q_len <= 16), PEC_F32 an fp32 FMA kernel with fp32 output.
+ * fp32 accumulation, probabilities rounded to bf16 - to 16 bits where Hq / Hkv * max_q_len <= 16, so that a decode row is a
+ * little less exact beside a chunk or without max_q_len), PEC_F32 an fp32 FMA kernel with fp32 output.
  * bf16: (num_pages - 1) * page stride + (Hkv - 1) * head stride must be below 2^31 times the greatest common divisor of the two
  * (any cache that a B200 holds with strides that are multiples of 128 elements is).
  * A value of a request that is not finite may spoil the rows of the same request that do not see it yet (0 * inf), never those
- * of another request.
+ * of another request.  A row with a NaN score, or one of +inf, gets NaN, never the 0 and -inf of a row without keys.
+ * A bf16 call that finds PEC_ERR_TIMEOUT in *status, from itself or from an earlier call, gives up: clear the word before the next.
  * max_q_len: an upper bound of the new tokens of any one request, 0 = none known (T); a request that brings more is a bad
  * index.  It chooses the kernels: Hq / Hkv * max_q_len <= 128 needs only the one for few rows.
  * workspace: device, 16-byte aligned, at least pec_paged_workspace_size() bytes; scratch for partial results of requests

@@ -295,8 +295,11 @@ kv_append_kernel(const Append p, const int parts, const int per)
     }
 }
 
-// Heads of a part: as many as a warp loads at once (8) where the call is too small to fill the GPU otherwise, four times that
-// where it is not, so that the angles are worked out for more heads.
+// Heads of a part: as many as a warp loads at once (8) where the call is too small to fill the GPU otherwise (a warp of each of 148 SMs'
+// 32 and 32 heads), four times that where it is not, so that the angles are worked out for more heads.  Both sides (parts of 8 / 32)
+// at T * H = 20000, 75000, 150000, 300000, 600000: norm of 72 heads 5.0 / 7.3, 12.6 / 12.8, 21.0 / 17.5, 35.3 / 30.8, 64.9 / 55.1 us, of 40
+// heads 4.9 / 7.5, 13.0 / 13.2, 21.8 / 18.6, 38.6 / 33.1, 71.4 / 61.2; append of 32 heads 4.8 / 7.6, 9.4 / 9.2, 17.8 / 14.5, 31.8 / 26.8,
+// 62.5 / 54.2, of 8 heads (one part either way) the same.  Ten heads would gain at every size: 6.8 / 6.2 to 118 / 98.6.
 inline int heads_per_part(int64_t T, int64_t H) { return T * H < (int64_t)148 * 32 * 32 ? 2 * kRows : 8 * kRows; }
 
 }  // namespace heads

@@ -20,15 +20,19 @@ namespace paged {
 // whole, unless one is longer than an SM's fair share of all tiles (slice0); of the rest, which would leave SMs idle for a whole
 // unit's time, the keys are cut into slices (slice1): as many as fill one, two or three waves, whichever has the shortest
 // estimated time, or none.  That holds for units of nearly one length, or for a batch of less than a wave; units of all lengths fill
-// the SMs by going longest first, and cutting some of them only adds work (24 requests of 4 to 30 tiles, 4.2 waves: 207 us cut, 193
-// not).  The estimate, in 1/32 of a tile's time: a wave of slices takes its tiles and item_cost for a CTA's
-// start and end; a slice's partial, written and read once, merge_cost.  On the tensor cores a tile takes 1.35 us, start and end 4
-// us, a partial of 132 KB 0.04 us both ways; with the FMA kernel, 17 us a tile, both are next to nothing.
+// the SMs by going longest first, and cutting some of them only adds work.  Both sides (cut / not), 32 / 8 heads: 24 requests of 1 to
+// 600 tokens on some 2000, 280-283 / 272-280 us; 40 of 128 on 100 to 3000, 167-199 / 157-174; three of 1024 on 1000, 4000 and 9000,
+// 251 / 221; nine of 256 on 4000 and one on 20000, 248 / 226; twelve of 256 on 1000 to 8000, 221-292 / 221-278; six of 512 on 2000 to
+// 12000 come out on either side.
+// The estimate, in 1/32 of a tile's time: a wave of slices takes its tiles and item_cost for a CTA's
+// start and end; a slice's partial, written and read once, merge_cost.  On the tensor cores a tile takes 1.5 us at the full clock (2.1
+// in a run of a millisecond and more, at the power limit), start and end 3.5 to 6 us (148 to 888 units of 16 tiles: 27 to 31 us a
+// wave), a partial of 132 KB 0.04 us both ways; with the FMA kernel, 17 us a tile, both are next to nothing.
 // Slots that cut units take: cutting units of length l into slices of S takes less than sum l / S + their number.  slice0 >= all
 // tiles / many_ctas, and units longer than that are fewer than many_ctas: 2 many_ctas.  The tail has less than many_ctas + Hkv
 // units of mean length m and slice1 >= m / cuts with cuts * units <= 3 many_ctas: 4 many_ctas + Hkv.
-// Items that cutting adds (the grid has a CTA for each, used or not, and one that finds nothing takes its SM 1.4 us: 888 more of them
-// cost 24 requests of 300 tokens 9 us of 195, 296 fewer saved 1.2 of 174.9): ceil(l / S) - 1 < l / S of a unit, in all many_ctas for slice0 and 3 many_ctas for slice1.
+// Items that cutting adds (the grid has a CTA for each, used or not, and one that finds nothing takes its SM 0.6 to 1.5 us: 888 more of
+// them, six an SM, cost 24 requests of 300 tokens 9 us of 195, 296 fewer saved 1.2 of 174.9): ceil(l / S) - 1 < l / S of a unit, in all many_ctas for slice0 and 3 many_ctas for slice1.
 // Items go into the list longest first (by 256 classes of visible tiles): an SM that falls free late finds short work.  The order
 // inside a class is whatever the atomics make it; it changes when an item runs, never what it computes.
 constexpr int kPlanThreads = 256, kClasses = 256;

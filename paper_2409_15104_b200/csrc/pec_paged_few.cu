@@ -610,7 +610,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sum[i] = make_float2(0.f, 0.f);
                     // p = 2^(s scale - m), rounded to bf16 as the product's operand (the tensor cores take no wider one beside a
-                    // bf16 V); the row's sum takes p before it is rounded.
+                    // bf16 V); the row's sum takes p before it is rounded.  A second part, as the narrow form has, would be a third
+                    // 128-row product a tile, in the form that draws the power limit already.
 #pragma unroll
                     for (int i = 0; i < kKeyTile / 2; ++i) {
                         const float2 x = __ffma2_rn(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), sc2, nm2);

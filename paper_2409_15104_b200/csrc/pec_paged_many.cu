@@ -350,7 +350,9 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 float2 sum[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[i] = make_float2(0.f, 0.f);
-                // p = 2^(s scale - m), rounded to bf16 as the product's operand; the row's sum takes p before it is rounded.
+                // p = 2^(s scale - m), rounded to bf16 as the product's operand; the row's sum takes p before it is rounded.  A second
+                // part of p (as the form for at most 16 rows has) would be a third product for every two in a kernel that the tensor
+                // pipe bounds, and 64 more columns for either stage of a tensor memory that is full: scores 128, P 2 x 64, O 2 x 128.
 #pragma unroll
                 for (int i = 0; i < kTile / 2; ++i) {
                     const float2 x = __ffma2_rn(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), sc2, nm2);
