@@ -28,33 +28,34 @@ __device__ __forceinline__ void raise_status(int32_t *status, int32_t code)
 
 // The request that owns token row t and that request's entry of kv_lens, searched by one converged warp, 32 requests at a
 // time: every lane's loads are independent of one another (a binary search would be a chain of log2(B) dependent ones) and the
-// owner's values come by shuffle.  Returns false for padding rows; offsets that are not ascending around t, or pass T, raise the
-// status word and give false as well.
+// owner's values come by shuffle.  Returns false for padding rows.  Offsets that are not ascending, or pass T, raise the status word in
+// each group that is looked at; the last row's warp looks at those after its owner's too, so that the rows together see all of them.
 __device__ __forceinline__ bool find_request(const PagedCache &c, int32_t t, int32_t *status, int32_t &b, int32_t &start, int32_t &end, int32_t &kv)
 {
     const int lane = threadIdx.x & 31;
     const int32_t first = c.cu_q[0];
     int32_t prev = first;                                       // the end of the request before this group of 32
+    bool found = false, bad = first < 0;
     for (int b0 = 0; b0 < c.B; b0 += 32) {
         int32_t e = INT32_MAX, k = 0;
-        if (b0 + lane < c.B) { e = c.cu_q[b0 + lane + 1]; k = c.kv_lens[b0 + lane]; }
+        const bool real = b0 + lane < c.B;
+        if (real) { e = c.cu_q[b0 + lane + 1]; k = c.kv_lens[b0 + lane]; }
+        int32_t before = __shfl_up_sync(0xffffffffu, e, 1);
+        if (lane == 0) before = prev;
+        bad = bad || e < before || (real && e > c.T);
         const int src = __popc(__ballot_sync(0xffffffffu, e <= t));       // requests of the group that end at or before t
-        if (src < 32) {
+        if (src < 32 && !found) {
             b = b0 + src;
+            start = __shfl_sync(0xffffffffu, before, src);
             end = __shfl_sync(0xffffffffu, e, src);
             kv = __shfl_sync(0xffffffffu, k, src);
-            const int32_t before = __shfl_sync(0xffffffffu, e, src > 0 ? src - 1 : 0);
-            start = src > 0 ? before : prev;
-            if (b >= c.B || t < first) return false;
-            if (start < 0 || t < start || t >= end || end > c.T) {
-                if (lane == 0) raise_status(status, PEC_ERR_BAD_INDEX);
-                return false;
-            }
-            return true;
+            found = b < c.B && t >= first;
+            if (t != c.T - 1) break;
         }
         prev = __shfl_sync(0xffffffffu, e, 31);
     }
-    return false;
+    if (__any_sync(0xffffffffu, bad) && lane == 0) raise_status(status, PEC_ERR_BAD_INDEX);
+    return found && start >= 0 && t >= start && t < end && end <= c.T;
 }
 
 // Host checks common to the entry points; returns a pec_status.

@@ -891,3 +891,23 @@ def test_calls_on_another_stream_keep_their_tensors(pec):
     torch.cuda.synchronize()
     assert torch.equal(kept, want_h)
     pec.check_status()
+
+
+@pytest.mark.parametrize("T,cu", [(8, [5, 3, 8]), (4, [0, 4, 9, 9]), (4, [0, 4, 100, 50]), (6, [0] * 40 + [6] * 40 + [2, 6]), (3, [0] + [3] * 700 + [1] + [3] * 20),
+                                  (0, None)])
+def test_append_reports_offsets_that_no_row_meets(pec, T, cu):
+    """Offsets that descend before the first row or after the last one, or pass T, in any group of requests: their tokens are not
+    stored, and the call says so.  Ascending ones with empty requests anywhere are fine."""
+    ok = cu is None
+    if ok:
+        T, cu = 6, [2] * 300 + [3] * 300 + [6] * 300
+    B = len(cu) - 1
+    kp, vp, table = ref.make_cache(15, [20] * B, 24, 1, F32, DEV, poison=False, wild=False)
+    k = torch.randn((T, 1, 128), device=DEV)
+    pec.pec_kv_append(k, k, kp, vp, table, dev(cu), dev([20] * B))
+    if ok:
+        pec.check_status()
+        return
+    with pytest.raises(binding.PecError) as e:
+        pec.check_status()
+    assert e.value.code == binding.PEC_ERR_BAD_INDEX
