@@ -588,6 +588,108 @@ int pec_paged_attn(const pec_paged_args *args, void *cuda_stream);
 size_t pec_paged_workspace_size(const pec_paged_args *args);
 
 /*
+ * A paged cache held in 4 bits (pec_kv_append_q4, pec_kv_read_q4, pec_paged_attn_q4): 132 bytes of a token's key and value of one
+ * head instead of 512 in bf16, for decode steps that are bound by the cache's bytes and long requests that are bound by its size.
+ * A head of a token is 128 codes of 4 bits and one scale.  Code: sign (bit 3), two bits of exponent, one of mantissa, standing
+ * for 0, 0.5, 1, 1.5, 2, 3, 4, 6; channel 2 i lies in the low half of byte i, channel 2 i + 1 in the high half.  Scale: bf16, the
+ * smallest number s of six significant bits with 6 s >= the head's largest magnitude, kept within [2^-100, 1.3125 * 2^125].
+ * A channel's code is the nearest to x / s (of two as near, the one whose mantissa bit is 0).  Two significant bits times six are
+ * eight: what is held is exactly a bf16 number, and whatever reads the cache reads that number.  A head with a value that is not
+ * finite is held with a scale of NaN, and every number read from it is NaN.
+ *
+ * k_pages, v_pages: device [num_pages, page_size, Hkv, 64] bytes, the 64 of a head contiguous, page, token and head strides free
+ * in bytes, multiples of 32; 32-byte aligned.  k_scales, v_scales: device bf16 [num_pages, page_size, Hkv], strides free in elements.
+ * Head-major pages (a head's tokens one after the other) are read with the fewest and longest transfers.
+ * Everything else (block_table, cu_q, kv_lens, padding rows, bad indices) as for the cache above.
+ */
+typedef struct {
+    void *k_pages, *v_pages;    /* device; written by pec_kv_append_q4 only                     */
+    int64_t k_pages_stride_p, k_pages_stride_t, k_pages_stride_h;        /* bytes               */
+    int64_t v_pages_stride_p, v_pages_stride_t, v_pages_stride_h;
+    void *k_scales, *v_scales;  /* device                                                       */
+    int64_t k_scales_stride_p, k_scales_stride_t, k_scales_stride_h;     /* elements            */
+    int64_t v_scales_stride_p, v_scales_stride_t, v_scales_stride_h;
+    int32_t page_size;          /* a multiple of 8                                              */
+    int64_t num_pages;
+    const int32_t *block_table;
+    int64_t table_stride;
+    int32_t max_pages;
+    const int32_t *cu_q, *kv_lens;
+    int32_t B;
+    int64_t T;
+    int32_t Hkv, D;             /* D must be 128                                                */
+} pec_q4_cache;
+
+/*
+ * pec_kv_append for such a cache: keys normalised (norm) and rotated (rope_table) as there, then quantised; values quantised.
+ * Keys that are normalised or rotated are worked out in fp64 from the table's fp32 entries, and not rounded before they are
+ * quantised: which code is the nearest does not depend on how a sum was rounded.  dtype: that of k, v and the weight.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA.
+ */
+typedef struct {
+    const void *k, *v;          /* device; 16-byte aligned                                      */
+    int64_t k_stride_t, k_stride_h, v_stride_t, v_stride_h;              /* elements; multiples of 16 bytes, >= D */
+    int32_t dtype;
+    pec_q4_cache cache;
+    const void *k_weight;       /* [D] or NULL for 1; used with norm                            */
+    int32_t norm;
+    float eps;
+    const float *rope_table;
+    int64_t n_pos;
+    int32_t *status;
+} pec_kv_append_q4_args;
+
+int pec_kv_append_q4(const pec_kv_append_q4_args *args, void *cuda_stream);
+
+/*
+ * Reads cached tokens back: row t of the packed outputs [T, Hkv, D] is the token that a call with the same cu_q and kv_lens would
+ * have as its new token t, i.e. request b gives its last cu_q[b + 1] - cu_q[b] cached tokens (all of them where cu_q counts
+ * kv_lens up).  The outputs are then the k and v of the calls that take contiguous tensors: a preempted prefill resumed through
+ * pec_prefill_attn, pec_decode_attn over a prefix, a request handed to another GPU.  dtype: that of both outputs; either type
+ * holds the numbers exactly.  Rows that belong to no request, or to a bad index, are left as they were.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA.
+ */
+typedef struct {
+    pec_q4_cache cache;
+    void *k_out, *v_out;        /* device; 16-byte aligned                                      */
+    int64_t k_out_stride_t, k_out_stride_h, v_out_stride_t, v_out_stride_h;   /* elements; multiples of 16 bytes, >= D */
+    int32_t dtype;
+    int32_t *status;
+} pec_kv_read_q4_args;
+
+int pec_kv_read_q4(const pec_kv_read_q4_args *args, void *cuda_stream);
+
+/*
+ * pec_paged_attn over such a cache: the same rows, masks, outputs and kinds of batches, with the numbers that the cache holds as
+ * keys and values.  dtype: that of q.  PEC_BF16 runs the tensor cores, PEC_F32 an fp32 FMA kernel with fp32 output.
+ * Keys and values past a request's end are never used, nor is a value that a row does not see.
+ * A row with a NaN score, or one of +inf, gets NaN.  max_q_len, workspace, status: as there.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE, CUDA.
+ */
+typedef struct {
+    const void *q;              /* device; 16-byte aligned                                      */
+    int64_t q_stride_t, q_stride_h;                                      /* elements; multiples of 16 bytes, >= D */
+    int32_t dtype;
+    pec_q4_cache cache;
+    int32_t max_q_len;
+    void *o;                    /* device; [T, Hq, D] contiguous, 16-byte aligned               */
+    int32_t o_dtype;
+    float *lse;                 /* device; [T, Hq]                                              */
+    int32_t Hq;                 /* Hkv | Hq; g = Hq / Hkv <= 128, T g < 2^31 - 1024             */
+    int32_t causal;
+    float softmax_scale;        /* 0 selects 1/sqrt(D)                                          */
+    void *workspace;
+    size_t workspace_bytes;
+    int32_t *status;
+} pec_paged_q4_args;
+
+int pec_paged_attn_q4(const pec_paged_q4_args *args, void *cuda_stream);
+
+/* Bytes of workspace pec_paged_attn_q4 needs for these arguments (0 if they are invalid): a function of the same numbers as
+ * pec_paged_workspace_size. */
+size_t pec_paged_q4_workspace_size(const pec_paged_q4_args *args);
+
+/*
  * Process-wide settings (the paper has no counterpart; they exist for operations and tests).
  *   PEC_CTL_WAIT_LIMIT_CYCLES   limit of every barrier wait inside the kernels, in SM clock cycles
  *                               (default 2e9, about a second).  A wait that runs out makes its CTA

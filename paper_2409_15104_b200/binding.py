@@ -124,6 +124,51 @@ class pec_paged_args(ctypes.Structure):
     ]
 
 
+class pec_q4_cache(ctypes.Structure):
+    _fields_ = [
+        *_PAGED_FIELDS[:8],
+        ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+        ("k_scales_stride_p", ctypes.c_int64), ("k_scales_stride_t", ctypes.c_int64), ("k_scales_stride_h", ctypes.c_int64),
+        ("v_scales_stride_p", ctypes.c_int64), ("v_scales_stride_t", ctypes.c_int64), ("v_scales_stride_h", ctypes.c_int64),
+        *_PAGED_FIELDS[8:],
+        ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+    ]
+
+
+class pec_kv_append_q4_args(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("k_stride_t", ctypes.c_int64), ("k_stride_h", ctypes.c_int64),
+        ("v_stride_t", ctypes.c_int64), ("v_stride_h", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("cache", pec_q4_cache),
+        ("k_weight", ctypes.c_void_p), ("norm", ctypes.c_int32), ("eps", ctypes.c_float),
+        ("rope_table", ctypes.c_void_p), ("n_pos", ctypes.c_int64),
+        ("status", ctypes.c_void_p),
+    ]
+
+
+class pec_kv_read_q4_args(ctypes.Structure):
+    _fields_ = [
+        ("cache", pec_q4_cache),
+        ("k_out", ctypes.c_void_p), ("v_out", ctypes.c_void_p),
+        ("k_out_stride_t", ctypes.c_int64), ("k_out_stride_h", ctypes.c_int64),
+        ("v_out_stride_t", ctypes.c_int64), ("v_out_stride_h", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("status", ctypes.c_void_p),
+    ]
+
+
+class pec_paged_q4_args(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("cache", pec_q4_cache),
+        ("max_q_len", ctypes.c_int32),
+        ("o", ctypes.c_void_p), ("o_dtype", ctypes.c_int32), ("lse", ctypes.c_void_p),
+        ("Hq", ctypes.c_int32), ("causal", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("status", ctypes.c_void_p),
+    ]
+
+
 class pec_sp_inputs(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in ("s", "d", "n_h", "n_kv", "d_h", "T", "G", "elem_bytes", "node_bw", "gpu_flops")]
 
@@ -151,7 +196,8 @@ EXPORTS = ("pec_prefill_attn", "pec_workspace_size", "pec_attn_merge", "pec_attn
            "pec_last_error", "pec_decode_attn", "pec_decode_workspace_size", "pec_decode_attn_static", "pec_select_sp", "pec_linear",
            "pec_plan_ring", "pec_balance_batches", "pec_plan_worklist", "pec_worklist_block_m", "pec_control",
            "pec_linear_merged", "pec_linear_rope", "pec_rope_table", "pec_rope_table_floats",
-           "pec_qk_norm_rope", "pec_kv_append", "pec_paged_attn", "pec_paged_workspace_size")
+           "pec_qk_norm_rope", "pec_kv_append", "pec_paged_attn", "pec_paged_workspace_size",
+           "pec_kv_append_q4", "pec_kv_read_q4", "pec_paged_attn_q4", "pec_paged_q4_workspace_size")
 PEC_CTL_WAIT_LIMIT_CYCLES, PEC_CTL_TEST_SKIP_LAST_LOAD = 1, 2
 PEC_DECODE_STATIC_SCRATCH_BYTES = 4 * 1024 * 1024
 PEC_MERGE_MAX_PARTS = 16
@@ -212,6 +258,14 @@ def load():
     lib.pec_paged_attn.argtypes = [ctypes.POINTER(pec_paged_args), ctypes.c_void_p]
     lib.pec_paged_workspace_size.restype = ctypes.c_size_t
     lib.pec_paged_workspace_size.argtypes = [ctypes.POINTER(pec_paged_args)]
+    lib.pec_kv_append_q4.restype = ctypes.c_int
+    lib.pec_kv_append_q4.argtypes = [ctypes.POINTER(pec_kv_append_q4_args), ctypes.c_void_p]
+    lib.pec_kv_read_q4.restype = ctypes.c_int
+    lib.pec_kv_read_q4.argtypes = [ctypes.POINTER(pec_kv_read_q4_args), ctypes.c_void_p]
+    lib.pec_paged_attn_q4.restype = ctypes.c_int
+    lib.pec_paged_attn_q4.argtypes = [ctypes.POINTER(pec_paged_q4_args), ctypes.c_void_p]
+    lib.pec_paged_q4_workspace_size.restype = ctypes.c_size_t
+    lib.pec_paged_q4_workspace_size.argtypes = [ctypes.POINTER(pec_paged_q4_args)]
     lib.pec_select_sp.restype = ctypes.c_int
     lib.pec_select_sp.argtypes = [ctypes.POINTER(pec_sp_inputs), ctypes.POINTER(pec_sp_choice)]
     lib.pec_plan_ring.restype = ctypes.c_int
@@ -532,7 +586,8 @@ def _marshal():
         except ImportError as e:
             raise RuntimeError("_pec_torch.so is missing or unloadable: build it with `python -m paper_2409_15104_b200.build`") from e
         _pec_torch.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
-                          (lib.pec_qk_norm_rope, lib.pec_kv_append, lib.pec_paged_attn, lib.pec_paged_workspace_size)))
+                          (lib.pec_qk_norm_rope, lib.pec_kv_append, lib.pec_paged_attn, lib.pec_paged_workspace_size,
+                           lib.pec_kv_append_q4, lib.pec_kv_read_q4, lib.pec_paged_attn_q4, lib.pec_paged_q4_workspace_size)))
         _torch_module = _pec_torch
     return _torch_module
 
@@ -631,6 +686,60 @@ def pec_paged_attn(q, k_pages, v_pages, block_table, cu_q, kv_lens, *, max_q_len
 def pec_paged_workspace_size(a) -> int:
     """Bytes of workspace for a filled pec_paged_args."""
     return int(load().pec_paged_workspace_size(ctypes.byref(a)))
+
+
+def pec_kv_append_q4(k, v, k_pages, k_scales, v_pages, v_scales, block_table, cu_q, kv_lens, *, norm=False, k_weight=None, eps=1e-6,
+                     tables=None, stream=None):
+    """pec_kv_append into a cache held in 4 bits: k_pages, v_pages [pages, page_size, Hkv, 64] uint8 (or torch.float4_e2m1fn_x2),
+    two codes to a byte, with k_scales, v_scales [pages, page_size, Hkv] bf16 (any strides but the pages' last; pages' strides are
+    multiples of 32 bytes).  Keys are normalised and rotated before they are quantised.
+    """
+    if stream is not None:
+        return _on_stream(lambda: pec_kv_append_q4(k, v, k_pages, k_scales, v_pages, v_scales, block_table, cu_q, kv_lens, norm=norm,
+                                                   k_weight=k_weight, eps=eps, tables=tables),
+                          k, stream, v, k_pages, k_scales, v_pages, v_scales, block_table, cu_q, kv_lens, k_weight, *(tables or ()))
+    rc = (_torch_module or _marshal()).kv_append_q4(k, v, k_pages, k_scales, v_pages, v_scales, block_table, cu_q, kv_lens, norm,
+                                                    k_weight, eps, *(tables or _NO_TABLE), _call_status(k))
+    if rc:
+        _check(rc)
+
+
+def pec_kv_read_q4(k_pages, k_scales, v_pages, v_scales, block_table, cu_q, kv_lens, tokens, *, dtype=torch.bfloat16, k_out=None,
+                   v_out=None, stream=None):
+    """The last cu_q[b + 1] - cu_q[b] cached tokens of every request b of a cache held in 4 bits, packed: returns k and v
+    [tokens, Hkv, 128] of dtype (bf16 or fp32; both hold the numbers exactly).  k_out, v_out: tensors to write to; rows that belong
+    to no request are left as they were.
+    """
+    if stream is not None:
+        return _on_stream(lambda: pec_kv_read_q4(k_pages, k_scales, v_pages, v_scales, block_table, cu_q, kv_lens, tokens, dtype=dtype,
+                                                 k_out=k_out, v_out=v_out),
+                          k_pages, stream, k_scales, v_pages, v_scales, block_table, cu_q, kv_lens, k_out, v_out)
+    rc, k, v = (_torch_module or _marshal()).kv_read_q4(k_pages, k_scales, v_pages, v_scales, block_table, cu_q, kv_lens, tokens, dtype,
+                                                        k_out, v_out, _call_status(k_pages))
+    if rc:
+        _check(rc)
+    return k, v
+
+
+def pec_paged_attn_q4(q, k_pages, k_scales, v_pages, v_scales, block_table, cu_q, kv_lens, *, max_q_len=0, causal=True,
+                      softmax_scale=0.0, out_dtype=None, o=None, lse=None, workspace=None, stream=None):
+    """pec_paged_attn over a cache held in 4 bits (see pec_kv_append_q4); q is bf16 or fp32; returns (o [T, Hq, 128], lse [T, Hq])."""
+    if stream is not None:
+        return _on_stream(lambda: pec_paged_attn_q4(q, k_pages, k_scales, v_pages, v_scales, block_table, cu_q, kv_lens,
+                                                    max_q_len=max_q_len, causal=causal, softmax_scale=softmax_scale,
+                                                    out_dtype=out_dtype, o=o, lse=lse, workspace=workspace),
+                          q, stream, k_pages, k_scales, v_pages, v_scales, block_table, cu_q, kv_lens, o, lse, workspace)
+    rc, o, lse = (_torch_module or _marshal()).paged_attn_q4(q, k_pages, k_scales, v_pages, v_scales, block_table, cu_q, kv_lens,
+                                                             max_q_len, causal, softmax_scale, out_dtype, o, lse, workspace,
+                                                             _call_status(q))
+    if rc:
+        _check(rc)
+    return o, lse
+
+
+def pec_paged_q4_workspace_size(a) -> int:
+    """Bytes of workspace for a filled pec_paged_q4_args."""
+    return int(load().pec_paged_q4_workspace_size(ctypes.byref(a)))
 
 
 def pec_select_sp(s, d, n_h, n_kv, d_h, T, G, elem_bytes=2.0, node_bw=1.0, gpu_flops=1.0):

@@ -20,6 +20,7 @@
 #include <cstdio>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include "pec_head_io.cuh"
 #include "pec_host.h"
 #include "pec_internal.h"
 #include "pec_paged.h"
@@ -29,44 +30,6 @@ namespace heads {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kRows = 4;                     // heads of a half warp in flight
-
-// Four channels of a head as they lie in memory.
-template <class E> struct Quad;
-template <> struct Quad<__nv_bfloat16> {
-    typedef uint2 Raw;
-    static __device__ __forceinline__ void unpack(const Raw &u, float (&x)[4])
-    {
-        x[0] = __uint_as_float(u.x << 16); x[1] = __uint_as_float(u.x & 0xffff0000u);
-        x[2] = __uint_as_float(u.y << 16); x[3] = __uint_as_float(u.y & 0xffff0000u);
-    }
-    static __device__ __forceinline__ Raw pack(const float (&x)[4])
-    {
-        const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
-        return make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
-    }
-};
-template <> struct Quad<float> {
-    typedef float4 Raw;
-    static __device__ __forceinline__ void unpack(const Raw &u, float (&x)[4]) { x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; }
-    static __device__ __forceinline__ Raw pack(const float (&x)[4]) { return make_float4(x[0], x[1], x[2], x[3]); }
-};
-template <class E> struct Head { typename Quad<E>::Raw lo, hi; };    // a lane's eight channels
-template <class E>
-__device__ __forceinline__ Head<E> load_head(const E *head, int l)
-{
-    typedef typename Quad<E>::Raw Raw;
-    Head<E> u;
-    u.lo = *reinterpret_cast<const Raw *>(head + 4 * l);
-    u.hi = *reinterpret_cast<const Raw *>(head + 64 + 4 * l);
-    return u;
-}
-template <class E>
-__device__ __forceinline__ void store_head(E *head, int l, const Head<E> &u)
-{
-    typedef typename Quad<E>::Raw Raw;
-    *reinterpret_cast<Raw *>(head + 4 * l) = u.lo;
-    *reinterpret_cast<Raw *>(head + 64 + 4 * l) = u.hi;
-}
 
 struct Turn { const float *table; int64_t n_pos; };            // table of pec_rope_table, or NULL: no rotation
 constexpr int kFine = 64 * 64;
@@ -316,7 +279,7 @@ static int check_strides(const char *who, const int64_t *s, int n, int64_t esz)
     return PEC_OK;
 }
 
-static int check_norm_rope(const char *who, int32_t norm, float eps, const float *table, int64_t n_pos)
+int check_norm_rope(const char *who, int32_t norm, float eps, const float *table, int64_t n_pos)
 {
     if (norm != 0 && norm != 1) { set_error("%s: norm must be 0 or 1", who); return PEC_ERR_INVALID_ARG; }
     if (norm && !(eps > 0.f && std::isfinite(eps))) { set_error("%s: eps must be finite and > 0", who); return PEC_ERR_INVALID_ARG; }
@@ -325,15 +288,8 @@ static int check_norm_rope(const char *who, int32_t norm, float eps, const float
     return PEC_OK;
 }
 
-int check_paged_cache(const char *who, const void *k_pages, const void *v_pages, const PagedCache &c, int64_t T, int32_t Hkv,
-                      int32_t D, int32_t dtype, const int32_t *status)
+int check_batch(const char *who, const PagedCache &c, int64_t T, int32_t Hkv)
 {
-    if (!k_pages || !v_pages || !c.table || !c.cu_q || !c.kv_lens || !status) {
-        set_error("%s: k_pages, v_pages, block_table, cu_q, kv_lens and status must be non-NULL", who);
-        return PEC_ERR_INVALID_ARG;
-    }
-    if (D != kHeadDim) { set_error("%s: D=%d unsupported (only 128)", who, D); return PEC_ERR_UNSUPPORTED; }
-    if (dtype != PEC_BF16 && dtype != PEC_F32) { set_error("%s: unknown dtype %d", who, dtype); return PEC_ERR_UNSUPPORTED; }
     if (Hkv < 1 || Hkv > 65535) { set_error("%s: need 1 <= Hkv <= 65535 (got %d)", who, Hkv); return PEC_ERR_INVALID_ARG; }
     if (c.B < 1 || T < 0) { set_error("%s: need B >= 1 and T >= 0", who); return PEC_ERR_INVALID_ARG; }
     if (c.B > (1 << 20) || T > ((int64_t)1 << 30)) { set_error("%s: more than 2^20 requests or 2^30 tokens unsupported", who); return PEC_ERR_UNSUPPORTED; }
@@ -347,8 +303,22 @@ int check_paged_cache(const char *who, const void *k_pages, const void *v_pages,
         return PEC_ERR_INVALID_ARG;
     }
     if ((int64_t)c.max_pages * c.page_size > ((int64_t)1 << 30)) { set_error("%s: more than 2^30 tokens of one request unsupported", who); return PEC_ERR_UNSUPPORTED; }
+    return PEC_OK;
+}
+
+int check_paged_cache(const char *who, const void *k_pages, const void *v_pages, const PagedCache &c, int64_t T, int32_t Hkv,
+                      int32_t D, int32_t dtype, const int32_t *status)
+{
+    if (!k_pages || !v_pages || !c.table || !c.cu_q || !c.kv_lens || !status) {
+        set_error("%s: k_pages, v_pages, block_table, cu_q, kv_lens and status must be non-NULL", who);
+        return PEC_ERR_INVALID_ARG;
+    }
+    if (D != kHeadDim) { set_error("%s: D=%d unsupported (only 128)", who, D); return PEC_ERR_UNSUPPORTED; }
+    if (dtype != PEC_BF16 && dtype != PEC_F32) { set_error("%s: unknown dtype %d", who, dtype); return PEC_ERR_UNSUPPORTED; }
+    int rc = check_batch(who, c, T, Hkv);
+    if (rc != PEC_OK) return rc;
     const int64_t esz = dtype == PEC_BF16 ? 2 : 4, s[6] = {c.k_sp, c.k_st, c.k_sh, c.v_sp, c.v_st, c.v_sh};
-    const int rc = check_strides(who, s, 6, esz);
+    rc = check_strides(who, s, 6, esz);
     if (rc != PEC_OK) return rc;
     if (!aligned16(k_pages) || !aligned16(v_pages)) { set_error("%s: k_pages and v_pages must be 16-byte aligned", who); return PEC_ERR_ALIGNMENT; }
     if ((reinterpret_cast<uintptr_t>(c.table) | reinterpret_cast<uintptr_t>(c.cu_q) | reinterpret_cast<uintptr_t>(c.kv_lens) |

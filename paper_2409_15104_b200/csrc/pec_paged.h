@@ -58,7 +58,9 @@ __device__ __forceinline__ bool find_request(const PagedCache &c, int32_t t, int
     return found && start >= 0 && t >= start && t < end && end <= c.T;
 }
 
-// Host checks common to the entry points; returns a pec_status.
+// Host checks common to the entry points; each returns a pec_status.
+int check_batch(const char *who, const PagedCache &c, int64_t T, int32_t Hkv);           // sizes of the batch and its tables
+int check_norm_rope(const char *who, int32_t norm, float eps, const float *table, int64_t n_pos);
 int check_paged_cache(const char *who, const void *k_pages, const void *v_pages, const PagedCache &c, int64_t T, int32_t Hkv,
                       int32_t D, int32_t dtype, const int32_t *status);
 

@@ -8,6 +8,7 @@
 #include "pec_internal.h"
 #include "pec_paged.h"
 #include "pec_paged_plan.cuh"
+#include "pec_q4.cuh"
 
 namespace pec {
 namespace paged {
@@ -235,6 +236,16 @@ __device__ __forceinline__ void copy16(float *dst, const float *src, bool ok)
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
+// A cache held in 4 bits: codes and scales are decoded on their way to shared memory, four channels a lane.
+// Four channels of a key or value, of the eight in a word of codes; zeros where !ok (nothing is read then).
+__device__ __forceinline__ float4 decode4(const uint8_t *codes, const uint16_t *scale, bool ok)
+{
+    uint32_t r[4] = {0u, 0u, 0u, 0u};
+    if (ok) q4::decode8(*reinterpret_cast<const uint16_t *>(codes), q4::twice(*scale), r);
+    return make_float4(__uint_as_float(r[0] << 16), __uint_as_float(r[0] & 0xffff0000u), __uint_as_float(r[1] << 16), __uint_as_float(r[1] & 0xffff0000u));
+}
+
+template <bool kQ4, class Q>
 __global__ void __launch_bounds__(kThreads, 2)
 paged_f32_kernel(const Params p)
 {
@@ -253,7 +264,14 @@ paged_f32_kernel(const Params p)
     for (int i = tid; i < kBM * (kHeadDim / 4); i += kThreads) {
         const int r = i / (kHeadDim / 4), c = (i % (kHeadDim / 4)) * 4;
         const int32_t rr = min(r, rows - 1), t = (row0 + rr) / p.g, h = kvh * p.g + (row0 + rr) % p.g;
-        copy16(sQ + r * kLd + c, static_cast<const float *>(p.q) + (int64_t)(it.r.start + t) * p.q_st + (int64_t)h * p.q_sh + c, r < rows);
+        const Q *src = static_cast<const Q *>(p.q) + (int64_t)(it.r.start + t) * p.q_st + (int64_t)h * p.q_sh + c;
+        if constexpr (sizeof(Q) == 4) {
+            copy16(sQ + r * kLd + c, src, r < rows);
+        } else {
+            const uint2 u = r < rows ? *reinterpret_cast<const uint2 *>(src) : make_uint2(0u, 0u);
+            *reinterpret_cast<float4 *>(sQ + r * kLd + c) = make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u),
+                                                                        __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
+        }
     }
 
     float m_run[4], l_run[4];
@@ -290,6 +308,12 @@ paged_f32_kernel(const Params p)
             page[i] = s_page[r];
             slot[i] = (k0 + r) % p.c.page_size;
             const bool ok = page[i] >= 0;
+            if constexpr (kQ4) {
+                *reinterpret_cast<float4 *>(sK + r * kLd + c4) =
+                    decode4(static_cast<const uint8_t *>(p.k_pages) + page[i] * p.c.k_sp + slot[i] * p.c.k_st + (int64_t)kvh * p.c.k_sh + c4 / 2,
+                            p.k_scales + page[i] * p.ks_sp + slot[i] * p.ks_st + (int64_t)kvh * p.ks_sh, ok);
+                continue;
+            }
             const float *src = static_cast<const float *>(p.k_pages) + (ok ? page[i] * p.c.k_sp + slot[i] * p.c.k_st : 0) + (int64_t)kvh * p.c.k_sh + c4;
             copy16(sK + r * kLd + c4, src, ok);
         }
@@ -298,6 +322,12 @@ paged_f32_kernel(const Params p)
         for (int i = 0; i < 8; ++i) {
             const int r = (tid >> 5) + 8 * i;
             const bool ok = page[i] >= 0;
+            if constexpr (kQ4) {
+                *reinterpret_cast<float4 *>(sV + r * kHeadDim + c4) =
+                    decode4(static_cast<const uint8_t *>(p.v_pages) + page[i] * p.c.v_sp + slot[i] * p.c.v_st + (int64_t)kvh * p.c.v_sh + c4 / 2,
+                            p.v_scales + page[i] * p.vs_sp + slot[i] * p.vs_st + (int64_t)kvh * p.vs_sh, ok);
+                continue;
+            }
             const float *src = static_cast<const float *>(p.v_pages) + (ok ? page[i] * p.c.v_sp + slot[i] * p.c.v_st : 0) + (int64_t)kvh * p.c.v_sh + c4;
             copy16(sV + r * kHeadDim + c4, src, ok);
         }
@@ -398,9 +428,15 @@ paged_f32_kernel(const Params p)
             if (tx == 0) p.many_lse[slot * p.many_rows + r] = lse;
         } else {
             const int64_t item = (int64_t)(it.r.start + (row0 + r) / p.g) * p.Hq + kvh * p.g + (row0 + r) % p.g;
-            float *o = static_cast<float *>(p.o) + item * kHeadDim;
-            *reinterpret_cast<float4 *>(o + tx * 4) = make_float4(out[0], out[1], out[2], out[3]);
-            *reinterpret_cast<float4 *>(o + 64 + tx * 4) = make_float4(out[4], out[5], out[6], out[7]);
+            if (sizeof(Q) == 2 && p.o_is_bf16) {
+                __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.o) + item * kHeadDim;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) o[(c & 4) * 16 + tx * 4 + (c & 3)] = __float2bfloat16_rn(out[c]);
+            } else {
+                float *o = static_cast<float *>(p.o) + item * kHeadDim;
+                *reinterpret_cast<float4 *>(o + tx * 4) = make_float4(out[0], out[1], out[2], out[3]);
+                *reinterpret_cast<float4 *>(o + 64 + tx * 4) = make_float4(out[4], out[5], out[6], out[7]);
+            }
             if (tx == 0) p.lse[item] = lse;
         }
     }
@@ -523,26 +559,30 @@ int launch_paged_plan(const Params &p, cudaStream_t stream)
 {
     paged_plan_kernel<<<1, kPlanThreads, 0, stream>>>(p, p.items_cap, p.many_cap / 2);
     const cudaError_t err = cudaGetLastError();
-    if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
+    if (err != cudaSuccess) { set_error("%s: launch failed: %s", p.who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
 }
 
-int launch_paged_f32(const Params &p, int64_t items, cudaStream_t stream)
+// Set-up and launch of one form of the FMA kernel.
+template <bool kQ4, class Q>
+static int launch_fma(const Params &p, int64_t items, cudaStream_t stream)
 {
     static unsigned char ready[host::kMaxDevices] = {};
     static std::mutex ready_mutex;
     if (!host::once_per_device(ready, ready_mutex, [] {
-            return cudaFuncSetAttribute(paged_f32_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kF32Smem) == cudaSuccess; })) {
+            return cudaFuncSetAttribute(paged_f32_kernel<kQ4, Q>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kF32Smem) == cudaSuccess; })) {
         (void)cudaGetLastError();
-        set_error("pec_paged_attn: cannot raise the shared-memory limit");
+        set_error("%s: cannot raise the shared-memory limit", p.who);
         return PEC_ERR_CUDA;
     }
-    if (items * p.Hkv > 0x7fffffff) { set_error("pec_paged_attn: grid too large"); return PEC_ERR_UNSUPPORTED; }
-    cudaError_t err = launch_dependent(paged_f32_kernel, dim3((unsigned)(items * p.Hkv)), kThreads, kF32Smem, stream, true, p);
+    if (items * p.Hkv > 0x7fffffff) { set_error("%s: grid too large", p.who); return PEC_ERR_UNSUPPORTED; }
+    cudaError_t err = launch_dependent(paged_f32_kernel<kQ4, Q>, dim3((unsigned)(items * p.Hkv)), kThreads, kF32Smem, stream, true, p);
     if (err == cudaSuccess) err = cudaGetLastError();
-    if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
+    if (err != cudaSuccess) { set_error("%s: launch failed: %s", p.who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
 }
+
+int launch_paged_f32(const Params &p, int64_t items, cudaStream_t stream) { return launch_fma<false, float>(p, items, stream); }
 
 int launch_paged_combine(const Params &p, cudaStream_t stream)
 {
@@ -560,7 +600,7 @@ int launch_paged_combine(const Params &p, cudaStream_t stream)
     cudaError_t err = launch_dependent(paged_combine_kernel, dim3((unsigned)(few_blocks + many_blocks)), kCombineWarps * 32, 0, stream, true,
                                        p, by_unit, few_groups, few_blocks, many_groups);
     if (err == cudaSuccess) err = cudaGetLastError();
-    if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
+    if (err != cudaSuccess) { set_error("%s: launch failed: %s", p.who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
 }
 
@@ -589,62 +629,81 @@ static bool fold_pages(int64_t sp, int64_t sh, int64_t num_pages, int64_t Hkv, F
     return true;
 }
 
-// Checks the arguments and works out the launch.
-static int resolve(const char *who, const pec_paged_args *a, Call &c)
+// What the entry points share: queries, outputs and options.
+struct Queries {
+    const void *q;
+    int64_t q_st, q_sh;
+    int32_t dtype;
+    int64_t T;
+    int32_t B, Hq, Hkv, max_pages, page_size;
+    int32_t max_q_len;
+    void *o;
+    int32_t o_dtype;
+    float *lse;
+    int32_t causal;
+    float softmax_scale;
+    void *workspace;
+    int32_t *status;
+};
+
+static int check_queries(const char *who, const Queries &a)
 {
-    if (!a) { set_error("%s: args is NULL", who); return PEC_ERR_INVALID_ARG; }
-    if (!a->q || !a->o || !a->lse) { set_error("%s: q, o and lse must be non-NULL", who); return PEC_ERR_INVALID_ARG; }
-    Params &p = c.p;
-    p = Params{};
-    p.c = {a->k_pages_stride_p, a->k_pages_stride_t, a->k_pages_stride_h, a->v_pages_stride_p, a->v_pages_stride_t, a->v_pages_stride_h,
-           a->block_table, a->table_stride, a->max_pages, a->page_size, a->num_pages, a->cu_q, a->kv_lens, a->B, (int32_t)a->T};
-    const int rc = check_paged_cache(who, a->k_pages, a->v_pages, p.c, a->T, a->Hkv, a->D, a->dtype, a->status);
-    if (rc != PEC_OK) return rc;
-    if (a->Hq < 1 || a->Hq % a->Hkv != 0 || a->Hq / a->Hkv > 128) {
-        set_error("%s: need Hkv | Hq and at most 128 query heads per KV head (got %d, %d)", who, a->Hq, a->Hkv);
+    if (a.Hq < 1 || a.Hq % a.Hkv != 0 || a.Hq / a.Hkv > 128) {
+        set_error("%s: need Hkv | Hq and at most 128 query heads per KV head (got %d, %d)", who, a.Hq, a.Hkv);
         return PEC_ERR_INVALID_ARG;
     }
-    if (a->o_dtype != PEC_BF16 && a->o_dtype != PEC_F32) { set_error("%s: unknown o_dtype %d", who, a->o_dtype); return PEC_ERR_UNSUPPORTED; }
-    if (a->dtype == PEC_F32 && a->o_dtype != PEC_F32) { set_error("%s: fp32 inputs produce fp32 output only", who); return PEC_ERR_UNSUPPORTED; }
-    if (a->causal != 0 && a->causal != 1) { set_error("%s: causal must be 0 or 1", who); return PEC_ERR_INVALID_ARG; }
-    if (!(a->softmax_scale >= 0.f) || std::isinf(a->softmax_scale)) { set_error("%s: softmax_scale must be finite and >= 0", who); return PEC_ERR_INVALID_ARG; }
-    if (a->max_q_len < 0) { set_error("%s: max_q_len must be >= 0", who); return PEC_ERR_INVALID_ARG; }
-    const int64_t esz = a->dtype == PEC_BF16 ? 2 : 4;
-    for (const int64_t s : {a->q_stride_t, a->q_stride_h}) {
+    if (a.o_dtype != PEC_BF16 && a.o_dtype != PEC_F32) { set_error("%s: unknown o_dtype %d", who, a.o_dtype); return PEC_ERR_UNSUPPORTED; }
+    if (a.dtype == PEC_F32 && a.o_dtype != PEC_F32) { set_error("%s: fp32 inputs produce fp32 output only", who); return PEC_ERR_UNSUPPORTED; }
+    if (a.causal != 0 && a.causal != 1) { set_error("%s: causal must be 0 or 1", who); return PEC_ERR_INVALID_ARG; }
+    if (!(a.softmax_scale >= 0.f) || std::isinf(a.softmax_scale)) { set_error("%s: softmax_scale must be finite and >= 0", who); return PEC_ERR_INVALID_ARG; }
+    if (a.max_q_len < 0) { set_error("%s: max_q_len must be >= 0", who); return PEC_ERR_INVALID_ARG; }
+    const int64_t esz = a.dtype == PEC_BF16 ? 2 : 4;
+    for (const int64_t s : {a.q_st, a.q_sh}) {
         if (s < kHeadDim) { set_error("%s: strides must be >= D", who); return PEC_ERR_INVALID_ARG; }
         if ((s * esz) % 16 != 0) { set_error("%s: strides must be multiples of 16 bytes", who); return PEC_ERR_ALIGNMENT; }
     }
-    if (!aligned16(a->q) || !aligned16(a->o) || (reinterpret_cast<uintptr_t>(a->lse) & 3u)) {
+    if (!aligned16(a.q) || !aligned16(a.o) || (reinterpret_cast<uintptr_t>(a.lse) & 3u)) {
         set_error("%s: q and o must be 16-byte aligned (lse 4-byte)", who);
         return PEC_ERR_ALIGNMENT;
     }
-    if (a->T * (a->Hq / a->Hkv) > ((int64_t)1 << 31) - 1024) { set_error("%s: T * Hq / Hkv near 2^31 or above unsupported", who); return PEC_ERR_UNSUPPORTED; }
-    if (a->dtype == PEC_BF16 && !(fold_pages(p.c.k_sp, p.c.k_sh, p.c.num_pages, a->Hkv, p.fk) && fold_pages(p.c.v_sp, p.c.v_sh, p.c.num_pages, a->Hkv, p.fv))) {
-        set_error("%s: the pages reach over 2^31 times the greatest common divisor of their page and head strides", who);
-        return PEC_ERR_UNSUPPORTED;
-    }
-    p.q = a->q; p.k_pages = a->k_pages; p.v_pages = a->v_pages;
-    p.q_st = a->q_stride_t; p.q_sh = a->q_stride_h;
-    p.o = a->o; p.lse = a->lse; p.o_is_bf16 = a->o_dtype == PEC_BF16;
-    p.Hq = a->Hq; p.Hkv = a->Hkv; p.g = a->Hq / a->Hkv;
-    p.causal = a->causal;
-    const float scale = a->softmax_scale > 0.f ? a->softmax_scale : (float)(1.0 / std::sqrt((double)kHeadDim));
+    if (a.T * (a.Hq / a.Hkv) > ((int64_t)1 << 31) - 1024) { set_error("%s: T * Hq / Hkv near 2^31 or above unsupported", who); return PEC_ERR_UNSUPPORTED; }
+    return PEC_OK;
+}
+
+// How the call's requests are divided between the kernels.
+struct Classes {
+    bool few;                                 // requests of at most few_limit packed rows go to a persistent kernel
+    int32_t few_limit, few_ctas_per_sm;
+    bool many_tensor;                         // the others to the tensor cores (two stages of whole tokens) or the FMA kernel (64 packed rows)
+};
+
+// The launch: classes of requests, grid bounds, workspace (checked arguments, p.c set).
+static int lay_out(const char *who, const Queries &a, const Classes &k, Call &c)
+{
+    Params &p = c.p;
+    p.who = who;
+    p.q = a.q;
+    p.q_st = a.q_st; p.q_sh = a.q_sh;
+    p.o = a.o; p.lse = a.lse; p.o_is_bf16 = a.o_dtype == PEC_BF16;
+    p.Hq = a.Hq; p.Hkv = a.Hkv; p.g = a.Hq / a.Hkv;
+    p.causal = a.causal;
+    const float scale = a.softmax_scale > 0.f ? a.softmax_scale : (float)(1.0 / std::sqrt((double)kHeadDim));
     p.scale_log2 = (float)((double)scale * 1.4426950408889634074);
-    p.max_q = (int32_t)(a->max_q_len > 0 && a->max_q_len < a->T ? a->max_q_len : a->T);
-    p.status = a->status;
+    p.max_q = (int32_t)(a.max_q_len > 0 && a.max_q_len < a.T ? a.max_q_len : a.T);
+    p.status = a.status;
     p.wait_cycles = wait_limit_cycles();
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) {
         (void)cudaGetLastError();
         sms = 148;                            // no device here (size queries on a host without one): a B200's
     }
-    // bf16 requests with at most 128 packed rows go to the persistent kernel.
-    const bool tensor = a->dtype == PEC_BF16;
-    p.few = tensor ? 1 : 0;
-    p.few_ctas = sms;
+    const bool tensor = k.many_tensor;
+    p.few = k.few ? 1 : 0;
+    p.few_limit = k.few_limit;
+    p.few_ctas = k.few ? sms * k.few_ctas_per_sm : sms;
     size_t floats = 0;
     if (p.few) {
-        p.few_rows = (int32_t)((int64_t)p.max_q * p.g < kFewRows ? p.max_q * p.g : kFewRows);
+        p.few_rows = (int32_t)((int64_t)p.max_q * p.g < k.few_limit ? p.max_q * p.g : k.few_limit);
         floats = 2 * (size_t)p.few_ctas * p.few_rows * (kHeadDim + 1);
         floats = (floats + 3) & ~(size_t)3;
     }
@@ -657,11 +716,11 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
     p.item_cost = tensor ? 96 : 8;
     p.merge_cost = tensor ? 1 : 0;
     c.many_items = 0;
-    if (!p.few || (int64_t)p.max_q * p.g > kFewRows) {
-        const int64_t shortest = p.few ? kFewRows / p.g + 1 : 1, most = a->T / shortest;       // new tokens of such a request; how many there can be
-        const int64_t blocks = a->T * p.blk_mul / p.blk_div + (a->B < most ? a->B : most);
+    if (!p.few || (int64_t)p.max_q * p.g > k.few_limit) {
+        const int64_t shortest = p.few ? k.few_limit / p.g + 1 : 1, most = a.T / shortest;       // new tokens of such a request; how many there can be
+        const int64_t blocks = a.T * p.blk_mul / p.blk_div + (a.B < most ? a.B : most);
         c.many_items = blocks + ceil_div(4 * (int64_t)p.many_ctas, p.Hkv) + 2;                 // blocks and what cutting adds to them
-        const int64_t most_slices = ceil_div(ceil_div((int64_t)a->max_pages * a->page_size, kKeyTile), p.min_slice);
+        const int64_t most_slices = ceil_div(ceil_div((int64_t)a.max_pages * a.page_size, kKeyTile), p.min_slice);
         int64_t cap = 6 * (int64_t)p.many_ctas + p.Hkv;
         if (most_slices <= 1) cap = 0;
         else if (blocks * most_slices * p.Hkv < cap) cap = blocks * most_slices * p.Hkv;
@@ -673,8 +732,8 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
     const size_t slots = (((size_t)p.many_cap * p.many_rows * (kHeadDim + 1)) + 3) & ~(size_t)3;
     const size_t list = c.many_items > 0 ? 4 + (c.many_items + p.many_cap / 2) * sizeof(Item) / sizeof(float) : 0;
     c.bytes = (floats + slots + list) * sizeof(float);
-    if (a->workspace) {
-        float *ws = static_cast<float *>(a->workspace);
+    if (a.workspace) {
+        float *ws = static_cast<float *>(a.workspace);
         p.few_o = ws;
         p.few_lse = ws + 2 * (size_t)p.few_ctas * p.few_rows * kHeadDim;
         p.many_o = ws + floats;
@@ -682,6 +741,60 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
         p.many_count = reinterpret_cast<int32_t *>(ws + floats + slots);
         p.many_items = reinterpret_cast<Item *>(p.many_count + 4);
         p.many_split = p.many_items + p.items_cap;
+    }
+    return PEC_OK;
+}
+
+// Checks the arguments and works out the launch.
+static int resolve(const char *who, const pec_paged_args *a, Call &c)
+{
+    if (!a) { set_error("%s: args is NULL", who); return PEC_ERR_INVALID_ARG; }
+    if (!a->q || !a->o || !a->lse) { set_error("%s: q, o and lse must be non-NULL", who); return PEC_ERR_INVALID_ARG; }
+    Params &p = c.p;
+    p = Params{};
+    p.c = {a->k_pages_stride_p, a->k_pages_stride_t, a->k_pages_stride_h, a->v_pages_stride_p, a->v_pages_stride_t, a->v_pages_stride_h,
+           a->block_table, a->table_stride, a->max_pages, a->page_size, a->num_pages, a->cu_q, a->kv_lens, a->B, (int32_t)a->T};
+    int rc = check_paged_cache(who, a->k_pages, a->v_pages, p.c, a->T, a->Hkv, a->D, a->dtype, a->status);
+    if (rc != PEC_OK) return rc;
+    const Queries qy = {a->q, a->q_stride_t, a->q_stride_h, a->dtype, a->T, a->B, a->Hq, a->Hkv, a->max_pages, a->page_size, a->max_q_len,
+                        a->o, a->o_dtype, a->lse, a->causal, a->softmax_scale, a->workspace, a->status};
+    rc = check_queries(who, qy);
+    if (rc != PEC_OK) return rc;
+    if (a->dtype == PEC_BF16 && !(fold_pages(p.c.k_sp, p.c.k_sh, p.c.num_pages, a->Hkv, p.fk) && fold_pages(p.c.v_sp, p.c.v_sh, p.c.num_pages, a->Hkv, p.fv))) {
+        set_error("%s: the pages reach over 2^31 times the greatest common divisor of their page and head strides", who);
+        return PEC_ERR_UNSUPPORTED;
+    }
+    p.k_pages = a->k_pages; p.v_pages = a->v_pages;
+    const bool tensor = a->dtype == PEC_BF16;
+    return lay_out(who, qy, {tensor, kFewRows, 1, tensor}, c);
+}
+
+static int resolve_q4(const char *who, const pec_paged_q4_args *a, Call &c)
+{
+    if (!a) { set_error("%s: args is NULL", who); return PEC_ERR_INVALID_ARG; }
+    if (!a->q || !a->o || !a->lse) { set_error("%s: q, o and lse must be non-NULL", who); return PEC_ERR_INVALID_ARG; }
+    if (a->dtype != PEC_BF16 && a->dtype != PEC_F32) { set_error("%s: unknown dtype %d", who, a->dtype); return PEC_ERR_UNSUPPORTED; }
+    Params &p = c.p;
+    p = Params{};
+    Q4Cache q;
+    int rc = resolve_q4_cache(who, a->cache, a->status, q);
+    if (rc != PEC_OK) return rc;
+    const pec_q4_cache &h = a->cache;
+    const Queries qy = {a->q, a->q_stride_t, a->q_stride_h, a->dtype, h.T, h.B, a->Hq, h.Hkv, h.max_pages, h.page_size, a->max_q_len,
+                        a->o, a->o_dtype, a->lse, a->causal, a->softmax_scale, a->workspace, a->status};
+    rc = check_queries(who, qy);
+    if (rc != PEC_OK) return rc;
+    p.c = q.c;
+    p.k_pages = q.k; p.v_pages = q.v; p.k_scales = q.ks; p.v_scales = q.vs;
+    p.ks_sp = q.ks_sp; p.ks_st = q.ks_st; p.ks_sh = q.ks_sh; p.vs_sp = q.vs_sp; p.vs_st = q.vs_st; p.vs_sh = q.vs_sh;
+    return lay_out(who, qy, {false, 0, 1, false}, c);
+}
+
+static int check_workspace(const char *who, const Call &c, const void *workspace, size_t bytes)
+{
+    if (c.bytes > 0 && (!workspace || bytes < c.bytes || !aligned16(workspace))) {
+        set_error("%s: workspace missing, misaligned or too small (%zu < %zu)", who, bytes, c.bytes);
+        return PEC_ERR_WORKSPACE;
     }
     return PEC_OK;
 }
@@ -704,15 +817,36 @@ extern "C" int pec_paged_attn(const pec_paged_args *args, void *cuda_stream)
     paged::Call c;
     int rc = paged::resolve(who, args, c);
     if (rc != PEC_OK) return rc;
-    if (c.bytes > 0 && (!args->workspace || args->workspace_bytes < c.bytes || !paged::aligned16(args->workspace))) {
-        set_error("%s: workspace missing, misaligned or too small (%zu < %zu)", who, args->workspace_bytes, c.bytes);
-        return PEC_ERR_WORKSPACE;
-    }
+    rc = paged::check_workspace(who, c, args->workspace, args->workspace_bytes);
+    if (rc != PEC_OK) return rc;
     if (args->T == 0) return PEC_OK;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (c.many_items > 0) rc = launch_paged_plan(c.p, stream);
     if (rc == PEC_OK && c.many_items > 0) rc = args->dtype == PEC_BF16 ? launch_paged_many(c.p, c.many_items, stream) : launch_paged_f32(c.p, c.many_items, stream);
     if (rc == PEC_OK && c.p.few) rc = launch_paged_few(c.p, c.many_items > 0, stream);
+    if (rc != PEC_OK || c.bytes == 0) return rc;
+    return launch_paged_combine(c.p, stream);
+}
+
+extern "C" size_t pec_paged_q4_workspace_size(const pec_paged_q4_args *args)
+{
+    paged::Call c;
+    if (paged::resolve_q4("pec_paged_q4_workspace_size", args, c) != PEC_OK) return 0;
+    return c.bytes;
+}
+
+extern "C" int pec_paged_attn_q4(const pec_paged_q4_args *args, void *cuda_stream)
+{
+    const char *who = "pec_paged_attn_q4";
+    paged::Call c;
+    int rc = paged::resolve_q4(who, args, c);
+    if (rc != PEC_OK) return rc;
+    rc = paged::check_workspace(who, c, args->workspace, args->workspace_bytes);
+    if (rc != PEC_OK) return rc;
+    if (args->cache.T == 0) return PEC_OK;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    rc = launch_paged_plan(c.p, stream);
+    if (rc == PEC_OK) rc = args->dtype == PEC_BF16 ? launch_fma<true, __nv_bfloat16>(c.p, c.many_items, stream) : launch_fma<true, float>(c.p, c.many_items, stream);
     if (rc != PEC_OK || c.bytes == 0) return rc;
     return launch_paged_combine(c.p, stream);
 }

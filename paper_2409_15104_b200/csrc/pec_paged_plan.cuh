@@ -28,10 +28,13 @@ constexpr int kFewRows = 128;                 // packed rows of the few class
 struct FoldedPages { int64_t unit; int32_t page, head; };
 
 struct Params {
+    const char *who;                          // entry point, for the host's error texts
     const void *q, *k_pages, *v_pages;
     int64_t q_st, q_sh;
     PagedCache c;
     FoldedPages fk, fv;                       // bf16
+    const uint16_t *k_scales, *v_scales;      // a cache held in 4 bits: bf16 bits, strides in elements (those of `c` are in bytes)
+    int64_t ks_sp, ks_st, ks_sh, vs_sp, vs_st, vs_sh;
     void *o;
     float *lse;
     int32_t o_is_bf16;
@@ -43,6 +46,7 @@ struct Params {
     int64_t wait_cycles;
     // few class
     int32_t few;                              // 0: every request is of the many class (fp32)
+    int32_t few_limit;                        // packed rows of such a request at most
     int32_t few_ctas;
     int32_t few_rows;                         // rows of a partial slot
     float *few_o, *few_lse;                   // [2 * few_ctas][few_rows][128], [..][few_rows]
@@ -78,7 +82,7 @@ __device__ __forceinline__ Request load_request(const Params &p, int b)
     r.start = (int32_t)start; r.n = (int32_t)n; r.kv = (int32_t)kv;
     return r;
 }
-__device__ __forceinline__ bool is_few(const Params &p, const Request &r) { return p.few && r.n > 0 && (int64_t)r.n * p.g <= kFewRows; }
+__device__ __forceinline__ bool is_few(const Params &p, const Request &r) { return p.few && r.n > 0 && (int64_t)r.n * p.g <= p.few_limit; }
 __device__ __forceinline__ bool is_many(const Params &p, const Request &r) { return r.n > 0 && !is_few(p, r); }
 __device__ __forceinline__ int32_t blocks_of(const Params &p, const Request &r) { return (r.n * p.blk_mul + p.blk_div - 1) / p.blk_div; }   // T * g < 2^31
 
