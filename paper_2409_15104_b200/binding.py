@@ -196,8 +196,8 @@ EXPORTS = ("pec_prefill_attn", "pec_workspace_size", "pec_attn_merge", "pec_attn
            "pec_last_error", "pec_decode_attn", "pec_decode_workspace_size", "pec_decode_attn_static", "pec_select_sp", "pec_linear",
            "pec_plan_ring", "pec_balance_batches", "pec_plan_worklist", "pec_worklist_block_m", "pec_control",
            "pec_linear_merged", "pec_linear_rope", "pec_rope_table", "pec_rope_table_floats",
-           "pec_qk_norm_rope", "pec_kv_append", "pec_paged_attn", "pec_paged_workspace_size",
-           "pec_kv_append_q4", "pec_kv_read_q4", "pec_paged_attn_q4", "pec_paged_q4_workspace_size")
+           "pec_qk_norm_rope", "pec_kv_append", "pec_paged_attn", "pec_paged_workspace_size")
+EXPORTS_Q4 = ("pec_kv_append_q4", "pec_kv_read_q4", "pec_paged_attn_q4", "pec_paged_q4_workspace_size")
 PEC_CTL_WAIT_LIMIT_CYCLES, PEC_CTL_TEST_SKIP_LAST_LOAD = 1, 2
 PEC_DECODE_STATIC_SCRATCH_BYTES = 4 * 1024 * 1024
 PEC_MERGE_MAX_PARTS = 16

@@ -1,6 +1,8 @@
 """CPU checks of the calls over a cache held in 4 bits: what the library refuses before any launch, workspace sizes, the binding's own
 checks, and the reference that the GPU tests compare with."""
 import ctypes
+import os
+import re
 
 import numpy as np
 import pytest
@@ -10,6 +12,14 @@ import q4_reference as q4
 from paper_2409_15104_b200 import binding
 
 BIG = 1 << 20                                                     # addresses are never dereferenced: validation fails first
+
+
+def test_library_exports_every_declared_symbol():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    header = open(os.path.join(root, "include", "pec.h")).read()
+    assert set(re.findall(r"^(?:int|size_t) (pec_[a-z_]*q4[a-z_]*)\(", header, re.M)) == set(binding.EXPORTS_Q4)
+    for name in binding.EXPORTS_Q4:
+        assert getattr(binding.load(), name) is not None
 
 
 def _cache(c, **over):
