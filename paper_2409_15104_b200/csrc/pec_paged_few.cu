@@ -115,56 +115,6 @@ __device__ __forceinline__ void mma_narrow(uint32_t d, uint64_t a0, uint64_t b0,
         "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, pt;\n\t}"
         ::"r"(d), "l"(a0), "l"(b0), "r"(idesc), "r"(accumulate), "n"(a1), "n"(a2), "n"(a3), "n"(a4), "n"(a5), "n"(a6), "n"(a7) : "memory");
 }
-// 16 consecutive columns of this warp's 32 TMEM lanes, and back.
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
-{
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n\t"
-        "tcgen05.wait::st.sync.aligned;"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
-}
-// Barrier of the 128 threads of a softmax group that also tells whether any of them says so.  It has no limit of its own, so the
-// four warps of a group reach every one of them together: whether to go on is always decided by such a vote.
-__device__ __forceinline__ bool group_any(int g, bool say)
-{
-    uint32_t any;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.u32 p, %2, 0;\n\t"
-        "barrier.cta.red.or.pred q, %1, 128, p;\n\t"
-        "selp.u32 %0, 1, 0, q;\n\t}"
-        : "=r"(any) : "r"(1 + g), "r"((uint32_t)say) : "memory");
-    return any != 0;
-}
-// Lane c (and c + 16) gets the result over the warp's lanes of value c: each step halves the values a lane is in charge of.
-template <class F>
-__device__ __forceinline__ float warp_reduce16(const float (&x)[kNarrowRows], int lane, F f)
-{
-    float y[kNarrowRows];
-#pragma unroll
-    for (int c = 0; c < kNarrowRows; ++c) y[c] = x[c];
-#pragma unroll
-    for (int d = 8; d > 0; d >>= 1) {
-        const bool upper = lane & d;
-#pragma unroll
-        for (int i = 0; i < d; ++i) {
-            const float keep = upper ? y[i + d] : y[i], send = upper ? y[i] : y[i + d];
-            y[i] = f(keep, __shfl_xor_sync(0xffffffffu, send, d));
-        }
-    }
-    return f(y[0], __shfl_xor_sync(0xffffffffu, y[0], 16));
-}
-
 template <bool kNarrow>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -449,7 +399,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     if (j > 0 && ok) ok = wait_all(&sh->pv_done[g], (pv + j - 1) & 1, sh, p);
                     stop = group_any(g, !ok);
                     if (stop) break;
-                    const float most = warp_reduce16(x, lane, [](float a, float b) { return fmaxf(a, b); });
+                    const float most = warp_reduce(x, lane, [](float a, float b) { return fmaxf(a, b); });
                     float4 *red = sh->red[g][turn ^= 1];
                     if (lane < kNarrowRows) reinterpret_cast<float *>(red + lane)[quarter] = most;
                     group_any(g, false);
@@ -504,7 +454,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             if (stop) break;
             pv += s.tiles;
             ok = wait_all(&sh->pv_done[g], (pv - 1) & 1, sh, p);
-            const float part = warp_reduce16(l, lane, [](float a, float b) { return a + b; });
+            const float part = warp_reduce(l, lane, [](float a, float b) { return a + b; });
             float4 *red = sh->red[g][turn ^= 1];
             if (lane < kNarrowRows) reinterpret_cast<float *>(red + lane)[quarter] = part;
             if (group_any(g, !ok)) break;

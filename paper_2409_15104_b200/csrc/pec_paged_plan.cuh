@@ -22,6 +22,7 @@ namespace paged {
 
 constexpr int kKeyTile = 128;                 // keys per tile
 constexpr int kFewRows = 128;                 // packed rows of the few class
+constexpr int kFewRowsQ4 = 16, kFewCtasQ4 = 2;   // the same of a cache held in 4 bits, and its kernel's CTAs per SM
 // Device-side description of one call, passed to the kernels by value.
 // Where the rows of a page's head begin, as one number for the tensor maps, whose five dimensions a box of both channel halves
 // takes up: (page * .page + head * .head) units of `unit` elements, the greatest common divisor of the two strides.
@@ -241,6 +242,7 @@ int launch_paged_plan(const paged::Params &p, cudaStream_t stream);             
 int launch_paged_f32(const paged::Params &p, int64_t items, cudaStream_t stream);       // fp32
 int launch_paged_many(const paged::Params &p, int64_t items, cudaStream_t stream);         // bf16
 int launch_paged_few(const paged::Params &p, bool after_many, cudaStream_t stream);         // bf16; after_many: overlaps that kernel's end
+int launch_paged_few_q4(const paged::Params &p, bool after_many, cudaStream_t stream);      // the same of a cache held in 4 bits, at most kFewRowsQ4 rows
 int launch_paged_combine(const paged::Params &p, cudaStream_t stream);
 
 }  // namespace pec

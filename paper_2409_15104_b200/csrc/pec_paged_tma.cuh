@@ -114,6 +114,40 @@ __device__ __forceinline__ void drain_products(uint64_t *bar, bool leader, const
     wait_quietly(bar, 0, p);
 }
 
+// Barrier of the 128 threads of a softmax group that also tells whether any of them says so.  It has no limit of its own, so the
+// four warps of a group reach every one of them together: whether to go on is always decided by such a vote.
+__device__ __forceinline__ bool group_any(int g, bool say)
+{
+    uint32_t any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %2, 0;\n\t"
+        "barrier.cta.red.or.pred q, %1, 128, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(any) : "r"(1 + g), "r"((uint32_t)say) : "memory");
+    return any != 0;
+}
+// Lane c (and c + kN, ...) gets the result over the warp's lanes of value c: each step halves the values a lane is in charge of.
+template <int kN, class F>
+__device__ __forceinline__ float warp_reduce(const float (&x)[kN], int lane, F f)
+{
+    float y[kN];
+#pragma unroll
+    for (int c = 0; c < kN; ++c) y[c] = x[c];
+#pragma unroll
+    for (int d = kN / 2; d > 0; d >>= 1) {
+        const bool upper = lane & d;
+#pragma unroll
+        for (int i = 0; i < d; ++i) {
+            const float keep = upper ? y[i + d] : y[i], send = upper ? y[i] : y[i + d];
+            y[i] = f(keep, __shfl_xor_sync(0xffffffffu, send, d));
+        }
+    }
+#pragma unroll
+    for (int d = kN; d < 32; d <<= 1) y[0] = f(y[0], __shfl_xor_sync(0xffffffffu, y[0], d));
+    return y[0];
+}
+
 namespace host_map {
 // bf16, 128-byte swizzle, rank 4.  Encoded for every call (well under a microsecond each).
 inline bool encode(CUtensorMap *map, const void *base, const uint64_t (&dims)[4], const int64_t (&strides)[3], const uint32_t (&box)[4])
@@ -142,6 +176,17 @@ inline bool pages(CUtensorMap *map, const Params &p, const void *base, int64_t s
     const cuuint64_t s[4] = {(cuuint64_t)st * 2, 128, (cuuint64_t)st * 16, (cuuint64_t)f.unit * 2};
     const cuuint32_t b[5] = {64, 8, 2, (cuuint32_t)box / 8, 1}, e[5] = {1, 1, 1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), d, s, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Pages held in 4 bits: 128 codes, tokens of a page, heads, pages; the copy spreads 16 codes over the first half of every 16 bytes.
+inline bool pages_q4(CUtensorMap *map, const Params &p, const void *base, int64_t sp, int64_t st, int64_t sh, int box)
+{
+    const host::EncodeTiledFn fn = host::encode_fn();
+    if (!fn) return false;
+    const cuuint64_t d[4] = {(cuuint64_t)kHeadDim, (cuuint64_t)p.c.page_size, (cuuint64_t)p.Hkv, (cuuint64_t)p.c.num_pages};
+    const cuuint64_t s[3] = {(cuuint64_t)st, (cuuint64_t)sh, (cuuint64_t)sp};
+    const cuuint32_t b[4] = {(cuuint32_t)kHeadDim, (cuuint32_t)box, 1, 1}, e[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, 4, const_cast<void *>(base), d, s, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 inline int box_rows(int page_size)

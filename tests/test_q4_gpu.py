@@ -209,9 +209,18 @@ def test_heads_that_are_not_finite_are_read_as_nan(pec):
 
 
 # ------------------------------------------------------------------------------------------ attention
-def p_error(hq, hkv, n, dtype):
-    """How far a probability may be off: see check_attend."""
-    return ref.HALF[BF16] if dtype == BF16 else 0.0
+def check(o, lse, want, dtype, cache, kv, most_rows, what):
+    """paged_reference.check_attend with the rounding of the probabilities here.  fp32 q: none.  bf16 q: requests of at most 16
+    packed rows hold the products of a probability and a value's scale to 2^-12 of themselves and, below that, to 2^-36 of twice
+    the largest scale, which a code of at most 6 makes 2^-35 * 6 * that scale for each key (the probabilities sum to 1 at
+    least); the others, by most_rows > 16, round probabilities to bf16."""
+    o64, lse64, A, B = want
+    error = None
+    if dtype == BF16:
+        error = 2.0 ** -12 if most_rows <= 16 else ref.HALF[BF16]
+        scales = cache[3].float()
+        A = A + max(kv) * 2.0 ** -35 * 6 * float(scales[torch.isfinite(scales)].max() if torch.isfinite(scales).any() else 0.0) / error
+    ref.check_attend(o, lse, (o64, lse64, A, B), dtype, what, error)
 
 
 def attend(pec, seed, n, kv, hq, hkv, page, dtype, *, head_major=False, causal=True, out_dtype=None, pad=0, fused=False, known=True,
@@ -230,7 +239,7 @@ def attend(pec, seed, n, kv, hq, hkv, page, dtype, *, head_major=False, causal=T
     want = q4.attend(q, cache, cu, kv, causal, scale or None)
     if pad:
         assert (o[cu[-1]:] == 7.0).all() and (lse[cu[-1]:] == 7.0).all(), "padding rows were written"
-    ref.check_attend(o, lse, want, dtype, what, p_error(hq, hkv, n, dtype))
+    check(o, lse, want, dtype, cache, kv, max(n) * (hq // hkv), what)
     first = (o.clone(), lse.clone())
     call()
     assert torch.equal(first[0], o) and torch.equal(first[1], lse), "the same call gave other bits"
