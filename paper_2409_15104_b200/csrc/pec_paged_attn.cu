@@ -673,7 +673,8 @@ static int check_queries(const char *who, const Queries &a)
 // How the call's requests are divided between the kernels.
 struct Classes {
     bool few;                                 // requests of at most few_limit packed rows go to a persistent kernel
-    int32_t few_limit, few_ctas_per_sm;
+    int32_t few_limit;
+    bool q4;                                  // of a cache held in 4 bits
     bool many_tensor;                         // the others to the tensor cores (two stages of whole tokens) or the FMA kernel (64 packed rows)
 };
 
@@ -700,7 +701,7 @@ static int lay_out(const char *who, const Queries &a, const Classes &k, Call &c)
     const bool tensor = k.many_tensor;
     p.few = k.few ? 1 : 0;
     p.few_limit = k.few_limit;
-    p.few_ctas = k.few ? sms * k.few_ctas_per_sm : sms;
+    p.few_ctas = sms * (k.q4 ? kFewCtasQ4 : 1);
     size_t floats = 0;
     if (p.few) {
         p.few_rows = (int32_t)((int64_t)p.max_q * p.g < k.few_limit ? p.max_q * p.g : k.few_limit);
@@ -766,7 +767,7 @@ static int resolve(const char *who, const pec_paged_args *a, Call &c)
     }
     p.k_pages = a->k_pages; p.v_pages = a->v_pages;
     const bool tensor = a->dtype == PEC_BF16;
-    return lay_out(who, qy, {tensor, kFewRows, 1, tensor}, c);
+    return lay_out(who, qy, {tensor, kFewRows, false, tensor}, c);
 }
 
 static int resolve_q4(const char *who, const pec_paged_q4_args *a, Call &c)
@@ -787,7 +788,7 @@ static int resolve_q4(const char *who, const pec_paged_q4_args *a, Call &c)
     p.c = q.c;
     p.k_pages = q.k; p.v_pages = q.v; p.k_scales = q.ks; p.v_scales = q.vs;
     p.ks_sp = q.ks_sp; p.ks_st = q.ks_st; p.ks_sh = q.ks_sh; p.vs_sp = q.vs_sp; p.vs_st = q.vs_st; p.vs_sh = q.vs_sh;
-    return lay_out(who, qy, {a->dtype == PEC_BF16 && a->Hq / h.Hkv <= kFewRowsQ4, kFewRowsQ4, kFewCtasQ4, false}, c);
+    return lay_out(who, qy, {a->dtype == PEC_BF16 && a->Hq / h.Hkv <= kFewRowsQ4, kFewRowsQ4, true, false}, c);
 }
 
 static int check_workspace(const char *who, const Call &c, const void *workspace, size_t bytes)

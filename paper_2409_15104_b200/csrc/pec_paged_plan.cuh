@@ -22,7 +22,7 @@ namespace paged {
 
 constexpr int kKeyTile = 128;                 // keys per tile
 constexpr int kFewRows = 128;                 // packed rows of the few class
-constexpr int kFewRowsQ4 = 16, kFewCtasQ4 = 2;   // the same of a cache held in 4 bits, and its kernel's CTAs per SM
+constexpr int kFewRowsQ4 = 16, kFewCtasQ4 = 2;   // the same of a cache held in 4 bits, and its kernel's CTAs on an SM
 // Device-side description of one call, passed to the kernels by value.
 // Where the rows of a page's head begin, as one number for the tensor maps, whose five dimensions a box of both channel halves
 // takes up: (page * .page + head * .head) units of `unit` elements, the greatest common divisor of the two strides.

@@ -37,16 +37,18 @@ namespace few_q4 {
 
 constexpr int kThreads = 256;
 constexpr int kMmaWarp = 4, kLoadWarp = 5, kQueryWarp = 6, kScaleWarp = 7;
-constexpr uint32_t kCodeTile = 128 * 128;                  // 128 tokens, their 64 bytes spread over 128
 constexpr int kScaleSlots = 4;
+constexpr int kSoftmaxRegs = 176, kLightRegs = 80;         // 128 * (176 + 80) = 256 * 128 (the launch allocation)
+constexpr float kNoKey = -3.0e38f;                         // reference maximum of a row that has seen no key
+constexpr uint32_t kCodeTile = 128 * 128;                  // 128 tokens, their 64 bytes spread over 128
 constexpr float kGrow = 3.0f;                              // log2 units: a row's reference maximum moves when outgrown by 2^3
 constexpr float kBase = 1024.0f;                           // p * sv / v_ref is at most 2^3 * 4; times 2^10 it stays below e5m2's 57344
 
 template <int kRows> struct Cfg {
-    static constexpr int kSlots = kRows == 8 ? 6 : 5;
-    static constexpr int kColsS = 2 * kRows, kColsO = 4 * kRows;
-    static constexpr uint32_t kQBytes = kColsS * 128, kPRow = kColsO, kPBytes = 128 * kPRow;
-    static constexpr uint32_t kTmemCols = kRows == 8 ? 64 : 128, kColO = 2 * kColsS;
+    static constexpr int kSlots = kRows == 16 ? 5 : 6;
+    static constexpr int kColsS = kRows == 4 ? 16 : 2 * kRows, kColsO = 4 * kRows;      // (a product has 16 columns at least)
+    static constexpr uint32_t kQBytes = kColsS * 128, kPRow = kRows == 16 ? 64 : 32, kPBytes = 128 * kPRow;
+    static constexpr uint32_t kTmemCols = kRows == 16 ? 128 : 64, kColO = 2 * kColsS;
     static constexpr uint32_t kOffQ = 0, kOffP = 2 * kQBytes, kOffRing = kOffP + 2 * kPBytes;
 };
 
@@ -54,7 +56,6 @@ struct Segment {
     int32_t tiles;                                         // 0: no more segments
     int32_t key0;                                          // position of the first tile's first key
     int32_t kv, pos0, rows;
-    int32_t tile0;                                         // the CTA's count of tiles before this segment
     int64_t out;                                           // whole unit: (first token row * Hq + first head); else partial slot * few_rows
     int32_t whole;
 };
@@ -67,7 +68,7 @@ struct Shared {
     Segment seg[2];
     float q_factor[2][16];                                 // of a row's scores: log2 units of the scaled score over that of the product
     float4 red[2][17];                                     // every other exchange: rows, the scales of V; one component per warp
-    uint16_t scale[kScaleSlots][2][kKeyTile];              // K, V; bf16 bits
+    uint32_t scale[kScaleSlots][kKeyTile];                 // bf16 bits: K, V << 16
     int32_t count;
     uint32_t tmem_base;
     volatile int abort_flag;
@@ -76,8 +77,8 @@ template <int kRows> constexpr size_t smem_bytes()
 {
     return Cfg<kRows>::kOffRing + Cfg<kRows>::kSlots * kCodeTile + 1024 /*alignment slack*/ + sizeof(Shared);
 }
-// Two CTAs on an SM of 228 KB, of which each takes 1 KB for itself.
-static_assert(smem_bytes<8>() <= 113 * 1024 && smem_bytes<16>() <= 113 * 1024, "two CTAs per SM");
+// An SM has 228 KB, of which each CTA takes 1 KB for itself.
+static_assert(smem_bytes<4>() <= 113 * 1024 && smem_bytes<8>() <= 113 * 1024 && smem_bytes<16>() <= 113 * 1024, "two CTAs per SM");
 
 __device__ __forceinline__ bool wait_all(uint64_t *bar, uint32_t parity, Shared *sh, const Params &p)   // warp-uniform
 {
@@ -110,20 +111,14 @@ __device__ __forceinline__ void mma4(uint32_t d, uint64_t a, uint64_t b, uint32_
         ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "n"(kA), "n"(kB) : "memory");
 }
 
-// Two numbers as e4m3 or e5m2, the first in the low byte.
+// Two numbers as e4m3, the first in the low byte.
 __device__ __forceinline__ uint32_t to_e4m3(float2 x)
 {
     uint16_t r;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(x.y), "f"(x.x));
     return r;
 }
-__device__ __forceinline__ uint32_t to_e5m2(float2 x)
-{
-    uint16_t r;
-    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(x.y), "f"(x.x));
-    return r;
-}
-// The part of x that such a number takes (returned), and the rest, scaled up.
+// The part of x that e4m3 takes (returned), and 16 times the rest.
 __device__ __forceinline__ uint32_t take_e4m3(float2 &x)
 {
     const uint32_t r = to_e4m3(x);
@@ -133,18 +128,27 @@ __device__ __forceinline__ uint32_t take_e4m3(float2 &x)
     x = __fmul2_rn(__fadd2_rn(x, make_float2(-f.x, -f.y)), make_float2(16.f, 16.f));
     return r;
 }
-__device__ __forceinline__ uint32_t take_e5m2(float2 &x)
+// Four numbers, as fp16, to four parts of e5m2 each (a word of four bytes a part).  e5m2 is the upper byte of fp16: a part is what is left
+// cut to its first three bits, and the eleven bits of an fp16 are 3 + 3 + 3 + 2.
+__device__ __forceinline__ void split_e5m2(float2 lo, float2 hi, uint32_t (&part)[4])
 {
-    const uint32_t r = to_e5m2(x), h = __byte_perm(r, 0u, 0x1404);     // e5m2 is the upper byte of fp16
-    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-    x = __fmul2_rn(__fadd2_rn(x, make_float2(-f.x, -f.y)), make_float2(8.f, 8.f));
-    return r;
+    __half2 a = __float22half2_rn(lo), b = __float22half2_rn(hi);
+    const __half2 eight = __half2half2(__ushort_as_half(0x4800));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t ua = *reinterpret_cast<const uint32_t *>(&a), ub = *reinterpret_cast<const uint32_t *>(&b);
+        part[i] = __byte_perm(ua, ub, 0x7531);
+        if (i == 3) break;
+        const uint32_t ta = ua & 0xff00ff00u, tb = ub & 0xff00ff00u;
+        a = __hmul2(__hsub2(a, *reinterpret_cast<const __half2 *>(&ta)), eight);
+        b = __hmul2(__hsub2(b, *reinterpret_cast<const __half2 *>(&tb)), eight);
+    }
 }
 
 template <int kRows>
 __global__ void __launch_bounds__(kThreads, kFewCtasQ4)
 paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Params p, const int box,
-                    const int skip_last)
+                    const int scales_by_four, const int skip_last)
 {
     typedef Cfg<kRows> C;
     constexpr int kSlots = C::kSlots;
@@ -193,6 +197,7 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     if (count == 0) {
     } else if (warp == kLoadWarp) {
         // ------------------------------------------------------------------ loader of the codes
+        reg_dealloc<kLightRegs>();
         const BoxLane bl = {lane * box, (uint32_t)(lane * box) * 128u, lane * box < kKeyTile};
         const int32_t end = first + count;
         const BoxStep step = box_step(p.c.page_size);
@@ -240,6 +245,9 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         __syncwarp();
     } else if (warp == kQueryWarp) {
         // ------------------------------------------------------------------ segments and their queries
+        reg_dealloc<kLightRegs>();
+        // An earlier CTA's wait has run out: the launch is lost, every wait of this CTA gives up at its next try.
+        if (lane == 0 && *reinterpret_cast<volatile int32_t *>(p.status) == PEC_ERR_TIMEOUT) sh->abort_flag = 1;
         const int32_t end = first + count;
         int segs = 0, n = 0;
         bool ok = true;
@@ -282,7 +290,8 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
                 const uint32_t one = take_e4m3(lo) | take_e4m3(hi) << 16, two = to_e4m3(lo) | to_e4m3(hi) << 16;
                 const uint32_t to = (uint32_t)c * 128u + (((uint32_t)(lane >> 2) ^ (uint32_t)(c & 7)) << 4);
                 *reinterpret_cast<uint32_t *>(dst + to) = one;
-                *reinterpret_cast<uint32_t *>(dst + kRows * 128 + to) = two;
+                const uint32_t to2 = (uint32_t)(kRows + c) * 128u + (((uint32_t)(lane >> 2) ^ (uint32_t)((kRows + c) & 7)) << 4);
+                *reinterpret_cast<uint32_t *>(dst + to2) = two;
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             if (lane == 0) {
@@ -290,7 +299,6 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
                 s.tiles = tiles;
                 s.key0 = walk.tile * kKeyTile;
                 s.kv = walk.r.kv; s.pos0 = walk.r.pos0(); s.rows = rows;
-                s.tile0 = n;
                 s.whole = tiles == walk.r.tiles();
                 s.out = s.whole ? (int64_t)walk.r.start * p.Hq + (int64_t)walk.kvh * p.g
                                 : (2 * (int64_t)blockIdx.x + (walk.u0 > first ? 1 : 0)) * p.few_rows;
@@ -309,77 +317,9 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             if (ok && lane == 0) { sh->seg[g].tiles = 0; mbar_arrive(smem_u32(&sh->q_full[g])); }
         }
         __syncwarp();
-    } else if (warp == kScaleWarp) {
-        // ------------------------------------------------------------------ scales: a lane takes keys lane + 32 i of each tile
-        // An earlier CTA's wait has run out: the launch is lost, every wait of this CTA gives up at its next try.
-        if (lane == 0 && *reinterpret_cast<volatile int32_t *>(p.status) == PEC_ERR_TIMEOUT) sh->abort_flag = 1;
-        // Three tiles under way: one's scales on their way to shared memory, the next one's being loaded, the pages of the one after
-        // being looked up.
-        const int32_t end = first + count;
-        const BoxStep step = box_step(p.c.page_size);
-        int32_t left = min(walk.u0 + walk.r.tiles(), end) - max(walk.u0, first), k0 = walk.tile * kKeyTile, seen = 0;
-        BoxPlace at[4];
-        auto place = [&] {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) at[i] = box_place(p.c.page_size, k0, {lane + 32 * i, 0u, true});
-        };
-        place();
-        struct Pages { int32_t page[4], row[4], kvh; };
-        auto look_up = [&](Pages &x) {                     // of the walk's tile; then to the next one
-            x.kvh = walk.kvh;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x.row[i] = at[i].row;
-                x.page[i] = k0 + lane + 32 * i < walk.r.kv ? __ldg(p.c.table + walk.b * p.c.table_stride + at[i].nth) : -1;
-            }
-            if (++seen >= count) return;
-            if (--left > 0) {
-                k0 += kKeyTile;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) at[i] = box_next(at[i], step);
-            } else {
-                walk_next(p, walk, lane);
-                left = min(walk.u0 + walk.r.tiles(), end) - walk.u0;
-                k0 = 0;
-                place();
-            }
-        };
-        uint16_t sk[4], sv[4];
-        auto load = [&](const Pages &x) {                  // bad page numbers (the loader reports them) and keys past the end: 0
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sk[i] = sv[i] = 0;
-                if (x.page[i] >= 0 && x.page[i] < p.c.num_pages) {
-                    sk[i] = __ldg(p.k_scales + x.page[i] * p.ks_sp + x.row[i] * p.ks_st + x.kvh * p.ks_sh);
-                    sv[i] = __ldg(p.v_scales + x.page[i] * p.vs_sp + x.row[i] * p.vs_st + x.kvh * p.vs_sh);
-                }
-            }
-        };
-        Pages next;
-        look_up(next);
-        load(next);
-        if (count > 1) look_up(next);
-        bool ok = true;
-        for (int n = 0; n < count && ok; ++n) {
-            uint16_t k[4], v[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { k[i] = sk[i]; v[i] = sv[i]; }
-            if (n + 1 < count) load(next);
-            if (n + 2 < count) look_up(next);
-            const int slot = n % kScaleSlots;
-            if (n >= kScaleSlots) ok = wait_all(&sh->sc_empty[slot], (n / kScaleSlots - 1) & 1, sh, p);
-            if (!ok) break;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sh->scale[slot][0][lane + 32 * i] = k[i];
-                sh->scale[slot][1][lane + 32 * i] = v[i];
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh->sc_full[slot]));
-        }
-        __syncwarp();
     } else if (warp == kMmaWarp) {
         // ------------------------------------------------------------------ MMA issuer (the whole warp walks, one lane issues)
+        reg_dealloc<kLightRegs>();
         const bool leader = elect_one();
         constexpr uint32_t idesc_qk = idesc_f8f6f4_f32(128, C::kColsS, kE2M1, kE4M3, 0, 0);
         constexpr uint32_t idesc_pv = idesc_f8f6f4_f32(kHeadDim, C::kColsO, kE2M1, kE5M2, 1, 1);
@@ -431,71 +371,173 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         }
         if (!ok) drain_products(&sh->drained, leader, p);
         __syncwarp();
+    } else if (warp == kScaleWarp) {
+        // ------------------------------------------------------------------ scales: a lane has keys 4 lane .. + 3 of each tile
+        // They lie in one page (boxes are eight keys at least).  Loads run two tiles ahead of the stores, the page's number one more.
+        reg_dealloc<kLightRegs>();
+        const int32_t end = first + count;
+        const BoxStep step = box_step(p.c.page_size);
+        const BoxLane bl = {4 * lane, 0u, true};
+        int32_t left = min(walk.u0 + walk.r.tiles(), end) - max(walk.u0, first), k0 = walk.tile * kKeyTile, seen = 0;
+        BoxPlace at = box_place(p.c.page_size, k0, bl);
+        int32_t page = -1, row = 0, keys = 0, kvh = 0;     // of the next tile to load: its keys before the request's end
+        auto look_up = [&] {                               // of the walk's tile; then to the next one
+            row = at.row; kvh = walk.kvh;
+            keys = min(max(walk.r.kv - k0 - 4 * lane, 0), 4);
+            page = keys > 0 ? __ldg(p.c.table + walk.b * p.c.table_stride + at.nth) : -1;
+            if (++seen >= count) return;
+            if (--left > 0) {
+                k0 += kKeyTile;
+                at = box_next(at, step);
+            } else {
+                walk_next(p, walk, lane);
+                left = min(walk.u0 + walk.r.tiles(), end) - walk.u0;
+                k0 = 0;
+                at = box_place(p.c.page_size, 0, bl);
+            }
+        };
+        struct Four { uint32_t k01, k23, v01, v23; };      // bf16 bits
+        Four set[3];
+        auto load = [&](Four &x) {                         // keys past the end, and pages out of range (the loader reports them): 0
+            x = {0u, 0u, 0u, 0u};
+            if (page < 0 || page >= p.c.num_pages) return;
+            const uint16_t *k = p.k_scales + page * p.ks_sp + row * p.ks_st + kvh * p.ks_sh, *v = p.v_scales + page * p.vs_sp + row * p.vs_st + kvh * p.vs_sh;
+            if (scales_by_four) {                          // (a page holds all four, whatever is in those past the end)
+                const uint2 a = __ldg(reinterpret_cast<const uint2 *>(k)), b = __ldg(reinterpret_cast<const uint2 *>(v));
+                x = {a.x, a.y, b.x, b.y};
+            } else {
+                x.k01 = __ldg(k) | (uint32_t)__ldg(k + p.ks_st) << 16;
+                x.k23 = __ldg(k + 2 * p.ks_st) | (uint32_t)__ldg(k + 3 * p.ks_st) << 16;
+                x.v01 = __ldg(v) | (uint32_t)__ldg(v + p.vs_st) << 16;
+                x.v23 = __ldg(v + 2 * p.vs_st) | (uint32_t)__ldg(v + 3 * p.vs_st) << 16;
+            }
+        };
+        int32_t valid[3];                                  // keys of each set
+        look_up();
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            valid[u] = 0;
+            if (u < count) {
+                load(set[u]);
+                valid[u] = keys;
+                if (u + 1 < count) look_up();
+            }
+        }
+        bool ok = true;
+        for (int n0 = 0; n0 < count && ok; n0 += 3) {
+#pragma unroll
+            for (int u = 0; u < 3; ++u) {
+                const int n = n0 + u;
+                if (n >= count || !ok) break;
+                if (n + 2 < count) {
+                    load(set[(u + 2) % 3]);
+                    valid[(u + 2) % 3] = keys;
+                    if (n + 3 < count) look_up();
+                }
+                const int slot = n % kScaleSlots;
+                if (n >= kScaleSlots) ok = wait_all(&sh->sc_empty[slot], (n / kScaleSlots - 1) & 1, sh, p);
+                if (!ok) break;
+                const Four x = set[u];
+                const int have = valid[u];
+                uint4 w = make_uint4(__byte_perm(x.k01, x.v01, 0x5410), __byte_perm(x.k01, x.v01, 0x7632),
+                                     __byte_perm(x.k23, x.v23, 0x5410), __byte_perm(x.k23, x.v23, 0x7632));
+                if (have < 4) {
+                    if (have < 1) w.x = 0u;
+                    if (have < 2) w.y = 0u;
+                    if (have < 3) w.z = 0u;
+                    w.w = 0u;
+                }
+                *reinterpret_cast<uint4 *>(&sh->scale[slot][4 * lane]) = w;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh->sc_full[slot]));
+            }
+        }
+        __syncwarp();
     } else {
         // ------------------------------------------------------------------ softmax and epilogue
+        reg_alloc<kSoftmaxRegs>();
         const int quarter = warp, key = tid;               // and channel `key` of the accumulator
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         const uint32_t tO = tmem + lane_base + C::kColO;
         // P'^T: a row of kPRow bytes per key, its 16-byte chunks XOR-swizzled by bits of the key.
         const uint32_t p_row = (uint32_t)key * C::kPRow, p_swizzle = (C::kPRow == 32 ? (uint32_t)(key >> 2) & 1u : (uint32_t)(key >> 1) & 3u) << 4;
+        constexpr int kPairs = kRows / 2;
         int n = 0, turn = 0;                               // tiles so far; exchanges take turns in two buffers (see pec_paged_few.cu)
         for (int k = 0;; ++k) {
             bool ok = wait_all(&sh->q_full[k & 1], (k >> 1) & 1, sh, p);
             if (group_any(0, !ok)) break;
             const Segment s = sh->seg[k & 1];
-            float factor[kRows];
+            float2 factor[kPairs];
 #pragma unroll
-            for (int c = 0; c < kRows; ++c) factor[c] = sh->q_factor[k & 1][c];
+            for (int c = 0; c < kPairs; ++c) factor[c] = make_float2(sh->q_factor[k & 1][2 * c], sh->q_factor[k & 1][2 * c + 1]);
             __syncwarp();
             if (s.tiles == 0) break;
             if (lane == 0) mbar_arrive(smem_u32(&sh->q_empty[k & 1]));
             const int32_t see_all = (p.causal && s.pos0 + 1 < s.kv) ? s.pos0 + 1 : s.kv;           // keys below it are visible to every row
-            float m[kRows], l[kRows];                      // per row: reference maximum (log2 units, the same in all threads), this thread's sum
+            // Per row: minus the reference maximum (log2 units, the same in all threads; rows past the segment's: -inf, and all their
+            // probabilities 0), this thread's sum.
+            float2 neg_m[kPairs], l[kPairs];
+            float m_row = (lane & (kRows - 1)) < s.rows ? kNoKey : INFINITY;   // reference of row lane % kRows
 #pragma unroll
-            for (int c = 0; c < kRows; ++c) { m[c] = -INFINITY; l[c] = 0.f; }
-            float m_row = -INFINITY;                       // m of row lane % kRows
+            for (int c = 0; c < kPairs; ++c) {
+                neg_m[c] = make_float2(2 * c < s.rows ? -kNoKey : -INFINITY, 2 * c + 1 < s.rows ? -kNoKey : -INFINITY);
+                l[c] = make_float2(0.f, 0.f);
+            }
             float v_ref = 0.f, v_factor = 0.f;             // a power of two that no scale of V passes four times; kBase / v_ref
             int32_t k0 = s.key0;
             bool stop = false;
             for (int j = 0; j < s.tiles; ++j, ++n, k0 += kKeyTile) {
                 const int buf = n & 1, slot = n % kScaleSlots;
                 ok = wait_all(&sh->sc_full[slot], (n / kScaleSlots) & 1, sh, p);
-                const float ks = __uint_as_float((uint32_t)sh->scale[slot][0][key] << 16), vs = __uint_as_float((uint32_t)sh->scale[slot][1][key] << 16);
+                const uint32_t scales = sh->scale[slot][key];
+                const float2 scale = make_float2(__uint_as_float(scales << 16), __uint_as_float(scales & 0xffff0000u));   // K, V
+                if (ok) ok = wait_all(&sh->s_full[buf], (n >> 1) & 1, sh, p);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&sh->sc_empty[slot]));
-                if (ok) ok = wait_all(&sh->s_full[buf], (n >> 1) & 1, sh, p);
                 tc_fence_after();
                 uint32_t r[C::kColsS];
-                if constexpr (kRows == 8) tmem_ld16(tmem + lane_base + (uint32_t)buf * C::kColsS, r);
+                if constexpr (C::kColsS == 16) tmem_ld16(tmem + lane_base + (uint32_t)buf * C::kColsS, r);
                 else tmem_ld32(tmem + lane_base + (uint32_t)buf * C::kColsS, r);
                 tc_fence_before();
-                float x[kRows];
+                float2 x[kPairs];
 #pragma unroll
-                for (int c = 0; c < kRows; ++c)
-                    x[c] = fmaf(__uint_as_float(r[kRows + c]), 1.f / 16.f, __uint_as_float(r[c])) * (factor[c] * ks);
+                for (int c = 0; c < kPairs; ++c) {
+                    const float2 hi = make_float2(__uint_as_float(r[2 * c]), __uint_as_float(r[2 * c + 1]));
+                    const float2 lo = make_float2(__uint_as_float(r[kRows + 2 * c]), __uint_as_float(r[kRows + 2 * c + 1]));
+                    x[c] = __fmul2_rn(__ffma2_rn(lo, make_float2(1.f / 16.f, 1.f / 16.f), hi), __fmul2_rn(factor[c], make_float2(scale.x, scale.x)));
+                }
                 const bool border = k0 + kKeyTile > see_all;
                 if (border) {                              // by choice, not by arithmetic: a masked score may be anything
+                    int t = 0, h = 0;                      // token and head of the row
 #pragma unroll
                     for (int c = 0; c < kRows; ++c) {
-                        const int32_t see = p.causal ? min(s.kv, s.pos0 + c / p.g + 1) : s.kv;
-                        x[c] = k0 + key < see ? x[c] : -INFINITY;
+                        const int32_t see = p.causal ? min(s.kv, s.pos0 + t + 1) : s.kv;
+                        float &y = c & 1 ? x[c / 2].y : x[c / 2].x;
+                        y = k0 + key < see ? y : -INFINITY;
+                        if (++h == p.g) { h = 0; ++t; }
                     }
                 }
-                bool grow = vs > 4.f * v_ref;
+                float2 d[kPairs];                          // over the reference maxima
+                float most_d = -INFINITY;
 #pragma unroll
-                for (int c = 0; c < kRows; ++c) {
-                    if (c < s.rows) grow = grow || x[c] > m[c] + kGrow;
+                for (int c = 0; c < kPairs; ++c) {
+                    d[c] = __fadd2_rn(x[c], neg_m[c]);
+                    most_d = fmax3(most_d, d[c].x, d[c].y);
                 }
+                const bool grow = most_d > kGrow || scale.y > 4.f * v_ref;
                 // The references move only when one is outgrown (and at first); O then waits for its product in flight.  (S(n) is
                 // complete, and with it PV(n - 2), issued before it; PV(n) needs this P(n): the parity tells PV(n - 1)'s phase.)
                 if (j == 0 || group_any(0, grow || !ok)) {
                     if (j > 0 && ok) ok = wait_all(&sh->pv_done, (n - 1) & 1, sh, p);
                     stop = group_any(0, !ok);
                     if (stop) break;
-                    const float most = warp_reduce(x, lane, [](float a, float b) { return fmaxf(a, b); });
-                    float v_most = fmaxf(vs, 0.f);
+                    float y[kRows];
 #pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) v_most = fmaxf(v_most, __shfl_xor_sync(0xffffffffu, v_most, d));
+                    for (int c = 0; c < kPairs; ++c) { y[2 * c] = x[c].x; y[2 * c + 1] = x[c].y; }
+                    const float most = warp_reduce(y, lane, [](float a, float b) { return fmaxf(a, b); });
+                    float v_most = fmaxf(scale.y, 0.f);
+#pragma unroll
+                    for (int i = 16; i > 0; i >>= 1) v_most = fmaxf(v_most, __shfl_xor_sync(0xffffffffu, v_most, i));
                     float4 *red = sh->red[turn ^= 1];
                     if (lane < kRows) reinterpret_cast<float *>(red + lane)[quarter] = most;
                     if (lane == 0) reinterpret_cast<float *>(red + 16)[quarter] = v_most;
@@ -511,65 +553,72 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
                         v_factor = kBase / ref;
                     }
                     const float top = fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w));
-                    const bool move = (lane & (kRows - 1)) < s.rows && top > m_row + kGrow;
+                    const bool move = top > m_row + kGrow;
                     const float a_row = move ? ex2(m_row - top) : 1.f;     // 0 when the row had no key so far
                     if (move) m_row = top;
                     float alpha[kRows];
 #pragma unroll
                     for (int c = 0; c < kRows; ++c) {
-                        m[c] = __shfl_sync(0xffffffffu, m_row, c);
+                        const float m = __shfl_sync(0xffffffffu, m_row, c);
                         alpha[c] = __shfl_sync(0xffffffffu, a_row, c);
-                        l[c] *= alpha[c];
+                        float &lc = c & 1 ? l[c / 2].y : l[c / 2].x, &nm = c & 1 ? neg_m[c / 2].y : neg_m[c / 2].x;
+                        lc *= alpha[c];
+                        nm = -m;
                         alpha[c] *= v_alpha;
                     }
+#pragma unroll
+                    for (int c = 0; c < kPairs; ++c) d[c] = __fadd2_rn(x[c], neg_m[c]);
                     if (j > 0) {
                         tc_fence_after();
-                        uint32_t o[32];
-                        tmem_ld32(tO, o);
+                        if constexpr (kRows == 4) {
+                            uint32_t o[16];
+                            tmem_ld16(tO, o);
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha[c % kRows]);
-                        tmem_st32(tO, o);
-                        if constexpr (kRows == 16) {
-                            tmem_ld32(tO + 32, o);
+                            for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha[c % kRows]);
+                            tmem_st16(tO, o);
+                        } else {
 #pragma unroll
-                            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha[c % kRows]);
-                            tmem_st32(tO + 32, o);
+                            for (int i = 0; i < C::kColsO; i += 32) {
+                                uint32_t o[32];
+                                tmem_ld32(tO + i, o);
+#pragma unroll
+                                for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha[c % kRows]);
+                                tmem_st32(tO + i, o);
+                            }
                         }
                         tmem_st_wait();
                         tc_fence_before();
                     }
                 }
                 // p = 2^(x - m); the row's sum takes p itself, the product p sv / v_ref in four parts.
-                float e[kRows];
-                const float f = vs * v_factor;
+                const float f = scale.y * v_factor;
 #pragma unroll
-                for (int c = 0; c < kRows; ++c) {
-                    e[c] = ex2(x[c] - (m[c] == -INFINITY ? 0.f : m[c]));
-                    l[c] += e[c];
-                    e[c] *= f;
+                for (int c = 0; c < kPairs; ++c) {
+                    d[c] = make_float2(ex2(d[c].x), ex2(d[c].y));
+                    l[c] = __fadd2_rn(l[c], d[c]);
+                    d[c] = __fmul2_rn(d[c], make_float2(f, f));
                 }
                 if (border && !(f < INFINITY)) {           // a value that is not finite spoils no row that does not see it
 #pragma unroll
-                    for (int c = 0; c < kRows; ++c)
-                        if (x[c] == -INFINITY) e[c] = 0.f;
+                    for (int c = 0; c < kPairs; ++c) {
+                        if (x[c].x == -INFINITY) d[c].x = 0.f;
+                        if (x[c].y == -INFINITY) d[c].y = 0.f;
+                    }
                 }
-                uint32_t parts[4][kRows / 4];
+                uint32_t parts[kRows / 4][4];
 #pragma unroll
-                for (int c = 0; c < kRows; c += 4) {
-                    float2 a = make_float2(e[c], e[c + 1]), b = make_float2(e[c + 2], e[c + 3]);
-#pragma unroll
-                    for (int i = 0; i < 3; ++i) parts[i][c / 4] = take_e5m2(a) | take_e5m2(b) << 16;
-                    parts[3][c / 4] = to_e5m2(a) | to_e5m2(b) << 16;
-                }
+                for (int c = 0; c < kRows / 4; ++c) split_e5m2(d[2 * c], d[2 * c + 1], parts[c]);
                 // (S(n) is complete, and with it PV(n - 2), which read this buffer.)
                 uint8_t *dst = smem + C::kOffP + (uint32_t)buf * C::kPBytes + p_row;
-                if constexpr (kRows == 8) {
-                    *reinterpret_cast<uint4 *>(dst + p_swizzle) = make_uint4(parts[0][0], parts[0][1], parts[1][0], parts[1][1]);
-                    *reinterpret_cast<uint4 *>(dst + (16u ^ p_swizzle)) = make_uint4(parts[2][0], parts[2][1], parts[3][0], parts[3][1]);
+                if constexpr (kRows == 4) {
+                    *reinterpret_cast<uint4 *>(dst + p_swizzle) = make_uint4(parts[0][0], parts[0][1], parts[0][2], parts[0][3]);
+                } else if constexpr (kRows == 8) {
+                    *reinterpret_cast<uint4 *>(dst + p_swizzle) = make_uint4(parts[0][0], parts[1][0], parts[0][1], parts[1][1]);
+                    *reinterpret_cast<uint4 *>(dst + (16u ^ p_swizzle)) = make_uint4(parts[0][2], parts[1][2], parts[0][3], parts[1][3]);
                 } else {
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i)
-                        *reinterpret_cast<uint4 *>(dst + ((i << 4) ^ p_swizzle)) = make_uint4(parts[i][0], parts[i][1], parts[i][2], parts[i][3]);
+                        *reinterpret_cast<uint4 *>(dst + ((i << 4) ^ p_swizzle)) = make_uint4(parts[0][i], parts[1][i], parts[2][i], parts[3][i]);
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
@@ -577,14 +626,21 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             }
             if (stop) break;
             ok = wait_all(&sh->pv_done, (n - 1) & 1, sh, p);
-            const float part = warp_reduce(l, lane, [](float a, float b) { return a + b; });
+            float y[kRows];
+#pragma unroll
+            for (int c = 0; c < kPairs; ++c) { y[2 * c] = l[c].x; y[2 * c + 1] = l[c].y; }
+            const float part = warp_reduce(y, lane, [](float a, float b) { return a + b; });
             float4 *red = sh->red[turn ^= 1];
             if (lane < kRows) reinterpret_cast<float *>(red + lane)[quarter] = part;
             if (group_any(0, !ok)) break;
             tc_fence_after();
             uint32_t o[C::kColsO];
-            tmem_ld32(tO, *reinterpret_cast<uint32_t (*)[32]>(o));
-            if constexpr (kRows == 16) tmem_ld32(tO + 32, *reinterpret_cast<uint32_t (*)[32]>(o + 32));
+            if constexpr (kRows == 4) {
+                tmem_ld16(tO, o);
+            } else {
+                tmem_ld32(tO, *reinterpret_cast<uint32_t (*)[32]>(o));
+                if constexpr (kRows == 16) tmem_ld32(tO + 32, *reinterpret_cast<uint32_t (*)[32]>(o + 32));
+            }
             tc_fence_before();
             // Lane c works out row c's factor, place and LSE.
             const int row = lane & (kRows - 1);
@@ -615,11 +671,14 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     griddep_wait();
 }
 
+// Whether the scales of four tokens can be loaded at once.
+static bool by_four(const uint16_t *s, int64_t sp, int64_t st, int64_t sh) { return st == 1 && sp % 4 == 0 && sh % 4 == 0 && reinterpret_cast<uintptr_t>(s) % 8 == 0; }
+
 template <int kRows>
 static cudaError_t launch(const Params &p, const CUtensorMap &tm_k, const CUtensorMap &tm_v, int box, bool after_many, cudaStream_t stream)
 {
     return launch_dependent(paged_few_q4_kernel<kRows>, dim3((unsigned)p.few_ctas), kThreads, smem_bytes<kRows>(), stream, after_many, tm_k, tm_v, p, box,
-                            (int)test_skip_last_load());
+                            by_four(p.k_scales, p.ks_sp, p.ks_st, p.ks_sh) && by_four(p.v_scales, p.vs_sp, p.vs_st, p.vs_sh), (int)test_skip_last_load());
 }
 
 }  // namespace few_q4
@@ -638,14 +697,16 @@ int launch_paged_few_q4(const paged::Params &p, bool after_many, cudaStream_t st
     static unsigned char ready[host::kMaxDevices] = {};
     static std::mutex ready_mutex;
     if (!host::once_per_device(ready, ready_mutex, [] {
-            return cudaFuncSetAttribute(few_q4::paged_few_q4_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_q4::smem_bytes<8>()) == cudaSuccess &&
+            return cudaFuncSetAttribute(few_q4::paged_few_q4_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_q4::smem_bytes<4>()) == cudaSuccess &&
+                   cudaFuncSetAttribute(few_q4::paged_few_q4_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_q4::smem_bytes<8>()) == cudaSuccess &&
                    cudaFuncSetAttribute(few_q4::paged_few_q4_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_q4::smem_bytes<16>()) == cudaSuccess; })) {
         (void)cudaGetLastError();
         set_error("%s: cannot raise the shared-memory limit", p.who);
         return PEC_ERR_CUDA;
     }
-    // Eight rows where no request can have more (p.few_rows is the most any can have).
-    cudaError_t err = p.few_rows <= 8 ? few_q4::launch<8>(p, tm_k, tm_v, box, after_many, stream) : few_q4::launch<16>(p, tm_k, tm_v, box, after_many, stream);
+    // The form for as many rows as a request can have (p.few_rows).
+    cudaError_t err = p.few_rows <= 4 ? few_q4::launch<4>(p, tm_k, tm_v, box, after_many, stream)
+                    : p.few_rows <= 8 ? few_q4::launch<8>(p, tm_k, tm_v, box, after_many, stream) : few_q4::launch<16>(p, tm_k, tm_v, box, after_many, stream);
     if (err == cudaSuccess) err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("%s: launch failed: %s", p.who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
