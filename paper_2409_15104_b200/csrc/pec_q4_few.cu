@@ -16,17 +16,22 @@
 // Products of such numbers are exact and their sums are kept in fp32.
 //
 // The split of the work is that of pec_paged_few.cu: the key tiles of all (request, KV head) units on one line, an equal piece of it
-// for each CTA, units that cross a cut merged by the combining kernel.  Two CTAs per SM, so that one's exchange of maxima and its
-// epilogues run beside the other's.
+// for each CTA, units that cross a cut merged by the combining kernel.
+//
+// A tile has 750 cycles at the rate of HBM, and every warp of the chain (where it lies, its copies, products, softmax, products) spends
+// most of its time on hand-overs.  So two CTAs per SM, and a step takes 256 keys where shared memory has room for it (up to 8 rows).
 //
 // Warp roles:
 //   warps 0-3  softmax and epilogue
-//   warp 4     MMA issuer      warp 5  TMA loader of the codes (a ring of K and V tiles)
-//   warp 6     segment descriptors and Q (two buffers)      warp 7  scales (a ring of tiles)
+//   warp 4     MMA issuer (one thread)
+//   warp 5, 7  loaders of K and V: codes by the copy unit, scales (rings of steps).  Two, because a copy of 128 rows of 64 bytes keeps the
+//              warp that starts it for 400 to 600 cycles
+//   warp 6     walks the line: where each step lies, for the loaders; descriptor and Q of each segment (two buffers)
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <cstddef>
 #include "pec_paged_tma.cuh"
 #include "pec_q4.cuh"
 
@@ -36,46 +41,52 @@ namespace paged {
 namespace few_q4 {
 
 constexpr int kThreads = 256;
-constexpr int kMmaWarp = 4, kLoadWarp = 5, kQueryWarp = 6, kScaleWarp = 7;
-constexpr int kScaleSlots = 4;
+constexpr int kMmaWarp = 4, kKeyWarp = 5, kPlanWarp = 6, kValueWarp = 7;
 constexpr int kSoftmaxRegs = 176, kLightRegs = 80;         // 128 * (176 + 80) = 256 * 128 (the launch allocation)
-constexpr float kNoKey = -3.0e38f;                         // reference maximum of a row that has seen no key
 constexpr uint32_t kCodeTile = 128 * 128;                  // 128 tokens, their 64 bytes spread over 128
+constexpr int kScaleSlots = 2, kPlanSlots = 3;
+constexpr float kNoKey = -3.0e38f;                         // reference maximum of a row that has seen no key
 constexpr float kGrow = 3.0f;                              // log2 units: a row's reference maximum moves when outgrown by 2^3
 constexpr float kBase = 1024.0f;                           // p * sv / v_ref is at most 2^3 * 4; times 2^10 it stays below e5m2's 57344
 
 template <int kRows> struct Cfg {
-    static constexpr int kSlots = kRows == 16 ? 5 : 6;
+    static constexpr int kSub = kRows == 16 ? 1 : 2;       // tiles of 128 keys in a step
+    // Rings of steps.  K's is the longer one: its products make the scores that the softmax waits for, those of V may run a step late.
+    static constexpr int kKeys = kSub * kKeyTile, kSlotsK = kRows == 16 ? 3 : 2, kSlotsV = kRows == 16 ? 2 : 1;
+    static constexpr uint32_t kSlotBytes = kSub * kCodeTile;
     static constexpr int kColsS = kRows == 4 ? 16 : 2 * kRows, kColsO = 4 * kRows;      // (a product has 16 columns at least)
-    static constexpr uint32_t kQBytes = kColsS * 128, kPRow = kRows == 16 ? 64 : 32, kPBytes = 128 * kPRow;
-    static constexpr uint32_t kTmemCols = kRows == 16 ? 128 : 64, kColO = 2 * kColsS;
-    static constexpr uint32_t kOffQ = 0, kOffP = 2 * kQBytes, kOffRing = kOffP + 2 * kPBytes;
+    static constexpr uint32_t kQBytes = kColsS * 128, kPRow = kRows == 16 ? 64 : 32, kPBytes = kKeys * kPRow;
+    static constexpr uint32_t kColO = 2 * kSub * kColsS, kTmemCols = kColO + kColsO <= 128 ? 128 : 256;
+    static constexpr uint32_t kOffQ = 0, kOffP = 2 * kQBytes, kOffK = kOffP + kPBytes, kOffV = kOffK + kSlotsK * kSlotBytes, kOffEnd = kOffV + kSlotsV * kSlotBytes;
 };
 
 struct Segment {
-    int32_t tiles;                                         // 0: no more segments
-    int32_t key0;                                          // position of the first tile's first key
-    int32_t kv, pos0, rows;
+    int32_t tiles;                                         // of 128 keys; 0: no more segments
+    int32_t key0, key_end;                                 // positions of its keys: a request's, or a piece of them
+    int32_t pos0, rows;
     int64_t out;                                           // whole unit: (first token row * Hq + first head); else partial slot * few_rows
     int32_t whole;
 };
+struct Plan { int32_t page[32], row[32], kvh, valid, last; };          // of a step: where each eight keys lie; its keys, < 0: no more steps
 struct Shared {
     uint64_t q_full[2], q_empty[2];                        // descriptor and Q of every other segment
-    uint64_t kv_full[6], kv_empty[6];
-    uint64_t sc_full[kScaleSlots], sc_empty[kScaleSlots];
-    uint64_t s_full[2], p_ready[2];                        // [TMEM buffer]
+    uint64_t kv_full[2][3], kv_empty[2][3];                // K, V
+    uint64_t sc_full[kScaleSlots], sc_empty[kScaleSlots], plan_full[kPlanSlots], plan_empty[kPlanSlots];
+    uint64_t s_full[2], p_ready;                           // [TMEM buffer]
     uint64_t pv_done, drained;
     Segment seg[2];
+    Plan plan[kPlanSlots];
     float q_factor[2][16];                                 // of a row's scores: log2 units of the scaled score over that of the product
     float4 red[2][17];                                     // every other exchange: rows, the scales of V; one component per warp
-    uint32_t scale[kScaleSlots][kKeyTile];                 // bf16 bits: K, V << 16
-    int32_t count;
+    __align__(16) uint16_t scale[kScaleSlots][2][2 * kKeyTile];           // K, V; bf16 bits
+    int32_t any;                                           // 0: the CTA's piece of the line is empty
     uint32_t tmem_base;
     volatile int abort_flag;
 };
+static_assert(offsetof(Shared, scale) % 16 == 0 && offsetof(Shared, red) % 16 == 0, "written four at a time");
 template <int kRows> constexpr size_t smem_bytes()
 {
-    return Cfg<kRows>::kOffRing + Cfg<kRows>::kSlots * kCodeTile + 1024 /*alignment slack*/ + sizeof(Shared);
+    return Cfg<kRows>::kOffEnd + 1024 /*alignment slack*/ + sizeof(Shared);
 }
 // An SM has 228 KB, of which each CTA takes 1 KB for itself.
 static_assert(smem_bytes<4>() <= 113 * 1024 && smem_bytes<8>() <= 113 * 1024 && smem_bytes<16>() <= 113 * 1024, "two CTAs per SM");
@@ -145,161 +156,195 @@ __device__ __forceinline__ void split_e5m2(float2 lo, float2 hi, uint32_t (&part
     }
 }
 
+// Slot and parity of a ring's successive items: wait for the slot's full barrier with `phase`, for its empty one, from the second round
+// on, with phase ^ 1.  One reader and one writer each: a writer a round ahead of another would take a phase's parity for an older one's.
+struct Ring {
+    uint32_t slot, phase;
+    __device__ __forceinline__ void next(uint32_t slots)
+    {
+        if (++slot == slots) { slot = 0; phase ^= 1u; }
+    }
+};
+
 template <int kRows>
 __global__ void __launch_bounds__(kThreads, kFewCtasQ4)
 paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Params p, const int box,
-                    const int scales_by_four, const int skip_last)
+                    const int scales_by_eight, const int skip_last)
 {
     typedef Cfg<kRows> C;
-    constexpr int kSlots = C::kSlots;
+    constexpr int kSub = C::kSub;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t *const smem = smem_raw + (base - raw);
-    const uint32_t sQ = base + C::kOffQ, sP = base + C::kOffP, sRing = base + C::kOffRing;
-    Shared *sh = reinterpret_cast<Shared *>(smem + C::kOffRing + kSlots * kCodeTile);
+    const uint32_t sQ = base + C::kOffQ, sP = base + C::kOffP;
+    Shared *sh = reinterpret_cast<Shared *>(smem + C::kOffEnd);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
-    // The loader, query and scale warps each find this CTA's piece of the line, and go on to their first loads while the others gather.
     Walk walk;
-    int32_t first = 0, n_tiles = 0;
-    if (warp >= kLoadWarp) {
-        if (warp == kLoadWarp && lane == 0) {
+    int32_t first = 0, count = 0;                          // this CTA's piece of the line (plan warp)
+    if (warp == kPlanWarp) {
+        if (lane == 0) {
             griddep_launch_dependents();                   // the combining kernel may be launched; it waits for this one's end
             sh->abort_flag = 0;
             for (int g = 0; g < 2; ++g) {
                 mbar_init(smem_u32(&sh->q_full[g]), 1);
                 mbar_init(smem_u32(&sh->q_empty[g]), 5);   // four softmax warps, the issuer's commit
                 mbar_init(smem_u32(&sh->s_full[g]), 1);
-                mbar_init(smem_u32(&sh->p_ready[g]), 4);
             }
-            for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&sh->kv_full[s]), 1); mbar_init(smem_u32(&sh->kv_empty[s]), 1); }
-            for (int s = 0; s < kScaleSlots; ++s) { mbar_init(smem_u32(&sh->sc_full[s]), 1); mbar_init(smem_u32(&sh->sc_empty[s]), 4); }
+            for (int w = 0; w < 2; ++w)
+                for (int s = 0; s < 3; ++s) { mbar_init(smem_u32(&sh->kv_full[w][s]), 1); mbar_init(smem_u32(&sh->kv_empty[w][s]), 1); }
+            for (int s = 0; s < kScaleSlots; ++s) { mbar_init(smem_u32(&sh->sc_full[s]), 2); mbar_init(smem_u32(&sh->sc_empty[s]), 4); }
+            for (int s = 0; s < kPlanSlots; ++s) { mbar_init(smem_u32(&sh->plan_full[s]), 1); mbar_init(smem_u32(&sh->plan_empty[s]), 2); }
+            mbar_init(smem_u32(&sh->p_ready), 4);
             mbar_init(smem_u32(&sh->pv_done), 1);
             mbar_init(smem_u32(&sh->drained), 1);
             mbar_init_fence();
         }
         const int32_t all = walk_tiles(p, walk, lane), piece = few_piece(p, all);
         first = (int32_t)blockIdx.x * piece;
-        n_tiles = min(max(all - first, 0), piece);
-        if (n_tiles > 0) walk_to(p, walk, first, lane);
-        if (warp == kLoadWarp && lane == 0) sh->count = n_tiles;
+        count = min(max(all - first, 0), piece);
+        if (count > 0) walk_to(p, walk, first, lane);
+        if (lane == 0) sh->any = count > 0;
     } else if (warp == kMmaWarp) {
         tmem_alloc(smem_u32(&sh->tmem_base), C::kTmemCols);
         tmem_relinquish();
-        if (lane == 0) { prefetch_tmap(&tm_k); prefetch_tmap(&tm_v); }
+    } else if (warp == kKeyWarp && lane == 0) {
+        prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const int32_t count = sh->count;
     const uint32_t tmem = sh->tmem_base;
 
-    if (count == 0) {
-    } else if (warp == kLoadWarp) {
-        // ------------------------------------------------------------------ loader of the codes
+    if (!sh->any) {
+    } else if (warp == kKeyWarp || warp == kValueWarp) {
+        // ------------------------------------------------------------------ loader of K or V
+        // Codes: a lane has a box of one page.  Scales: a lane has eight keys (four, in a step of one tile: two lanes share a box's).
         reg_dealloc<kLightRegs>();
-        const BoxLane bl = {lane * box, (uint32_t)(lane * box) * 128u, lane * box < kKeyTile};
-        const int32_t end = first + count;
-        const BoxStep step = box_step(p.c.page_size);
-        BoxPlace at = box_place(p.c.page_size, walk.tile * kKeyTile, bl);      // this lane's box of the current tile, and its page
-        int32_t page = box_page(p, walk.b, walk.tile * kKeyTile, walk.r.kv, bl, at);
+        const int which = warp == kValueWarp;
+        const CUtensorMap *map = which ? &tm_v : &tm_k;
+        const uint16_t *scales = which ? p.v_scales : p.k_scales;
+        const int64_t s_p = which ? p.vs_sp : p.ks_sp, s_t = which ? p.vs_st : p.ks_st, s_h = which ? p.vs_sh : p.ks_sh;
+        const int32_t mine = lane * box;                   // this lane's first key of each step
+        const int slots = which ? C::kSlotsV : C::kSlotsK;
+        const uint32_t sRing = base + (which ? C::kOffV : C::kOffK);
+        Ring ring = {0u, 0u}, sc = {0u, 0u}, pl = {0u, 0u};
         int n = 0;
-        uint32_t issued = 0;
         bool ok = true;
-        while (n < count && ok) {
-            const int32_t tiles = min(walk.u0 + walk.r.tiles(), end) - max(walk.u0, first);
-            const int32_t b = walk.b, kv = walk.r.kv, kvh = walk.kvh;
-            int32_t k0 = walk.tile * kKeyTile;
-            if (n + tiles < count) walk_next(p, walk, lane);
-            for (int j = 0; j < tiles && ok; ++j, ++n, k0 += kKeyTile) {
-                int32_t page_next = 0;
-                BoxPlace at_next = box_next(at, step);
-                if (j + 1 < tiles) {
-                    page_next = box_page(p, b, k0 + kKeyTile, kv, bl, at_next);
-                } else if (n + 1 < count) {                // the next unit, from its first tile
-                    at_next = box_place(p.c.page_size, 0, bl);
-                    page_next = box_page(p, walk.b, 0, walk.r.kv, bl, at_next);
+        for (;; ++n) {
+            ok = wait_all(&sh->plan_full[pl.slot], pl.phase, sh, p);
+            const Plan &plan = sh->plan[pl.slot];
+            const int group = (mine >> 3) & 31;
+            const int32_t page = plan.page[group], row = plan.row[group], kvh = plan.kvh, valid = plan.valid;
+            const int32_t sc_page = plan.page[kSub == 2 ? lane : lane & 15], sc_row = plan.row[kSub == 2 ? lane : lane & 15];
+            const bool leave_out = skip_last && which && n > 0 && plan.last;         // test hook: the wait for it runs out
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->plan_empty[pl.slot]));
+            if (!ok || valid < 0) break;
+            pl.next(kPlanSlots);
+            // Scales.  Keys past the end have 0: what is in their place may be anything.  (A page holds all eight, whatever is in those.)
+            uint4 x = make_uint4(0u, 0u, 0u, 0u);
+            const int32_t own = kSub == 2 || lane < 16 ? valid - 8 * lane : 0;       // of this lane's eight keys
+            if (own > 0) {
+                const uint16_t *at = scales + sc_page * s_p + sc_row * s_t + kvh * s_h;
+                if (scales_by_eight) x = __ldg(reinterpret_cast<const uint4 *>(at));
+                else {
+                    auto two = [&](int i) { return __ldg(at + i * s_t) | (uint32_t)__ldg(at + (i + 1) * s_t) << 16; };
+                    x = make_uint4(two(0), two(2), two(4), two(6));
                 }
-                const uint32_t bytes = tile_bytes(k0, kv, box) / 4;            // 64 bytes a token
-#pragma unroll
-                for (int which = 0; which < 2; ++which) {  // K, V
-                    const int item = 2 * n + which, slot = item % kSlots, fill = item / kSlots;
-                    if (skip_last && count > 1 && item == 2 * count - 1) { ok = false; break; }   // test hook: the wait for it runs out
-                    if (fill > 0) ok = wait_all(&sh->kv_empty[slot], (fill - 1) & 1, sh, p);
-                    if (!ok) break;
-                    const uint32_t bar = smem_u32(&sh->kv_full[slot]);
-                    if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
-                    __syncwarp();
-                    if (bl.used && k0 + bl.first < kv)
-                        tma_load_4d(sRing + (uint32_t)slot * kCodeTile + bl.offset, which ? (const void *)&tm_v : (const void *)&tm_k, bar, 0, at.row, kvh, page);
-                    ++issued;
-                }
-                page = page_next;
-                at = at_next;
             }
+            if (n >= slots) ok = wait_all(&sh->kv_empty[which][ring.slot], ring.phase ^ 1u, sh, p);
+            ok = ok && !leave_out;
+            if (!ok) break;
+            const int32_t keys = (valid + box - 1) & -box; // whole boxes (box is a power of two)
+            const uint32_t bar = smem_u32(&sh->kv_full[which][ring.slot]);
+            if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)keys * 64u);
+            __syncwarp();
+            if (mine < keys) tma_load_4d(sRing + ring.slot * C::kSlotBytes + (uint32_t)mine * 128u, map, bar, 0, row, kvh, page);
+            ring.next(slots);
+            if (n >= kScaleSlots) ok = wait_all(&sh->sc_empty[sc.slot], sc.phase ^ 1u, sh, p);
+            if (!ok) { ++n; break; }
+            if (own < 8) {
+                uint32_t *w = &x.x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = own > 2 * i + 1 ? w[i] : own > 2 * i ? w[i] & 0xffffu : 0u;
+            }
+            if (kSub == 2 || lane < 16) *reinterpret_cast<uint4 *>(&sh->scale[sc.slot][which][8 * lane]) = x;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->sc_full[sc.slot]));
+            sc.next(kScaleSlots);
         }
-        if (!ok && lane == 0) {
-            // Given up: the copies under way must land before the CTA may leave.
-            for (uint32_t i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i) wait_quietly(&sh->kv_full[i % kSlots], (i / kSlots) & 1, p);
-        }
+        // Given up: the copies under way must land before the CTA may leave.
+        if (!ok && lane == 0)
+            for (int i = max(n - slots, 0); i < n; ++i) wait_quietly(&sh->kv_full[which][i % slots], (i / slots) & 1, p);
         __syncwarp();
-    } else if (warp == kQueryWarp) {
-        // ------------------------------------------------------------------ segments and their queries
+    } else if (warp == kPlanWarp) {
+        // ------------------------------------------------------------------ walk along the line, two steps ahead of the plans
         reg_dealloc<kLightRegs>();
         // An earlier CTA's wait has run out: the launch is lost, every wait of this CTA gives up at its next try.
         if (lane == 0 && *reinterpret_cast<volatile int32_t *>(p.status) == PEC_ERR_TIMEOUT) sh->abort_flag = 1;
         const int32_t end = first + count;
-        int segs = 0, n = 0;
-        bool ok = true;
-        while (n < count && ok) {
-            const int g = segs & 1;
-            const int32_t tiles = min(walk.u0 + walk.r.tiles(), end) - max(walk.u0, first), rows = walk.r.n * p.g;
-            // A lane has four channels of every row.
-            uint2 raw_q[kRows];
+        const BoxStep step = {C::kKeys / p.c.page_size, C::kKeys % p.c.page_size, p.c.page_size};
+        const BoxLane bl = {8 * lane, 0u, true};            // eight keys: one page, as boxes are eight at least
+        int32_t k0 = walk.tile * kKeyTile, left = min(walk.u0 + walk.r.tiles(), end) - max(walk.u0, first);    // of the walk's step; of its segment, in tiles
+        int32_t key_end = min(walk.r.kv, k0 + left * kKeyTile);
+        count -= left;                                     // tiles of later segments
+        BoxPlace at = box_place(p.c.page_size, k0, bl);
+        int segs = 0;
+        // The walk's segment begins: descriptor and Q.
+        auto begin = [&] {
+            const int g = segs & 1, rows = walk.r.n * p.g;
+            if (segs >= 2 && !wait_all(&sh->q_empty[g], ((segs >> 1) - 1) & 1, sh, p)) return false;
+            // Four rows at a time, a lane with four channels of each.
             const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(p.q) + (int64_t)walk.r.start * p.q_st + (int64_t)walk.kvh * p.g * p.q_sh + 4 * lane;
             int h = 0;
+            uint2 raw_q[4];
+            auto fetch = [&](int c0) {
 #pragma unroll
-            for (int c = 0; c < kRows; ++c) {
-                raw_q[c] = make_uint2(0u, 0u);
-                if (c < rows) raw_q[c] = *reinterpret_cast<const uint2 *>(q + h * p.q_sh);
-                if (++h == p.g) { h = 0; q += p.q_st; }
-            }
-            float most[kRows];
-            float2 x[kRows][2];
+                for (int c = 0; c < 4; ++c) {
+                    raw_q[c] = make_uint2(0u, 0u);
+                    if (c0 + c < rows) raw_q[c] = *reinterpret_cast<const uint2 *>(q + h * p.q_sh);
+                    if (++h == p.g) { h = 0; q += p.q_st; }
+                }
+            };
+            fetch(0);
+#pragma unroll 1
+            for (int c0 = 0; c0 < kRows; c0 += 4) {
+                float2 x[4][2];
+                float most[4];
 #pragma unroll
-            for (int c = 0; c < kRows; ++c) {
-                x[c][0] = make_float2(__uint_as_float(raw_q[c].x << 16), __uint_as_float(raw_q[c].x & 0xffff0000u));
-                x[c][1] = make_float2(__uint_as_float(raw_q[c].y << 16), __uint_as_float(raw_q[c].y & 0xffff0000u));
-                // As whole numbers magnitudes compare as they do as numbers, NaN above all.
-                const uint32_t a = max(__float_as_uint(x[c][0].x) & 0x7fffffffu, __float_as_uint(x[c][0].y) & 0x7fffffffu);
-                const uint32_t b = max(__float_as_uint(x[c][1].x) & 0x7fffffffu, __float_as_uint(x[c][1].y) & 0x7fffffffu);
-                most[c] = __uint_as_float(max(a, b));
-            }
-            const float top = warp_reduce(most, lane, [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); });
-            // Lane c: 2^(7 - exponent) of row c's largest channel, at most 2^107; NaN for a row that is not finite.
-            const uint32_t e = max(__float_as_uint(top) >> 23, 27u);
-            float f_row = e == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((261u - e) << 23);
-            if (segs >= 2) ok = wait_all(&sh->q_empty[g], ((segs >> 1) - 1) & 1, sh, p);
-            if (!ok) break;
-            if (lane < kRows) sh->q_factor[g][lane] = p.scale_log2 / f_row;
-            uint8_t *dst = smem + C::kOffQ + (uint32_t)g * C::kQBytes + (lane & 3) * 4;
+                for (int c = 0; c < 4; ++c) {
+                    x[c][0] = make_float2(__uint_as_float(raw_q[c].x << 16), __uint_as_float(raw_q[c].x & 0xffff0000u));
+                    x[c][1] = make_float2(__uint_as_float(raw_q[c].y << 16), __uint_as_float(raw_q[c].y & 0xffff0000u));
+                    // As whole numbers magnitudes compare as they do as numbers, NaN above all.
+                    const uint32_t a = max(__float_as_uint(x[c][0].x) & 0x7fffffffu, __float_as_uint(x[c][0].y) & 0x7fffffffu);
+                    const uint32_t b = max(__float_as_uint(x[c][1].x) & 0x7fffffffu, __float_as_uint(x[c][1].y) & 0x7fffffffu);
+                    most[c] = __uint_as_float(max(a, b));
+                }
+                if (c0 + 4 < kRows) fetch(c0 + 4);
+                const float top = warp_reduce(most, lane, [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); });
+                // Lane c: 2^(7 - exponent) of row c's largest channel, at most 2^107; NaN for a row that is not finite.
+                const uint32_t e = max(__float_as_uint(top) >> 23, 27u);
+                const float f_row = e == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((261u - e) << 23);
+                if (lane < 4) sh->q_factor[g][c0 + lane] = p.scale_log2 / f_row;
+                uint8_t *dst = smem + C::kOffQ + (uint32_t)g * C::kQBytes + (lane & 3) * 4;
 #pragma unroll
-            for (int c = 0; c < kRows; ++c) {
-                const float f = __shfl_sync(0xffffffffu, f_row, c);
-                float2 lo = __fmul2_rn(x[c][0], make_float2(f, f)), hi = __fmul2_rn(x[c][1], make_float2(f, f));
-                const uint32_t one = take_e4m3(lo) | take_e4m3(hi) << 16, two = to_e4m3(lo) | to_e4m3(hi) << 16;
-                const uint32_t to = (uint32_t)c * 128u + (((uint32_t)(lane >> 2) ^ (uint32_t)(c & 7)) << 4);
-                *reinterpret_cast<uint32_t *>(dst + to) = one;
-                const uint32_t to2 = (uint32_t)(kRows + c) * 128u + (((uint32_t)(lane >> 2) ^ (uint32_t)((kRows + c) & 7)) << 4);
-                *reinterpret_cast<uint32_t *>(dst + to2) = two;
+                for (int c = 0; c < 4; ++c) {
+                    const float f = __shfl_sync(0xffffffffu, f_row, c);
+                    float2 lo = __fmul2_rn(x[c][0], make_float2(f, f)), hi = __fmul2_rn(x[c][1], make_float2(f, f));
+                    const uint32_t one = take_e4m3(lo) | take_e4m3(hi) << 16, two = to_e4m3(lo) | to_e4m3(hi) << 16;
+                    const uint32_t r1 = (uint32_t)(c0 + c), r2 = r1 + kRows;
+                    *reinterpret_cast<uint32_t *>(dst + r1 * 128u + (((uint32_t)(lane >> 2) ^ (r1 & 7u)) << 4)) = one;
+                    *reinterpret_cast<uint32_t *>(dst + r2 * 128u + (((uint32_t)(lane >> 2) ^ (r2 & 7u)) << 4)) = two;
+                }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             if (lane == 0) {
                 Segment s;
-                s.tiles = tiles;
-                s.key0 = walk.tile * kKeyTile;
-                s.kv = walk.r.kv; s.pos0 = walk.r.pos0(); s.rows = rows;
-                s.whole = tiles == walk.r.tiles();
+                s.tiles = left;
+                s.key0 = k0; s.key_end = key_end;
+                s.pos0 = walk.r.pos0(); s.rows = rows;
+                s.whole = left == walk.r.tiles();
                 s.out = s.whole ? (int64_t)walk.r.start * p.Hq + (int64_t)walk.kvh * p.g
                                 : (2 * (int64_t)blockIdx.x + (walk.u0 > first ? 1 : 0)) * p.few_rows;
                 sh->seg[g] = s;
@@ -307,8 +352,60 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->q_full[g]));
             ++segs;
-            n += tiles;
-            if (n < count) walk_next(p, walk, lane);
+            return true;
+        };
+        struct Spot { int32_t page, row, kvh, valid; };
+        auto spot = [&] {                                  // of the walk's step; the page's number is looked at two steps later
+            Spot x = {-1, at.row, walk.kvh, max(min(key_end - k0, C::kKeys), 0)};
+            if (bl.first < x.valid) x.page = __ldg(p.c.table + walk.b * p.c.table_stride + at.nth);
+            return x;
+        };
+        bool ok = true;
+        auto advance = [&] {                               // to the next step; false: there is none
+            left -= kSub;
+            if (left > 0) {
+                k0 += C::kKeys;
+                at = box_next(at, step);
+                return true;
+            }
+            if (count <= 0) return false;
+            walk_next(p, walk, lane);
+            left = min(walk.r.tiles(), count);
+            count -= left;
+            k0 = 0;
+            key_end = min(walk.r.kv, left * kKeyTile);
+            at = box_place(p.c.page_size, 0, bl);
+            ok = begin();
+            return ok;
+        };
+        const Spot none = {-1, 0, 0, -1};
+        ok = begin();
+        Spot now = spot(), after = none;
+        bool more = ok && advance();
+        if (more) after = spot();
+        Ring pl = {0u, 0u};
+        for (int n = 0; ok; ++n) {
+            if (n >= kPlanSlots) ok = wait_all(&sh->plan_empty[pl.slot], pl.phase ^ 1u, sh, p);
+            if (!ok) break;
+            // A page number out of range is reported, and page 0 read in its place.
+            if (bl.first < now.valid && (now.page < 0 || now.page >= p.c.num_pages)) {
+                raise_status(p.status, PEC_ERR_BAD_INDEX);
+                now.page = 0;
+            }
+            Plan &plan = sh->plan[pl.slot];
+            plan.page[lane] = now.page;
+            plan.row[lane] = now.row;
+            if (lane == 0) { plan.kvh = now.kvh; plan.valid = now.valid; plan.last = after.valid < 0; }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->plan_full[pl.slot]));
+            pl.next(kPlanSlots);
+            if (now.valid < 0) break;
+            now = after;
+            after = none;
+            if (more) {
+                more = advance();
+                if (more) after = spot();
+            }
         }
         // No more segments, in either buffer.
         for (int e = 0; e < 2 && ok; ++e, ++segs) {
@@ -318,151 +415,81 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
-        // ------------------------------------------------------------------ MMA issuer (the whole warp walks, one lane issues)
+        // ------------------------------------------------------------------ MMA issuer, one thread
         reg_dealloc<kLightRegs>();
         const bool leader = elect_one();
-        constexpr uint32_t idesc_qk = idesc_f8f6f4_f32(128, C::kColsS, kE2M1, kE4M3, 0, 0);
-        constexpr uint32_t idesc_pv = idesc_f8f6f4_f32(kHeadDim, C::kColsO, kE2M1, kE5M2, 1, 1);
-        const uint64_t ring = smem_desc_sw128(sRing, 16, 1024);
-        auto kv_wait = [&](int item) { return wait_all(&sh->kv_full[item % kSlots], (item / kSlots) & 1, sh, p); };
-        auto kv_release = [&](int item) { if (leader) tc_commit(smem_u32(&sh->kv_empty[item % kSlots])); };
-        // S(n) of a segment of Q buffer g; `last`: the segment's Q is not needed after it
-        auto issue_qk = [&](int n, int g, bool last) {
-            if (!kv_wait(2 * n)) return false;
-            if (leader) {
-                mma4<2, 2>(tmem + (uint32_t)(n & 1) * C::kColsS, ring + (uint32_t)(((2 * n) % kSlots) * (kCodeTile >> 4)),
-                           smem_desc_sw128(sQ + (uint32_t)g * C::kQBytes, 16, 1024), idesc_qk, 0u);
-                tc_commit(smem_u32(&sh->s_full[n & 1]));
-                if (last) tc_commit(smem_u32(&sh->q_empty[g]));
-            }
-            kv_release(2 * n);
-            return true;
-        };
-        int segs = 0, n = 0;
-        bool ok = wait_all(&sh->q_full[0], 0, sh, p);
-        int32_t tiles = ok ? sh->seg[0].tiles : 0;
-        if (ok) ok = issue_qk(0, 0, tiles == 1);
-        while (ok) {
-            const int g = segs & 1;
-            int32_t next = 0;
-            for (int j = 0; j < tiles && ok; ++j, ++n) {
-                if (j + 1 < tiles) {
-                    ok = issue_qk(n + 1, g, j + 2 == tiles);
-                } else if (n + 1 < count) {
-                    ok = wait_all(&sh->q_full[g ^ 1], ((segs + 1) >> 1) & 1, sh, p);
-                    if (!ok) break;
-                    next = sh->seg[g ^ 1].tiles;
-                    ok = issue_qk(n + 1, g ^ 1, next == 1);
-                }
-                if (ok) ok = kv_wait(2 * n + 1);
-                if (ok) ok = wait_all(&sh->p_ready[n & 1], (n >> 1) & 1, sh, p);
-                if (!ok) break;
-                tc_fence_after();
-                if (leader) {
-                    mma4<256, (32 * C::kPRow >> 4)>(tmem + C::kColO, ring + (uint32_t)(((2 * n + 1) % kSlots) * (kCodeTile >> 4)),
-                                                    desc_rows<C::kPRow>(sP + (uint32_t)(n & 1) * C::kPBytes), idesc_pv, j > 0 ? 1u : 0u);
-                    tc_commit(smem_u32(&sh->pv_done));
-                }
-                kv_release(2 * n + 1);
-            }
-            if (next == 0) break;
-            tiles = next;
-            ++segs;
-        }
-        if (!ok) drain_products(&sh->drained, leader, p);
-        __syncwarp();
-    } else if (warp == kScaleWarp) {
-        // ------------------------------------------------------------------ scales: a lane has keys 4 lane .. + 3 of each tile
-        // They lie in one page (boxes are eight keys at least).  Loads run two tiles ahead of the stores, the page's number one more.
-        reg_dealloc<kLightRegs>();
-        const int32_t end = first + count;
-        const BoxStep step = box_step(p.c.page_size);
-        const BoxLane bl = {4 * lane, 0u, true};
-        int32_t left = min(walk.u0 + walk.r.tiles(), end) - max(walk.u0, first), k0 = walk.tile * kKeyTile, seen = 0;
-        BoxPlace at = box_place(p.c.page_size, k0, bl);
-        int32_t page = -1, row = 0, keys = 0, kvh = 0;     // of the next tile to load: its keys before the request's end
-        auto look_up = [&] {                               // of the walk's tile; then to the next one
-            row = at.row; kvh = walk.kvh;
-            keys = min(max(walk.r.kv - k0 - 4 * lane, 0), 4);
-            page = keys > 0 ? __ldg(p.c.table + walk.b * p.c.table_stride + at.nth) : -1;
-            if (++seen >= count) return;
-            if (--left > 0) {
-                k0 += kKeyTile;
-                at = box_next(at, step);
-            } else {
-                walk_next(p, walk, lane);
-                left = min(walk.u0 + walk.r.tiles(), end) - walk.u0;
-                k0 = 0;
-                at = box_place(p.c.page_size, 0, bl);
-            }
-        };
-        struct Four { uint32_t k01, k23, v01, v23; };      // bf16 bits
-        Four set[3];
-        auto load = [&](Four &x) {                         // keys past the end, and pages out of range (the loader reports them): 0
-            x = {0u, 0u, 0u, 0u};
-            if (page < 0 || page >= p.c.num_pages) return;
-            const uint16_t *k = p.k_scales + page * p.ks_sp + row * p.ks_st + kvh * p.ks_sh, *v = p.v_scales + page * p.vs_sp + row * p.vs_st + kvh * p.vs_sh;
-            if (scales_by_four) {                          // (a page holds all four, whatever is in those past the end)
-                const uint2 a = __ldg(reinterpret_cast<const uint2 *>(k)), b = __ldg(reinterpret_cast<const uint2 *>(v));
-                x = {a.x, a.y, b.x, b.y};
-            } else {
-                x.k01 = __ldg(k) | (uint32_t)__ldg(k + p.ks_st) << 16;
-                x.k23 = __ldg(k + 2 * p.ks_st) | (uint32_t)__ldg(k + 3 * p.ks_st) << 16;
-                x.v01 = __ldg(v) | (uint32_t)__ldg(v + p.vs_st) << 16;
-                x.v23 = __ldg(v + 2 * p.vs_st) | (uint32_t)__ldg(v + 3 * p.vs_st) << 16;
-            }
-        };
-        int32_t valid[3];                                  // keys of each set
-        look_up();
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            valid[u] = 0;
-            if (u < count) {
-                load(set[u]);
-                valid[u] = keys;
-                if (u + 1 < count) look_up();
-            }
-        }
         bool ok = true;
-        for (int n0 = 0; n0 < count && ok; n0 += 3) {
+        if (leader) {
+            constexpr uint32_t idesc_qk = idesc_f8f6f4_f32(128, C::kColsS, kE2M1, kE4M3, 0, 0);
+            constexpr uint32_t idesc_pv = idesc_f8f6f4_f32(kHeadDim, C::kColsO, kE2M1, kE5M2, 1, 1);
+            const uint64_t k_desc = smem_desc_sw128(base + C::kOffK, 16, 1024), v_desc = smem_desc_sw128(base + C::kOffV, 16, 1024), q_desc = smem_desc_sw128(sQ, 16, 1024), p_desc = desc_rows<C::kPRow>(sP);
+            auto wait = [&](uint64_t *bar, uint32_t parity) {
+                return mbar_wait_bounded(smem_u32(bar), parity, &sh->abort_flag, p.status, p.wait_cycles, (int)PEC_ERR_TIMEOUT);
+            };
+            Ring k_ring = {0u, 0u}, v_ring = {0u, 0u};
+            // S(n) of a segment of Q buffer g; `last`: the segment's Q is not needed after it.  (A step of one tile has a second one of
+            // whatever codes lie there: its keys are masked.)
+            auto issue_qk = [&](int n, int g, bool last) {
+                if (!wait(&sh->kv_full[0][k_ring.slot], k_ring.phase)) return false;
 #pragma unroll
-            for (int u = 0; u < 3; ++u) {
-                const int n = n0 + u;
-                if (n >= count || !ok) break;
-                if (n + 2 < count) {
-                    load(set[(u + 2) % 3]);
-                    valid[(u + 2) % 3] = keys;
-                    if (n + 3 < count) look_up();
+                for (int i = 0; i < kSub; ++i)
+                    mma4<2, 2>(tmem + (uint32_t)((n & 1) * kSub + i) * C::kColsS, k_desc + ((k_ring.slot * C::kSlotBytes + i * kCodeTile) >> 4),
+                               q_desc + (uint32_t)g * (C::kQBytes >> 4), idesc_qk, 0u);
+                tc_commit(smem_u32(&sh->s_full[n & 1]));
+                tc_commit(smem_u32(&sh->kv_empty[0][k_ring.slot]));
+                if (last) tc_commit(smem_u32(&sh->q_empty[g]));
+                k_ring.next(C::kSlotsK);
+                return true;
+            };
+            auto steps_of = [&](int g) { return (sh->seg[g].tiles + kSub - 1) / kSub; };
+            int segs = 0, n = 0;
+            ok = wait(&sh->q_full[0], 0);
+            int32_t steps = ok ? steps_of(0) : 0;
+            if (ok) ok = issue_qk(0, 0, steps == 1);
+            while (ok) {
+                const int g = segs & 1;
+                int32_t next = 0;
+                for (int j = 0; j < steps && ok; ++j, ++n) {
+                    if (j + 1 < steps) {
+                        ok = issue_qk(n + 1, g, j + 2 == steps);
+                    } else {
+                        ok = wait(&sh->q_full[g ^ 1], ((segs + 1) >> 1) & 1);
+                        if (!ok) break;
+                        next = steps_of(g ^ 1);
+                        if (next > 0) ok = issue_qk(n + 1, g ^ 1, next == 1);
+                    }
+                    if (ok) ok = wait(&sh->kv_full[1][v_ring.slot], v_ring.phase);
+                    if (ok) ok = wait(&sh->p_ready, n & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int i = 0; i < kSub; ++i)
+                        mma4<256, (32 * C::kPRow >> 4)>(tmem + C::kColO, v_desc + ((v_ring.slot * C::kSlotBytes + i * kCodeTile) >> 4),
+                                                        p_desc + (uint32_t)i * (128 * C::kPRow >> 4), idesc_pv, j > 0 || i > 0 ? 1u : 0u);
+                    tc_commit(smem_u32(&sh->pv_done));
+                    tc_commit(smem_u32(&sh->kv_empty[1][v_ring.slot]));
+                    v_ring.next(C::kSlotsV);
                 }
-                const int slot = n % kScaleSlots;
-                if (n >= kScaleSlots) ok = wait_all(&sh->sc_empty[slot], (n / kScaleSlots - 1) & 1, sh, p);
-                if (!ok) break;
-                const Four x = set[u];
-                const int have = valid[u];
-                uint4 w = make_uint4(__byte_perm(x.k01, x.v01, 0x5410), __byte_perm(x.k01, x.v01, 0x7632),
-                                     __byte_perm(x.k23, x.v23, 0x5410), __byte_perm(x.k23, x.v23, 0x7632));
-                if (have < 4) {
-                    if (have < 1) w.x = 0u;
-                    if (have < 2) w.y = 0u;
-                    if (have < 3) w.z = 0u;
-                    w.w = 0u;
-                }
-                *reinterpret_cast<uint4 *>(&sh->scale[slot][4 * lane]) = w;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh->sc_full[slot]));
+                if (next == 0) break;
+                steps = next;
+                ++segs;
             }
         }
+        __syncwarp();
+        if (!__all_sync(0xffffffffu, ok)) drain_products(&sh->drained, leader, p);
         __syncwarp();
     } else {
         // ------------------------------------------------------------------ softmax and epilogue
         reg_alloc<kSoftmaxRegs>();
-        const int quarter = warp, key = tid;               // and channel `key` of the accumulator
+        const int quarter = warp, key = tid;               // key of each tile, and channel `key` of the accumulator
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         const uint32_t tO = tmem + lane_base + C::kColO;
         // P'^T: a row of kPRow bytes per key, its 16-byte chunks XOR-swizzled by bits of the key.
-        const uint32_t p_row = (uint32_t)key * C::kPRow, p_swizzle = (C::kPRow == 32 ? (uint32_t)(key >> 2) & 1u : (uint32_t)(key >> 1) & 3u) << 4;
+        uint8_t *const p_row = smem + C::kOffP + (uint32_t)key * C::kPRow;
+        const uint32_t p_swizzle = (C::kPRow == 32 ? (uint32_t)(key >> 2) & 1u : (uint32_t)(key >> 1) & 3u) << 4;
         constexpr int kPairs = kRows / 2;
-        int n = 0, turn = 0;                               // tiles so far; exchanges take turns in two buffers (see pec_paged_few.cu)
+        Ring sc = {0u, 0u};
+        int n = 0, turn = 0;                               // steps so far; exchanges take turns in two buffers (see pec_paged_few.cu)
         for (int k = 0;; ++k) {
             bool ok = wait_all(&sh->q_full[k & 1], (k >> 1) & 1, sh, p);
             if (group_any(0, !ok)) break;
@@ -473,7 +500,7 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             __syncwarp();
             if (s.tiles == 0) break;
             if (lane == 0) mbar_arrive(smem_u32(&sh->q_empty[k & 1]));
-            const int32_t see_all = (p.causal && s.pos0 + 1 < s.kv) ? s.pos0 + 1 : s.kv;           // keys below it are visible to every row
+            const int32_t see_all = (p.causal && s.pos0 + 1 < s.key_end) ? s.pos0 + 1 : s.key_end;   // keys below it are visible to every row
             // Per row: minus the reference maximum (log2 units, the same in all threads; rows past the segment's: -inf, and all their
             // probabilities 0), this thread's sum.
             float2 neg_m[kPairs], l[kPairs];
@@ -486,61 +513,77 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             float v_ref = 0.f, v_factor = 0.f;             // a power of two that no scale of V passes four times; kBase / v_ref
             int32_t k0 = s.key0;
             bool stop = false;
-            for (int j = 0; j < s.tiles; ++j, ++n, k0 += kKeyTile) {
-                const int buf = n & 1, slot = n % kScaleSlots;
-                ok = wait_all(&sh->sc_full[slot], (n / kScaleSlots) & 1, sh, p);
-                const uint32_t scales = sh->scale[slot][key];
-                const float2 scale = make_float2(__uint_as_float(scales << 16), __uint_as_float(scales & 0xffff0000u));   // K, V
+            for (int j = 0; j < s.tiles; j += kSub, ++n, k0 += C::kKeys) {
+                const int buf = n & 1;
+                ok = wait_all(&sh->sc_full[sc.slot], sc.phase, sh, p);
+                float ks[kSub], vs[kSub];
+#pragma unroll
+                for (int i = 0; i < kSub; ++i) {
+                    ks[i] = __uint_as_float((uint32_t)sh->scale[sc.slot][0][i * kKeyTile + key] << 16);
+                    vs[i] = __uint_as_float((uint32_t)sh->scale[sc.slot][1][i * kKeyTile + key] << 16);
+                }
                 if (ok) ok = wait_all(&sh->s_full[buf], (n >> 1) & 1, sh, p);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh->sc_empty[slot]));
+                if (lane == 0) mbar_arrive(smem_u32(&sh->sc_empty[sc.slot]));
+                sc.next(kScaleSlots);
                 tc_fence_after();
-                uint32_t r[C::kColsS];
-                if constexpr (C::kColsS == 16) tmem_ld16(tmem + lane_base + (uint32_t)buf * C::kColsS, r);
-                else tmem_ld32(tmem + lane_base + (uint32_t)buf * C::kColsS, r);
+                uint32_t r[kSub * C::kColsS];
+                static_assert(kSub * C::kColsS == 32, "a step's scores");
+                tmem_ld32(tmem + lane_base + (uint32_t)buf * 32u, r);
                 tc_fence_before();
-                float2 x[kPairs];
+                float2 x[kSub][kPairs];
 #pragma unroll
-                for (int c = 0; c < kPairs; ++c) {
-                    const float2 hi = make_float2(__uint_as_float(r[2 * c]), __uint_as_float(r[2 * c + 1]));
-                    const float2 lo = make_float2(__uint_as_float(r[kRows + 2 * c]), __uint_as_float(r[kRows + 2 * c + 1]));
-                    x[c] = __fmul2_rn(__ffma2_rn(lo, make_float2(1.f / 16.f, 1.f / 16.f), hi), __fmul2_rn(factor[c], make_float2(scale.x, scale.x)));
-                }
-                const bool border = k0 + kKeyTile > see_all;
+                for (int i = 0; i < kSub; ++i)
+#pragma unroll
+                    for (int c = 0; c < kPairs; ++c) {
+                        const uint32_t *q = r + i * C::kColsS + 2 * c;
+                        const float2 hi = make_float2(__uint_as_float(q[0]), __uint_as_float(q[1]));
+                        const float2 lo = make_float2(__uint_as_float(q[kRows]), __uint_as_float(q[kRows + 1]));
+                        x[i][c] = __fmul2_rn(__ffma2_rn(lo, make_float2(1.f / 16.f, 1.f / 16.f), hi), __fmul2_rn(factor[c], make_float2(ks[i], ks[i])));
+                    }
+                const bool border = k0 + C::kKeys > see_all;
                 if (border) {                              // by choice, not by arithmetic: a masked score may be anything
                     int t = 0, h = 0;                      // token and head of the row
 #pragma unroll
                     for (int c = 0; c < kRows; ++c) {
-                        const int32_t see = p.causal ? min(s.kv, s.pos0 + t + 1) : s.kv;
-                        float &y = c & 1 ? x[c / 2].y : x[c / 2].x;
-                        y = k0 + key < see ? y : -INFINITY;
+                        const int32_t see = (p.causal ? min(s.key_end, s.pos0 + t + 1) : s.key_end) - k0 - key;
+#pragma unroll
+                        for (int i = 0; i < kSub; ++i) {
+                            float &y = c & 1 ? x[i][c / 2].y : x[i][c / 2].x;
+                            y = i * kKeyTile < see ? y : -INFINITY;
+                        }
                         if (++h == p.g) { h = 0; ++t; }
                     }
                 }
-                float2 d[kPairs];                          // over the reference maxima
-                float most_d = -INFINITY;
+                float2 d[kSub][kPairs];                    // over the reference maxima
+                float most_d = -INFINITY, most_v = 0.f;
 #pragma unroll
-                for (int c = 0; c < kPairs; ++c) {
-                    d[c] = __fadd2_rn(x[c], neg_m[c]);
-                    most_d = fmax3(most_d, d[c].x, d[c].y);
+                for (int i = 0; i < kSub; ++i) {
+                    most_v = fmaxf(most_v, vs[i]);
+#pragma unroll
+                    for (int c = 0; c < kPairs; ++c) {
+                        d[i][c] = __fadd2_rn(x[i][c], neg_m[c]);
+                        most_d = fmax3(most_d, d[i][c].x, d[i][c].y);
+                    }
                 }
-                const bool grow = most_d > kGrow || scale.y > 4.f * v_ref;
-                // The references move only when one is outgrown (and at first); O then waits for its product in flight.  (S(n) is
-                // complete, and with it PV(n - 2), issued before it; PV(n) needs this P(n): the parity tells PV(n - 1)'s phase.)
-                if (j == 0 || group_any(0, grow || !ok)) {
+                // The references move only when one is outgrown (and at first); O then waits for its product in flight, PV(n - 1).  (PV(n)
+                // needs this P(n), and PV(n - 2) was waited for before P(n - 1) was stored: the parity tells the one phase between.)
+                if (j == 0 || group_any(0, most_d > kGrow || most_v > 4.f * v_ref || !ok)) {
                     if (j > 0 && ok) ok = wait_all(&sh->pv_done, (n - 1) & 1, sh, p);
                     stop = group_any(0, !ok);
                     if (stop) break;
                     float y[kRows];
 #pragma unroll
-                    for (int c = 0; c < kPairs; ++c) { y[2 * c] = x[c].x; y[2 * c + 1] = x[c].y; }
+                    for (int c = 0; c < kPairs; ++c) {
+                        y[2 * c] = x[0][c].x; y[2 * c + 1] = x[0][c].y;
+                        if constexpr (kSub == 2) { y[2 * c] = fmaxf(y[2 * c], x[1][c].x); y[2 * c + 1] = fmaxf(y[2 * c + 1], x[1][c].y); }
+                    }
                     const float most = warp_reduce(y, lane, [](float a, float b) { return fmaxf(a, b); });
-                    float v_most = fmaxf(scale.y, 0.f);
 #pragma unroll
-                    for (int i = 16; i > 0; i >>= 1) v_most = fmaxf(v_most, __shfl_xor_sync(0xffffffffu, v_most, i));
+                    for (int i = 16; i > 0; i >>= 1) most_v = fmaxf(most_v, __shfl_xor_sync(0xffffffffu, most_v, i));
                     float4 *red = sh->red[turn ^= 1];
                     if (lane < kRows) reinterpret_cast<float *>(red + lane)[quarter] = most;
-                    if (lane == 0) reinterpret_cast<float *>(red + 16)[quarter] = v_most;
+                    if (lane == 0) reinterpret_cast<float *>(red + 16)[quarter] = most_v;
                     group_any(0, false);
                     // Lane c works out row c's new reference; the others get it by shuffle.
                     const float4 t = red[lane & (kRows - 1)], tv = red[16];
@@ -567,62 +610,60 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
                         alpha[c] *= v_alpha;
                     }
 #pragma unroll
-                    for (int c = 0; c < kPairs; ++c) d[c] = __fadd2_rn(x[c], neg_m[c]);
+                    for (int i = 0; i < kSub; ++i)
+#pragma unroll
+                        for (int c = 0; c < kPairs; ++c) d[i][c] = __fadd2_rn(x[i][c], neg_m[c]);
                     if (j > 0) {
                         tc_fence_after();
-                        if constexpr (kRows == 4) {
+#pragma unroll
+                        for (int i = 0; i < C::kColsO; i += 16) {
                             uint32_t o[16];
-                            tmem_ld16(tO, o);
+                            tmem_ld16(tO + i, o);
 #pragma unroll
                             for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha[c % kRows]);
-                            tmem_st16(tO, o);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < C::kColsO; i += 32) {
-                                uint32_t o[32];
-                                tmem_ld32(tO + i, o);
-#pragma unroll
-                                for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha[c % kRows]);
-                                tmem_st32(tO + i, o);
-                            }
+                            tmem_st16(tO + i, o);
                         }
-                        tmem_st_wait();
                         tc_fence_before();
                     }
+                } else if (j > 0) {
+                    // P(n - 1) is read by its product until that is done.
+                    if (!wait_all(&sh->pv_done, (n - 1) & 1, sh, p)) sh->abort_flag = 1;       // (voted on with the next step)
                 }
                 // p = 2^(x - m); the row's sum takes p itself, the product p sv / v_ref in four parts.
-                const float f = scale.y * v_factor;
 #pragma unroll
-                for (int c = 0; c < kPairs; ++c) {
-                    d[c] = make_float2(ex2(d[c].x), ex2(d[c].y));
-                    l[c] = __fadd2_rn(l[c], d[c]);
-                    d[c] = __fmul2_rn(d[c], make_float2(f, f));
-                }
-                if (border && !(f < INFINITY)) {           // a value that is not finite spoils no row that does not see it
+                for (int i = 0; i < kSub; ++i) {
+                    const float f = vs[i] * v_factor;
 #pragma unroll
                     for (int c = 0; c < kPairs; ++c) {
-                        if (x[c].x == -INFINITY) d[c].x = 0.f;
-                        if (x[c].y == -INFINITY) d[c].y = 0.f;
+                        d[i][c] = make_float2(ex2(d[i][c].x), ex2(d[i][c].y));
+                        l[c] = __fadd2_rn(l[c], d[i][c]);
+                        d[i][c] = __fmul2_rn(d[i][c], make_float2(f, f));
                     }
-                }
-                uint32_t parts[kRows / 4][4];
+                    if (border && !(f < INFINITY)) {       // a value that is not finite spoils no row that does not see it
 #pragma unroll
-                for (int c = 0; c < kRows / 4; ++c) split_e5m2(d[2 * c], d[2 * c + 1], parts[c]);
-                // (S(n) is complete, and with it PV(n - 2), which read this buffer.)
-                uint8_t *dst = smem + C::kOffP + (uint32_t)buf * C::kPBytes + p_row;
-                if constexpr (kRows == 4) {
-                    *reinterpret_cast<uint4 *>(dst + p_swizzle) = make_uint4(parts[0][0], parts[0][1], parts[0][2], parts[0][3]);
-                } else if constexpr (kRows == 8) {
-                    *reinterpret_cast<uint4 *>(dst + p_swizzle) = make_uint4(parts[0][0], parts[1][0], parts[0][1], parts[1][1]);
-                    *reinterpret_cast<uint4 *>(dst + (16u ^ p_swizzle)) = make_uint4(parts[0][2], parts[1][2], parts[0][3], parts[1][3]);
-                } else {
+                        for (int c = 0; c < kPairs; ++c) {
+                            if (x[i][c].x == -INFINITY) d[i][c].x = 0.f;
+                            if (x[i][c].y == -INFINITY) d[i][c].y = 0.f;
+                        }
+                    }
+                    uint32_t parts[kRows / 4][4];
 #pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i)
-                        *reinterpret_cast<uint4 *>(dst + ((i << 4) ^ p_swizzle)) = make_uint4(parts[0][i], parts[1][i], parts[2][i], parts[3][i]);
+                    for (int c = 0; c < kRows / 4; ++c) split_e5m2(d[i][2 * c], d[i][2 * c + 1], parts[c]);
+                    uint8_t *dst = p_row + i * kKeyTile * C::kPRow;
+                    if constexpr (kRows == 4) {
+                        *reinterpret_cast<uint4 *>(dst + p_swizzle) = make_uint4(parts[0][0], parts[0][1], parts[0][2], parts[0][3]);
+                    } else if constexpr (kRows == 8) {
+                        *reinterpret_cast<uint4 *>(dst + p_swizzle) = make_uint4(parts[0][0], parts[1][0], parts[0][1], parts[1][1]);
+                        *reinterpret_cast<uint4 *>(dst + (16u ^ p_swizzle)) = make_uint4(parts[0][2], parts[1][2], parts[0][3], parts[1][3]);
+                    } else {
+#pragma unroll
+                        for (uint32_t q = 0; q < 4; ++q)
+                            *reinterpret_cast<uint4 *>(dst + ((q << 4) ^ p_swizzle)) = make_uint4(parts[0][q], parts[1][q], parts[2][q], parts[3][q]);
+                    }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh->p_ready[buf]));
+                if (lane == 0) mbar_arrive(smem_u32(&sh->p_ready));
             }
             if (stop) break;
             ok = wait_all(&sh->pv_done, (n - 1) & 1, sh, p);
@@ -658,9 +699,9 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
                 float sum_o = __uint_as_float(o[3 * kRows + c]);
 #pragma unroll
                 for (int i = 2; i >= 0; --i) sum_o = fmaf(sum_o, 0.125f, __uint_as_float(o[i * kRows + c]));
-                const float y = f == 0.f ? 0.f : sum_o * f;
-                if (s.whole && p.o_is_bf16) static_cast<__nv_bfloat16 *>(p.o)[to] = __float2bfloat16_rn(y);
-                else (s.whole ? static_cast<float *>(p.o) : p.few_o)[to] = y;
+                const float out = f == 0.f ? 0.f : sum_o * f;
+                if (s.whole && p.o_is_bf16) static_cast<__nv_bfloat16 *>(p.o)[to] = __float2bfloat16_rn(out);
+                else (s.whole ? static_cast<float *>(p.o) : p.few_o)[to] = out;
             }
         }
     }
@@ -671,14 +712,22 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     griddep_wait();
 }
 
-// Whether the scales of four tokens can be loaded at once.
-static bool by_four(const uint16_t *s, int64_t sp, int64_t st, int64_t sh) { return st == 1 && sp % 4 == 0 && sh % 4 == 0 && reinterpret_cast<uintptr_t>(s) % 8 == 0; }
+// Whether the scales of eight tokens can be loaded at once.
+static bool by_eight(const uint16_t *s, int64_t sp, int64_t st, int64_t sh) { return st == 1 && sp % 8 == 0 && sh % 8 == 0 && reinterpret_cast<uintptr_t>(s) % 16 == 0; }
 
 template <int kRows>
 static cudaError_t launch(const Params &p, const CUtensorMap &tm_k, const CUtensorMap &tm_v, int box, bool after_many, cudaStream_t stream)
 {
     return launch_dependent(paged_few_q4_kernel<kRows>, dim3((unsigned)p.few_ctas), kThreads, smem_bytes<kRows>(), stream, after_many, tm_k, tm_v, p, box,
-                            by_four(p.k_scales, p.ks_sp, p.ks_st, p.ks_sh) && by_four(p.v_scales, p.vs_sp, p.vs_st, p.vs_sh), (int)test_skip_last_load());
+                            by_eight(p.k_scales, p.ks_sp, p.ks_st, p.ks_sh) && by_eight(p.v_scales, p.vs_sp, p.vs_st, p.vs_sh), (int)test_skip_last_load());
+}
+
+template <int kRows>
+static bool set_up()
+{
+    cudaFuncAttributes attr;
+    return cudaFuncSetAttribute(paged_few_q4_kernel<kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<kRows>()) == cudaSuccess &&
+           cudaFuncGetAttributes(&attr, paged_few_q4_kernel<kRows>) == cudaSuccess && attr.numRegs * kThreads >= 128 * (kSoftmaxRegs + kLightRegs);
 }
 
 }  // namespace few_q4
@@ -696,12 +745,9 @@ int launch_paged_few_q4(const paged::Params &p, bool after_many, cudaStream_t st
     }
     static unsigned char ready[host::kMaxDevices] = {};
     static std::mutex ready_mutex;
-    if (!host::once_per_device(ready, ready_mutex, [] {
-            return cudaFuncSetAttribute(few_q4::paged_few_q4_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_q4::smem_bytes<4>()) == cudaSuccess &&
-                   cudaFuncSetAttribute(few_q4::paged_few_q4_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_q4::smem_bytes<8>()) == cudaSuccess &&
-                   cudaFuncSetAttribute(few_q4::paged_few_q4_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_q4::smem_bytes<16>()) == cudaSuccess; })) {
+    if (!host::once_per_device(ready, ready_mutex, [] { return few_q4::set_up<4>() && few_q4::set_up<8>() && few_q4::set_up<16>(); })) {
         (void)cudaGetLastError();
-        set_error("%s: cannot raise the shared-memory limit", p.who);
+        set_error("%s: kernel set-up failed (shared-memory limit, or the register allocation does not cover the warp-role split)", p.who);
         return PEC_ERR_CUDA;
     }
     // The form for as many rows as a request can have (p.few_rows).
