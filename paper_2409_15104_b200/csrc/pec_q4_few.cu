@@ -219,7 +219,7 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
     if (!sh->any) {
     } else if (warp == kKeyWarp || warp == kValueWarp) {
         // ------------------------------------------------------------------ loader of K or V
-        // Codes: a lane has a box of one page.  Scales: a lane has eight keys (four, in a step of one tile: two lanes share a box's).
+        // Codes: a lane has a box of one page.  Scales: a lane has eight keys; they go a step ahead of the codes, whose slot may be taken.
         reg_dealloc<kLightRegs>();
         const int which = warp == kValueWarp;
         const CUtensorMap *map = which ? &tm_v : &tm_k;
@@ -229,50 +229,61 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
         const int slots = which ? C::kSlotsV : C::kSlotsK;
         const uint32_t sRing = base + (which ? C::kOffV : C::kOffK);
         Ring ring = {0u, 0u}, sc = {0u, 0u}, pl = {0u, 0u};
-        int n = 0;
+        struct Step { int32_t page, row, kvh, valid, last; } now, next = {};
+        uint4 x;                                           // the next step's scales
+        int32_t own = 0;                                   // of this lane's eight keys, those before the end
         bool ok = true;
-        for (;; ++n) {
+        auto take_plan = [&] {                             // into `next`; starts the load of its scales
             ok = wait_all(&sh->plan_full[pl.slot], pl.phase, sh, p);
             const Plan &plan = sh->plan[pl.slot];
             const int group = (mine >> 3) & 31;
-            const int32_t page = plan.page[group], row = plan.row[group], kvh = plan.kvh, valid = plan.valid;
-            const int32_t sc_page = plan.page[kSub == 2 ? lane : lane & 15], sc_row = plan.row[kSub == 2 ? lane : lane & 15];
-            const bool leave_out = skip_last && which && n > 0 && plan.last;         // test hook: the wait for it runs out
+            next = {plan.page[group], plan.row[group], plan.kvh, plan.valid, plan.last};
+            const int32_t sc_page = plan.page[lane], sc_row = plan.row[lane];
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->plan_empty[pl.slot]));
-            if (!ok || valid < 0) break;
             pl.next(kPlanSlots);
-            // Scales.  Keys past the end have 0: what is in their place may be anything.  (A page holds all eight, whatever is in those.)
-            uint4 x = make_uint4(0u, 0u, 0u, 0u);
-            const int32_t own = kSub == 2 || lane < 16 ? valid - 8 * lane : 0;       // of this lane's eight keys
-            if (own > 0) {
-                const uint16_t *at = scales + sc_page * s_p + sc_row * s_t + kvh * s_h;
-                if (scales_by_eight) x = __ldg(reinterpret_cast<const uint4 *>(at));
-                else {
-                    auto two = [&](int i) { return __ldg(at + i * s_t) | (uint32_t)__ldg(at + (i + 1) * s_t) << 16; };
-                    x = make_uint4(two(0), two(2), two(4), two(6));
-                }
+            // (Keys past the end have scale 0: what is in their place may be anything.  A page holds all eight, whatever is in those.)
+            x = make_uint4(0u, 0u, 0u, 0u);
+            own = next.valid - 8 * lane;
+            if (!ok || own <= 0) return;
+            const uint16_t *at = scales + sc_page * s_p + sc_row * s_t + next.kvh * s_h;
+            if (scales_by_eight) {
+                x = __ldg(reinterpret_cast<const uint4 *>(at));
+            } else {
+                auto two = [&](int i) { return __ldg(at + i * s_t) | (uint32_t)__ldg(at + (i + 1) * s_t) << 16; };
+                x = make_uint4(two(0), two(2), two(4), two(6));
             }
-            if (n >= slots) ok = wait_all(&sh->kv_empty[which][ring.slot], ring.phase ^ 1u, sh, p);
-            ok = ok && !leave_out;
-            if (!ok) break;
-            const int32_t keys = (valid + box - 1) & -box; // whole boxes (box is a power of two)
-            const uint32_t bar = smem_u32(&sh->kv_full[which][ring.slot]);
-            if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)keys * 64u);
-            __syncwarp();
-            if (mine < keys) tma_load_4d(sRing + ring.slot * C::kSlotBytes + (uint32_t)mine * 128u, map, bar, 0, row, kvh, page);
-            ring.next(slots);
-            if (n >= kScaleSlots) ok = wait_all(&sh->sc_empty[sc.slot], sc.phase ^ 1u, sh, p);
-            if (!ok) { ++n; break; }
+        };
+        auto store_scales = [&](int m) {                   // of step m, taken last
+            if (m >= kScaleSlots) ok = wait_all(&sh->sc_empty[sc.slot], sc.phase ^ 1u, sh, p);
+            if (!ok) return;
             if (own < 8) {
                 uint32_t *w = &x.x;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[i] = own > 2 * i + 1 ? w[i] : own > 2 * i ? w[i] & 0xffffu : 0u;
             }
-            if (kSub == 2 || lane < 16) *reinterpret_cast<uint4 *>(&sh->scale[sc.slot][which][8 * lane]) = x;
+            if (8 * lane < C::kKeys) *reinterpret_cast<uint4 *>(&sh->scale[sc.slot][which][8 * lane]) = x;
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->sc_full[sc.slot]));
             sc.next(kScaleSlots);
+        };
+        int n = 0;
+        take_plan();
+        if (ok) store_scales(0);
+        for (; ok; ++n) {
+            now = next;
+            if (now.valid < 0) break;
+            take_plan();
+            if (ok && n >= slots) ok = wait_all(&sh->kv_empty[which][ring.slot], ring.phase ^ 1u, sh, p);
+            if (skip_last && which && n > 0 && now.last) ok = false;       // test hook: the wait for it runs out
+            if (!ok) break;
+            const int32_t keys = (now.valid + box - 1) & -box;             // whole boxes (box is a power of two)
+            const uint32_t bar = smem_u32(&sh->kv_full[which][ring.slot]);
+            if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)keys * 64u);
+            __syncwarp();
+            if (mine < keys) tma_load_4d(sRing + ring.slot * C::kSlotBytes + (uint32_t)mine * 128u, map, bar, 0, now.row, now.kvh, now.page);
+            ring.next(slots);
+            if (next.valid >= 0) store_scales(n + 1);
         }
         // Given up: the copies under way must land before the CTA may leave.
         if (!ok && lane == 0)
