@@ -788,7 +788,7 @@ static int resolve_q4(const char *who, const pec_paged_q4_args *a, Call &c)
     p.c = q.c;
     p.k_pages = q.k; p.v_pages = q.v; p.k_scales = q.ks; p.v_scales = q.vs;
     p.ks_sp = q.ks_sp; p.ks_st = q.ks_st; p.ks_sh = q.ks_sh; p.vs_sp = q.vs_sp; p.vs_st = q.vs_st; p.vs_sh = q.vs_sh;
-    return lay_out(who, qy, {a->dtype == PEC_BF16 && a->Hq / h.Hkv <= kFewRowsQ4, kFewRowsQ4, true, false}, c);
+    return lay_out(who, qy, {a->dtype == PEC_BF16 && a->Hq / h.Hkv <= kFewRowsQ4, kFewRowsQ4, true, a->dtype == PEC_BF16}, c);
 }
 
 static int check_workspace(const char *who, const Call &c, const void *workspace, size_t bytes)
@@ -848,7 +848,7 @@ extern "C" int pec_paged_attn_q4(const pec_paged_q4_args *args, void *cuda_strea
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (c.many_items > 0) rc = launch_paged_plan(c.p, stream);
     if (rc == PEC_OK && c.many_items > 0)
-        rc = args->dtype == PEC_BF16 ? launch_fma<true, __nv_bfloat16>(c.p, c.many_items, stream) : launch_fma<true, float>(c.p, c.many_items, stream);
+        rc = args->dtype == PEC_BF16 ? launch_paged_many_q4(c.p, c.many_items, stream) : launch_fma<true, float>(c.p, c.many_items, stream);
     if (rc == PEC_OK && c.p.few) rc = launch_paged_few_q4(c.p, c.many_items > 0, stream);
     if (rc != PEC_OK || c.bytes == 0) return rc;
     return launch_paged_combine(c.p, stream);

@@ -242,6 +242,7 @@ int launch_paged_plan(const paged::Params &p, cudaStream_t stream);             
 int launch_paged_f32(const paged::Params &p, int64_t items, cudaStream_t stream);       // fp32
 int launch_paged_many(const paged::Params &p, int64_t items, cudaStream_t stream);         // bf16
 int launch_paged_few(const paged::Params &p, bool after_many, cudaStream_t stream);         // bf16; after_many: overlaps that kernel's end
+int launch_paged_many_q4(const paged::Params &p, int64_t items, cudaStream_t stream);      // bf16 queries, a cache held in 4 bits
 int launch_paged_few_q4(const paged::Params &p, bool after_many, cudaStream_t stream);      // the same of a cache held in 4 bits, at most kFewRowsQ4 rows
 int launch_paged_combine(const paged::Params &p, cudaStream_t stream);
 
