@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libpec.so")
 TORCH_SOURCE = "pec_torch.cpp"
 TORCH_MODULE = os.path.join(HERE, "_pec_torch.so")
 SOURCES = ["pec_api.cpp", "pec_plan.cpp", "pec_merge.cu", "pec_attn_f32.cu", "pec_attn_prefill_bf16.cu", "pec_attn_split_bf16.cu", "pec_decode.cu", "pec_linear.cu", "pec_linear_merged.cu",
-           "pec_heads.cu", "pec_q4_cache.cu", "pec_q4_few.cu", "pec_paged_attn.cu", "pec_paged_few.cu", "pec_paged_many.cu"]
+           "pec_heads.cu", "pec_q4_cache.cu", "pec_q4_few.cu", "pec_q4_many.cu", "pec_paged_attn.cu", "pec_paged_few.cu", "pec_paged_many.cu"]
 
 
 def _stale() -> bool:

@@ -8,15 +8,10 @@
 // One 128-column score buffer that both stages use in turns, a P region per stage, K and V tiles of 128 keys through a ring of
 // four slots; per stage the issue order is S(j + 1), PV(j).  The tiles come page by page (see pec_paged_tma.cuh).
 // TMEM columns: scores [0, 128); P_s [128 + 64 s, +64); O_s [256 + 128 s, +128).
-//
-// A cache held in 4 bits: warps 12-15 write the tiles into the ring instead, in bf16, which holds code times scale exactly; everything
-// behind the ring is the same.  A warp takes eight keys at a time (lane: a key, and 32 of its channels), loads of the next item under
-// the decoding of this one.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include "pec_paged_tma.cuh"
-#include "pec_q4.cuh"
 
 namespace pec {
 using namespace sm100;
@@ -25,11 +20,9 @@ namespace many {
 
 constexpr int kTile = 128;
 constexpr int kSlots = 4;                                  // K/V ring
-constexpr int kMmaWarp0 = 8, kLoadWarp = 9, kMmaWarp1 = 10, kDecodeWarp = 12;
-// Registers: 256 * kSoftmax + the other threads' kLight is what a CTA is launched with (384 * 168, 512 * 128).
-template <bool kQ4> struct Cfg {
-    static constexpr int kThreads = kQ4 ? 512 : 384, kSoftmaxRegs = kQ4 ? 184 : 224, kLightRegs = kQ4 ? 72 : 56;
-};
+constexpr int kThreads = 384;
+constexpr int kMmaWarp0 = 8, kLoadWarp = 9, kMmaWarp1 = 10;
+constexpr int kLightRegs = 56, kSoftmaxRegs = 224;         // 256 * 224 + 128 * 56 = 384 * 168 (the launch allocation)
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColP = 128, kColO = 256;
 constexpr float kRescaleThreshold = 8.0f;                  // log2 units
 
@@ -60,12 +53,10 @@ __device__ __forceinline__ bool wait_all(uint64_t *bar, uint32_t parity, Shared 
     return __all_sync(0xffffffffu, mbar_wait_bounded(smem_u32(bar), parity, &sh->abort_flag, p.status, p.wait_cycles, (int)PEC_ERR_TIMEOUT));
 }
 
-template <bool kQ4>
-__global__ void __launch_bounds__(Cfg<kQ4>::kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                   const __grid_constant__ CUtensorMap tm_v, const Params p, const int box, const int skip_last)
 {
-    constexpr int kSoftmaxRegs = Cfg<kQ4>::kSoftmaxRegs, kLightRegs = Cfg<kQ4>::kLightRegs;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t sQ = (raw + 1023u) & ~1023u, sRing = sQ + 2 * kTileBytes;
@@ -94,7 +85,7 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             griddep_launch_dependents();
             sh->abort_flag = 0;
             for (int st = 0; st < 2; ++st) mbar_init(smem_u32(&sh->bar_q[st]), 1);
-            for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&sh->kv_full[s]), kQ4 ? 4 : 1); mbar_init(smem_u32(&sh->kv_empty[s]), 2); }
+            for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&sh->kv_full[s]), 1); mbar_init(smem_u32(&sh->kv_empty[s]), 2); }
         }
         griddep_wait();
         const Item it = p.many_items[blockIdx.x / p.Hkv];  // (inside the list's room, filled or not)
@@ -130,10 +121,8 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         __syncwarp();
         if (found && g.n_max > 0) {
 
-            if constexpr (!kQ4) {
-                at = box_place(p.c.page_size, g.key_lo, bl);
-                page = box_page(p, g.b, g.key_lo, g.kv, bl, at);
-            }
+            at = box_place(p.c.page_size, g.key_lo, bl);
+            page = box_page(p, g.b, g.key_lo, g.kv, bl, at);
             if (lane == 0) {
                 // The second stage's tokens may lie past the request's, or past q (zero fill): those rows are not used.
                 for (int st = 0; st < 2; ++st) {
@@ -143,14 +132,12 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     tma_load_4d(dst + kHalfTileBytes, &tm_q, bar, 64, 0, kvh, g.tok_row + st * tps);
                 }
             }
-            if constexpr (!kQ4) {
-                const uint32_t bytes = tile_bytes(g.key_lo, g.kv, box);
-                const bool mine = bl.used && g.key_lo + bl.first < g.kv;
-                load_tile(0, 0, bytes, mine);
-                load_tile(1, 1, bytes, mine);
-                at = box_next(at, step);
-                if (g.n_max > 1) page = box_page(p, g.b, g.key_lo + kTile, g.kv, bl, at);
-            }
+            const uint32_t bytes = tile_bytes(g.key_lo, g.kv, box);
+            const bool mine = bl.used && g.key_lo + bl.first < g.kv;
+            load_tile(0, 0, bytes, mine);
+            load_tile(1, 1, bytes, mine);
+            at = box_next(at, step);
+            if (g.n_max > 1) page = box_page(p, g.b, g.key_lo + kTile, g.kv, bl, at);
         }
     } else if (tid == kMmaWarp0 * 32) {
         for (int st = 0; st < 2; ++st) {
@@ -160,8 +147,7 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             mbar_init(smem_u32(&sh->drained[st]), 1);
         }
         mbar_init_fence();
-        prefetch_tmap(&tm_q);
-        if (!kQ4) { prefetch_tmap(&tm_k); prefetch_tmap(&tm_v); }
+        prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
     } else if (warp == 4) {
         tmem_alloc(smem_u32(&sh->tmem_base), kTmemCols);
         tmem_relinquish();
@@ -179,9 +165,7 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     if (warp == kLoadWarp) {
         // ------------------------------------------------------------------ TMA loader (one box per lane); tile 0 is under way
         reg_dealloc<kLightRegs>();
-        if constexpr (kQ4) {                               // Q is all that it loads; whoever gives up may not have waited for it
-            if (n_max > 0 && lane == 0) { wait_quietly(&sh->bar_q[0], 0, p); wait_quietly(&sh->bar_q[1], 0, p); }
-        } else if (n_max > 0) {
+        if (n_max > 0) {
             const int32_t b = sh->g.b, kv = sh->g.kv;
             int32_t k0 = sh->g.key_lo + kTile;
             int issued = 2;
@@ -278,7 +262,7 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (j < n_st) {
                     const int32_t valid = kv - key_lo - j * kTile;
                     // (both issuers write the same zeros; neither's product reads anything else there)
-                    if (!kQ4 && valid < kTile) clear_tail(sRing + (uint32_t)((2 * j + 1) % kSlots) * kTileBytes, valid, lane);
+                    if (valid < kTile) clear_tail(sRing + (uint32_t)((2 * j + 1) % kSlots) * kTileBytes, valid, lane);
                     ok = wait_all(&sh->p_ready[st], j & 1, sh, p);
                     if (!ok) break;
                     tc_fence_after();
@@ -287,71 +271,6 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 kv_release(2 * j + 1);
             }
             if (!ok) drain_products(&sh->drained[st], leader, p);
-        }
-        __syncwarp();
-    } else if (kQ4 && warp >= kDecodeWarp) {
-        // ------------------------------------------------------------------ tiles of a cache held in 4 bits
-        reg_dealloc<kLightRegs>();
-        const int w = warp - kDecodeWarp, row8 = lane & 7, quarter = lane >> 3;        // this warp: keys 32 w .. + 31 of each tile
-        const int32_t b = sh->g.b, kv = sh->g.kv, key_lo = sh->g.key_lo;
-        // Lane i & 3 looks after eight keys, 32 w + 8 i ..: the number in the request's list of pages, the row of the page.
-        const BoxLane own = {32 * w + 8 * (lane & 3), 0u, true};
-        at = box_place(p.c.page_size, key_lo, own);
-        auto look_up = [&](int j) { return j < n_max ? box_page(p, b, key_lo + j * kTile, kv, own, at) : 0; };
-        const uint8_t *k_codes = static_cast<const uint8_t *>(p.k_pages) + kvh * p.c.k_sh + 16 * quarter, *v_codes = static_cast<const uint8_t *>(p.v_pages) + kvh * p.c.v_sh + 16 * quarter;
-        const uint16_t *k_scales = p.k_scales + kvh * p.ks_sh, *v_scales = p.v_scales + kvh * p.vs_sh;
-        struct Item { uint4 codes[4]; uint16_t scale[4]; };
-        auto fetch = [&](int j, int which, int32_t pg, int32_t row0, Item &x) {
-            const uint8_t *codes = which ? v_codes : k_codes;
-            const uint16_t *scales = which ? v_scales : k_scales;
-            const int64_t sp = which ? p.c.v_sp : p.c.k_sp, st = which ? p.c.v_st : p.c.k_st, s_p = which ? p.vs_sp : p.ks_sp, s_t = which ? p.vs_st : p.ks_st;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t pi = __shfl_sync(0xffffffffu, pg, i);
-                const int32_t ri = __shfl_sync(0xffffffffu, row0, i) + row8;
-                x.codes[i] = make_uint4(0u, 0u, 0u, 0u);
-                x.scale[i] = 0;                            // keys past the end are zeros: nothing there meets a product
-                if (j < n_max && key_lo + j * kTile + 32 * w + 8 * i + row8 < kv) {
-                    x.codes[i] = __ldg(reinterpret_cast<const uint4 *>(codes + pi * sp + ri * st));
-                    x.scale[i] = __ldg(scales + pi * s_p + ri * s_t);
-                }
-            }
-        };
-        const uint32_t half = (uint32_t)(quarter >> 1) * kGroupHalf + (uint32_t)row8 * 128u, chunk = (uint32_t)(quarter & 1) * 4u;
-        bool ok = true;
-        auto decode = [&](int item, const Item &x) {
-            const int slot = item % kSlots, fill = item / kSlots;
-            if (fill > 0) ok = wait_all(&sh->kv_empty[slot], (fill - 1) & 1, sh, p);
-            if (!ok) return;
-            const uint32_t dst = sRing + (uint32_t)slot * kTileBytes + (uint32_t)w * 4u * kGroupBytes + half;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const __nv_bfloat162 s2 = q4::twice(x.scale[i]);
-                const uint32_t words[4] = {x.codes[i].x, x.codes[i].y, x.codes[i].z, x.codes[i].w};
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t r[4];
-                    q4::decode8(words[c], s2, r);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                                 ::"r"(dst + (uint32_t)i * kGroupBytes + (((chunk + c) ^ (uint32_t)row8) << 4)), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
-                }
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh->kv_full[slot]));
-        };
-        Item kx, vx;
-        int32_t pg = look_up(0), row0 = at.row;
-        fetch(0, 0, pg, row0, kx);
-        for (int j = 0; j < n_max && ok; ++j) {
-            at = box_next(at, step);
-            const int32_t pg_next = look_up(j + 1);
-            fetch(j, 1, pg, row0, vx);
-            decode(2 * j, kx);
-            pg = pg_next; row0 = at.row;
-            fetch(j + 1, 0, pg, row0, kx);
-            if (skip_last && n_max > 1 && j == n_max - 1) ok = false;      // test hook: the wait for it runs out
-            if (ok) decode(2 * j + 1, vx);
         }
         __syncwarp();
     } else if (warp > kMmaWarp1) {
@@ -534,38 +453,33 @@ paged_many_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 }  // namespace many
 }  // namespace paged
 
-template <bool kQ4>
-static int launch(const paged::Params &p, int64_t items, cudaStream_t stream)
+int launch_paged_many(const paged::Params &p, int64_t items, cudaStream_t stream)
 {
     using namespace paged;
-    const int box = kQ4 ? 8 : host_map::box_rows(p.c.page_size);
-    CUtensorMap tm_q, tm_k = {}, tm_v = {};
-    if (!host_map::queries(&tm_q, p, kFewRows / p.g) ||
-        (!kQ4 && (!host_map::pages(&tm_k, p, p.k_pages, p.c.k_st, p.fk, box) || !host_map::pages(&tm_v, p, p.v_pages, p.c.v_st, p.fv, box)))) {
-        set_error("%s: cuTensorMapEncodeTiled failed (driver too old, or strides/addresses not encodable)", p.who);
+    const int box = host_map::box_rows(p.c.page_size);
+    CUtensorMap tm_q, tm_k, tm_v;
+    if (!host_map::queries(&tm_q, p, kFewRows / p.g) || !host_map::pages(&tm_k, p, p.k_pages, p.c.k_st, p.fk, box) ||
+        !host_map::pages(&tm_v, p, p.v_pages, p.c.v_st, p.fv, box)) {
+        set_error("pec_paged_attn: cuTensorMapEncodeTiled failed (driver too old, or strides/addresses not encodable)");
         return PEC_ERR_CUDA;
     }
-    typedef many::Cfg<kQ4> C;
     static unsigned char ready[host::kMaxDevices] = {};
     static std::mutex ready_mutex;
     if (!host::once_per_device(ready, ready_mutex, [] {
             cudaFuncAttributes attr;
-            return cudaFuncSetAttribute(many::paged_many_kernel<kQ4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)many::kSmemBytes) == cudaSuccess &&
-                   cudaFuncGetAttributes(&attr, many::paged_many_kernel<kQ4>) == cudaSuccess &&
-                   attr.numRegs * C::kThreads >= 256 * C::kSoftmaxRegs + (C::kThreads - 256) * C::kLightRegs; })) {
+            return cudaFuncSetAttribute(many::paged_many_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)many::kSmemBytes) == cudaSuccess &&
+                   cudaFuncGetAttributes(&attr, many::paged_many_kernel) == cudaSuccess &&
+                   attr.numRegs * many::kThreads >= 256 * many::kSoftmaxRegs + 128 * many::kLightRegs; })) {
         (void)cudaGetLastError();
-        set_error("%s: kernel set-up failed (shared-memory limit, or the register allocation does not cover the warp-role split)", p.who);
+        set_error("pec_paged_attn: kernel set-up failed (shared-memory limit, or the register allocation does not cover the warp-role split)");
         return PEC_ERR_CUDA;
     }
-    if (items * p.Hkv > 0x7fffffff) { set_error("%s: grid too large", p.who); return PEC_ERR_UNSUPPORTED; }
-    cudaError_t err = launch_dependent(many::paged_many_kernel<kQ4>, dim3((unsigned)(items * p.Hkv)), C::kThreads, many::kSmemBytes, stream, true,
+    if (items * p.Hkv > 0x7fffffff) { set_error("pec_paged_attn: grid too large"); return PEC_ERR_UNSUPPORTED; }
+    cudaError_t err = launch_dependent(many::paged_many_kernel, dim3((unsigned)(items * p.Hkv)), many::kThreads, many::kSmemBytes, stream, true,
                                        tm_q, tm_k, tm_v, p, box, (int)test_skip_last_load());
     if (err == cudaSuccess) err = cudaGetLastError();
-    if (err != cudaSuccess) { set_error("%s: launch failed: %s", p.who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
+    if (err != cudaSuccess) { set_error("pec_paged_attn: launch failed: %s", cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
 }
-
-int launch_paged_many(const paged::Params &p, int64_t items, cudaStream_t stream) { return launch<false>(p, items, stream); }
-int launch_paged_many_q4(const paged::Params &p, int64_t items, cudaStream_t stream) { return launch<true>(p, items, stream); }
 
 }  // namespace pec

@@ -3,6 +3,7 @@
 #pragma once
 #include <cstdint>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include "pec_paged.h"
 
@@ -56,6 +57,19 @@ __device__ __forceinline__ void decode8(uint32_t w, __nv_bfloat162 s2, uint32_t 
         const uint32_t x = __byte_perm(w, w4, (uint32_t)(i << 12) | (uint32_t)((4 + i) << 4));
         const uint32_t t = (x & 0x80008000u) | ((x >> 6) & 0x01c001c0u);
         const __nv_bfloat162 y = __hmul2(__hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&t), up), s2);
+        r[i] = *reinterpret_cast<const uint32_t *>(&y);
+    }
+}
+// The same to fp16, times a scale that fp16 holds.
+__device__ __forceinline__ void decode8_f16(uint32_t w, __half2 s2, uint32_t (&r)[4])
+{
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "mov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\tcvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&r[i]), s2);
         r[i] = *reinterpret_cast<const uint32_t *>(&y);
     }
 }

@@ -198,6 +198,8 @@ __host__ __device__ constexpr uint32_t idesc_bf16_f32(int m, int n, int a_mn_maj
          | ((uint32_t)(m >> 4) << 24);
 }
 
+// The same for fp16 A/B.
+__host__ __device__ constexpr uint32_t idesc_f16_f32(int m, int n, int a_mn_major, int b_mn_major) { return idesc_bf16_f32(m, n, a_mn_major, b_mn_major) & ~(1u << 7 | 1u << 10); }
 // For kind::f8f6f4 (8 bits and fewer) with fp32 accumulation; formats: 0 e4m3, 1 e5m2, 5 e2m1 (in shared memory 16 codes in the first 8 of
 // every 16 bytes).
 constexpr int kE4M3 = 0, kE5M2 = 1, kE2M1 = 5;
@@ -382,6 +384,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
 
