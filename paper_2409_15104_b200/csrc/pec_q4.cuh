@@ -30,7 +30,7 @@ constexpr uint16_t kNaN = 0x7fff;
 __device__ __forceinline__ float scale_of(float most)
 {
     constexpr uint32_t step = 1u << 18;      // of 23 bits after the first, five stay
-    uint32_t b = __float_as_uint(__fdiv_rn(most, 6.f)) & ~(step - 1);
+    uint32_t b = __float_as_uint(most * (0x1.555552p-3f)) & ~(step - 1);               // at most two numbers short
     if (6.f * __uint_as_float(b) < most) b += step;
     if (6.f * __uint_as_float(b) < most) b += step;
     return fminf(fmaxf(__uint_as_float(b), 0x1p-100f), 1.3125f * 0x1p125f);
