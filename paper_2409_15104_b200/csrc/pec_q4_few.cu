@@ -371,7 +371,7 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             if (bl.first < x.valid) x.page = __ldg(p.c.table + walk.b * p.c.table_stride + at.nth);
             return x;
         };
-        bool ok = true;
+        bool fresh = false;                                // the walk's step is the first of a segment that is to begin
         auto advance = [&] {                               // to the next step; false: there is none
             left -= kSub;
             if (left > 0) {
@@ -386,11 +386,10 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             k0 = 0;
             key_end = min(walk.r.kv, left * kKeyTile);
             at = box_place(p.c.page_size, 0, bl);
-            ok = begin();
-            return ok;
+            return fresh = true;
         };
         const Spot none = {-1, 0, 0, -1};
-        ok = begin();
+        bool ok = begin();
         Spot now = spot(), after = none;
         bool more = ok && advance();
         if (more) after = spot();
@@ -413,7 +412,11 @@ paged_few_q4_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_const
             if (now.valid < 0) break;
             now = after;
             after = none;
-            if (more) {
+            // Not before the plan of the step before has been handed over: a segment begins in the place of the one before the last, whose
+            // last keys are loaded when the step after them is known.
+            if (fresh) ok = begin();
+            fresh = false;
+            if (ok && more) {
                 more = advance();
                 if (more) after = spot();
             }
