@@ -662,8 +662,13 @@ int pec_kv_read_q4(const pec_kv_read_q4_args *args, void *cuda_stream);
 /*
  * pec_paged_attn over such a cache: the same rows, masks, outputs and kinds of batches, with the numbers that the cache holds as
  * keys and values.  dtype: that of q.  PEC_BF16 runs the tensor cores, PEC_F32 an fp32 FMA kernel with fp32 output.
- * Keys and values past a request's end are never used, nor is a value that a row does not see.
- * A row with a NaN score, or one of +inf, gets NaN.  max_q_len, workspace, status: as there.
+ * PEC_BF16: products are exact, sums fp32.  Requests of at most 16 packed rows (n * Hq / Hkv) with Hq / Hkv <= 16 hold probabilities
+ * times values' scales to 2^-12 of themselves, and below 2^-24 of the row's largest probability times the largest scale to 2^-36 of
+ * that; of q, channels below 2^-13 of the row's largest magnitude to 2^-22 of it.  The others hold probabilities to 2^-12 of
+ * themselves, below 2^-24 of the row's largest to 2^-35 of it, and values to 2^-34 of the largest scale that the request has had so far.
+ * Keys and values past a request's end are never used.  A value of a request that is not finite may spoil the rows of the same request
+ * that do not see it yet, never those of another request.  A row with a NaN score, or one of +inf, gets NaN.
+ * max_q_len, workspace, status, a call that finds PEC_ERR_TIMEOUT in *status: as there (the kernel for few rows takes 16, not 128).
  * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, WORKSPACE, CUDA.
  */
 typedef struct {
@@ -686,7 +691,7 @@ typedef struct {
 int pec_paged_attn_q4(const pec_paged_q4_args *args, void *cuda_stream);
 
 /* Bytes of workspace pec_paged_attn_q4 needs for these arguments (0 if they are invalid): a function of the same numbers as
- * pec_paged_workspace_size. */
+ * pec_paged_workspace_size; on 148 SMs at most 122.3 MB, 0.133 MB for every KV head, and 48 bytes for every request and block of rows. */
 size_t pec_paged_q4_workspace_size(const pec_paged_q4_args *args);
 
 /*
@@ -700,7 +705,7 @@ size_t pec_paged_q4_workspace_size(const pec_paged_q4_args *args);
  *   PEC_CTL_TEST_SKIP_LAST_LOAD test hook, 0 / 1: the loader of the tensor-core kernels leaves out its
  *                               last tile (attention: the last V tile of a CTA that walks at least two
  *                               key tiles; pec_linear, pec_linear_merged: the last K step (pec_linear: of its last tile)
- *                               of the second CTA of each pair; pec_paged_attn: as for attention),
+ *                               of the second CTA of each pair; pec_paged_attn, pec_paged_attn_q4: as for attention),
  *                               so that the waits for it run out and the timeout path can be checked.
  *                               Results of such a launch are undefined; the status word tells.
  * Applies to launches enqueued after the call.  Errors: INVALID_ARG.

@@ -236,8 +236,8 @@ __device__ __forceinline__ void copy16(float *dst, const float *src, bool ok)
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
-// A cache held in 4 bits: codes and scales are decoded on their way to shared memory, four channels a lane.
-// Four channels of a key or value, of the eight in a word of codes; zeros where !ok (nothing is read then).
+// A cache held in 4 bits (fp32 queries): codes and scales are decoded on their way to shared memory, four channels a lane.
+// Zeros where !ok (nothing is read then).
 __device__ __forceinline__ float4 decode4(const uint8_t *codes, const uint16_t *scale, bool ok)
 {
     uint32_t r[4] = {0u, 0u, 0u, 0u};
@@ -245,7 +245,7 @@ __device__ __forceinline__ float4 decode4(const uint8_t *codes, const uint16_t *
     return make_float4(__uint_as_float(r[0] << 16), __uint_as_float(r[0] & 0xffff0000u), __uint_as_float(r[1] << 16), __uint_as_float(r[1] & 0xffff0000u));
 }
 
-template <bool kQ4, class Q>
+template <bool kQ4>
 __global__ void __launch_bounds__(kThreads, 2)
 paged_f32_kernel(const Params p)
 {
@@ -264,14 +264,7 @@ paged_f32_kernel(const Params p)
     for (int i = tid; i < kBM * (kHeadDim / 4); i += kThreads) {
         const int r = i / (kHeadDim / 4), c = (i % (kHeadDim / 4)) * 4;
         const int32_t rr = min(r, rows - 1), t = (row0 + rr) / p.g, h = kvh * p.g + (row0 + rr) % p.g;
-        const Q *src = static_cast<const Q *>(p.q) + (int64_t)(it.r.start + t) * p.q_st + (int64_t)h * p.q_sh + c;
-        if constexpr (sizeof(Q) == 4) {
-            copy16(sQ + r * kLd + c, src, r < rows);
-        } else {
-            const uint2 u = r < rows ? *reinterpret_cast<const uint2 *>(src) : make_uint2(0u, 0u);
-            *reinterpret_cast<float4 *>(sQ + r * kLd + c) = make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u),
-                                                                        __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
-        }
+        copy16(sQ + r * kLd + c, static_cast<const float *>(p.q) + (int64_t)(it.r.start + t) * p.q_st + (int64_t)h * p.q_sh + c, r < rows);
     }
 
     float m_run[4], l_run[4];
@@ -428,15 +421,9 @@ paged_f32_kernel(const Params p)
             if (tx == 0) p.many_lse[slot * p.many_rows + r] = lse;
         } else {
             const int64_t item = (int64_t)(it.r.start + (row0 + r) / p.g) * p.Hq + kvh * p.g + (row0 + r) % p.g;
-            if (sizeof(Q) == 2 && p.o_is_bf16) {
-                __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.o) + item * kHeadDim;
-#pragma unroll
-                for (int c = 0; c < 8; ++c) o[(c & 4) * 16 + tx * 4 + (c & 3)] = __float2bfloat16_rn(out[c]);
-            } else {
-                float *o = static_cast<float *>(p.o) + item * kHeadDim;
-                *reinterpret_cast<float4 *>(o + tx * 4) = make_float4(out[0], out[1], out[2], out[3]);
-                *reinterpret_cast<float4 *>(o + 64 + tx * 4) = make_float4(out[4], out[5], out[6], out[7]);
-            }
+            float *o = static_cast<float *>(p.o) + item * kHeadDim;
+            *reinterpret_cast<float4 *>(o + tx * 4) = make_float4(out[0], out[1], out[2], out[3]);
+            *reinterpret_cast<float4 *>(o + 64 + tx * 4) = make_float4(out[4], out[5], out[6], out[7]);
             if (tx == 0) p.lse[item] = lse;
         }
     }
@@ -564,25 +551,25 @@ int launch_paged_plan(const Params &p, cudaStream_t stream)
 }
 
 // Set-up and launch of one form of the FMA kernel.
-template <bool kQ4, class Q>
+template <bool kQ4>
 static int launch_fma(const Params &p, int64_t items, cudaStream_t stream)
 {
     static unsigned char ready[host::kMaxDevices] = {};
     static std::mutex ready_mutex;
     if (!host::once_per_device(ready, ready_mutex, [] {
-            return cudaFuncSetAttribute(paged_f32_kernel<kQ4, Q>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kF32Smem) == cudaSuccess; })) {
+            return cudaFuncSetAttribute(paged_f32_kernel<kQ4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kF32Smem) == cudaSuccess; })) {
         (void)cudaGetLastError();
         set_error("%s: cannot raise the shared-memory limit", p.who);
         return PEC_ERR_CUDA;
     }
     if (items * p.Hkv > 0x7fffffff) { set_error("%s: grid too large", p.who); return PEC_ERR_UNSUPPORTED; }
-    cudaError_t err = launch_dependent(paged_f32_kernel<kQ4, Q>, dim3((unsigned)(items * p.Hkv)), kThreads, kF32Smem, stream, true, p);
+    cudaError_t err = launch_dependent(paged_f32_kernel<kQ4>, dim3((unsigned)(items * p.Hkv)), kThreads, kF32Smem, stream, true, p);
     if (err == cudaSuccess) err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("%s: launch failed: %s", p.who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
 }
 
-int launch_paged_f32(const Params &p, int64_t items, cudaStream_t stream) { return launch_fma<false, float>(p, items, stream); }
+int launch_paged_f32(const Params &p, int64_t items, cudaStream_t stream) { return launch_fma<false>(p, items, stream); }
 
 int launch_paged_combine(const Params &p, cudaStream_t stream)
 {
@@ -848,7 +835,7 @@ extern "C" int pec_paged_attn_q4(const pec_paged_q4_args *args, void *cuda_strea
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (c.many_items > 0) rc = launch_paged_plan(c.p, stream);
     if (rc == PEC_OK && c.many_items > 0)
-        rc = args->dtype == PEC_BF16 ? launch_paged_many_q4(c.p, c.many_items, stream) : launch_fma<true, float>(c.p, c.many_items, stream);
+        rc = args->dtype == PEC_BF16 ? launch_paged_many_q4(c.p, c.many_items, stream) : launch_fma<true>(c.p, c.many_items, stream);
     if (rc == PEC_OK && c.p.few) rc = launch_paged_few_q4(c.p, c.many_items > 0, stream);
     if (rc != PEC_OK || c.bytes == 0) return rc;
     return launch_paged_combine(c.p, stream);
