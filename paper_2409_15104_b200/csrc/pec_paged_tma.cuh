@@ -178,16 +178,18 @@ inline bool pages(CUtensorMap *map, const Params &p, const void *base, int64_t s
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(base), d, s, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// Pages held in 4 bits: 128 codes, tokens of a page, heads, pages; the copy spreads 16 codes over the first half of every 16 bytes.
-inline bool pages_q4(CUtensorMap *map, const Params &p, const void *base, int64_t sp, int64_t st, int64_t sh, int box)
+// Pages held in 4 bits, tokens of a page, heads, pages: codes spread over the first half of every 16 bytes, 128-byte swizzle, or as they are.
+inline bool pages_q4(CUtensorMap *map, const Params &p, const void *base, int64_t sp, int64_t st, int64_t sh, int box, bool spread)
 {
     const host::EncodeTiledFn fn = host::encode_fn();
     if (!fn) return false;
-    const cuuint64_t d[4] = {(cuuint64_t)kHeadDim, (cuuint64_t)p.c.page_size, (cuuint64_t)p.Hkv, (cuuint64_t)p.c.num_pages};
+    const int width = spread ? kHeadDim : kHeadDim / 2;
+    const cuuint64_t d[4] = {(cuuint64_t)width, (cuuint64_t)p.c.page_size, (cuuint64_t)p.Hkv, (cuuint64_t)p.c.num_pages};
     const cuuint64_t s[3] = {(cuuint64_t)st, (cuuint64_t)sh, (cuuint64_t)sp};
-    const cuuint32_t b[4] = {(cuuint32_t)kHeadDim, (cuuint32_t)box, 1, 1}, e[4] = {1, 1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B, 4, const_cast<void *>(base), d, s, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint32_t b[4] = {(cuuint32_t)width, (cuuint32_t)box, 1, 1}, e[4] = {1, 1, 1, 1};
+    return fn(map, spread ? CU_TENSOR_MAP_DATA_TYPE_16U4_ALIGN16B : CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(base), d, s, b, e,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, spread ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 inline int box_rows(int page_size)
 {

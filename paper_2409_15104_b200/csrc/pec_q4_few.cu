@@ -752,8 +752,8 @@ int launch_paged_few_q4(const paged::Params &p, bool after_many, cudaStream_t st
     using namespace paged;
     const int box = host_map::box_rows(p.c.page_size);
     CUtensorMap tm_k, tm_v;
-    if (!host_map::pages_q4(&tm_k, p, p.k_pages, p.c.k_sp, p.c.k_st, p.c.k_sh, box) ||
-        !host_map::pages_q4(&tm_v, p, p.v_pages, p.c.v_sp, p.c.v_st, p.c.v_sh, box)) {
+    if (!host_map::pages_q4(&tm_k, p, p.k_pages, p.c.k_sp, p.c.k_st, p.c.k_sh, box, true) ||
+        !host_map::pages_q4(&tm_v, p, p.v_pages, p.c.v_sp, p.c.v_st, p.c.v_sh, box, true)) {
         set_error("%s: cuTensorMapEncodeTiled failed (driver too old, or strides/addresses not encodable)", p.who);
         return PEC_ERR_CUDA;
     }

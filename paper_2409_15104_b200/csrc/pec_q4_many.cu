@@ -3,8 +3,10 @@
 // Tensor-bound by its operations, 4 * 128 per visible (row, key) pair; in practice by 2^x of every pair (16 a cycle and SM).  One CTA =
 // one item of the plan: up to 256 packed rows (two stages of 128 / g whole tokens each) of one KV head against one slice of the keys.
 //   warps 0-3, 4-7  softmax and epilogue of stage 0 and 1 (a thread = a packed row = a TMEM lane)
-//   warps 8, 10     MMA issuers of stage 0 and 1       warp 9  loader of Q       warp 11  idle
-//   warps 12-15     K and V: from the pages, decoded, into a ring of four tiles of 128 keys, 32 keys each
+//   warps 8, 10     MMA issuers of stage 0 and 1       warp 9  loader of Q and codes       warp 11  idle
+//   warps 12-15     K and V: codes decoded into a ring of four tiles of 128 keys, 32 keys each
+// The codes come ahead of their decoding, in a ring of their own: with 16 bytes a lane in flight instead few rows waited for memory
+// (32 requests of 8 tokens and 4000 keys, 32 heads on 8: 206 us, now 167; 2048 tokens on 30720 1323 us, now 1261).
 // The tiles are decoded to fp16, to which the hardware converts codes (two an instruction).  fp16 has no range to hold scales, so what
 // is multiplied is in units, powers of two that the other side makes up for:
 //     K   of one for each 32 keys of a tile, such that scales are below 2^13 of it: a factor of those scores
@@ -13,11 +15,10 @@
 // A code times its scale has eight bits at most and is exact down to 2^-29 (V: 2^-26) of the largest scale, as is a channel of Q to 2^-31
 // of its row's largest.  Probabilities are rounded to fp16, to 2^-12 of themselves: the largest of a row is held in [2^10, 2^15], and
 // those below 2^-24 of it, in fp16's subnormals, are off by at most 2^-35 of it.
-// A thread cannot hold its row's 128 scores next to warps that decode: with the score buffer of the bf16 cache's kernel, which has to be
-// emptied at once, 184 registers for a row and 72 for a decoding thread spill, 1493 us where this takes 1325 (2048 tokens on 30720 keys,
-// 32 heads on 8).  So a row is taken in two halves, one of them twice, and scores stay in tensor memory until probabilities take their
-// place: 144 and 112 registers.  S(j + 1) of a stage then begins when PV(j) is done, 2100 cycles in which the other stage has the unit of
-// 2^x to itself: the stages take turns (without that 1366 us), and hand P over by halves (1351).
+// Scores stay in tensor memory until probabilities take their place; S(j + 1) of a stage begins when PV(j) is done, some 2000 cycles in
+// which the other stage has the unit of 2^x to itself: the stages take turns (1195 us, without that 1263) and hand P over by halves.  A
+// row's 128 scores are in registers from its maximum on (1121 us; read a second time, by halves, 1195), which leaves the other warps 64.
+// With the score buffer of the bf16 cache's kernel, one that both stages use in turns, and tiles decoded to bf16 it was 1493 us.
 // TMEM columns: S_s [128 s, +128), P_s its first 64; O_s [256 + 128 s, +128).
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -32,9 +33,11 @@ namespace many_q4 {
 
 constexpr int kTile = 128;
 constexpr int kSlots = 4;                                  // K/V ring
+constexpr int kCodeSlots = 4;                              // ring of the tiles' codes
+constexpr uint32_t kCodeBytes = kTile * q4::kHeadBytes;
 constexpr int kMmaWarp0 = 8, kLoadWarp = 9, kMmaWarp1 = 10, kDecodeWarp = 12;
 constexpr int kThreads = 512;
-constexpr int kSoftmaxRegs = 144, kLightRegs = 112;        // 256 * 144 + 256 * 112 = 512 * 128 (the launch allocation)
+constexpr int kSoftmaxRegs = 192, kLightRegs = 64;         // 256 * 192 + 256 * 64 = 512 * 128 (the launch allocation)
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
 // The largest probability of a row lies in [2^kLift, 2^(kLift + kGrow)].
 constexpr float kLift = 10.f, kGrow = 5.f;
@@ -51,6 +54,7 @@ struct Geom {
 };
 struct Shared {
     uint64_t bar_q[2];
+    uint64_t code_full[kCodeSlots], code_empty[kCodeSlots];
     uint64_t kv_full[kSlots], kv_empty[kSlots];
     uint64_t s_full[2], p_ready[2][2], pv_done[2];         // [stage], one phase per key tile; P by halves
     uint64_t drained[2];
@@ -62,7 +66,8 @@ struct Shared {
     uint32_t tmem_base;
     volatile int abort_flag;
 };
-constexpr size_t kSmemBytes = (2 + kSlots) * kTileBytes + 1024 /*alignment slack*/ + sizeof(Shared);
+constexpr size_t kSmemBytes = (2 + kSlots) * kTileBytes + kCodeSlots * kCodeBytes + 1024 /*alignment slack*/ + sizeof(Shared);
+static_assert(kSmemBytes <= 227 * 1024, "");
 
 __device__ __forceinline__ bool wait_all(uint64_t *bar, uint32_t parity, Shared *sh, const Params &p)   // warp-uniform
 {
@@ -94,24 +99,38 @@ __device__ __forceinline__ float row_to_f16(uint8_t *at, int row)
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
-paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const Params p, int skip_last)
+paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                     const Params p, const int box, const int skip_last)
 {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
-    const uint32_t sQ = (raw + 1023u) & ~1023u, sRing = sQ + 2 * kTileBytes;
-    Shared *sh = reinterpret_cast<Shared *>(smem_raw + (sQ - raw) + (2 + kSlots) * kTileBytes);
+    const uint32_t sQ = (raw + 1023u) & ~1023u, sRing = sQ + 2 * kTileBytes, sCodes = sRing + kSlots * kTileBytes;
+    Shared *sh = reinterpret_cast<Shared *>(smem_raw + (sQ - raw) + (2 + kSlots) * kTileBytes + kCodeSlots * kCodeBytes);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, kvh = blockIdx.x % p.Hkv;
     const int tps = kTile / p.g, srows = tps * p.g;        // tokens and packed rows of a stage
 
-    // The loader warp reads the CTA's item, works out the geometry and starts the loads of Q before the CTA-wide sync; meanwhile others
-    // set up the remaining barriers and the tensor memory.
+    // The loader warp reads the CTA's item, works out the geometry and starts the first loads (Q, codes of K(0), V(0)) before the CTA-wide
+    // sync; meanwhile others set up the remaining barriers and the tensor memory.
+    const BoxLane bl = box_lane(box, lane);
+    const BoxStep box_by = box_step(p.c.page_size);
+    BoxPlace box_at = {0, 0};                              // this lane's box of the next tile, and its page
+    int32_t page = 0;
     bool found = false;
+    // This lane's box (if it is one to load) of the codes of K (which = 0) or V of the tile at position k0.
+    auto load_codes = [&](int which, int slot, int32_t k0, int32_t kv) {
+        const uint32_t bar = smem_u32(&sh->code_full[slot]);
+        if (lane == 0) mbar_arrive_expect_tx(bar, tile_bytes(k0, kv, box) / (2 * kHeadDim) * q4::kHeadBytes);
+        __syncwarp();
+        if (bl.used && k0 + bl.first < kv)
+            tma_load_4d(sCodes + (uint32_t)slot * kCodeBytes + (uint32_t)bl.first * q4::kHeadBytes, which ? (const void *)&tm_v : (const void *)&tm_k, bar, 0, box_at.row, kvh, page);
+    };
     if (warp == kLoadWarp) {
         // The kernel for few rows may start on SMs that this grid leaves.  The plan has to be complete before its list is read.
         if (lane == 0) {
             griddep_launch_dependents();
             sh->abort_flag = 0;
             for (int st = 0; st < 2; ++st) mbar_init(smem_u32(&sh->bar_q[st]), 1);
+            for (int s = 0; s < kCodeSlots; ++s) { mbar_init(smem_u32(&sh->code_full[s]), 1); mbar_init(smem_u32(&sh->code_empty[s]), 4); }
             for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&sh->kv_full[s]), 4); mbar_init(smem_u32(&sh->kv_empty[s]), 2); }
         }
         griddep_wait();
@@ -145,14 +164,22 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const Params p, i
             mbar_init_fence();
         }
         __syncwarp();
-        if (found && g.n_max > 0 && lane == 0) {
-            // The second stage's tokens may lie past the request's, or past q (zero fill): those rows are not used.
-            for (int st = 0; st < 2; ++st) {
-                const uint32_t bar = smem_u32(&sh->bar_q[st]), dst = sQ + st * kTileBytes;
-                mbar_arrive_expect_tx(bar, (uint32_t)srows * 256u);
-                tma_load_4d(dst, &tm_q, bar, 0, 0, kvh, g.tok_row + st * tps);
-                tma_load_4d(dst + kHalfTileBytes, &tm_q, bar, 64, 0, kvh, g.tok_row + st * tps);
+        if (found && g.n_max > 0) {
+            box_at = box_place(p.c.page_size, g.key_lo, bl);
+            page = box_page(p, g.b, g.key_lo, g.kv, bl, box_at);
+            if (lane == 0) {
+                // The second stage's tokens may lie past the request's, or past q (zero fill): those rows are not used.
+                for (int st = 0; st < 2; ++st) {
+                    const uint32_t bar = smem_u32(&sh->bar_q[st]), dst = sQ + st * kTileBytes;
+                    mbar_arrive_expect_tx(bar, (uint32_t)srows * 256u);
+                    tma_load_4d(dst, &tm_q, bar, 0, 0, kvh, g.tok_row + st * tps);
+                    tma_load_4d(dst + kHalfTileBytes, &tm_q, bar, 64, 0, kvh, g.tok_row + st * tps);
+                }
             }
+            load_codes(0, 0, g.key_lo, g.kv);
+            load_codes(1, 1, g.key_lo, g.kv);
+            box_at = box_next(box_at, box_by);
+            if (g.n_max > 1) page = box_page(p, g.b, g.key_lo + kTile, g.kv, bl, box_at);
         }
     } else if (tid == kMmaWarp0 * 32) {
         for (int st = 0; st < 2; ++st) {
@@ -163,7 +190,7 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const Params p, i
             mbar_init(smem_u32(&sh->q_ready[st]), 4);      // one arrival per softmax warp
         }
         mbar_init_fence();
-        prefetch_tmap(&tm_q);
+        prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
     } else if (warp == 4) {
         tmem_alloc(smem_u32(&sh->tmem_base), kTmemCols);
         tmem_relinquish();
@@ -180,8 +207,33 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const Params p, i
 
     if (warp >= 8) reg_dealloc<kLightRegs>();
     if (warp == kLoadWarp) {
-        // ------------------------------------------------------------------ Q is loaded; whoever gives up may not have waited for it
-        if (n_max > 0 && lane == 0) { wait_quietly(&sh->bar_q[0], 0, p); wait_quietly(&sh->bar_q[1], 0, p); }
+        // ------------------------------------------------------------------ loader of codes (one box per lane); tile 0 is under way
+        if (n_max > 0) {
+            const int32_t b = sh->g.b, kv = sh->g.kv;
+            int32_t k0 = sh->g.key_lo + kTile;
+            int issued = 2;
+            bool ok = true;
+            for (int j = 1; j < n_max && ok; ++j, k0 += kTile) {
+                const BoxPlace at_next = box_next(box_at, box_by);
+                const int32_t page_next = j + 1 < n_max ? box_page(p, b, k0 + kTile, kv, bl, at_next) : 0;
+#pragma unroll
+                for (int which = 0; which < 2; ++which) {  // K, V
+                    const int item = 2 * j + which, slot = item % kCodeSlots, fill = item / kCodeSlots;
+                    if (skip_last && item == 2 * n_max - 1) { ok = false; break; }   // test hook: the wait for it runs out
+                    if (fill > 0) ok = wait_all(&sh->code_empty[slot], (fill - 1) & 1, sh, p);
+                    if (!ok) break;
+                    load_codes(which, slot, k0, kv);
+                    ++issued;
+                }
+                page = page_next;
+                box_at = at_next;
+            }
+            if (lane == 0) {
+                // Copies must land before the CTA may leave; those that give up do not wait for them.
+                wait_quietly(&sh->bar_q[0], 0, p); wait_quietly(&sh->bar_q[1], 0, p);
+                for (int i = issued > kCodeSlots ? issued - kCodeSlots : 0; i < issued; ++i) wait_quietly(&sh->code_full[i % kCodeSlots], (i / kCodeSlots) & 1, p);
+            }
+        }
         __syncwarp();
     } else if (warp == kMmaWarp0 || warp == kMmaWarp1) {
         // ------------------------------------------------------------------ MMA issuers, one warp per stage
@@ -239,87 +291,76 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const Params p, i
         __syncwarp();
     } else if (warp >= kDecodeWarp) {
         // ------------------------------------------------------------------ tiles of a cache held in 4 bits
-        const int w = warp - kDecodeWarp, row8 = lane & 7, quarter = lane >> 3;        // this warp: keys 32 w .. + 31 of each tile
+        // This warp: keys 32 w .. + 31 of each tile, eight at a time; a lane has 32 channels of one of the eight.  The scale of key 32 w + i is
+        // loaded by lane i, two tiles ahead, the number of its page three, and looked at a tile later: nothing here waits for memory.
+        const int w = warp - kDecodeWarp, row8 = lane >> 2, quarter = lane & 3;
         const int32_t b = sh->g.b, kv = sh->g.kv, key_lo = sh->g.key_lo;
-        // Lane i & 3 looks after eight keys, 32 w + 8 i ..: the number in the request's list of pages, the row of the page.
-        const BoxLane own = {32 * w + 8 * (lane & 3), 0u, true};
+        const BoxLane own = {32 * w + lane, 0u, true};
         const BoxStep step = box_step(p.c.page_size);
         BoxPlace at = box_place(p.c.page_size, key_lo, own);
-        // What is loaded is looked at a tile later, the page's number too: nothing here waits for memory.
-        auto look_up = [&](int j) { return j < n_max && key_lo + j * kTile + own.first < kv ? __ldg(p.c.table + b * p.c.table_stride + at.nth) : 0; };
-        auto checked = [&](int32_t page) {
-            if (page >= 0 && page < p.c.num_pages) return page;
-            raise_status(p.status, PEC_ERR_BAD_INDEX);
-            return 0;
-        };
-        const uint8_t *k_codes = static_cast<const uint8_t *>(p.k_pages) + kvh * p.c.k_sh + 16 * quarter, *v_codes = static_cast<const uint8_t *>(p.v_pages) + kvh * p.c.v_sh + 16 * quarter;
+        auto valid = [&](int j) { return j < n_max && key_lo + j * kTile + own.first < kv; };
+        auto look_up = [&](int j) { return valid(j) ? __ldg(p.c.table + b * p.c.table_stride + at.nth) : 0; };
         const uint16_t *k_scales = p.k_scales + kvh * p.ks_sh, *v_scales = p.v_scales + kvh * p.vs_sh;
-        // Lane's four keys of tile j: codes of K or V; scales (keys past the end: 0, so that nothing there meets a product).
-        auto valid = [&](int j, int i) { return j < n_max && key_lo + j * kTile + 32 * w + 8 * i + row8 < kv; };
-        auto fetch_codes = [&](int j, int which, int32_t pg, int32_t row0, int i) {
-            const int64_t pi = __shfl_sync(0xffffffffu, pg, i);
-            const int32_t ri = __shfl_sync(0xffffffffu, row0, i) + row8;
-            const uint8_t *codes = which ? v_codes + pi * p.c.v_sp + ri * p.c.v_st : k_codes + pi * p.c.k_sp + ri * p.c.k_st;
-            return valid(j, i) ? __ldg(reinterpret_cast<const uint4 *>(codes)) : make_uint4(0u, 0u, 0u, 0u);
+        struct Scales { uint32_t k, v; };                  // (keys past the end: 0, so that nothing there meets a product)
+        auto fetch = [&](int j, int32_t pg) {
+            if (!valid(j)) return Scales{0u, 0u};
+            if (pg < 0 || pg >= p.c.num_pages) { raise_status(p.status, PEC_ERR_BAD_INDEX); pg = 0; }
+            return Scales{__ldg(k_scales + pg * p.ks_sp + at.row * p.ks_st), __ldg(v_scales + pg * p.vs_sp + at.row * p.vs_st)};
         };
-        auto fetch_scale = [&](int j, int which, int32_t pg, int32_t row0, int i) {
-            const int64_t pi = __shfl_sync(0xffffffffu, pg, i);
-            const int32_t ri = __shfl_sync(0xffffffffu, row0, i) + row8;
-            const uint16_t *scale = which ? v_scales + pi * p.vs_sp + ri * p.vs_st : k_scales + pi * p.ks_sp + ri * p.ks_st;
-            return valid(j, i) ? (uint32_t)__ldg(scale) : 0u;
-        };
-        const uint32_t half = (uint32_t)(quarter >> 1) * kGroupHalf + (uint32_t)row8 * 128u, chunk = (uint32_t)(quarter & 1) * 4u;
+        // A lane's place in the group of eight keys: its half of the channels, and from which chunk of 16 bytes on.  Lanes of either half
+        // store their four chunks in another order, which keeps eight lanes out of one another's banks.
+        const uint32_t to = (uint32_t)(quarter >> 1) * kGroupHalf + (uint32_t)row8 * 128u, chunk = (uint32_t)(quarter & 1) * 4u, turned = (uint32_t)(quarter >> 1) * 2u;
+        const uint32_t from = sCodes + (uint32_t)(32 * w + row8) * q4::kHeadBytes + (uint32_t)quarter * 16u;
         bool ok = true;
-        // K (which = 0) or V of tile j into the ring, if it is free, in units of 1 / inverse; x takes the codes of the item after meanwhile.
-        uint4 x[4];
-        uint32_t scales[4];                                // K's in the lower half, V's in the upper one
-        auto decode = [&](int j, int which, float inverse, int32_t pg, int32_t row0) {
-            const int item = 2 * j + which;
-            const int slot = item % kSlots, fill = item / kSlots;
+        // K (which = 0) or V of tile j into the ring in units of 1 / inverse.
+        auto decode = [&](int j, int which, uint32_t scales, float inverse) {
+            const int item = 2 * j + which, slot = item % kSlots, fill = item / kSlots, code_slot = item % kCodeSlots;
+            ok = wait_all(&sh->code_full[code_slot], (item / kCodeSlots) & 1, sh, p);
+            if (!ok) return;
+            uint4 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[i].x), "=r"(x[i].y), "=r"(x[i].z), "=r"(x[i].w)
+                             : "r"(from + (uint32_t)code_slot * kCodeBytes + (uint32_t)i * 8u * q4::kHeadBytes) : "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->code_empty[code_slot]));
             if (fill > 0) ok = wait_all(&sh->kv_empty[slot], (fill - 1) & 1, sh, p);
             if (!ok) return;
-            const uint32_t dst = sRing + (uint32_t)slot * kTileBytes + (uint32_t)w * 4u * kGroupBytes + half;
+            const uint32_t dst = sRing + (uint32_t)slot * kTileBytes + (uint32_t)w * 4u * kGroupBytes + to;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const __half2 s2 = __float2half2_rn(__uint_as_float(which ? scales[i] & 0xffff0000u : scales[i] << 16) * inverse);
-                const uint32_t words[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-                x[i] = fetch_codes(j + which, which ^ 1, pg, row0, i);
+                const uint32_t bits = __shfl_sync(0xffffffffu, scales, 8 * i + row8);
+                const __half2 s2 = __float2half2_rn(__uint_as_float(bits << 16) * inverse);
+                const uint32_t words[4] = {turned ? x[i].z : x[i].x, turned ? x[i].w : x[i].y, turned ? x[i].x : x[i].z, turned ? x[i].y : x[i].w};
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (uint32_t c = 0; c < 4; ++c) {
                     uint32_t r[4];
                     q4::decode8_f16(words[c], s2, r);
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
-                                 ::"r"(dst + (uint32_t)i * kGroupBytes + (((chunk + c) ^ (uint32_t)row8) << 4)), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+                                 ::"r"(dst + (uint32_t)i * kGroupBytes + (((chunk + (c ^ turned)) ^ (uint32_t)row8) << 4)), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->kv_full[slot]));
         };
-        // The largest of the warp's scales (NaN left out).
-        auto most_of = [&](int which) {
-            float m = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) m = fmaxf(m, __uint_as_float(which ? scales[i] & 0xffff0000u : scales[i] << 16));
-#pragma unroll
-            for (int d = 4; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-            return m;
-        };
+        // The largest of the warp's scales (bf16 bits; NaN left out).
+        auto most_of = [&](uint32_t x) { return __uint_as_float(__reduce_max_sync(0xffffffffu, x > 0x7f80u ? 0u : x) << 16); };
         // m's power of two or the next, times 2^less: what brings scales up to m below 2^-less.
         auto unit_of = [](float m, int less) { return __uint_as_float((__float_as_uint(fmaxf(m, 0x1p-100f)) & 0x7f800000u) + ((uint32_t)(1 + less) << 23)); };
         auto inverse_of = [](float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); };
-        uint32_t ks[4], vs[4];
-        int32_t row0 = at.row, pg = checked(look_up(0));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { ks[i] = fetch_scale(0, 0, pg, row0, i); vs[i] = fetch_scale(0, 1, pg, row0, i); x[i] = fetch_codes(0, 0, pg, row0, i); }
+        Scales now = fetch(0, look_up(0));
         at = box_next(at, step);
-        int32_t raw_page = look_up(1);                     // of the next tile, as is `at`
+        Scales next = fetch(1, look_up(1));
+        at = box_next(at, step);
+        int32_t raw_page = look_up(2);                     // of the tile that `at` is at
         float v_unit = 0.f;
         for (int j = 0; j < n_max; ++j) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) scales[i] = ks[i] | vs[i] << 16;
+            const Scales after = fetch(j + 2, raw_page);
+            at = box_next(at, step);
+            raw_page = look_up(j + 3);
             // The four warps go on, and move V's unit, by common votes alone.
-            const float k_unit = unit_of(most_of(0), -13), v_most = most_of(1);
+            const float k_unit = unit_of(most_of(now.k), -13), v_most = most_of(now.v);
             if (group_any(0, v_most >= 0x1p13f * v_unit || !ok)) {
                 if (group_any(0, !ok)) break;
                 if (lane == 0) sh->v_most[w] = v_most;
@@ -333,14 +374,10 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const Params p, i
                 if (w == 0) sh->unit[j & 3].v = v_unit;
             }
             __syncwarp();
-            decode(j, 0, inverse_of(k_unit), pg, row0);
-            pg = checked(raw_page); row0 = at.row;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { ks[i] = fetch_scale(j + 1, 0, pg, row0, i); vs[i] = fetch_scale(j + 1, 1, pg, row0, i); }
-            at = box_next(at, step);
-            raw_page = look_up(j + 2);
-            if (ok && !(skip_last && n_max > 1 && j == n_max - 1))         // (test hook: the wait for it runs out)
-                decode(j, 1, inverse_of(v_unit), pg, row0);
+            decode(j, 0, now.k, inverse_of(k_unit));
+            if (ok) decode(j, 1, now.v, inverse_of(v_unit));
+            now = next;
+            next = after;
         }
         __syncwarp();
     } else if (warp > kMmaWarp1) {
@@ -384,29 +421,23 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const Params p, i
             const bool masked = k0 + kTile > see_all;
             int n_vis = see - k0;
             n_vis = n_vis < 0 ? 0 : (n_vis > kTile ? kTile : n_vis);
-            uint32_t r[64];
+            uint32_t r[kTile];
+            tmem_ld128(tS, r);
+            if (masked) {                                  // by choice, not by arithmetic: a masked score may be anything
+#pragma unroll
+                for (int c = 0; c < kTile; ++c) r[c] = c < n_vis ? r[c] : 0xff800000u;
+            }
             float top[4];
-            auto scores = [&](int half) {                  // the half's scores and their largest
-                tmem_ld64(tS + half * 64, r);
-                if (masked) {                              // by choice, not by arithmetic: a masked score may be anything
 #pragma unroll
-                    for (int c = 0; c < 64; ++c) r[c] = (half * 64 + c < n_vis) ? r[c] : 0xff800000u;
+            for (int q = 0; q < 4; ++q) {
+                float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+                for (int c = 32 * q; c < 32 * q + 32; c += 4) {
+                    m0 = fmax3(m0, __uint_as_float(r[c]), __uint_as_float(r[c + 1]));
+                    m1 = fmax3(m1, __uint_as_float(r[c + 2]), __uint_as_float(r[c + 3]));
                 }
-            };
-            auto largest = [&](int half) {
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float m0 = -INFINITY, m1 = -INFINITY;
-#pragma unroll
-                    for (int c = 0; c < 32; c += 4) {
-                        m0 = fmax3(m0, __uint_as_float(r[32 * q + c]), __uint_as_float(r[32 * q + c + 1]));
-                        m1 = fmax3(m1, __uint_as_float(r[32 * q + c + 2]), __uint_as_float(r[32 * q + c + 3]));
-                    }
-                    top[2 * half + q] = fmaxf(m0, m1) * factor[2 * half + q];
-                }
-            };
-            scores(1); largest(1);
-            scores(0); largest(0);
+                top[q] = fmaxf(m0, m1) * factor[q];
+            }
             const float m_new = fmax3(top[0], top[1], fmaxf(top[2], top[3]));
             float alpha = 1.f;
             bool grow = m_new > m_ref + (kLift + kGrow);
@@ -444,17 +475,16 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const Params p, i
             // p = 2^(s - m), rounded to fp16 as the product's operand; the row's sum takes p before it is rounded.
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                if (half) scores(1);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     const float f = factor[2 * half + (i >> 4)];
-                    const float2 x = __ffma2_rn(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), make_float2(f, f), nm2);
+                    const float2 x = __ffma2_rn(make_float2(__uint_as_float(r[64 * half + 2 * i]), __uint_as_float(r[64 * half + 2 * i + 1])), make_float2(f, f), nm2);
                     const float2 e = make_float2(ex2(x.x), ex2(x.y));
                     sum[i & 3] = __fadd2_rn(sum[i & 3], e);
-                    r[i] = pack_f16(e.x, e.y);
+                    r[64 * half + i] = pack_f16(e.x, e.y);
                 }
                 if (half && lane == 0) mbar_arrive(smem_u32(&sh->turn[st][quarter]));
-                tmem_st32(tS + half * 32, r);
+                tmem_st32(tS + half * 32, r + 64 * half);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -544,8 +574,10 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const Params p, i
 int launch_paged_many_q4(const paged::Params &p, int64_t items, cudaStream_t stream)
 {
     using namespace paged;
-    CUtensorMap tm_q;
-    if (!host_map::queries(&tm_q, p, kFewRows / p.g)) {
+    const int box = host_map::box_rows(p.c.page_size);
+    CUtensorMap tm_q, tm_k, tm_v;
+    if (!host_map::queries(&tm_q, p, kFewRows / p.g) || !host_map::pages_q4(&tm_k, p, p.k_pages, p.c.k_sp, p.c.k_st, p.c.k_sh, box, false) ||
+        !host_map::pages_q4(&tm_v, p, p.v_pages, p.c.v_sp, p.c.v_st, p.c.v_sh, box, false)) {
         set_error("%s: cuTensorMapEncodeTiled failed (driver too old, or strides/addresses not encodable)", p.who);
         return PEC_ERR_CUDA;
     }
@@ -562,7 +594,7 @@ int launch_paged_many_q4(const paged::Params &p, int64_t items, cudaStream_t str
     }
     if (items * p.Hkv > 0x7fffffff) { set_error("%s: grid too large", p.who); return PEC_ERR_UNSUPPORTED; }
     cudaError_t err = launch_dependent(many_q4::paged_many_q4_kernel, dim3((unsigned)(items * p.Hkv)), many_q4::kThreads, many_q4::kSmemBytes, stream, true,
-                                       tm_q, p, (int)test_skip_last_load());
+                                       tm_q, tm_k, tm_v, p, box, (int)test_skip_last_load());
     if (err == cudaSuccess) err = cudaGetLastError();
     if (err != cudaSuccess) { set_error("%s: launch failed: %s", p.who, cudaGetErrorString(err)); return PEC_ERR_CUDA; }
     return PEC_OK;
