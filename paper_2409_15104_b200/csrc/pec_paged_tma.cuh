@@ -5,6 +5,7 @@
 #include "pec_host.h"
 #include "pec_paged_plan.cuh"
 #include "pec_sm100.cuh"
+#include "pec_sm100_paged.cuh"
 
 namespace pec {
 namespace paged {

@@ -6,7 +6,7 @@
 //
 // Both are bound by memory, a head of bf16 being 256 bytes on one side and 66 on the other: 131072 rows of 8 + 8 heads are read in 116 us
 // where memory takes 103.  Appending has some 150 instructions and three dependent loads (the request, the page, the angles) for each four
-// heads and does not reach that: 7302 tokens with norm and rotation, and 9805 read, 38 us where memory takes 13 (all of it in fp64 took 49).
+// heads and does not reach that: 7302 tokens with norm and rotation, and 8901 read, 38 us where memory takes 13 (all of it in fp64 took 49).
 //
 // Which code is the nearest is decided exactly.  bf16 channels that are quantised as they are: x / s is either a border between two
 // codes or 2^-11 away from it (x has 8 bits, s 6, a border 3), while the product with the reciprocal is off by 2^-19: put on a grid of
@@ -477,10 +477,10 @@ kv_read_q4_kernel(const Read p, const int parts, const int per, const int tokens
 }
 
 // Few heads to a warp where there are too few warps to fill the SMs (a token's for each of 64 requests, 8 + 8 heads: 10.4 us with 4 and
-// 11.2 with 8, appending and reading 5152; five chunks of 1460 tokens: 41.6 and 38.3).
+// 11.2 with 8, appending and reading 2133; 7302 and 8901: 41.6 and 38.3).
 inline int heads_per_part(int64_t T, int64_t H) { return T * H < (int64_t)148 * 32 * 4 ? 4 : T * H < (int64_t)148 * 32 * 32 ? 8 : 32; }
 // Rows of a reading warp in turn: more of them in flight, where that leaves warps enough (131072 rows of 8 + 8 heads: 185 us one by one,
-// 126 by twos, 114 by fours; 6300 rows 13.8, 14.7 and 14.6).
+// 126 by twos, 114 by fours; 4629 rows 13.8, 14.7 and 14.6).
 inline int tokens_per_warp(int64_t T, int parts) { return T * 2 * parts < (int64_t)148 * 32 * 4 ? 1 : T * 2 * parts < (int64_t)148 * 32 * 16 ? 2 : 4; }
 
 }  // namespace q4
