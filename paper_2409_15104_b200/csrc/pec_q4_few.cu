@@ -21,6 +21,10 @@
 // A tile has 750 cycles at the rate of HBM, and every warp of the chain (where it lies, its copies, products, softmax, products) spends
 // most of its time on hand-overs.  So two CTAs per SM, and a step takes 256 keys where shared memory has room for it (up to 8 rows).
 //
+// Measured: 64 requests of 2400 keys, 32 heads on 8: 47 us (3.4 TB/s); three of 102000, 64 on 8: 72 us (4.5 TB/s, 5.5 without the 12 us of
+// start and combine); one of 4100: 14 us; 16 requests of 4 tokens (16 rows) and 9000 keys: 74 us, 2000 cycles a tile, which the
+// softmax warps take with 16 rows a key and four parts of each probability.
+//
 // Warp roles:
 //   warps 0-3  softmax and epilogue
 //   warp 4     MMA issuer (one thread)

@@ -6,7 +6,7 @@
 //   warps 8, 10     MMA issuers of stage 0 and 1       warp 9  loader of Q and codes       warp 11  idle
 //   warps 12-15     K and V: codes decoded into a ring of four tiles of 128 keys, 32 keys each
 // The codes come ahead of their decoding, in a ring of their own: with 16 bytes a lane in flight instead few rows waited for memory
-// (32 requests of 8 tokens and 4000 keys, 32 heads on 8: 206 us, now 167; 2048 tokens on 30720 1323 us, now 1261).
+// (32 requests of 4 tokens and 4000 keys, 32 heads on 8: 206 us, now 169; 2048 tokens on 30720 1323 us, now 1261).
 // The tiles are decoded to fp16, to which the hardware converts codes (two an instruction).  fp16 has no range to hold scales, so what
 // is multiplied is in units, powers of two that the other side makes up for:
 //     K   of one for each 32 keys of a tile, such that scales are below 2^13 of it: a factor of those scores
@@ -302,10 +302,10 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         auto look_up = [&](int j) { return valid(j) ? __ldg(p.c.table + b * p.c.table_stride + at.nth) : 0; };
         const uint16_t *k_scales = p.k_scales + kvh * p.ks_sh, *v_scales = p.v_scales + kvh * p.vs_sh;
         struct Scales { uint32_t k, v; };                  // (keys past the end: 0, so that nothing there meets a product)
-        auto fetch = [&](int j, int32_t pg) {
+        auto fetch = [&](int j, int32_t pg, int32_t row) {
             if (!valid(j)) return Scales{0u, 0u};
             if (pg < 0 || pg >= p.c.num_pages) { raise_status(p.status, PEC_ERR_BAD_INDEX); pg = 0; }
-            return Scales{__ldg(k_scales + pg * p.ks_sp + at.row * p.ks_st), __ldg(v_scales + pg * p.vs_sp + at.row * p.vs_st)};
+            return Scales{__ldg(k_scales + pg * p.ks_sp + row * p.ks_st), __ldg(v_scales + pg * p.vs_sp + row * p.vs_st)};
         };
         // A lane's place in the group of eight keys: its half of the channels, and from which chunk of 16 bytes on.  Lanes of either half
         // store their four chunks in another order, which keeps eight lanes out of one another's banks.
@@ -349,14 +349,15 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         // m's power of two or the next, times 2^less: what brings scales up to m below 2^-less.
         auto unit_of = [](float m, int less) { return __uint_as_float((__float_as_uint(fmaxf(m, 0x1p-100f)) & 0x7f800000u) + ((uint32_t)(1 + less) << 23)); };
         auto inverse_of = [](float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); };
-        Scales now = fetch(0, look_up(0));
+        const int32_t page0 = look_up(0), row0 = at.row;   // (the first three at once)
         at = box_next(at, step);
-        Scales next = fetch(1, look_up(1));
+        const int32_t page1 = look_up(1), row1 = at.row;
         at = box_next(at, step);
         int32_t raw_page = look_up(2);                     // of the tile that `at` is at
+        Scales now = fetch(0, page0, row0), next = fetch(1, page1, row1);
         float v_unit = 0.f;
         for (int j = 0; j < n_max; ++j) {
-            const Scales after = fetch(j + 2, raw_page);
+            const Scales after = fetch(j + 2, raw_page, at.row);
             at = box_next(at, step);
             raw_page = look_up(j + 3);
             // The four warps go on, and move V's unit, by common votes alone.
