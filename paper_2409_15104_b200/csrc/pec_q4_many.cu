@@ -19,6 +19,8 @@
 // which the other stage has the unit of 2^x to itself: the stages take turns (1195 us, without that 1263) and hand P over by halves.  A
 // row's 128 scores are in registers from its maximum on (1121 us; read a second time, by halves, 1195), which leaves the other warps 64.
 // With the score buffer of the bf16 cache's kernel, one that both stages use in turns, and tiles decoded to bf16 it was 1493 us.
+// A block that has rows for one stage only gives them to both, even tiles to one and odd tiles to the other, and merges what they have
+// added up at its end (32 requests of 8 tokens and 4000 keys 169 -> 145 us, one of 32 tokens and 60000 119 -> 105).
 // TMEM columns: S_s [128 s, +128), P_s its first 64; O_s [256 + 128 s, +128).
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -49,6 +51,7 @@ struct Geom {
     int32_t rows[2];                                       // valid packed rows per stage
     int32_t pos0[2];                                       // position of each stage's first token
     int32_t n[2], n_max;                                   // key tiles of each stage (a prefix of the CTA's walk)
+    int32_t shared;                                        // both stages have the first one's rows: even tiles and odd ones
     int32_t slices;
     int64_t slot;                                          // partial slot, where slices > 1
 };
@@ -59,9 +62,12 @@ struct Shared {
     uint64_t s_full[2], p_ready[2][2], pv_done[2];         // [stage], one phase per key tile; P by halves
     uint64_t drained[2];
     uint64_t turn[2][4];                                   // [stage][warp]: 2^x of a tile done
+    uint64_t merged;                                       // (shared) the second stage's sums are complete
     uint64_t q_ready[2];                                   // [stage]: Q is in fp16
     struct { float4 k; float v; } unit[4];                 // of every fourth tile: K's for each 32 keys, V's
     float v_most[4];
+    float v_units[4];
+    float2 sums[kTile];                                    // (shared) of the second stage's rows: reference maximum, sum
     Geom g;
     uint32_t tmem_base;
     volatile int abort_flag;
@@ -154,6 +160,8 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 g.n[st] = (nt > 0 && end > it.key_lo) ? (end - it.key_lo + kTile - 1) / kTile : 0;
             }
             g.n_max = g.n[0] > g.n[1] ? g.n[0] : g.n[1];
+            g.shared = g.rows[1] == 0 && g.n[0] > 1;
+            if (g.shared) { g.rows[1] = g.rows[0]; g.pos0[1] = g.pos0[0]; g.n[1] = g.n[0]; }
             if (g.slices > 1 && g.slot >= p.many_cap) found = false;       // cannot happen (see the plan); never write past the scratch
         }
         g.found = found;
@@ -172,8 +180,9 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 for (int st = 0; st < 2; ++st) {
                     const uint32_t bar = smem_u32(&sh->bar_q[st]), dst = sQ + st * kTileBytes;
                     mbar_arrive_expect_tx(bar, (uint32_t)srows * 256u);
-                    tma_load_4d(dst, &tm_q, bar, 0, 0, kvh, g.tok_row + st * tps);
-                    tma_load_4d(dst + kHalfTileBytes, &tm_q, bar, 64, 0, kvh, g.tok_row + st * tps);
+                    const int32_t row = g.tok_row + (g.shared ? 0 : st * tps);
+                    tma_load_4d(dst, &tm_q, bar, 0, 0, kvh, row);
+                    tma_load_4d(dst + kHalfTileBytes, &tm_q, bar, 64, 0, kvh, row);
                 }
             }
             load_codes(0, 0, g.key_lo, g.kv);
@@ -186,6 +195,7 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             mbar_init(smem_u32(&sh->s_full[st]), 1);
             mbar_init(smem_u32(&sh->pv_done[st]), 1);
             mbar_init(smem_u32(&sh->drained[st]), 1);
+            if (st == 0) mbar_init(smem_u32(&sh->merged), 4);
             for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&sh->turn[st][i]), 1);
             mbar_init(smem_u32(&sh->q_ready[st]), 4);      // one arrival per softmax warp
         }
@@ -250,39 +260,42 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             for (int ks = 0; ks < 8; ++ks)
                 a_desc[ks] = smem_desc_sw128(sQ + st * kTileBytes + (uint32_t)(ks >> 2) * kHalfTileBytes + (uint32_t)(ks & 3) * 32u, 16, 1024);
             const uint64_t k_ring = smem_desc_sw128(sRing, 16, kGroupBytes), v_ring = smem_desc_sw128(sRing, kGroupHalf, kGroupBytes);
-            const int n_st = sh->g.n[st];
+            const int n_st = sh->g.n[st], shared = sh->g.shared;
             auto issue_qk = [&](int j) {
                 const uint64_t k0 = k_ring + (uint32_t)((((2 * j) % kSlots) * kTileBytes) >> 4);
                 if (leader) mma_ss_k128_commit<(kGroupHalf >> 4)>(tS, a_desc, k0, idesc_qk, smem_u32(&sh->s_full[st]));
             };
-            auto issue_pv = [&](int j, int half) {
+            auto issue_pv = [&](int j, int m, int half) {
                 const uint64_t v0 = v_ring + (uint32_t)((((2 * j + 1) % kSlots) * kTileBytes + half * 8 * kGroupBytes) >> 4);
                 if (leader) {
-                    mma_pv_k64(tO, tS + 32 * half, v0, idesc_pv, j > 0 || half ? 1u : 0u);
+                    mma_pv_k64(tO, tS + 32 * half, v0, idesc_pv, m > 0 || half ? 1u : 0u);
                     if (half) tc_commit(smem_u32(&sh->pv_done[st]));
                 }
             };
             bool ok = wait_all(&sh->q_ready[st], 0, sh, p);
+            int m = 0;                                             // this stage's tiles so far
             for (int j = 0; j < n_max && ok; ++j) {
+                const bool mine = shared ? (j & 1) == st : j < n_st;
                 ok = kv_wait(2 * j);                               // K(j)
                 if (!ok) break;
-                if (j < n_st) {
-                    // P(j - 1) lies where S(j) goes.  (Two products into different accumulators need not run in the order of their issue.)
-                    if (j > 0) ok = wait_all(&sh->pv_done[st], (j - 1) & 1, sh, p);
+                if (mine) {
+                    // P(m - 1) lies where S(m) goes.  (Two products into different accumulators need not run in the order of their issue.)
+                    if (m > 0) ok = wait_all(&sh->pv_done[st], (m - 1) & 1, sh, p);
                     if (!ok) break;
                     issue_qk(j);
                 }
                 kv_release(2 * j);
                 ok = kv_wait(2 * j + 1);                           // V(j)
                 if (!ok) break;
-                if (j < n_st) {
+                if (mine) {
                     for (int half = 0; half < 2 && ok; ++half) {
-                        ok = wait_all(&sh->p_ready[st][half], j & 1, sh, p);
+                        ok = wait_all(&sh->p_ready[st][half], m & 1, sh, p);
                         if (!ok) break;
                         tc_fence_after();
-                        issue_pv(j, half);
+                        issue_pv(j, m, half);
                     }
                     if (!ok) break;
+                    ++m;
                 }
                 kv_release(2 * j + 1);
             }
@@ -391,14 +404,15 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         const uint32_t tS = tmem + lane_base + kColS + st * kTile;
         const uint32_t tO = tmem + lane_base + kColO + st * kTile;
-        const int n_t = sh->g.n[st], rows_valid = sh->g.rows[st] - quarter * 32;   // of this warp's 32 rows
+        const int shared = sh->g.shared, n_all = sh->g.n[st];
+        const int n_t = shared ? (n_all + 1 - st) / 2 : n_all, rows_valid = sh->g.rows[st] - quarter * 32;   // of this warp's 32 rows
         const bool works = rows_valid > 0;                 // a warp without rows only gives its share of the score buffer back
         const int32_t tok = row / p.g, head = row - tok * p.g;
         const int32_t pos0 = sh->g.pos0[st], my_pos = pos0 + tok, key_hi = sh->g.key_hi;
         const int32_t see_all = (p.causal && pos0 + 1 < key_hi) ? pos0 + 1 : key_hi;       // keys below it are visible to every row
         const int32_t see = (p.causal && my_pos + 1 < key_hi) ? my_pos + 1 : key_hi;       // ... to this row
-        int32_t k0 = sh->g.key_lo;
-        const int n_other = sh->g.n[st ^ 1];
+        int32_t k0 = sh->g.key_lo + (shared ? st * kTile : 0);
+        const int n_other = shared ? (n_all + st) / 2 : sh->g.n[st ^ 1];       // of the other stage
         const bool paired = sh->g.rows[st ^ 1] > quarter * 32;
 
         float m_ref = -INFINITY, l_run = 0.f;              // log2 units; a probability of 1 is 2^kLift at least
@@ -410,12 +424,13 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->q_ready[st]));
         }
-        for (int j = 0; j < n_t && ok && works; ++j, k0 += kTile) {
+        for (int j = 0; j < n_t && ok && works; ++j, k0 += shared ? 2 * kTile : kTile) {      // this stage's tiles
             ok = wait_all(&sh->s_full[st], j & 1, sh, p);  // (PV(j - 1) is done as well)
             if (!ok) break;
             tc_fence_after();
-            const float4 k_unit = sh->unit[j & 3].k;
-            const float v_now = sh->unit[j & 3].v;
+            const int tile = shared ? 2 * j + st : j;
+            const float4 k_unit = sh->unit[tile & 3].k;
+            const float v_now = sh->unit[tile & 3].v;
             // (never 0, by which a masked score would be NaN)
             const float factor[4] = {fmaxf(row_scale * k_unit.x, 0x1p-126f), fmaxf(row_scale * k_unit.y, 0x1p-126f),
                                      fmaxf(row_scale * k_unit.z, 0x1p-126f), fmaxf(row_scale * k_unit.w, 0x1p-126f)};
@@ -502,7 +517,24 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         // A stage without keys never waited for its Q tile: the load must have landed before the tile is reused.  The other
         // stage's products do not read it.
         if (ok && n_t == 0 && n_max > 0) ok = wait_all(&sh->bar_q[st], 0, sh, p);
-        if (ok && works) {
+        // Stages that share rows: the first one writes them, with what the second has added up.
+        float mine = v_unit, others = 0.f;                 // what either stage's O counts
+        if (shared && st == 1) {
+            sh->sums[row] = make_float2(m_ref, l_run);
+            sh->v_units[row >> 5] = v_unit;
+            __syncwarp();
+            if (ok && lane == 0) mbar_arrive(smem_u32(&sh->merged));
+        }
+        if (shared && st == 0 && ok) {
+            ok = wait_all(&sh->merged, 0, sh, p) && wait_all(&sh->pv_done[1], (n_other - 1) & 1, sh, p);
+            const float2 o = sh->sums[row];
+            const float top = fmaxf(m_ref, o.x), base = top == -INFINITY ? 0.f : top, a = ex2(m_ref - base), b = ex2(o.x - base);
+            mine *= a;
+            others = sh->v_units[row >> 5] * b;
+            l_run = l_run * a + o.y * b;
+            m_ref = top;
+        }
+        if (ok && works && !(shared && st == 1)) {
             tc_fence_after();
             const bool empty = (l_run == 0.f);
             const float inv = empty ? 0.f : 1.f / l_run;
@@ -529,7 +561,12 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     }
                     float f[64];
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) f[i] = empty ? 0.f : __uint_as_float(r[i]) * inv * v_unit;
+                    for (int i = 0; i < 64; ++i) f[i] = empty ? 0.f : __uint_as_float(r[i]) * inv * mine;
+                    if (shared) {
+                        tmem_ld64(tmem + lane_base + kColO + kTile + (bf16_out ? half : pass) * 64, r);
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) f[i] = empty ? 0.f : fmaf(__uint_as_float(r[i]) * inv, others, f[i]);
+                    }
                     if (bf16_out) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
