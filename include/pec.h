@@ -663,9 +663,9 @@ int pec_kv_read_q4(const pec_kv_read_q4_args *args, void *cuda_stream);
  * pec_paged_attn over such a cache: the same rows, masks, outputs and kinds of batches, with the numbers that the cache holds as
  * keys and values.  dtype: that of q.  PEC_BF16 runs the tensor cores, PEC_F32 an fp32 FMA kernel with fp32 output.
  * PEC_BF16: products are exact, sums fp32.  Requests of at most 16 packed rows (n * Hq / Hkv) with Hq / Hkv <= 16 hold probabilities
- * times values' scales to 2^-12 of themselves, and below 2^-24 of the row's largest probability times the largest scale to 2^-36 of
- * that; of q, channels below 2^-13 of the row's largest magnitude to 2^-22 of it.  The others hold probabilities to 2^-12 of
- * themselves, below 2^-24 of the row's largest to 2^-35 of it, and values to 2^-34 of the largest scale that the request has had so far.
+ * times values' scales to 2^-11 of themselves (half a step of fp16), and below 2^-23 of the row's largest probability times the largest
+ * scale to 2^-34 of that; of q, channels below 2^-13 of the row's largest magnitude to 2^-22 of it.  The others hold probabilities to
+ * 2^-11 of themselves, below 2^-24 of the row's largest to 2^-35 of it, and values to 2^-34 of the largest scale that came so far.
  * Keys and values past a request's end are never used.  A value of a request that is not finite may spoil the rows of the same request
  * that do not see it yet, never those of another request.  A row with a NaN score, or one of +inf, gets NaN.
  * max_q_len, workspace, status, a call that finds PEC_ERR_TIMEOUT in *status: as there (the kernel for few rows takes 16, not 128).

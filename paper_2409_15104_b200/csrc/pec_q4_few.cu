@@ -10,7 +10,7 @@
 // up in fp32:
 //     Q   two parts of e4m3 of the row divided by a power of two (its largest channel in [2^7, 2^8)): 4 + 4 significant bits are a
 //         bf16's eight; channels under 2^-13 of the row's largest are held to 2^-22 of it
-//     P'  four parts of e5m2, to 2^-12 of itself down to 2^-24 of the largest and to 2^-36 of that below, so that a bf16 result errs by
+//     P'  four parts of e5m2: rounded to fp16, 2^-11 of itself down to 2^-24 v_ref and 2^-35 v_ref below, so that a bf16 result errs by
 //         its own rounding alone.  (Parts of e4m3, three for as many bits, end at 2^-21: a hundred thousand keys behind one that takes
 //         most of the weight, which long prompts have, would be held to two bits.)
 // Products of such numbers are exact and their sums are kept in fp32.

@@ -210,17 +210,19 @@ def test_heads_that_are_not_finite_are_read_as_nan(pec):
 
 # ------------------------------------------------------------------------------------------ attention
 def check(o, lse, want, dtype, cache, kv, most_rows, what):
-    """paged_reference.check_attend with the rounding of the probabilities here.  fp32 q: none.  bf16 q: requests of at most 16
-    packed rows hold the products of a probability and a value's scale to 2^-12 of themselves and, below that, to 2^-36 of twice
-    the largest scale, which a code of at most 6 makes 2^-35 * 6 * that scale for each key (the probabilities sum to 1 at
-    least); the others, by most_rows > 16, round probabilities to bf16."""
+    """paged_reference.check_attend with the rounding of the probabilities here.  fp32 q: none.  bf16 q: fp16 parts, off by half a step,
+    2^-11 of themselves, and in its subnormals (steps of 2^-24) by 2^-25.
+    At most 16 packed rows: p sv 2^10 / v_ref, v_ref a power of two of at most twice the largest scale s, the row's largest p 1 or more:
+    2^-25 is 2^-35 v_ref <= 2^-34 s for each key, times a code of at most 6.
+    More: p times 2^10 or more, so 2^-35 of the largest p, times 6 s, for each key; and values in units in which s is 2^9 or more, so
+    2^-34 s once (the p sum to 1): 2^-35 * 6 s * keys + 2^-34 s <= 2^-34 * 6 s * keys, the same."""
     o64, lse64, A, B = want
     error = None
     if dtype == BF16:
-        error = 2.0 ** -12 if most_rows <= 16 else ref.HALF[BF16]
+        error = 2.0 ** -11
         scales = cache[3].float()
-        A = A + max(kv) * 2.0 ** -35 * 6 * float(scales[torch.isfinite(scales)].max() if torch.isfinite(scales).any() else 0.0) / error
-    ref.check_attend(o, lse, (o64, lse64, A, B), dtype, what, error)
+        A = A + max(kv) * 2.0 ** -34 * 6 * float(scales[torch.isfinite(scales)].max() if torch.isfinite(scales).any() else 0.0) / error
+    ref.check_attend(o, lse, (o64, lse64, A, B), dtype, f"{what}, {most_rows} rows", error)
 
 
 def attend(pec, seed, n, kv, hq, hkv, page, dtype, *, head_major=False, causal=True, out_dtype=None, pad=0, fused=False, known=True,
