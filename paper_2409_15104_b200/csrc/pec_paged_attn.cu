@@ -302,6 +302,7 @@ paged_f32_kernel(const Params p)
         const int32_t rr = min(r, rows - 1), t = (row0 + rr) / p.g, h = kvh * p.g + (row0 + rr) % p.g;
         copy16(sQ + r * kLd + c, static_cast<const float *>(p.q) + (int64_t)(it.r.start + t) * p.q_st + (int64_t)h * p.q_sh + c, r < rows);
     }
+    copy_commit();                           // a group of its own: waits cover committed copies only
 
     float m_run[4], l_run[4];
     float2 acc[4][4];                        // channels 4 tx .. + 3, 64 + 4 tx .. + 3
@@ -361,7 +362,7 @@ paged_f32_kernel(const Params p)
                 copy16(sV + r * kHeadDim + c4, src, ok);
             }
             copy_commit();
-            copy_wait<1>();                      // the keys (and Q)
+            copy_wait<1>();                      // Q and the keys; the values may be under way
             __syncthreads();
         }
 
@@ -416,7 +417,7 @@ paged_f32_kernel(const Params p)
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[i][c] = __fmul2_rn(acc[i][c], make_float2(alpha, alpha));
         }
-        copy_wait<0>();                      // the values
+        if constexpr (!kQ4) copy_wait<0>();  // the values
         __syncthreads();
 #pragma unroll 2
         for (int j = 0; j < kBN; j += 4) {
