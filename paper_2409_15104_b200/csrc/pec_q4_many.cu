@@ -514,9 +514,9 @@ paged_many_q4_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         // quarter of the stage's Q tile (no longer read: the stage's last product is done) and writes them out two rows per
         // instruction, 256 contiguous bytes each; where a row goes is fetched by shuffle from the lane that owns it.
         if (ok && works && n_t > 0) ok = wait_all(&sh->pv_done[st], (n_t - 1) & 1, sh, p);
-        // A stage without keys never waited for its Q tile: the load must have landed before the tile is reused.  The other
-        // stage's products do not read it.
-        if (ok && n_t == 0 && n_max > 0) ok = wait_all(&sh->bar_q[st], 0, sh, p);
+        // A stage without keys has no product to wait for: its four warps must be done with their rows of Q, which lie in one another's
+        // quarters, before any of them reuses the tile.  The other stage's products do not read it.
+        if (ok && n_t == 0 && n_max > 0) ok = wait_all(&sh->q_ready[st], 0, sh, p);
         // Stages that share rows: the first one writes them, with what the second has added up.
         float mine = v_unit, others = 0.f;                 // what either stage's O counts
         if (shared && st == 1) {

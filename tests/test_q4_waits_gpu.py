@@ -5,7 +5,7 @@ import torch
 
 import paged_reference as ref
 import q4_reference as q4
-from test_q4_gpu import BF16, DEV, F32, check, dev
+from test_q4_gpu import BF16, DEV, F32, attend, check, dev
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +67,30 @@ def test_calls_of_both_types_at_once(pec):
         for (_, _, want), have in zip(cases, got):
             assert torch.equal(want[0], have[0]) and torch.equal(want[1], have[1])
     pec.check_status()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n,kv,hq,hkv,page", [([200], [100], 4, 2, 16), ([300], [70], 8, 2, 24), ([256, 3, 400], [100, 50, 270], 1, 1, 8), ([700], [596], 16, 1, 64),
+                                              ([200] * 30, [100] * 30, 16, 8, 16)])
+def test_leading_rows_that_see_nothing(pec, n, kv, hq, hkv, page, causal):
+    """Requests with more new tokens than cached ones: whole stages without keys beside stages with some, many times over."""
+    for seed in range(4):
+        attend(pec, 200 + seed, n, kv, hq, hkv, page, BF16, causal=causal, out_dtype=F32 if seed % 2 else None, what=f"{n[:3]} of {kv[:3]}")
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("prefix", [128, 1152, 3968])
+def test_leading_rows_of_a_slice_that_see_nothing_of_it(pec, prefix, bad):
+    """Keys cut into slices of which a block's first stage sees none and its second one some; a query that is not finite in the first
+    stage's rows stays in its row."""
+    n, kv, bad_row = 256, prefix + 256, 70
+    cache = q4.make_cache(51, [kv], 16, 1, DEV)
+    q = torch.randn((n, 1, 128), generator=torch.Generator().manual_seed(52)).to(BF16).to(DEV)
+    want = q4.attend(q, cache, [0, n], [kv])
+    want[1][bad_row, 0] = want[0][bad_row, 0] = float("nan")       # (rows that check passes over)
+    q[bad_row, 0, 7] = bad
+    for _ in range(8):
+        o, lse = pec.pec_paged_attn_q4(q, *cache, dev([0, n]), dev([kv]), max_q_len=n)
+        pec.check_status()
+        assert torch.isnan(o[bad_row]).all() and torch.isnan(lse[bad_row]).all()
+        check(o, lse, want, BF16, cache, [kv], n, f"beside a query of {bad}, prefix {prefix}")
