@@ -662,10 +662,13 @@ int pec_kv_read_q4(const pec_kv_read_q4_args *args, void *cuda_stream);
 /*
  * pec_paged_attn over such a cache: the same rows, masks, outputs and kinds of batches, with the numbers that the cache holds as
  * keys and values.  dtype: that of q.  PEC_BF16 runs the tensor cores, PEC_F32 an fp32 FMA kernel with fp32 output.
- * PEC_BF16: products are exact, sums fp32.  Requests of at most 16 packed rows (n * Hq / Hkv) with Hq / Hkv <= 16 hold probabilities
- * times values' scales to 2^-11 of themselves (half a step of fp16), and below 2^-23 of the row's largest probability times the largest
- * scale to 2^-34 of that; of q, channels below 2^-13 of the row's largest magnitude to 2^-22 of it.  The others hold probabilities to
- * 2^-11 of themselves, below 2^-24 of the row's largest to 2^-35 of it, and values to 2^-34 of the largest scale that came so far.
+ * PEC_BF16: products are exact, sums fp32.  What the products take is exact but for this.  Requests of at most 16 packed rows
+ * (n * Hq / Hkv) with Hq / Hkv <= 16 hold probabilities times values' scales to 2^-11 of themselves (half a step of fp16), and below 2^-23
+ * of the row's largest probability times the largest scale to 2^-34 of that; channels of q below 2^-13 of the row's largest magnitude to
+ * 2^-21 of it (of 2^-100, where that is larger).  The others hold probabilities to 2^-11 of themselves, below 2^-24 of the row's largest
+ * to 2^-35 of it; values whose scale is below 2^-27 of the largest that came so far to 6 * 2^-34 of that; keys whose scale is below 2^-30
+ * of the largest among the 32 from a multiple of 32 on to 6 * 2^-37 of it; channels of q below 2^-31 of the row's largest magnitude to 2^-39
+ * of it (of 2^-93, where that is larger).
  * Keys and values past a request's end are never used.  A value of a request that is not finite may spoil the rows of the same request
  * that do not see it yet, never those of another request.  A row with a NaN score, or one of +inf, gets NaN.
  * max_q_len, workspace, status, a call that finds PEC_ERR_TIMEOUT in *status: as there (the kernel for few rows takes 16, not 128).

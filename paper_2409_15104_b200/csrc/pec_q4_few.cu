@@ -9,7 +9,7 @@
 // The operands that are not codes come in parts, each the rest of the one before scaled up, in columns of their own that are added
 // up in fp32:
 //     Q   two parts of e4m3 of the row divided by a power of two (its largest channel in [2^7, 2^8)): 4 + 4 significant bits are a
-//         bf16's eight; channels under 2^-13 of the row's largest are held to 2^-22 of it
+//         bf16's eight; channels under 2^-13 of the row's largest are held to 2^-21 of it (half of e4m3's last step, 2^-9 / 16)
 //     P'  four parts of e5m2: rounded to fp16, 2^-11 of itself down to 2^-24 v_ref and 2^-35 v_ref below, so that a bf16 result errs by
 //         its own rounding alone.  (Parts of e4m3, three for as many bits, end at 2^-21: a hundred thousand keys behind one that takes
 //         most of the weight, which long prompts have, would be held to two bits.)

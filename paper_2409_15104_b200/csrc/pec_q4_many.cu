@@ -12,8 +12,9 @@
 //     K   of one for each 32 keys of a tile, such that scales are below 2^13 of it: a factor of those scores
 //     V   of one for all, which moves when a tile's scales pass 2^13 of it: a factor of O
 //     Q   of one for each row (its largest channel in [2^14, 2^15)), in place, before the first product
-// A code times its scale has eight bits at most and is exact down to 2^-29 (V: 2^-26) of the largest scale, as is a channel of Q to 2^-31
-// of its row's largest.  Probabilities are rounded to fp16, to 2^-11 of themselves: the largest of a row is held in [2^10, 2^15], and
+// A code times its scale has eight bits at most and is exact down to scales of 2^-30 (V: 2^-27) of the largest; below, the scale is a
+// multiple of 2^-24 units, off by 2^-25, and the product by six times that at most: 6 * 2^-37 (V: 6 * 2^-34) of the largest scale.  A channel
+// of Q is exact to 2^-31 of its row's largest, and off by 2^-39 of it below.  Probabilities are rounded to fp16, to 2^-11 of themselves: the largest of a row is held in [2^10, 2^15], and
 // those below 2^-24 of it, in fp16's subnormals, are off by at most 2^-35 of it.
 // Scores stay in tensor memory until probabilities take their place; S(j + 1) of a stage begins when PV(j) is done, some 2000 cycles in
 // which the other stage has the unit of 2^x to itself: the stages take turns (1195 us, without that 1263) and hand P over by halves.  A
