@@ -476,12 +476,35 @@ kv_read_q4_kernel(const Read p, const int parts, const int per, const int tokens
     }
 }
 
-// Few heads to a warp where there are too few warps to fill the SMs (a token's for each of 64 requests, 8 + 8 heads: 10.4 us with 4 and
-// 11.2 with 8, appending and reading 2133; 7302 and 8901: 41.6 and 38.3).
-inline int heads_per_part(int64_t T, int64_t H) { return T * H < (int64_t)148 * 32 * 4 ? 4 : T * H < (int64_t)148 * 32 * 32 ? 8 : 32; }
-// Rows of a reading warp in turn: more of them in flight, where that leaves warps enough (131072 rows of 8 + 8 heads: 185 us one by one,
-// 126 by twos, 114 by fours; 4629 rows 13.8, 14.7 and 14.6).
-inline int tokens_per_warp(int64_t T, int parts) { return T * 2 * parts < (int64_t)148 * 32 * 4 ? 1 : T * 2 * parts < (int64_t)148 * 32 * 16 ? 2 : 4; }
+// Heads of a warp.  (T new tokens of H key heads; limits by T * 2 H, 148 SMs with 32 warps.)
+// Appending.  Four where there are too few warps to fill the SMs, and where a token has no more: with norm and rotation, one request, 1024
+// tokens of 8 heads 7.8 us with 4 and 7.9 with 8, 2048 10.8 and 9.2; 16384 of 4 heads 36.8, and 43.9 in the form for more (two in flight).
+// 32, which share a token's angles, where there are warps enough even so: 1024 of 16 heads 9.4 with 8 and 9.8 with 32, 2048 13.5 and 11.9;
+// 1024 of 32 heads 13.4 and 13.7, 2048 25.3 and 19.8; 512 of 64 heads 13.2 and 14.3, 1024 25.3 and 19.9.
+inline int append_heads(int64_t T, int64_t H)
+{
+    const int64_t all = T * 2 * H;
+    return H <= 4 || all < (int64_t)148 * 32 * 4 ? 4 : all < (int64_t)148 * 32 * 12 ? 8 : 32;
+}
+// Reading (head-major and token-major pages alike, but where two figures are given).  To bf16: 256 tokens of 8 heads 3.0 us with 4 and 2.9 with 8,
+// 1024 4.0 and 3.4, 8192 13.7 and 10.9; 16384 of 16 heads 32.0 with 8 and 31.7 with 32, 65536 115.8 and 111.1; 8192 of 32 heads 31.9 and 33.2,
+// 16384 59.4 and 59.3; 16384 of 64 heads 116.0 and 111.6.  To fp32, whose rows are twice as long: 8192 of 8 heads 21.0 / 19.3 with 8 and
+// 19.5 / 20.3 with 4, 16384 36.0 / 32.6 and 31.0 / 30.9, 65536 120.0 / 112.7 and 105.8 / 104.0.
+inline int read_heads(int64_t T, int64_t H, bool f32)
+{
+    const int64_t all = T * 2 * H;
+    return f32 ? (all < (int64_t)148 * 32 * 40 ? 8 : 4) : all < (int64_t)148 * 32 * 256 ? 8 : 32;
+}
+// Rows of a reading warp in turn: more of them in flight, where that leaves warps enough.  One by one, by twos, by fours: 2048 rows of 8 + 8
+// heads 4.4, 4.9 and 5.1 us, 4096 8.2, 6.7 and 7.3, 8192 14.5, 11.6 and 10.9, 65536 93.5, 64.5 and 59.7; of 1 + 1 heads 2048 3.8, 4.1 and 4.5,
+// 4096 6.1, 5.1 and 5.0, 8192 10.2, 7.7 and 6.6.  With 32 heads a warp 16384 of 64 + 64 heads 136, 112 and 118; with eight of fp32, 2048 of
+// 8 + 8 heads 6.8, 7.5 and 7.7, 8192 19.3, 23.2 and 21.8.
+inline int tokens_per_warp(int64_t T, int parts, int64_t heads, bool f32)
+{
+    const int64_t warps = T * 2 * parts;
+    if (warps < (int64_t)148 * 40 || (f32 && heads > 4)) return 1;
+    return warps < (int64_t)148 * 80 || heads > 8 ? 2 : 4;
+}
 
 }  // namespace q4
 
@@ -554,7 +577,7 @@ extern "C" int pec_kv_append_q4(const pec_kv_append_q4_args *a, void *cuda_strea
     if (T == 0) return PEC_OK;
     p.k = a->k; p.v = a->v; p.k_st = s[0]; p.k_sh = s[1]; p.v_st = s[2]; p.v_sh = s[3];
     p.kw = a->k_weight; p.norm = a->norm; p.eps = a->eps; p.table = a->rope_table; p.n_pos = a->n_pos; p.status = a->status;
-    const int per = q4::heads_per_part(T, 2 * (int64_t)p.q.Hkv), parts = (p.q.Hkv + per - 1) / per;
+    const int per = q4::append_heads(T, p.q.Hkv), parts = (p.q.Hkv + per - 1) / per;
     const dim3 grid((unsigned)((T + q4::kWarps - 1) / q4::kWarps), (unsigned)(2 * parts));
     const bool turn = p.table != nullptr;
     const auto pick = [&](auto deep) {
@@ -586,7 +609,8 @@ extern "C" int pec_kv_read_q4(const pec_kv_read_q4_args *a, void *cuda_stream)
     const int64_t T = a->cache.T;
     if (T == 0) return PEC_OK;
     p.k = a->k_out; p.v = a->v_out; p.k_st = s[0]; p.k_sh = s[1]; p.v_st = s[2]; p.v_sh = s[3]; p.status = a->status;
-    const int per = q4::heads_per_part(T, 2 * (int64_t)p.q.Hkv), parts = (p.q.Hkv + per - 1) / per, tokens = q4::tokens_per_warp(T, parts);
+    const int per = q4::read_heads(T, p.q.Hkv, esz == 4), parts = (p.q.Hkv + per - 1) / per;
+    const int tokens = q4::tokens_per_warp(T, parts, per < p.q.Hkv ? per : p.q.Hkv, esz == 4);
     const dim3 grid((unsigned)((T + q4::kWarps * tokens - 1) / (q4::kWarps * tokens)), (unsigned)(2 * parts));
     const auto kernel = esz == 2 ? q4::kv_read_q4_kernel<__nv_bfloat16> : q4::kv_read_q4_kernel<float>;
     kernel<<<grid, q4::kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p, parts, per, tokens);
