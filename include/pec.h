@@ -600,6 +600,11 @@ size_t pec_paged_workspace_size(const pec_paged_args *args);
  * k_pages, v_pages: device [num_pages, page_size, Hkv, 64] bytes, the 64 of a head contiguous, page, token and head strides free
  * in bytes, multiples of 32; 32-byte aligned.  k_scales, v_scales: device bf16 [num_pages, page_size, Hkv], strides free in elements.
  * Head-major pages (a head's tokens one after the other) are read with the fewest and longest transfers.
+ * What four bits cost, against the same call over a bf16 cache (2-norm, relative; 4 to 256 tokens on 4096 to 65536 keys): channels of N(0, 1)
+ * are held to 0.11, attention over them comes out to 0.16, with queries four times as large, whose weight lies on few keys, to 0.30 to 0.33.
+ * A few channels that are ten times the others take the scale of their heads: with four such channels keys are held to 0.20 and outputs to
+ * 0.62 to 0.77, with two such channels values and outputs to 0.20 and 0.22.  (Over a bf16 cache all of these are 0.002.)  A part that all values
+ * share comes out as it is held on the average: outputs to 0.01.
  * Everything else (block_table, cu_q, kv_lens, padding rows, bad indices) as for the cache above.
  */
 typedef struct {

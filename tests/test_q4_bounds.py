@@ -109,3 +109,16 @@ def test_a_small_channel_of_a_query(pec, n, bound, scale):
         assert (off <= 6 * scale * bound + 4 * 2.0 ** -24 * want + 2.0 ** -20).all(), (off / (6 * scale * bound)).max()
         worst = max(worst, float((off / (6 * scale)).max()))
     print(f"[parity] {n} tokens: off by {worst / bound:.3f} of the bound")
+
+
+# ------------------------------------------------------------------------------------------ what four bits cost
+def test_what_heads_are_held_to():
+    """The documented errors of held heads against what was quantised (2-norm, relative): means over 4000 heads, whose own errors differ by a
+    tenth, so that a mean is known to 0.0005 and its third digit to be tested."""
+    x = np.random.RandomState(7).standard_normal((4000, 128))
+    outliers, pair = x.copy(), x.copy()
+    outliers[:, [5, 69, 40, 104]] *= 10
+    pair[:, [3, 77]] *= 10
+    for y, want in ((x, 0.109), (pair, 0.198), (outliers, 0.195)):
+        off = np.linalg.norm(q4.quantise(y)[0] - y) / np.linalg.norm(y)
+        assert abs(off - want) <= 0.003, (off, want)
