@@ -613,7 +613,8 @@ int launch_paged_f32(const Params &p, int64_t items, cudaStream_t stream) { retu
 int launch_paged_combine(const Params &p, cudaStream_t stream)
 {
     // Every cut of the line; every block that can be cut: one has two slots or more.
-    // One row a warp where the units are so few that this takes no more than two CTAs per SM.
+    // One row a warp where the units are so few that this takes no more than two CTAs for each of the kernel for few rows (which has one an
+    // SM, over a cache held in 4 bits two).
     const int64_t units = (int64_t)(p.c.B < p.c.T ? p.c.B : p.c.T) * p.Hkv;
     const int by_unit = units < p.few_ctas, most_groups = (p.few_rows + kCombineWarps - 1) / kCombineWarps;
     int few_groups = by_unit ? (int)(2 * p.few_ctas / units) : 2, few_blocks = 0;

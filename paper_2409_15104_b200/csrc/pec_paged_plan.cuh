@@ -13,7 +13,7 @@
 // Both sides of 128 rows, measured (64 requests of 3000 keys, 8 KV heads, few / many): 4 rows a request 128 / 163 us, 32 138 / 174,
 // 128 160 / 181; 200 requests of 132 keys, 64 rows 49 / 99; one request of 32000 keys, 128 rows 40 / 55.
 // A cache held in 4 bits: few is at most 16 rows, what its kernel's registers take (bf16 queries; fp32 has none here either).  16 rows a
-// request, 8 KV heads, few / many: 32 requests of 4000 keys 61 / 143 us, 8 of 64000 138 / 574, 256 of 600 88 / 269, one of 8000 23 / 36.
+// request, 8 KV heads, few / many: 32 requests of 4000 keys 71 / 144 us, 8 of 64000 152 / 575, 256 of 600 122 / 272, one of 8000 23 / 35.
 // Partials are merged by their LSE by one kernel for both classes (combine), which finds them by the same arithmetic.
 #pragma once
 #include "pec_internal.h"

@@ -6,7 +6,8 @@
 //
 // Both are bound by memory, a head of bf16 being 256 bytes on one side and 66 on the other: 131072 rows of 8 + 8 heads are read in 116 us
 // where memory takes 103.  Appending has some 150 instructions and three dependent loads (the request, the page, the angles) for each four
-// heads and does not reach that: 7302 tokens with norm and rotation, and 8901 read, 38 us where memory takes 13 (all of it in fp64 took 49).
+// heads and does not reach that: 7302 tokens with norm and rotation, and 8901 read, 34 us (23 and 10 by themselves) where
+// memory takes 13 (all of it in fp64 took 49).
 //
 // Which code is the nearest is decided exactly.  bf16 channels that are quantised as they are: x / s is either a border between two
 // codes or 2^-11 away from it (x has 8 bits, s 6, a border 3), while the product with the reciprocal is off by 2^-19: put on a grid of

@@ -5,8 +5,10 @@
 //   warps 0-3, 4-7  softmax and epilogue of stage 0 and 1 (a thread = a packed row = a TMEM lane)
 //   warps 8, 10     MMA issuers of stage 0 and 1       warp 9  loader of Q and codes       warp 11  idle
 //   warps 12-15     K and V: codes decoded into a ring of four tiles of 128 keys, 32 keys each
-// The codes come ahead of their decoding, in a ring of their own: with 16 bytes a lane in flight instead few rows waited for memory
-// (32 requests of 4 tokens and 4000 keys, 32 heads on 8: 206 us, now 169; 2048 tokens on 30720 1323 us, now 1261).
+// Measured, 32 heads on 8: 2048 tokens on 30720 1120 us, 32 requests of 8 tokens and 4000 keys 145, one of 32 tokens and 60000 110.  What
+// follows gives for each choice the first of these with it and without, everything else as it was at that time.
+// The codes come ahead of their decoding, in a ring of their own: with 16 bytes a lane in flight instead few rows waited for memory (1261
+// with it, 1323 without; 32 requests of 8 tokens 169 and 206).
 // The tiles are decoded to fp16, to which the hardware converts codes (two an instruction).  fp16 has no range to hold scales, so what
 // is multiplied is in units, powers of two that the other side makes up for:
 //     K   of one for each 32 keys of a tile, such that scales are below 2^13 of it: a factor of those scores
@@ -17,11 +19,11 @@
 // of Q is exact to 2^-31 of its row's largest, and off by 2^-39 of it below.  Probabilities are rounded to fp16, to 2^-11 of themselves: the largest of a row is held in [2^10, 2^15], and
 // those below 2^-24 of it, in fp16's subnormals, are off by at most 2^-35 of it.
 // Scores stay in tensor memory until probabilities take their place; S(j + 1) of a stage begins when PV(j) is done, some 2000 cycles in
-// which the other stage has the unit of 2^x to itself: the stages take turns (1195 us, without that 1263) and hand P over by halves.  A
-// row's 128 scores are in registers from its maximum on (1121 us; read a second time, by halves, 1195), which leaves the other warps 64.
-// With the score buffer of the bf16 cache's kernel, one that both stages use in turns, and tiles decoded to bf16 it was 1493 us.
+// which the other stage has the unit of 2^x to itself: the stages take turns (1195 with, 1263 without) and hand P over by halves.  A
+// row's 128 scores are in registers from its maximum on (1121; read a second time, by halves, 1195), which leaves the other warps 64.
+// With the score buffer of the bf16 cache's kernel, one that both stages use in turns, and tiles decoded to bf16 it was 1493.
 // A block that has rows for one stage only gives them to both, even tiles to one and odd tiles to the other, and merges what they have
-// added up at its end (32 requests of 8 tokens and 4000 keys 169 -> 145 us, one of 32 tokens and 60000 119 -> 105).
+// added up at its end (32 requests of 8 tokens 145 with, 169 without; one of 32 tokens and 60000 keys 110 and 119).
 // TMEM columns: S_s [128 s, +128), P_s its first 64; O_s [256 + 128 s, +128).
 #include <cuda.h>
 #include <cuda_bf16.h>
