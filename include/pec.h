@@ -628,7 +628,9 @@ typedef struct {
 /*
  * pec_kv_append for such a cache: keys normalised (norm) and rotated (rope_table) as there, then quantised; values quantised.
  * Keys that are normalised or rotated are worked out in fp64 from the table's fp32 entries, and not rounded before they are
- * quantised: which code is the nearest does not depend on how a sum was rounded.  dtype: that of k, v and the weight.
+ * quantised: which code is the nearest does not depend on how a sum was rounded.  (But for what norm and rotation bring next to a border
+ * without being on it, as heads whose channels are all of one magnitude far above eps: within 2^-41 of itself a channel counts as on a
+ * border of two codes, and within 2^-50 a head's largest may get either of two scales.)  dtype: that of k, v and the weight.
  * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT, CUDA.
  */
 typedef struct {

@@ -6,16 +6,16 @@
 //
 // Both are bound by memory, a head of bf16 being 256 bytes on one side and 66 on the other: 131072 rows of 8 + 8 heads are read in 116 us
 // where memory takes 103.  Appending has some 150 instructions and three dependent loads (the request, the page, the angles) for each four
-// heads and does not reach that: 7302 tokens with norm and rotation, and 8901 read, 34 us (23 and 10 by themselves) where
-// memory takes 13 (all of it in fp64 took 49).
+// heads and does not reach that: 7302 tokens with norm and rotation, and 8901 read, 34 us (23 and 10 by themselves) where memory takes 13
+// (all of it in fp64 took 49).
 //
-// Which code is the nearest is decided exactly.  bf16 channels that are quantised as they are: x / s is either a border between two
-// codes or 2^-11 away from it (x has 8 bits, s 6, a border 3), while the product with the reciprocal is off by 2^-19: put on a grid of
-// 2^-14 it is a border where x / s is one, and on its side elsewhere.  Everything else is worked out in fp32 with a bound of its error.
-// Where the least and the largest number within the bound have different codes (one of 200 usual heads has such a channel), the channel
-// goes through fp64, where they would have different scales the head: z times 1 / s, rounded to 41 bits for the same reason (an fp32 x is
-// 2^-25 away from a border at least), then to fp32 with the last bit set where anything was cut off, so that nothing becomes a border
-// that is none.
+// Which code is the nearest is decided exactly (but for normalised or rotated channels within 2^-41 of a border, where fp64 ends).  bf16
+// channels that are quantised as they are: x / s is either a border between two codes or 2^-11 away from it (x has 8 bits, s 6, a border 3),
+// while the product with the reciprocal is off by 2^-19: put on a grid of 2^-14 it is a border where x / s is one, and on its side
+// elsewhere.  Everything else is worked out in fp32 with a bound of its error.  Where the least and the largest number within the bound have
+// different codes (one of 200 usual heads has such a channel), the channel goes through fp64, where they would have different scales the
+// head: z times 1 / s, rounded to 41 bits for the same reason (an fp32 x is 2^-25 away from a border at least), then to fp32 with the last
+// bit set where anything was cut off, so that nothing becomes a border that is none.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <type_traits>

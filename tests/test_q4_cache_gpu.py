@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import q4_reference as q4
-from test_q4_gpu import BF16, DEV, F32, THETA, dev
+from test_q4_gpu import BF16, DEV, F32, THETA, angles, dev
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +44,38 @@ def test_large_calls_do_what_small_ones_do(pec, dtype, T, hkv):
         assert torch.equal(whole[which][at].double().cpu(), torch.from_numpy(held))
         if which:
             assert (held == q4.quantise(v[at].double().cpu().numpy())[0]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("turn", [False, True])
+def test_heads_that_norm_brings_next_to_borders(pec, dtype, turn):
+    """Heads whose channels are all of one magnitude become the weight's to within eps / x^2, which lies on borders of codes and scales or
+    just below them: the scale and the codes are the definition's to 2^-50 and 2^-41 (and the 2^-50 that the check's own fp64 is off by)."""
+    T, hkv, page = 600, 4, 64
+    g = torch.Generator().manual_seed(12)
+    size = torch.exp(torch.rand((T, hkv, 1), generator=g).double() * 30 - 3)
+    x = (size * torch.sign(torch.randn((T, hkv, 128), generator=g).double())).to(dtype).to(DEV)
+    w = (torch.randn(128, generator=g) * 3).to(BF16).to(dtype).to(DEV)
+    pages = -(-T // page)
+    order = torch.randperm(pages, device=DEV)[None].int()
+    codes = [torch.zeros((pages, page, hkv, 64), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    scales = [torch.zeros((pages, page, hkv), dtype=BF16, device=DEV) for _ in range(2)]
+    tables = pec.pec_rope_table(THETA, T, DEV) if turn else None
+    pec.pec_kv_append_q4(x, x, codes[0], scales[0], codes[1], scales[1], order, dev([0, T]), dev([T]), norm=True, k_weight=w, tables=tables)
+    pec.check_status()
+    pos = torch.arange(T, device=DEV)
+    pg, slot = order[0, pos // page].long(), pos % page
+    held = torch.from_numpy(q4.values(codes[0][pg, slot], scales[0][pg, slot]))
+    s = scales[0][pg, slot].double().cpu()[..., None]
+    z = x.double().cpu()
+    z = z * torch.rsqrt(z.square().mean(-1, keepdim=True) + float(torch.tensor(1e-6))) * w.double().cpu()
+    if turn:
+        c, t = (torch.from_numpy(v)[:, None] for v in angles(tables, list(range(T))))
+        z = torch.cat([z[..., :64] * c - z[..., 64:] * t, z[..., 64:] * c + z[..., :64] * t], -1)
+    most = z.abs().amax(-1, keepdim=True)
+    m, e = torch.frexp(s)                                          # the number before s has six significant bits as well
+    before = torch.ldexp(torch.where(m == 0.5, torch.tensor(63 / 128, dtype=torch.float64), m - 1 / 64), e)
+    assert (6 * s >= most * (1 - 2.0 ** -49)).all() and (6 * before < most * (1 + 2.0 ** -49)).all()
+    off = (z - held).abs()
+    nearest = ((z.abs() / s)[..., None] - torch.from_numpy(q4.MAGNITUDES)).abs().amin(-1) * s
+    assert (off <= nearest + z.abs() * 2.0 ** -40).all()           # (a channel off a border by d is off one code by 2 d more than the other)
